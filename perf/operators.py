@@ -164,7 +164,19 @@ def _inputs(case, seed):
 
 
 def prepare(case, seed):
-    return _inputs(case, seed)
+    s = _inputs(case, seed)
+    if own:  # the library's objects for the same tensors
+        from paper_2506_11209_amd import experts, fp8
+        kind = case["kind"]
+        rows = {"product": case.get("M"), "grouped": s["A"][0].shape[0] if "A" in s else 0, "grouped_gradient": case.get("N")}
+        if kind in rows:
+            deep = s["A"][0].shape[1] if kind == "grouped_gradient" else case["K"]
+            s["A"] = fp8.Fp8Matrix(*s["A"], rows[kind], deep, 1)
+            s["B"] = fp8.Fp8Matrix(*s["B"], case["K"] if kind == "grouped_gradient" else case["N"], deep,
+                                   1 if kind == "grouped_gradient" or case.get("form") == "rows" else BLOCK)
+        elif "place" in s:
+            s["routes"] = experts.Routes(s["offsets"], s["token"], s["place"])
+    return s
 
 
 # -- plain forms ------------------------------------------------------------------
@@ -321,24 +333,17 @@ def _own(s):
             return _whole(fp8.quantize_rows(s["x"]))
         return tuple(map(_whole, fp8.quantize_both(s["x"]) if case["form"] == "both" else fp8.quantize_weight(s["x"])))
     if kind == "product":
-        M, N, K = case["M"], case["N"], case["K"]
-        A = fp8.Fp8Matrix(*s["A"], M, K, 1)
-        B = fp8.Fp8Matrix(*s["B"], N, K, 1 if case["form"] == "rows" else BLOCK)
-        return fp8.product(A, B, out_dtype=case["out"], beta=case["beta"], C0=s.get("C0"))
+        return fp8.product(s["A"], s["B"], out_dtype=case["out"], beta=case["beta"], C0=s.get("C0"))
     if kind == "grouped":
-        A = fp8.Fp8Matrix(*s["A"], s["A"][0].shape[0], case["K"], 1)
-        return fp8.grouped_product(A, fp8.Fp8Matrix(*s["B"], case["N"], case["K"], BLOCK), s["offsets"], out_dtype=case["out"])
+        return fp8.grouped_product(s["A"], s["B"], s["offsets"], out_dtype=case["out"])
     if kind == "grouped_gradient":
-        rows = s["A"][0].shape[1]
-        return fp8.grouped_gradient(fp8.Fp8Matrix(*s["A"], case["N"], rows, 1), fp8.Fp8Matrix(*s["B"], case["K"], rows, 1),
-                                    s["offsets"], out_dtype=case["out"])
+        return fp8.grouped_gradient(s["A"], s["B"], s["token"].shape[0], s["offsets"], out_dtype=case["out"])
     if kind == "route":
         routes = experts.sort(s["ids"], case["E"])
         return routes.offsets, routes.token, routes.place, experts.gather(s["x"], routes)
-    routes = experts.Routes(s["offsets"], s["token"], s["place"])
     if kind == "combine":
-        return experts.combine(s["h"], routes, s["weights"])
-    return experts.combine_gradient(s["dy"], s["h"], routes, s["weights"])
+        return experts.combine(s["h"], s["routes"], s["weights"])
+    return experts.combine_gradient(s["dy"], s["h"], s["routes"], s["weights"])
 
 
 def run(state):
