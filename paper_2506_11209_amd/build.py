@@ -33,6 +33,8 @@ HIP_FLAGS = [
     "-I" + CSRC, "-I" + os.path.join(ROOT, "include"), "-I" + BUILD,
 ]
 
+# The 8-bit path and the routing of tokens to experts (ws_fp8.h, ws_experts.h).
+OPERATOR_SOURCES = ["ws_fp8_product.hip", "ws_fp8_quantize.hip", "ws_experts.hip"]
 
 # Kernel modes (KernelMode in ws_gemm_kernel.hpp): the GEMM and the
 # calibration kernels of the performance model.
@@ -200,6 +202,7 @@ def build(jobs: int | None = None, n_units: int = 32, verbose: bool = True) -> s
     host_srcs = [api_src, os.path.join(CSRC, "ws_model.cpp")]
     host_jobs = [(h, os.path.join(BUILD, os.path.basename(h)[:-4] + ".o")) for h in host_srcs]
     kernel_jobs = [(u, u[:-4] + ".o") for u in units]
+    kernel_jobs += [(os.path.join(CSRC, n), os.path.join(BUILD, n[:-4] + ".o")) for n in OPERATOR_SOURCES]
     reports = []
     with cf.ThreadPoolExecutor(max_workers=jobs) as ex:
         # kernels first: the host API is compiled against their register table

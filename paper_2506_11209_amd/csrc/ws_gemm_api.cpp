@@ -10,6 +10,7 @@
 #include <mutex>
 #include <new>
 
+#include "ws_error.hpp"
 #include "ws_gemm_kernel.hpp"
 #include "ws_gemm_plan.hpp"
 #include "ws_gemm_registry.hpp"
@@ -33,11 +34,17 @@ constexpr int kClockOffset = 64;
 
 thread_local char g_last_error[256] = "";
 
+}  // namespace
+
 // Records the failing HIP call for ws_gemm_last_error() and maps it to WS_ERR_HIP.
-ws_status hip_fail(const char* what, hipError_t e) {
+ws_status wsg::hip_fail(const char* what, hipError_t e) {
   snprintf(g_last_error, sizeof(g_last_error), "%s: %s (%d)", what, hipGetErrorString(e), (int)e);
   return WS_ERR_HIP;
 }
+
+namespace {
+
+using wsg::hip_fail;
 
 #define WSG_HIP(call)                                 \
   do {                                                \

@@ -1,0 +1,140 @@
+"""Routing of tokens to experts and back over torch tensors (declared in
+include/ws_experts.h; computed by the HIP kernels of libwsgemm.so).
+
+    routes = sort(ids, experts)                    # ids: tokens x k
+    xs = gather(x, routes)                         # rows by expert
+    h = ...                                        # the experts' work on their rows
+    y = combine(h, routes, weights)                # tokens x columns
+    dh, dweights = combine_gradient(dy, h, routes, weights)
+    dx = combine(dxs, routes)                      # gradient of gather
+
+Streams and errors as in ``fp8``.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import wsgemm as _w
+from .fp8 import _Call, _check, _index, _matrix, _mp, _need
+
+MAX_EXPERTS = 1024
+
+_lib = _w.library()
+_p, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+for _name, _args, _res in (
+        ("ws_expert_sort_workspace", [_i64, _i32, _i32], _i64),
+        ("ws_expert_sort", [_i64, _i32, _i32, _p, _i32, _p, _p, _p, _p, _i64, _p], _i32),
+        ("ws_expert_gather", [_mp, _p, _mp, _p], _i32),
+        ("ws_expert_combine", [_mp, _i32, _p, _p, _mp, _p], _i32),
+        ("ws_expert_combine_gradient", [_mp, _mp, _i32, _i32, _p, _p, _p, _mp, _p, _p], _i32)):
+    getattr(_lib, _name).argtypes, getattr(_lib, _name).restype = _args, _res
+
+
+class Routes:
+    """Where every token's choices go: ``offsets`` (experts + 1), the ``token`` of
+    each sorted row (-1: none) and the ``place`` of each choice (tokens x k; -1:
+    none), int32 on the device."""
+
+    __slots__ = ("offsets", "token", "place")
+
+    def __init__(self, offsets, token, place):
+        _need(offsets, "offsets", (torch.int32,), (1,))
+        _need(token, "token", (torch.int32,), (1,), offsets.device)
+        _need(place, "place", (torch.int32,), (2,), offsets.device)
+        if offsets.numel() < 2 or token.numel() != place.numel() or not (
+                offsets.is_contiguous() and token.is_contiguous() and place.is_contiguous()):
+            raise ValueError("routes: offsets %s, token %s and place %s do not belong together" % (
+                tuple(offsets.shape), tuple(token.shape), tuple(place.shape)))
+        self.offsets, self.token, self.place = offsets, token, place
+
+    @property
+    def experts(self) -> int:
+        return self.offsets.numel() - 1
+
+
+def sort(ids, experts: int, stream=None) -> Routes:
+    """Sorts the choices (tokens x k; int32 or int64; outside 0 .. experts - 1: none)
+    by expert, each expert's in the order of the choices."""
+    _need(ids, "ids", (torch.int32, torch.int64), (2,))
+    if not ids.is_contiguous() or ids.shape[1] < 1:
+        raise ValueError("ids: expected contiguous tokens x k, k at least 1, got %s of strides %s" % (tuple(ids.shape), ids.stride()))
+    tokens, k = ids.shape
+    need = _lib.ws_expert_sort_workspace(tokens, k, experts)
+    if need < 0:
+        raise ValueError("sort: 1 to %d experts, got %r, and at most 2^30 choices, got %d" % (MAX_EXPERTS, experts, ids.numel()))
+    n, device = tokens * k, ids.device
+    with _Call(device, stream, (ids,)) as st:
+        # one allocation: offsets, token, place and the work memory
+        flat = torch.empty(experts + 1 + 2 * n + need // 4, dtype=torch.int32, device=device)
+        r = Routes(flat[: experts + 1], flat[experts + 1: experts + 1 + n],
+                   flat[experts + 1 + n: experts + 1 + 2 * n].view(tokens, k))
+        at = flat.data_ptr()
+        _check(_lib.ws_expert_sort(tokens, k, experts, ids.data_ptr(), ids.element_size(), at, at + 4 * (experts + 1),
+                                   at + 4 * (experts + 1 + n), at + 4 * (experts + 1 + 2 * n), need, st), "ws_expert_sort")
+    return r
+
+
+def _out(out, what, shape, like):
+    if out is None:
+        return torch.empty(shape, dtype=like.dtype, device=like.device)
+    if tuple(out.shape) != tuple(shape) or out.dtype != like.dtype:
+        raise ValueError("%s: expected %s %s, got %s %s" % (what, tuple(shape), like.dtype, tuple(out.shape), out.dtype))
+    return out
+
+
+def _weights(weights, routes):
+    if weights is None:
+        return 0
+    _need(weights, "weights", (torch.float32,), (2,), routes.place.device)
+    if weights.shape != routes.place.shape or not weights.is_contiguous():
+        raise ValueError("weights: expected contiguous %s, got %s" % (tuple(routes.place.shape), tuple(weights.shape)))
+    return weights.data_ptr()
+
+
+def gather(x, routes: Routes, out=None, stream=None):
+    """x (tokens x columns; f32, bf16 or f16) by sorted row; zeros for rows of no token."""
+    m = _matrix(x, "x", device=routes.token.device)
+    if m.rows != routes.place.shape[0]:
+        raise ValueError("x: %d rows for %d tokens" % (m.rows, routes.place.shape[0]))
+    with _Call(x.device, stream, (x, routes.token, out)) as st:
+        out = _out(out, "out", (routes.token.numel(), m.cols), x)
+        _check(_lib.ws_expert_gather(m, routes.token.data_ptr(), _matrix(out, "out", device=x.device), st), "ws_expert_gather")
+    return out
+
+
+def combine(h, routes: Routes, weights=None, out=None, stream=None):
+    """Each token's sum of its choices' rows of h, times weights (tokens x k, f32)
+    where given; summed in binary32.  A token without a place gets zeros."""
+    m = _matrix(h, "h", device=routes.token.device)
+    if m.rows != routes.token.numel():
+        raise ValueError("h: %d rows for %d choices" % (m.rows, routes.token.numel()))
+    w, (tokens, k) = _weights(weights, routes), routes.place.shape
+    with _Call(h.device, stream, (h, routes.place, weights, out)) as st:
+        out = _out(out, "out", (tokens, m.cols), h)
+        _check(_lib.ws_expert_combine(m, k, routes.place.data_ptr(), w, _matrix(out, "out", device=h.device), st),
+               "ws_expert_combine")
+    return out
+
+
+def combine_gradient(dy, h, routes: Routes, weights=None, dh=None, stream=None):
+    """(dh, dweights) of combine: dh like h, rows without a token zero; dweights
+    tokens x k in binary32, None where weights is None (then h may be None)."""
+    m = _matrix(dy, "dy", device=routes.token.device)
+    w, (tokens, k) = _weights(weights, routes), routes.place.shape
+    if m.rows != tokens:
+        raise ValueError("dy: %d rows for %d tokens" % (m.rows, tokens))
+    if weights is not None:
+        mh = _matrix(h, "h", device=dy.device)
+        if (mh.rows, mh.cols) != (routes.token.numel(), m.cols) or h.dtype != dy.dtype:
+            raise ValueError("h: expected %s %s, got %s %s" % ((routes.token.numel(), m.cols), dy.dtype, tuple(h.shape), h.dtype))
+    else:
+        mh = None
+    with _Call(dy.device, stream, (dy, h, routes.offsets, routes.place, weights, dh)) as st:
+        dh = _out(dh, "dh", (routes.token.numel(), m.cols), dy)
+        dw = torch.empty(tokens, k, dtype=torch.float32, device=dy.device) if weights is not None else None
+        _check(_lib.ws_expert_combine_gradient(m, mh, k, routes.experts, routes.offsets.data_ptr(), routes.place.data_ptr(), w,
+                                               _matrix(dh, "dh", device=dy.device), dw.data_ptr() if dw is not None else 0, st),
+               "ws_expert_combine_gradient")
+    return dh, dw

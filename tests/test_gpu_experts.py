@@ -1,0 +1,204 @@
+"""Routing of tokens to experts and back against plain definitions."""
+import numpy as np
+import pytest
+import torch
+
+from tests import fp8_ref as ref
+from tests.gpu_helpers import log
+
+experts = pytest.importorskip("paper_2506_11209_amd.experts")
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def make_ids(T, k, E, seed, none=0.1, dtype=torch.int32, skew=False):
+    g = torch.Generator().manual_seed(seed)
+    ids = (torch.rand(T, k, generator=g).pow(4 if skew else 1) * E).long().clamp(max=E - 1)
+    gone = torch.rand(T, k, generator=g) < none
+    ids[gone] = torch.tensor([-1, E, -(1 << 31), (1 << 31) - 1])[torch.arange(int(gone.sum())) % 4]
+    return ids.to(dtype)
+
+
+def plain_sort(ids, E):
+    flat = ids.reshape(-1).tolist()
+    rows = sorted((e, s) for s, e in enumerate(flat) if 0 <= e < E)
+    token = [s // ids.shape[1] for _, s in rows] + [-1] * (len(flat) - len(rows))
+    place = [-1] * len(flat)
+    for r, (_, s) in enumerate(rows):
+        place[s] = r
+    counts = np.bincount([e for e, _ in rows], minlength=E) if rows else np.zeros(E, int)
+    return [0] + np.cumsum(counts).tolist(), token, place
+
+
+# up to 4096 choices one workgroup, beyond several
+SORTS = [(1, 1, 1), (1, 1, 1024), (1, 8, 64), (7, 2, 3), (64, 4, 64), (1024, 4, 8), (1025, 4, 8), (3000, 3, 257), (5000, 8, 1024), (20000, 2, 5),
+         (4097, 1, 2)]
+
+
+@pytest.mark.parametrize("T,k,E", SORTS)
+@pytest.mark.parametrize("dtype", (torch.int32, torch.int64))
+def test_sort(T, k, E, dtype):
+    log("case sort %d x %d of %d %s" % (T, k, E, dtype))
+    for none, skew in ((0.1, False), (0.0, True), (1.0, False)):
+        ids = make_ids(T, k, E, T + k, none, dtype, skew)
+        r = experts.sort(ids.cuda(), E)
+        offsets, token, place = plain_sort(ids, E)
+        assert r.offsets.tolist() == offsets and r.token.tolist() == token and r.place.flatten().tolist() == place
+
+
+def test_sort_of_many_choices():
+    """More choices than 256 chunks of the ordinary size hold."""
+    log("case sort many")
+    T, k, E = 300001, 2, 300
+    ids = make_ids(T, k, E, 1)
+    r = experts.sort(ids.cuda(), E)
+    flat = ids.flatten().numpy().astype(np.int64)
+    key = np.where((flat >= 0) & (flat < E), flat, E)
+    order = np.argsort(key, kind="stable")
+    n = int((key < E).sum())
+    assert r.offsets.tolist() == np.searchsorted(key[order], np.arange(E + 1)).tolist()
+    assert np.array_equal(r.token.cpu().numpy()[:n], order[:n] // k) and (r.token[n:] == -1).all()
+    place = np.full(flat.size, -1)
+    place[order[:n]] = np.arange(n)
+    assert np.array_equal(r.place.flatten().cpu().numpy(), place)
+
+
+def test_sort_of_no_tokens():
+    log("case sort nothing")
+    r = experts.sort(torch.empty(0, 2, dtype=torch.int64, device="cuda"), 5)
+    assert r.offsets.tolist() == [0] * 6 and r.token.numel() == 0 and r.place.shape == (0, 2)
+    assert experts.gather(torch.empty(0, 8, device="cuda"), r).shape == (0, 8)
+    assert experts.combine(torch.empty(0, 8, device="cuda"), r).shape == (0, 8)
+    dh, dw = experts.combine_gradient(torch.empty(0, 8, device="cuda"), torch.empty(0, 8, device="cuda"), r,
+                                      torch.empty(0, 2, device="cuda"))
+    assert dh.shape == (0, 8) and dw.shape == (0, 2)
+
+
+ROWS = [(1, 1, 4, 1), (5, 2, 3, 7), (33, 4, 16, 64), (64, 5, 8, 513), (40, 9, 12, 2049), (200, 2, 4, 4100)]
+
+
+@pytest.mark.parametrize("T,k,E,C", ROWS)
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_gather_combine_and_gradient(T, k, E, C, dtype):
+    log("case rows %d x %d of %d, %d columns %s" % (T, k, E, C, dtype))
+    typ = TYPES[dtype]
+    g = torch.Generator().manual_seed(T)
+    ids = make_ids(T, k, E, T, 0.2)
+    if T > 4:
+        ids[3] = -1  # a token without experts
+    r = experts.sort(ids.cuda(), E)
+    token, place = r.token.cpu().long(), r.place.cpu().long()
+    n = int(r.offsets[-1])
+    x = torch.randn(T, C, generator=g).to(typ)
+    xs = experts.gather(x.cuda(), r).cpu()
+    assert torch.equal(xs[:n], x[token[:n]]) and (xs[n:] == 0).all()
+
+    h, wt = torch.randn(T * k, C, generator=g).to(typ), torch.randn(T, k, generator=g)
+    h[n:] = float("nan")  # rows of no token are not read
+    hn, wn = ref.f64(h), wt.double().numpy()
+    half = ref.HALF_ULP[typ]
+    for weights in (wt, None):
+        want, size = np.zeros((T, C)), np.zeros((T, C))
+        for t in range(T):
+            for j in range(k):
+                if place[t, j] >= 0:
+                    term = (wn[t, j] if weights is not None else 1.0) * hn[place[t, j]]
+                    want[t] += term
+                    size[t] += np.abs(term)
+        got = experts.combine(h.cuda(), r, weights.cuda() if weights is not None else None)
+        # k fused additions in binary32, then one rounding (f16 subnormals: 2^-25)
+        ref.assert_within(ref.f64(got), want, (k + 1) * 2.0 ** -24 * size + 1.01 * half * np.abs(want) + 2.0 ** -25 * (typ == torch.float16))
+
+    dy = torch.randn(T, C, generator=g).to(typ)
+    dyn = ref.f64(dy)
+    dh, dw = experts.combine_gradient(dy.cuda(), h.cuda(), r, wt.cuda())
+    want_h, want_w, size_w = np.zeros((T * k, C)), np.zeros((T, k)), np.zeros((T, k))
+    for t in range(T):
+        for j in range(k):
+            if place[t, j] >= 0:
+                want_h[place[t, j]] = wn[t, j] * dyn[t]
+                want_w[t, j] = dyn[t] @ hn[place[t, j]]
+                size_w[t, j] = np.abs(dyn[t]) @ np.abs(hn[place[t, j]])
+    ref.assert_within(ref.f64(dh), want_h, (2.0 ** -24 + 1.01 * half) * np.abs(want_h) + 2.0 ** -25 * (typ == torch.float16))
+    ref.assert_within(dw.cpu().double().numpy(), want_w, (C + 1) * 2.0 ** -24 * size_w)
+    dh1, none = experts.combine_gradient(dy.cuda(), None, r)
+    assert none is None
+    want_1 = torch.zeros(T * k, C, dtype=typ)
+    want_1[:n] = dy[token[:n]]
+    assert torch.equal(dh1.cpu(), want_1)
+
+
+def test_gradients_against_differences():
+    """combine is linear in h and in weights, so a central difference of the loss is
+    its gradient but for roundings; gather's gradient is combine without weights."""
+    log("case rows differences")
+    T, k, E, C = 30, 3, 6, 40
+    g = torch.Generator().manual_seed(0)
+    r = experts.sort(make_ids(T, k, E, 1).cuda(), E)
+    n = int(r.offsets[-1])
+    h, wt, dy = (torch.randn(*s, generator=g).cuda() for s in ((T * k, C), (T, k), (T, C)))
+    dh, dw = experts.combine_gradient(dy, h, r, wt)
+    loss = lambda hh, ww: (dy.double() * experts.combine(hh, r, ww).double()).sum().item()  # noqa: E731
+    uh, uw, s = torch.randn(T * k, C, generator=g).cuda(), torch.randn(T, k, generator=g).cuda(), 0.125
+    # loss sums T C terms of k products; each output is off by (k + 1) 2^-24 of its terms: 8 of them
+    # times sqrt(T C) * |dy| |w| |h| stay far below 1e-3 of what is compared here
+    for got, diff in (((dh.double() * uh.double()).sum().item(), loss(h + s * uh, wt) - loss(h - s * uh, wt)),
+                      ((dw.double() * uw.double()).sum().item(), loss(h, wt + s * uw) - loss(h, wt - s * uw))):
+        assert abs(diff / (2 * s) - got) <= 2e-2
+    x, dxs = torch.randn(T, C, generator=g).cuda(), torch.randn(T * k, C, generator=g).cuda()
+    dx = experts.combine(dxs, r)
+    ux = torch.randn(T, C, generator=g).cuda()
+    got = (dx.double() * ux.double()).sum().item()
+    want = (dxs.double() * experts.gather(ux, r).double())[:n].sum().item()
+    assert abs(got - want) <= 1e-2
+
+
+def test_indices_out_of_range_count_as_none():
+    log("case rows out of range")
+    T, k, C = 4, 2, 24
+    place = torch.tensor([[0, 99], [-5, 3], [8, 1 << 30], [7, -(1 << 31)]], dtype=torch.int32, device="cuda")
+    token = torch.tensor([0, 1, -1, 4, 1 << 30, 2, 3, -9], dtype=torch.int32, device="cuda")
+    r = experts.Routes(torch.tensor([0, 3, 8], dtype=torch.int32, device="cuda"), token, place)
+    x, h = torch.randn(T, C, device="cuda"), torch.randn(T * k, C, device="cuda")
+    xs = experts.gather(x, r)
+    zero = torch.zeros(C, device="cuda")
+    assert torch.equal(xs, torch.stack([x[0], x[1], zero, zero, zero, x[2], x[3], zero]))
+    assert torch.equal(experts.combine(h, r), torch.stack([h[0], h[3], zero, h[7]]))
+    _, dw = experts.combine_gradient(x, h, r, torch.ones(T, k, device="cuda"))
+    assert dw[0, 1] == 0 and dw[1, 0] == 0 and (dw[2] == 0).all() and dw[3, 1] == 0
+
+
+def test_strided_rows_and_another_stream():
+    log("case rows strided")
+    T, k, E, C = 50, 2, 5, 100
+    r = experts.sort(make_ids(T, k, E, 3).cuda(), E)
+    x = torch.randn(T, 130, device="cuda").bfloat16()[:, 7:7 + C]
+    room = torch.full((T * k, 131), 4.0, dtype=torch.bfloat16, device="cuda")
+    xs = experts.gather(x, r, out=room[:, 3:3 + C])
+    assert torch.equal(xs, experts.gather(x.contiguous(), r)) and (room[:, :3] == 4).all() and (room[:, 3 + C:] == 4).all()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    y = experts.combine(xs, r, stream=side)
+    side.synchronize()
+    assert torch.equal(y, experts.combine(xs, r))
+
+
+def test_refusals():
+    log("case rows refusals")
+    ids = torch.zeros(6, 2, dtype=torch.int32, device="cuda")
+    r = experts.sort(ids, 3)
+    x, h, wt = torch.zeros(6, 8, device="cuda"), torch.zeros(12, 8, device="cuda"), torch.zeros(6, 2, device="cuda")
+    for call in (lambda: experts.sort(ids.float(), 3), lambda: experts.sort(ids[:, 0], 3), lambda: experts.sort(ids.t(), 3),
+                 lambda: experts.sort(ids, 0), lambda: experts.sort(ids, 1025), lambda: experts.sort(ids[:, :0], 3),
+                 lambda: experts.gather(h, r), lambda: experts.gather(x.t(), r), lambda: experts.gather(x.int(), r),
+                 lambda: experts.gather(x, r, out=torch.zeros(12, 9, device="cuda")),
+                 lambda: experts.combine(x, r), lambda: experts.combine(h, r, wt.bfloat16()), lambda: experts.combine(h, r, wt[:5]),
+                 lambda: experts.combine(h, r, wt, out=x.bfloat16()),
+                 lambda: experts.combine_gradient(h, h, r, wt), lambda: experts.combine_gradient(x, x, r, wt),
+                 lambda: experts.combine_gradient(x, h.bfloat16(), r, wt), lambda: experts.combine_gradient(x, None, r, wt),
+                 lambda: experts.Routes(r.offsets[:1], r.token, r.place), lambda: experts.Routes(r.offsets, r.token[:5], r.place),
+                 lambda: experts.Routes(r.offsets, r.token, r.place.t())):
+        with pytest.raises(ValueError):
+            call()
