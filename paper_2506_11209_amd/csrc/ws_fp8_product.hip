@@ -21,6 +21,8 @@
 // a wave covers 64 neighbouring bytes of every row.  The operands are passed in
 // exchanged order (B's rows first): a lane then ends up with four neighbouring
 // columns of one row of C.
+#include <type_traits>
+
 #include "ws_fp8_common.hpp"
 
 namespace wsg {
@@ -227,6 +229,236 @@ __global__ __launch_bounds__(512) void direct_kernel(ProductArgs a) {
   }
 }
 
+// -- tiles -----------------------------------------------------------------------
+
+#define WSG_LDS __attribute__((address_space(3)))
+
+// Byte position, in a row of 128, of 16-byte chunk c of tile row r.  Sixteen
+// rows' reads of one chunk fall on different banks, and the choice depends on
+// r % 16 only, which is fixed for a lane.
+__device__ __forceinline__ int chunk_at(int r, int c) { return (c ^ ((r ^ ((r >> 3) & 1)) & 7)) * 16; }
+
+// A buffer descriptor as four scalars, for asm.
+__device__ __forceinline__ i32x4_t raw_buffer(const uint8_t* base, uint32_t bytes) {
+  const uint64_t at = (uint64_t)base;
+  return i32x4_t{(int)__builtin_amdgcn_readfirstlane((uint32_t)at), (int)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)),
+                 (int)__builtin_amdgcn_readfirstlane(bytes), 0x00027000};
+}
+
+// 64 lanes' 16 bytes from buffer offsets `at` + k straight to 1 KiB of LDS at
+// `to` (zeros where `at` is outside).  As asm, so that the compiler does not wait
+// for it before LDS reads of other addresses; whoever reads what it brings waits
+// for vmcnt himself.  Nothing else in these kernels uses m0.
+__device__ __forceinline__ void load_to_lds(i32x4_t r, uint32_t at, uint32_t k, uint32_t to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile(
+      "s_mov_b32 m0, %3\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(at),
+      "s"(r), "s"(__builtin_amdgcn_readfirstlane(k)), "s"(__builtin_amdgcn_readfirstlane(to)));
+#endif
+}
+
+// Waits for this wave's loads and LDS accesses, then for the workgroup.
+__device__ __forceinline__ void drain_and_meet() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#endif
+}
+
+// Writes a wave's part of a tile, 16 rows at a time by way of its own part of LDS,
+// so that a store covers whole stretches of a row.  rows, cols: of the tile, inside C.
+template <typename T, int WM, int WN>
+__device__ __forceinline__ void store_tile(const ProductArgs& a, const Part& p, const f32x4_t (&acc)[WM][WN], uint8_t* smem, int wm,
+                                           int wn, int rows, int cols) {
+  constexpr int kCols = 16 * WN, kPitch = kCols + 4;  // floats; the pitch spreads rows over the banks
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  float* own = (float*)smem + (threadIdx.x >> 6) * 16 * kPitch;
+#pragma unroll
+  for (int i = 0; i < WM; ++i) {
+#pragma unroll
+    for (int j = 0; j < WN; ++j) *(f32x4_t*)(own + r * kPitch + 16 * j + 4 * g) = acc[i][j];
+    __builtin_amdgcn_wave_barrier();  // a wave's LDS accesses keep their order
+#pragma unroll 1
+    for (int e = lane; e < 4 * kCols; e += 64) {
+      const int row = (wm * WM + i) * 16 + e / (kCols / 4), at = e % (kCols / 4) * 4, col = wn * kCols + at;
+      float v[4];
+      *(f32x4_t*)v = *(const f32x4_t*)(own + e / (kCols / 4) * kPitch + at);
+      if (row < rows && col < cols) store4<T>(a, p, p.m0 + row, p.n0 + col, v);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+template <int N, typename F>
+__device__ __forceinline__ void static_for(const F& f) {
+  if constexpr (N > 0) {
+    static_for<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
+
+// acc[i][j] += A's rows i times B's rows j; the scales' bytes are chosen by the instruction.
+template <int i, int j, int WM, int WN>
+__device__ __forceinline__ void multiply(f32x4_t (&acc)[WM][WN], const i32x8_t (&fa)[WM], const i32x8_t (&fb)[WN], const uint32_t* sa,
+                                         const uint32_t* sb) {
+  acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i], acc[i][j], 0, 0, j % 4, (int)sb[j / 4], i % 4,
+                                                               (int)sa[i / 4]);
+}
+
+// Keeps what computes four accumulators before the asm statements that follow (a
+// product has no side effects, so the compiler would move it past a barrier).
+__device__ __forceinline__ void stay_before(f32x4_t* acc) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+a"(acc[0]), "+a"(acc[1]), "+a"(acc[2]), "+a"(acc[3]));
+#endif
+}
+
+// A tile of 32 WM x 32 WN by four waves, 2 x 2, of WM x WN matrix instructions
+// each.  Blocks of 128 columns are double-buffered in LDS, and a block's products
+// come in two halves:
+//
+//   rows 0 .. WM / 2 - 1, row by row: the rest of A of block b is read
+//   meet: b + 1 has landed everywhere, b has been read everywhere
+//   rows WM / 2 .., column by column: b + 2 is loaded over b; the first rows of A
+//   of b + 1 are read, and every column of B of b + 1 once that of b is done
+//
+// so there is one barrier a block, no wait for memory that had less than a
+// block's time, and one set of registers for each operand.  Scales lie in LDS as
+// [row % 16][row / 16], so that a lane reads those of all its rows at once and
+// the instruction picks a byte.
+template <int WM, int WN, int MODE>
+__global__ __launch_bounds__(256, (WM * WN > 32 ? 1 : 2)) void tile_kernel(ProductArgs a) {
+  constexpr int TM = 32 * WM, TN = 32 * WN, kStage = (TM + TN) * kBlock, kRows = TM + TN, kHalf = WM / 2;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
+
+  // neighbouring tiles on one XCD (workgroups go round the XCDs in turn), eight
+  // rows of tiles at a time
+  const uint32_t tiles = a.tiles_m * a.tiles_n, group = MODE == kDepthGroups ? blockIdx.x / tiles : 0;
+  uint32_t id = MODE == kDepthGroups ? blockIdx.x % tiles : blockIdx.x;
+  {
+    const uint32_t per = tiles / 8, rest = tiles % 8, x = id % 8;
+    id = x * per + min(x, rest) + id / 8;
+  }
+  const uint32_t wide = 8 * (uint32_t)a.tiles_n, first = id / wide * 8, high = min(8u, (uint32_t)a.tiles_m - first);
+  const uint32_t in = id % wide;
+  Part p;
+  if (!find_part<MODE>(a, first + in % high, in / high, group, TM, TN, &p)) return;
+  const int rows = (int)min(p.m_end - p.m0, (int64_t)TM), cols = (int)min(a.N - p.n0, (int64_t)TN);
+  const int K = p.zero ? 0 : (int)p.K, blocks = (K + kBlock - 1) / kBlock;
+  const i32x4_t ra = raw_buffer(p.A + p.m0 * a.lda, (uint32_t)(rows * a.lda));
+  const i32x4_t rb = raw_buffer(p.B + p.n0 * a.ldb, (uint32_t)(cols * a.ldb));
+
+  // loads: wave w takes the tile's row octets w, w + 4, ..
+  const int lr = 8 * wave + (lane >> 3), lc = chunk_at(lr, lane & 7);  // chunk_at is its own inverse
+  const uint32_t at_a = (uint32_t)(lr * a.lda + lc), at_b = (uint32_t)(lr * a.ldb + lc);
+  const uint32_t step_a = __builtin_amdgcn_readfirstlane((uint32_t)(32 * a.lda)), step_b = __builtin_amdgcn_readfirstlane((uint32_t)(32 * a.ldb));
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(WSG_LDS uint8_t*)smem + wave * 1024;
+  const auto load = [&](int b) {
+    const bool inside = b * kBlock + lc < K;  // else zeros: past the last column
+    const uint32_t ia = inside ? at_a : kOutside, ib = inside ? at_b : kOutside;
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + (b & 1) * kStage);
+#pragma unroll
+    for (int t = 0; t < TM / 32; ++t) load_to_lds(ra, ia + t * step_a, b * kBlock, to + t * 4096);
+#pragma unroll
+    for (int t = 0; t < TN / 32; ++t) load_to_lds(rb, ib + t * step_b, b * kBlock, to + (t + TM / 32) * 4096);
+  };
+
+  // scales of this thread's rows of the tile
+  constexpr int kMine = (kRows + 255) / 256;
+  uint8_t* scales = smem + 2 * kStage;
+  uint8_t byte[kMine];
+  const auto fetch_scales = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int row = tid + 256 * i, block = min(b, blocks - 1);
+      byte[i] = row < TM ? p.sa[block * a.ldsa + p.m0 + min(row, rows - 1)]
+                         : p.sb[block * a.ldsb + ((p.n0 + min(row - TM, cols - 1)) >> a.b_shift)];
+    }
+  };
+  const auto keep_scales = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int row = tid + 256 * i;
+      if (kRows % 256 == 0 || row < kRows)
+        scales[(b & 1) * kRows + (row < TM ? row % 16 * (2 * WM) + row / 16 : TM + (row - TM) % 16 * (2 * WN) + (row - TM) / 16)] =
+            byte[i];
+    }
+  };
+
+  f32x4_t acc[WM][WN];
+#pragma unroll
+  for (int i = 0; i < WM; ++i)
+#pragma unroll
+    for (int j = 0; j < WN; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
+
+  if (blocks > 0) {
+    const int fa0 = (wm * WM * 16 + r) * kBlock, fb0 = (TM + wn * WN * 16 + r) * kBlock, c0 = chunk_at(r, g), c1 = chunk_at(r, g + 4);
+    i32x8_t fa[WM], fb[WN];
+    uint32_t sa[(WM + 3) / 4], sb[(WN + 3) / 4];
+    const auto frag = [&](int row, int stage) {
+      const uint8_t* f = smem + stage + row;
+      return join(*(const i32x4_t*)(f + c0), *(const i32x4_t*)(f + c1));
+    };
+    const auto read_scales = [&](int b, uint32_t* sa, uint32_t* sb) {
+      const uint8_t* s = scales + (b & 1) * kRows;
+      __builtin_memcpy(sa, __builtin_assume_aligned(s + (2 * r + wm) * WM, WM), WM);
+      __builtin_memcpy(sb, __builtin_assume_aligned(s + TM + (2 * r + wn) * WN, WN), WN);
+    };
+    fetch_scales(0);
+    keep_scales(0);
+    fetch_scales(1);
+    keep_scales(1);
+    load(0);
+    drain_and_meet();
+    load(1);
+    fetch_scales(2);
+    read_scales(0, sa, sb);
+#pragma unroll
+    for (int j = 0; j < WN; ++j) fb[j] = frag(fb0 + j * 2048, 0);
+#pragma unroll
+    for (int i = 0; i < kHalf; ++i) fa[i] = frag(fa0 + i * 2048, 0);
+
+    for (int b = 0; b < blocks; ++b) {
+      const int here = (b & 1) * kStage, next = kStage - here;
+      static_for<kHalf>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        fa[kHalf + i] = frag(fa0 + (kHalf + i) * 2048, here);
+        static_for<WN>([&](auto jc) { multiply<i, decltype(jc)::value>(acc, fa, fb, sa, sb); });
+        static_for<WN / 4>([&](auto jc) { stay_before(&acc[i][4 * decltype(jc)::value]); });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      drain_and_meet();
+      keep_scales(b + 2);
+      __builtin_amdgcn_sched_barrier(0);
+      load(b + 2);
+      fetch_scales(b + 3);
+      uint32_t next_sa[(WM + 3) / 4], next_sb[(WN + 3) / 4];
+      read_scales(b + 1, next_sa, next_sb);
+      static_for<WN>([&](auto jc) {
+        constexpr int j = decltype(jc)::value;
+#pragma unroll
+        for (int i = j * kHalf / WN; i < (j + 1) * kHalf / WN; ++i) fa[i] = frag(fa0 + i * 2048, next);
+        static_for<kHalf>([&](auto ic) { multiply<kHalf + decltype(ic)::value, j>(acc, fa, fb, sa, sb); });
+        fb[j] = frag(fb0 + j * 2048, next);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+#pragma unroll
+      for (int i = 0; i < (WM + 3) / 4; ++i) sa[i] = next_sa[i];
+#pragma unroll
+      for (int j = 0; j < (WN + 3) / 4; ++j) sb[j] = next_sb[j];
+    }
+    drain_and_meet();  // no load may land in what LDS is used for next, here or in another workgroup
+  }
+  switch (a.dtype) {  // the same for the whole launch
+    case WS_OUT_F32: return store_tile<float, WM, WN>(a, p, acc, smem, wm, wn, rows, cols);
+    case WS_OUT_BF16: return store_tile<bf16_t, WM, WN>(a, p, acc, smem, wm, wn, rows, cols);
+    default: return store_tile<f16_t, WM, WN>(a, p, acc, smem, wm, wn, rows, cols);
+  }
+}
+
 // -- host --------------------------------------------------------------------------
 
 // Bytes between rows so that a tile's offsets stay below kOutside.
@@ -245,9 +477,26 @@ ws_status run_direct(ProductArgs a, hipStream_t stream) {
   return launch("fp8_product", kernel, grid, 64 * waves, waves * MT * 1024, stream, a);
 }
 
+template <int WM, int WN, int MODE>
+ws_status run_tiles(ProductArgs a, hipStream_t stream) {
+  constexpr int TM = 32 * WM, TN = 32 * WN, kLds = 2 * (TM + TN) * (kBlock + 1);
+  a.tiles_n = ceil_div(a.N, TN);
+  a.tiles_m = MODE == kRowGroups ? group_tiles(a.M, a.groups, TM, true) : ceil_div(a.M, TM);
+  const int64_t tiles = a.tiles_n * a.tiles_m, grid = tiles * (MODE == kDepthGroups ? a.groups : 1);
+  if (a.tiles_m > kMaxGrid || tiles > kMaxGrid || grid > kMaxGrid) return WS_ERR_INVALID_ARG;
+  const void* fn = (const void*)&tile_kernel<WM, WN, MODE>;
+  const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  if (e != hipSuccess) return hip_fail("hipFuncSetAttribute", e);
+  return launch("fp8_product", &tile_kernel<WM, WN, MODE>, grid, 256, kLds, stream, a);
+}
+
 template <int MODE>
 ws_status run_product(const ProductArgs& a, hipStream_t stream) {
   const int64_t rows = MODE == kRowGroups ? ceil_div(a.M, a.groups) : a.M;
+  if (a.dtype != WS_OUT_F32 && rows > 64) {
+    if (rows > 512) return run_tiles<8, 8, MODE>(a, stream);
+    return run_tiles<4, 4, MODE>(a, stream);
+  }
   if (rows <= 16) return run_direct<1, 4, MODE>(a, stream);
   if (rows <= 32) return run_direct<2, 4, MODE>(a, stream);
   return run_direct<4, 2, MODE>(a, stream);
