@@ -298,19 +298,27 @@ __device__ __forceinline__ void static_for(const F& f) {
   }
 }
 
-// acc[i][j] += A's rows i times B's rows j; the scales' bytes are chosen by the instruction.
-template <int i, int j, int WM, int WN>
-__device__ __forceinline__ void multiply(f32x4_t (&acc)[WM][WN], const i32x8_t (&fa)[WM], const i32x8_t (&fb)[WN], const uint32_t* sa,
-                                         const uint32_t* sb) {
-  acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i], acc[i][j], 0, 0, j % 4, (int)sb[j / 4], i % 4,
-                                                               (int)sa[i / 4]);
+// acc += A's 16 rows times B's 16 rows, each operand's scale in byte SA or SB of
+// its dword.  As asm with the sum in place: the compiler's own form of it moved
+// sums between registers (4 copies and a wait for each of a row's products), and
+// what has no side effects does not stay on its side of a barrier.  The wait
+// states are those after a VALU write of an operand; they pass while the matrix
+// unit is busy with the product before.
+template <int SA, int SB>
+__device__ __forceinline__ void multiply(f32x4_t& acc, const i32x8_t& fa, const i32x8_t& fb, uint32_t sa, uint32_t sb) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile(
+      "s_nop 1\n\t"
+      "v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
+      : "+a"(acc)
+      : "v"(fb), "v"(fa), "v"(sb), "v"(sa), "n"(SB & 1), "n"(SA & 1), "n"(SB >> 1), "n"(SA >> 1));
+#endif
 }
 
-// Keeps what computes four accumulators before the asm statements that follow (a
-// product has no side effects, so the compiler would move it past a barrier).
-__device__ __forceinline__ void stay_before(f32x4_t* acc) {
+// Lets the last products into acc finish before anything reads it.
+__device__ __forceinline__ void settle(f32x4_t& acc) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("" : "+a"(acc[0]), "+a"(acc[1]), "+a"(acc[2]), "+a"(acc[3]));
+  asm volatile("s_nop 15" : "+a"(acc));
 #endif
 }
 
@@ -356,27 +364,32 @@ __global__ __launch_bounds__(256, (WM * WN > 32 ? 1 : 2)) void tile_kernel(Produ
   const uint32_t at_a = (uint32_t)(lr * a.lda + lc), at_b = (uint32_t)(lr * a.ldb + lc);
   const uint32_t step_a = __builtin_amdgcn_readfirstlane((uint32_t)(32 * a.lda)), step_b = __builtin_amdgcn_readfirstlane((uint32_t)(32 * a.ldb));
   const uint32_t lds0 = (uint32_t)(uintptr_t)(WSG_LDS uint8_t*)smem + wave * 1024;
-  const auto load = [&](int b) {
+  constexpr int kLoads = (TM + TN) / 32;  // of a wave and block, 1 KiB each
+  const auto load = [&](int b, int from, int to) {
     const bool inside = b * kBlock + lc < K;  // else zeros: past the last column
-    const uint32_t ia = inside ? at_a : kOutside, ib = inside ? at_b : kOutside;
-    const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + (b & 1) * kStage);
+    const uint32_t ia = inside ? at_a : kOutside, ib = inside ? at_b : kOutside, lds = lds0 + (b & 1) * kStage;
 #pragma unroll
-    for (int t = 0; t < TM / 32; ++t) load_to_lds(ra, ia + t * step_a, b * kBlock, to + t * 4096);
-#pragma unroll
-    for (int t = 0; t < TN / 32; ++t) load_to_lds(rb, ib + t * step_b, b * kBlock, to + (t + TM / 32) * 4096);
+    for (int t = from; t < to; ++t) {
+      if (t < TM / 32) load_to_lds(ra, ia + t * step_a, b * kBlock, lds + t * 4096);
+      else load_to_lds(rb, ib + (t - TM / 32) * step_b, b * kBlock, lds + t * 4096);
+    }
   };
 
   // scales of this thread's rows of the tile
   constexpr int kMine = (kRows + 255) / 256;
   uint8_t* scales = smem + 2 * kStage;
   uint8_t byte[kMine];
+  const uint8_t* scale_at[kMine];
+  int64_t scale_ld[kMine];
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int row = tid + 256 * i;
+    scale_at[i] = row < TM ? p.sa + p.m0 + min(row, rows - 1) : p.sb + ((p.n0 + min(row - TM, cols - 1)) >> a.b_shift);
+    scale_ld[i] = row < TM ? a.ldsa : a.ldsb;
+  }
   const auto fetch_scales = [&](int b) {
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int row = tid + 256 * i, block = min(b, blocks - 1);
-      byte[i] = row < TM ? p.sa[block * a.ldsa + p.m0 + min(row, rows - 1)]
-                         : p.sb[block * a.ldsb + ((p.n0 + min(row - TM, cols - 1)) >> a.b_shift)];
-    }
+    for (int i = 0; i < kMine; ++i) byte[i] = scale_at[i][min(b, blocks - 1) * scale_ld[i]];
   };
   const auto keep_scales = [&](int b) {
 #pragma unroll
@@ -411,9 +424,9 @@ __global__ __launch_bounds__(256, (WM * WN > 32 ? 1 : 2)) void tile_kernel(Produ
     keep_scales(0);
     fetch_scales(1);
     keep_scales(1);
-    load(0);
+    load(0, 0, kLoads);
     drain_and_meet();
-    load(1);
+    load(1, 0, kLoads);
     fetch_scales(2);
     read_scales(0, sa, sb);
 #pragma unroll
@@ -421,19 +434,21 @@ __global__ __launch_bounds__(256, (WM * WN > 32 ? 1 : 2)) void tile_kernel(Produ
 #pragma unroll
     for (int i = 0; i < kHalf; ++i) fa[i] = frag(fa0 + i * 2048, 0);
 
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): in the loop the compiler then counts LDS reads only
     for (int b = 0; b < blocks; ++b) {
       const int here = (b & 1) * kStage, next = kStage - here;
       static_for<kHalf>([&](auto ic) {
         constexpr int i = decltype(ic)::value;
-        fa[kHalf + i] = frag(fa0 + (kHalf + i) * 2048, here);
-        static_for<WN>([&](auto jc) { multiply<i, decltype(jc)::value>(acc, fa, fb, sa, sb); });
-        static_for<WN / 4>([&](auto jc) { stay_before(&acc[i][4 * decltype(jc)::value]); });
+        static_for<WN>([&](auto jc) {
+          constexpr int j = decltype(jc)::value;
+          if (j == 1) fa[kHalf + i] = frag(fa0 + (kHalf + i) * 2048, here);
+          multiply<i % 4, j % 4>(acc[i][j], fa[i], fb[j], sa[i / 4], sb[j / 4]);
+        });
         __builtin_amdgcn_sched_barrier(0);
       });
       drain_and_meet();
       keep_scales(b + 2);
       __builtin_amdgcn_sched_barrier(0);
-      load(b + 2);
       fetch_scales(b + 3);
       uint32_t next_sa[(WM + 3) / 4], next_sb[(WN + 3) / 4];
       read_scales(b + 1, next_sa, next_sb);
@@ -441,7 +456,11 @@ __global__ __launch_bounds__(256, (WM * WN > 32 ? 1 : 2)) void tile_kernel(Produ
         constexpr int j = decltype(jc)::value;
 #pragma unroll
         for (int i = j * kHalf / WN; i < (j + 1) * kHalf / WN; ++i) fa[i] = frag(fa0 + i * 2048, next);
-        static_for<kHalf>([&](auto ic) { multiply<kHalf + decltype(ic)::value, j>(acc, fa, fb, sa, sb); });
+        load(b + 2, j * kLoads / WN, (j + 1) * kLoads / WN);
+        static_for<kHalf>([&](auto ic) {
+          constexpr int i = kHalf + decltype(ic)::value;
+          multiply<i % 4, j % 4>(acc[i][j], fa[i], fb[j], sa[i / 4], sb[j / 4]);
+        });
         fb[j] = frag(fb0 + j * 2048, next);
         __builtin_amdgcn_sched_barrier(0);
       });
@@ -452,6 +471,10 @@ __global__ __launch_bounds__(256, (WM * WN > 32 ? 1 : 2)) void tile_kernel(Produ
     }
     drain_and_meet();  // no load may land in what LDS is used for next, here or in another workgroup
   }
+#pragma unroll
+  for (int i = 0; i < WM; ++i)
+#pragma unroll
+    for (int j = 0; j < WN; ++j) settle(acc[i][j]);
   switch (a.dtype) {  // the same for the whole launch
     case WS_OUT_F32: return store_tile<float, WM, WN>(a, p, acc, smem, wm, wn, rows, cols);
     case WS_OUT_BF16: return store_tile<bf16_t, WM, WN>(a, p, acc, smem, wm, wn, rows, cols);
