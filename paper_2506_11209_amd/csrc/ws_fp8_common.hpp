@@ -127,6 +127,12 @@ __device__ __forceinline__ GroupTile find_group_tile(const int32_t* offsets, int
   return GroupTile{-1, 0, 0, 0, before};
 }
 
+// All tiles of the groups and of the rows after the last one.
+__device__ __forceinline__ int64_t count_group_tiles(const int32_t* offsets, int groups, int64_t rows, int size) {
+  const GroupTile g = find_group_tile(offsets, groups, rows, size, (int64_t)1 << 60, true);
+  return uniform(g.before);
+}
+
 // -- host ---------------------------------------------------------------------
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

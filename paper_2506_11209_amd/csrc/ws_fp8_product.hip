@@ -21,6 +21,7 @@
 // a wave covers 64 neighbouring bytes of every row.  The operands are passed in
 // exchanged order (B's rows first): a lane then ends up with four neighbouring
 // columns of one row of C.
+#include <atomic>
 #include <type_traits>
 
 #include "ws_fp8_common.hpp"
@@ -149,7 +150,8 @@ __device__ __forceinline__ i32x8_t join(i32x4_t lo, i32x4_t hi) {
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
-__device__ __forceinline__ float scale_value(int byte) { return __uint_as_float(byte ? (uint32_t)byte << 23 : 1u << 22); }
+// 2^(byte - 127); 2^-127 is subnormal.
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(max(byte << 23, 1u << 22)); }
 
 // Eight codes (two dwords) times a scale, exactly.
 __device__ __forceinline__ bf16x8_t widen(int lo, int hi, float scale) {
@@ -233,10 +235,12 @@ __global__ __launch_bounds__(512) void direct_kernel(ProductArgs a) {
 
 #define WSG_LDS __attribute__((address_space(3)))
 
-// Byte position, in a row of 128, of 16-byte chunk c of tile row r.  Sixteen
-// rows' reads of one chunk fall on different banks, and the choice depends on
-// r % 16 only, which is fixed for a lane.
-__device__ __forceinline__ int chunk_at(int r, int c) { return (c ^ ((r ^ ((r >> 3) & 1)) & 7)) * 16; }
+// Byte position, in a row of 128, of 16-byte chunk c of tile row r.  The operand
+// read (lane l: row l % 16, chunk l / 16 or four more) is free of bank conflicts
+// so; with (r ^ r / 8 % 2) % 8, which suits reads of 32 rows, it took twice as long
+// (SQ_LDS_BANK_CONFLICT).  The choice depends on r % 16 only, which is fixed for
+// a lane.
+__device__ __forceinline__ int chunk_at(int r, int c) { return (c ^ (r & 7)) * 16; }
 
 // A buffer descriptor as four scalars, for asm.
 __device__ __forceinline__ i32x4_t raw_buffer(const uint8_t* base, uint32_t bytes) {
@@ -266,28 +270,92 @@ __device__ __forceinline__ void drain_and_meet() {
 #endif
 }
 
+template <int WM, int WN>
+struct TileShape {
+  static constexpr int TM = 32 * WM, TN = 32 * WN, kStage = (TM + TN) * kBlock;
+  static constexpr int kMine = (TM + TN + 255) / 256;  // a thread's rows of scales
+  // One wave a SIMD with sums in accumulation registers, or two with all in the others.
+  static constexpr int kWaves = WM * WN > 16 ? 1 : 2;
+  static constexpr bool kAgpr = kWaves == 1;
+  // LDS: two stages, two blocks of scales, and for every wave 16 rows of what it
+  // stores at a time, as many columns as fit
+  static constexpr int kStoreAt = 2 * kStage + 2 * (TM + TN), kStoreCols = kWaves == 1 ? 64 : 32, kStoreParts = 16 * WN / kStoreCols;
+  static constexpr int kPitch = kStoreCols + 4;  // the pitch spreads rows over the banks
+  static constexpr int kStoreBytes = 16 * kPitch * 4, kLds = kStoreAt + 4 * kStoreBytes;
+  static_assert(kWaves * kLds <= 160 * 1024, "LDS of a CU");
+};
+
+// A column of B just widened, two wait states before its first product.
+__device__ __forceinline__ void settle_wide(i32x4_t& f) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_nop 1" : "+v"(f));
+#endif
+}
+
+// Keeps what reads acc behind the asm statements before, the wait for the last
+// products among them.
+template <bool AGPR>
+__device__ __forceinline__ void settle(f32x4_t& acc) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (AGPR) asm volatile("" : "+a"(acc));
+  else asm volatile("" : "+v"(acc));
+#endif
+}
+
 // Writes a wave's part of a tile, 16 rows at a time by way of its own part of LDS,
-// so that a store covers whole stretches of a row.  rows, cols: of the tile, inside C.
+// so that a store covers whole stretches of a row.  Whole tiles to which nothing
+// is added are rounded before LDS and leave in 16-byte pieces, at addresses that
+// differ by scalars only; others pass LDS in binary32.
+// rows, cols: of the tile, inside C.
 template <typename T, int WM, int WN>
-__device__ __forceinline__ void store_tile(const ProductArgs& a, const Part& p, const f32x4_t (&acc)[WM][WN], uint8_t* smem, int wm,
-                                           int wn, int rows, int cols) {
-  constexpr int kCols = 16 * WN, kPitch = kCols + 4;  // floats; the pitch spreads rows over the banks
+__device__ __forceinline__ void store_tile(const ProductArgs& a, const Part& p, f32x4_t (&acc)[WM][WN], uint8_t* own, int wm, int wn,
+                                           int rows, int cols) {
+  typedef TileShape<WM, WN> Shape;
+  constexpr int kCols = Shape::kStoreCols, kPitch = Shape::kPitch, kTiles = kCols / 16;
+  constexpr int N = 16 / sizeof(T), kRow = kCols * (int)sizeof(T) + 16, kPieces = kCols / N, kAtOnce = 64 / kPieces;  // kRow: bytes
+  static_assert(16 * kRow <= Shape::kStoreBytes && 64 % kPieces == 0 && 16 % kAtOnce == 0, "16 rows in whole stores");
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  float* own = (float*)smem + (threadIdx.x >> 6) * 16 * kPitch;
+  const bool whole = a.beta == 0.0f && rows == Shape::TM && cols == Shape::TN && a.ldc <= (1 << 22);
+  const uint32_t ld = (uint32_t)a.ldc * (uint32_t)sizeof(T);  // bytes; used where whole
+  uint8_t* const to = (uint8_t*)a.C + uniform((p.c_at + (p.m0 + wm * 16 * WM) * a.ldc + p.n0 + wn * 16 * WN) * (int64_t)sizeof(T));
+  const uint32_t mine = lane / kPieces * ld + lane % kPieces * 16;
+  const uint8_t* const from = own + lane / kPieces * kRow + lane % kPieces * 16;
 #pragma unroll
-  for (int i = 0; i < WM; ++i) {
+  for (int i = 0; i < WM; ++i)
 #pragma unroll
-    for (int j = 0; j < WN; ++j) *(f32x4_t*)(own + r * kPitch + 16 * j + 4 * g) = acc[i][j];
-    __builtin_amdgcn_wave_barrier();  // a wave's LDS accesses keep their order
+    for (int h = 0; h < Shape::kStoreParts; ++h) {
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j) settle<Shape::kAgpr>(acc[i][h * kTiles + j]);
+      if (whole) {
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) {
+          T t[4];
+          for (int k = 0; k < 4; ++k) t[k] = from_f32<T>(a.alpha * acc[i][h * kTiles + j][k]);
+          __builtin_memcpy(__builtin_assume_aligned(own + r * kRow + (16 * j + 4 * g) * sizeof(T), 4 * sizeof(T)), t, sizeof(t));
+        }
+        __builtin_amdgcn_wave_barrier();  // a wave's LDS accesses keep their order
+#pragma unroll
+        for (int e = 0; e < 16; e += kAtOnce) {
+          T t[N];
+          __builtin_memcpy(t, __builtin_assume_aligned(from + e * kRow, 16), 16);
+          store_n<T, N>((T*)(to + (uint64_t)(16 * i + e) * ld + h * kCols * sizeof(T) + mine), t);
+        }
+      } else {
+        float* f = (float*)own;
+        const int n0 = wn * 16 * WN + h * kCols;
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) *(f32x4_t*)(f + r * kPitch + 16 * j + 4 * g) = acc[i][h * kTiles + j];
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-    for (int e = lane; e < 4 * kCols; e += 64) {
-      const int row = (wm * WM + i) * 16 + e / (kCols / 4), at = e % (kCols / 4) * 4, col = wn * kCols + at;
-      float v[4];
-      *(f32x4_t*)v = *(const f32x4_t*)(own + e / (kCols / 4) * kPitch + at);
-      if (row < rows && col < cols) store4<T>(a, p, p.m0 + row, p.n0 + col, v);
+        for (int e = lane; e < 4 * kCols; e += 64) {
+          const int row = (wm * WM + i) * 16 + e / (kCols / 4), at = e % (kCols / 4) * 4, col = n0 + at;
+          float v[4];
+          *(f32x4_t*)v = *(const f32x4_t*)(f + e / (kCols / 4) * kPitch + at);
+          if (row < rows && col < cols) store4<T>(a, p, p.m0 + row, p.n0 + col, v);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_wave_barrier();
-  }
 }
 
 template <int N, typename F>
@@ -301,24 +369,48 @@ __device__ __forceinline__ void static_for(const F& f) {
 // acc += A's 16 rows times B's 16 rows, each operand's scale in byte SA or SB of
 // its dword.  As asm with the sum in place: the compiler's own form of it moved
 // sums between registers (4 copies and a wait for each of a row's products), and
-// what has no side effects does not stay on its side of a barrier.  The wait
-// states are those after a VALU write of an operand; they pass while the matrix
-// unit is busy with the product before.
-template <int SA, int SB>
+// what has no side effects does not stay on its side of a barrier.  An operand may
+// not come from a VALU instruction less than two wait states before: fragments
+// come from LDS, scales by way of settle_scales.
+template <bool AGPR, int SA, int SB>
 __device__ __forceinline__ void multiply(f32x4_t& acc, const i32x8_t& fa, const i32x8_t& fb, uint32_t sa, uint32_t sb) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile(
-      "s_nop 1\n\t"
-      "v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]"
-      : "+a"(acc)
-      : "v"(fb), "v"(fa), "v"(sb), "v"(sa), "n"(SB & 1), "n"(SA & 1), "n"(SB >> 1), "n"(SA >> 1));
+#define WSG_MULTIPLY(c)                                                                            \
+  asm volatile(                                                                                    \
+      "v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[%5,%6,0] op_sel_hi:[%7,%8,0]" \
+      : c(acc)                                                                                     \
+      : "v"(fb), "v"(fa), "v"(sb), "v"(sa), "n"(SB & 1), "n"(SA & 1), "n"(SB >> 1), "n"(SA >> 1))
+  if constexpr (AGPR) WSG_MULTIPLY("+a");
+  else WSG_MULTIPLY("+v");
+#undef WSG_MULTIPLY
 #endif
 }
 
-// Lets the last products into acc finish before anything reads it.
-__device__ __forceinline__ void settle(f32x4_t& acc) {
+// The same for 32 of the 128 columns with operands widened to bf16.
+template <bool AGPR>
+__device__ __forceinline__ void multiply_wide(f32x4_t& acc, const i32x4_t& fa, const i32x4_t& fb) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("s_nop 15" : "+a"(acc));
+  if constexpr (AGPR) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(fb), "v"(fa));
+  else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(fb), "v"(fa));
+#endif
+}
+
+// An operand's 128 columns in bf16, from its codes and byte `i` of its scales.
+struct Wide {
+  i32x4_t part[4];
+};
+__device__ __forceinline__ Wide widen_all(const i32x8_t& f, uint32_t scales, int i) {
+  const float s = scale_value((scales >> 8 * i) & 255u);
+  Wide w;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) w.part[q] = __builtin_bit_cast(i32x4_t, widen(f[2 * q], f[2 * q + 1], s));
+  return w;
+}
+
+// Scales just moved, two wait states before their first product.
+__device__ __forceinline__ void settle_scales(uint32_t& s) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_nop 1" : "+v"(s));
 #endif
 }
 
@@ -335,30 +427,35 @@ __device__ __forceinline__ void settle(f32x4_t& acc) {
 // block's time, and one set of registers for each operand.  Scales lie in LDS as
 // [row % 16][row / 16], so that a lane reads those of all its rows at once and
 // the instruction picks a byte.
-template <int WM, int WN, int MODE>
-__global__ __launch_bounds__(256, (WM * WN > 32 ? 1 : 2)) void tile_kernel(ProductArgs a) {
-  constexpr int TM = 32 * WM, TN = 32 * WN, kStage = (TM + TN) * kBlock, kRows = TM + TN, kHalf = WM / 2;
+// WIDE: results in 32 bits.  A half's rows of A are widened at its start, a column
+// of B before its products, those of the next column between them.
+//
+// A workgroup takes every gridDim.x-th of an XCD's tiles.  It starts the loads of its
+// next tile before it stores the one it has, in LDS of their own, so that memory
+// is written and read while neither is waited for.
+template <int WM, int WN, int MODE, bool WIDE>
+__global__ __launch_bounds__(256, (TileShape<WM, WN>::kWaves)) void tile_kernel(ProductArgs a) {
+  typedef TileShape<WM, WN> Shape;
+  constexpr int TM = Shape::TM, TN = Shape::TN, kStage = Shape::kStage, kRows = TM + TN, kHalf = WM / 2;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
 
-  // neighbouring tiles on one XCD (workgroups go round the XCDs in turn), eight
-  // rows of tiles at a time
-  const uint32_t tiles = a.tiles_m * a.tiles_n, group = MODE == kDepthGroups ? blockIdx.x / tiles : 0;
-  uint32_t id = MODE == kDepthGroups ? blockIdx.x % tiles : blockIdx.x;
-  {
-    const uint32_t per = tiles / 8, rest = tiles % 8, x = id % 8;
-    id = x * per + min(x, rest) + id / 8;
-  }
-  const uint32_t wide = 8 * (uint32_t)a.tiles_n, first = id / wide * 8, high = min(8u, (uint32_t)a.tiles_m - first);
-  const uint32_t in = id % wide;
-  Part p;
-  if (!find_part<MODE>(a, first + in % high, in / high, group, TM, TN, &p)) return;
-  const int rows = (int)min(p.m_end - p.m0, (int64_t)TM), cols = (int)min(a.N - p.n0, (int64_t)TN);
-  const int K = p.zero ? 0 : (int)p.K, blocks = (K + kBlock - 1) / kBlock;
-  const i32x4_t ra = raw_buffer(p.A + p.m0 * a.lda, (uint32_t)(rows * a.lda));
-  const i32x4_t rb = raw_buffer(p.B + p.n0 * a.ldb, (uint32_t)(cols * a.ldb));
+  // Tiles: an XCD (workgroups go round them in turn) has a run of them, eight rows
+  // of tiles at a time, so that those of one moment share operands in its L2.
+  uint32_t tiles_m = (uint32_t)a.tiles_m;
+  if (MODE == kRowGroups) tiles_m = (uint32_t)count_group_tiles(a.offsets, a.groups, a.M, TM);
+  const uint32_t tiles_n = (uint32_t)a.tiles_n, plane = tiles_m * tiles_n, tiles = plane * (MODE == kDepthGroups ? a.groups : 1);
+  const uint32_t xcd = blockIdx.x % 8, share = tiles / 8, extra = tiles % 8, begin = xcd * share + min(xcd, extra),
+                 end = begin + share + (xcd < extra), stride = (gridDim.x + 7 - xcd) / 8;
+  uint32_t id = begin + blockIdx.x / 8;
 
+  struct Tile {
+    Part p;
+    int rows, cols, K, blocks;
+    i32x4_t ra, rb;
+    const uint8_t* scale_at[Shape::kMine];
+  } t;
   // loads: wave w takes the tile's row octets w, w + 4, ..
   const int lr = 8 * wave + (lane >> 3), lc = chunk_at(lr, lane & 7);  // chunk_at is its own inverse
   const uint32_t at_a = (uint32_t)(lr * a.lda + lc), at_b = (uint32_t)(lr * a.ldb + lc);
@@ -366,123 +463,193 @@ __global__ __launch_bounds__(256, (WM * WN > 32 ? 1 : 2)) void tile_kernel(Produ
   const uint32_t lds0 = (uint32_t)(uintptr_t)(WSG_LDS uint8_t*)smem + wave * 1024;
   constexpr int kLoads = (TM + TN) / 32;  // of a wave and block, 1 KiB each
   const auto load = [&](int b, int from, int to) {
-    const bool inside = b * kBlock + lc < K;  // else zeros: past the last column
+    const bool inside = b * kBlock + lc < t.K;  // else zeros: past the last column
     const uint32_t ia = inside ? at_a : kOutside, ib = inside ? at_b : kOutside, lds = lds0 + (b & 1) * kStage;
 #pragma unroll
-    for (int t = from; t < to; ++t) {
-      if (t < TM / 32) load_to_lds(ra, ia + t * step_a, b * kBlock, lds + t * 4096);
-      else load_to_lds(rb, ib + (t - TM / 32) * step_b, b * kBlock, lds + t * 4096);
+    for (int i = from; i < to; ++i) {
+      if (i < TM / 32) load_to_lds(t.ra, ia + i * step_a, b * kBlock, lds + i * 4096);
+      else load_to_lds(t.rb, ib + (i - TM / 32) * step_b, b * kBlock, lds + i * 4096);
     }
   };
-
   // scales of this thread's rows of the tile
-  constexpr int kMine = (kRows + 255) / 256;
   uint8_t* scales = smem + 2 * kStage;
-  uint8_t byte[kMine];
-  const uint8_t* scale_at[kMine];
-  int64_t scale_ld[kMine];
+  typedef uint8_t bytes_t[Shape::kMine];
+  const auto fetch_scales = [&](int b, bytes_t& byte) {
 #pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    const int row = tid + 256 * i;
-    scale_at[i] = row < TM ? p.sa + p.m0 + min(row, rows - 1) : p.sb + ((p.n0 + min(row - TM, cols - 1)) >> a.b_shift);
-    scale_ld[i] = row < TM ? a.ldsa : a.ldsb;
-  }
-  const auto fetch_scales = [&](int b) {
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) byte[i] = scale_at[i][min(b, blocks - 1) * scale_ld[i]];
+    for (int i = 0; i < Shape::kMine; ++i)
+      byte[i] = t.scale_at[i][min(b, t.blocks - 1) * (tid + 256 * i < TM ? a.ldsa : a.ldsb)];
   };
-  const auto keep_scales = [&](int b) {
+  const auto keep_scales = [&](int b, const bytes_t& byte) {
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
+    for (int i = 0; i < Shape::kMine; ++i) {
       const int row = tid + 256 * i;
       if (kRows % 256 == 0 || row < kRows)
         scales[(b & 1) * kRows + (row < TM ? row % 16 * (2 * WM) + row / 16 : TM + (row - TM) % 16 * (2 * WN) + (row - TM) / 16)] =
             byte[i];
     }
   };
-
-  f32x4_t acc[WM][WN];
+  bytes_t byte0, byte1, byte;
+  // Finds tile `id` and starts on its first two blocks.
+  const auto begin_tile = [&]() {
+    const uint32_t group = MODE == kDepthGroups ? id / plane : 0, at = MODE == kDepthGroups ? id % plane : id;
+    const uint32_t wide = 8 * tiles_n, first = at / wide * 8, high = min(8u, tiles_m - first), in = at % wide;
+    find_part<MODE>(a, first + in % high, in / high, group, TM, TN, &t.p);
+    t.rows = (int)min(t.p.m_end - t.p.m0, (int64_t)TM);
+    t.cols = (int)min(a.N - t.p.n0, (int64_t)TN);
+    t.K = t.p.zero ? 0 : (int)t.p.K;
+    t.blocks = (t.K + kBlock - 1) / kBlock;
+    if (t.blocks == 0) return;
+    t.ra = raw_buffer(t.p.A + t.p.m0 * a.lda, (uint32_t)(t.rows * a.lda));
+    t.rb = raw_buffer(t.p.B + t.p.n0 * a.ldb, (uint32_t)(t.cols * a.ldb));
 #pragma unroll
-  for (int i = 0; i < WM; ++i)
-#pragma unroll
-    for (int j = 0; j < WN; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
-
-  if (blocks > 0) {
-    const int fa0 = (wm * WM * 16 + r) * kBlock, fb0 = (TM + wn * WN * 16 + r) * kBlock, c0 = chunk_at(r, g), c1 = chunk_at(r, g + 4);
-    i32x8_t fa[WM], fb[WN];
-    uint32_t sa[(WM + 3) / 4], sb[(WN + 3) / 4];
-    const auto frag = [&](int row, int stage) {
-      const uint8_t* f = smem + stage + row;
-      return join(*(const i32x4_t*)(f + c0), *(const i32x4_t*)(f + c1));
-    };
-    const auto read_scales = [&](int b, uint32_t* sa, uint32_t* sb) {
-      const uint8_t* s = scales + (b & 1) * kRows;
-      __builtin_memcpy(sa, __builtin_assume_aligned(s + (2 * r + wm) * WM, WM), WM);
-      __builtin_memcpy(sb, __builtin_assume_aligned(s + TM + (2 * r + wn) * WN, WN), WN);
-    };
-    fetch_scales(0);
-    keep_scales(0);
-    fetch_scales(1);
-    keep_scales(1);
-    load(0, 0, kLoads);
-    drain_and_meet();
-    load(1, 0, kLoads);
-    fetch_scales(2);
-    read_scales(0, sa, sb);
-#pragma unroll
-    for (int j = 0; j < WN; ++j) fb[j] = frag(fb0 + j * 2048, 0);
-#pragma unroll
-    for (int i = 0; i < kHalf; ++i) fa[i] = frag(fa0 + i * 2048, 0);
-
-    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): in the loop the compiler then counts LDS reads only
-    for (int b = 0; b < blocks; ++b) {
-      const int here = (b & 1) * kStage, next = kStage - here;
-      static_for<kHalf>([&](auto ic) {
-        constexpr int i = decltype(ic)::value;
-        static_for<WN>([&](auto jc) {
-          constexpr int j = decltype(jc)::value;
-          if (j == 1) fa[kHalf + i] = frag(fa0 + (kHalf + i) * 2048, here);
-          multiply<i % 4, j % 4>(acc[i][j], fa[i], fb[j], sa[i / 4], sb[j / 4]);
-        });
-        __builtin_amdgcn_sched_barrier(0);
-      });
-      drain_and_meet();
-      keep_scales(b + 2);
-      __builtin_amdgcn_sched_barrier(0);
-      fetch_scales(b + 3);
-      uint32_t next_sa[(WM + 3) / 4], next_sb[(WN + 3) / 4];
-      read_scales(b + 1, next_sa, next_sb);
-      static_for<WN>([&](auto jc) {
-        constexpr int j = decltype(jc)::value;
-#pragma unroll
-        for (int i = j * kHalf / WN; i < (j + 1) * kHalf / WN; ++i) fa[i] = frag(fa0 + i * 2048, next);
-        load(b + 2, j * kLoads / WN, (j + 1) * kLoads / WN);
-        static_for<kHalf>([&](auto ic) {
-          constexpr int i = kHalf + decltype(ic)::value;
-          multiply<i % 4, j % 4>(acc[i][j], fa[i], fb[j], sa[i / 4], sb[j / 4]);
-        });
-        fb[j] = frag(fb0 + j * 2048, next);
-        __builtin_amdgcn_sched_barrier(0);
-      });
-#pragma unroll
-      for (int i = 0; i < (WM + 3) / 4; ++i) sa[i] = next_sa[i];
-#pragma unroll
-      for (int j = 0; j < (WN + 3) / 4; ++j) sb[j] = next_sb[j];
+    for (int i = 0; i < Shape::kMine; ++i) {
+      const int row = tid + 256 * i;
+      t.scale_at[i] = row < TM ? t.p.sa + t.p.m0 + min(row, t.rows - 1) : t.p.sb + ((t.p.n0 + min(row - TM, t.cols - 1)) >> a.b_shift);
     }
-    drain_and_meet();  // no load may land in what LDS is used for next, here or in another workgroup
-  }
+    fetch_scales(0, byte0);
+    fetch_scales(1, byte1);
+    fetch_scales(2, byte);
+    load(0, 0, kLoads);
+    load(1, 0, kLoads);
+  };
+
+  if (id < end) begin_tile();
+  while (id < end) {
+    f32x4_t acc[WM][WN];
 #pragma unroll
-  for (int i = 0; i < WM; ++i)
+    for (int i = 0; i < WM; ++i)
 #pragma unroll
-    for (int j = 0; j < WN; ++j) settle(acc[i][j]);
-  switch (a.dtype) {  // the same for the whole launch
-    case WS_OUT_F32: return store_tile<float, WM, WN>(a, p, acc, smem, wm, wn, rows, cols);
-    case WS_OUT_BF16: return store_tile<bf16_t, WM, WN>(a, p, acc, smem, wm, wn, rows, cols);
-    default: return store_tile<f16_t, WM, WN>(a, p, acc, smem, wm, wn, rows, cols);
+      for (int j = 0; j < WN; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
+    if (t.blocks > 0) {
+      const int fa0 = (wm * WM * 16 + r) * kBlock, fb0 = (TM + wn * WN * 16 + r) * kBlock, c0 = chunk_at(r, g), c1 = chunk_at(r, g + 4);
+      i32x8_t fa[WM], fb[WN];
+      uint32_t sa[(WM + 3) / 4], sb[(WN + 3) / 4];
+      const auto frag = [&](int row, int stage) {
+        const uint8_t* f = smem + stage + row;
+        return join(*(const i32x4_t*)(f + c0), *(const i32x4_t*)(f + c1));
+      };
+      const auto read_scales = [&](int b, uint32_t* sa, uint32_t* sb) {
+        const uint8_t* s = scales + (b & 1) * kRows;
+        __builtin_memcpy(sa, __builtin_assume_aligned(s + (2 * r + wm) * WM, WM), WM);
+        __builtin_memcpy(sb, __builtin_assume_aligned(s + TM + (2 * r + wn) * WN, WN), WN);
+      };
+      keep_scales(0, byte0);
+      keep_scales(1, byte1);
+      drain_and_meet();
+      read_scales(0, sa, sb);
+#pragma unroll
+      for (int j = 0; j < WN; ++j) fb[j] = frag(fb0 + j * 2048, 0);
+#pragma unroll
+      for (int i = 0; i < kHalf; ++i) fa[i] = frag(fa0 + i * 2048, 0);
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): in the loop the compiler then counts LDS reads only
+      for (int b = 0; b < t.blocks; ++b) {
+        const int here = (b & 1) * kStage, next = kStage - here;
+        if constexpr (WIDE) {
+          Wide wa[kHalf], wb = widen_all(fb[0], sb[0], 0);
+#pragma unroll
+          for (int i = 0; i < kHalf; ++i) wa[i] = widen_all(fa[i], sa[i / 4], i % 4);
+          static_for<WN>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            __builtin_amdgcn_sched_barrier(0);
+            settle_wide(wb.part[0]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)  // a sum's next product comes after the other rows'
+#pragma unroll
+              for (int i = 0; i < kHalf; ++i) multiply_wide<Shape::kAgpr>(acc[i][j], wa[i].part[q], wb.part[q]);
+#pragma unroll
+            for (int k = j * kHalf / WN; k < (j + 1) * kHalf / WN; ++k) fa[kHalf + k] = frag(fa0 + (kHalf + k) * 2048, here);
+            if constexpr (j + 1 < WN) wb = widen_all(fb[j + 1], sb[(j + 1) / 4], (j + 1) % 4);
+          });
+          __builtin_amdgcn_sched_barrier(0);
+        } else {
+          static_for<kHalf>([&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            static_for<WN>([&](auto jc) {
+              constexpr int j = decltype(jc)::value;
+              if (j == 1) fa[kHalf + i] = frag(fa0 + (kHalf + i) * 2048, here);
+              multiply<Shape::kAgpr, i % 4, j % 4>(acc[i][j], fa[i], fb[j], sa[i / 4], sb[j / 4]);
+            });
+            __builtin_amdgcn_sched_barrier(0);
+          });
+        }
+        drain_and_meet();
+        keep_scales(b + 2, byte);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_scales(b + 3, byte);
+        uint32_t next_sa[(WM + 3) / 4], next_sb[(WN + 3) / 4];
+        read_scales(b + 1, next_sa, next_sb);
+        // loads one at a time between products: two at once hold up the products behind them
+        constexpr int kPer = kLoads / WN;
+        if constexpr (WIDE) {
+          Wide wa[kHalf], wb = widen_all(fb[0], sb[0], 0);
+#pragma unroll
+          for (int i = 0; i < kHalf; ++i) wa[i] = widen_all(fa[kHalf + i], sa[(kHalf + i) / 4], (kHalf + i) % 4);
+          static_for<WN>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            __builtin_amdgcn_sched_barrier(0);
+            settle_wide(wb.part[0]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+#pragma unroll
+              for (int i = 0; i < kHalf; ++i) multiply_wide<Shape::kAgpr>(acc[kHalf + i][j], wa[i].part[q], wb.part[q]);
+              load(b + 2, j * kPer + q * kPer / 4, j * kPer + (q + 1) * kPer / 4);
+            }
+#pragma unroll
+            for (int k = j * kHalf / WN; k < (j + 1) * kHalf / WN; ++k) fa[k] = frag(fa0 + k * 2048, next);
+            fb[j] = frag(fb0 + j * 2048, next);
+            if constexpr (j + 1 < WN) wb = widen_all(fb[j + 1], sb[(j + 1) / 4], (j + 1) % 4);
+          });
+          __builtin_amdgcn_sched_barrier(0);
+        } else {
+          static_for<WN>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            static_for<kHalf>([&](auto ic) {
+              constexpr int i = decltype(ic)::value, row = kHalf + i;
+              multiply<Shape::kAgpr, row % 4, j % 4>(acc[row][j], fa[row], fb[j], sa[row / 4], sb[j / 4]);
+              load(b + 2, j * kPer + i * kPer / kHalf, j * kPer + (i + 1) * kPer / kHalf);
+              if (i == 0) {
+#pragma unroll
+                for (int k = j * kHalf / WN; k < (j + 1) * kHalf / WN; ++k) fa[k] = frag(fa0 + k * 2048, next);
+                if constexpr (j > 0) fb[j - 1] = frag(fb0 + (j - 1) * 2048, next);
+              }
+            });
+            __builtin_amdgcn_sched_barrier(0);
+          });
+          fb[WN - 1] = frag(fb0 + (WN - 1) * 2048, next);
+        }
+#pragma unroll
+        for (int i = 0; i < (WM + 3) / 4; ++i) settle_scales(sa[i] = next_sa[i]);
+#pragma unroll
+        for (int j = 0; j < (WN + 3) / 4; ++j) settle_scales(sb[j] = next_sb[j]);
+      }
+      asm volatile("s_nop 15\n\ts_nop 15");  // the last sums, before anything may move them
+      drain_and_meet();  // no load of this tile lands, and no wave reads, after this
+    }
+    const Part p = t.p;
+    const int rows = t.rows, cols = t.cols;
+    id += stride;
+    if (id < end) begin_tile();
+    uint8_t* own = smem + Shape::kStoreAt + wave * Shape::kStoreBytes;
+    if constexpr (WIDE) store_tile<float, WM, WN>(a, p, acc, own, wm, wn, rows, cols);
+    else if (a.dtype == WS_OUT_BF16) store_tile<bf16_t, WM, WN>(a, p, acc, own, wm, wn, rows, cols);
+    else store_tile<f16_t, WM, WN>(a, p, acc, own, wm, wn, rows, cols);
   }
 }
 
 // -- host --------------------------------------------------------------------------
+
+// Compute units of the current device, asked for once (256 where it does not say).
+int compute_units() {
+  static std::atomic<int> known[64];
+  int dev = 0, n = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+  n = known[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
+    known[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
 
 // Bytes between rows so that a tile's offsets stay below kOutside.
 constexpr int64_t kMaxLd = 1 << 22;
@@ -500,25 +667,28 @@ ws_status run_direct(ProductArgs a, hipStream_t stream) {
   return launch("fp8_product", kernel, grid, 64 * waves, waves * MT * 1024, stream, a);
 }
 
-template <int WM, int WN, int MODE>
+template <int WM, int WN, int MODE, bool WIDE>
 ws_status run_tiles(ProductArgs a, hipStream_t stream) {
-  constexpr int TM = 32 * WM, TN = 32 * WN, kLds = 2 * (TM + TN) * (kBlock + 1);
+  typedef TileShape<WM, WN> Shape;
+  constexpr int TM = Shape::TM, TN = Shape::TN;
   a.tiles_n = ceil_div(a.N, TN);
   a.tiles_m = MODE == kRowGroups ? group_tiles(a.M, a.groups, TM, true) : ceil_div(a.M, TM);
   const int64_t tiles = a.tiles_n * a.tiles_m, grid = tiles * (MODE == kDepthGroups ? a.groups : 1);
   if (a.tiles_m > kMaxGrid || tiles > kMaxGrid || grid > kMaxGrid) return WS_ERR_INVALID_ARG;
-  const void* fn = (const void*)&tile_kernel<WM, WN, MODE>;
-  const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  const int64_t most = (int64_t)compute_units() * Shape::kWaves;
+  const auto kernel = &tile_kernel<WM, WN, MODE, WIDE>;
+  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, Shape::kLds);
   if (e != hipSuccess) return hip_fail("hipFuncSetAttribute", e);
-  return launch("fp8_product", &tile_kernel<WM, WN, MODE>, grid, 256, kLds, stream, a);
+  return launch("fp8_product", kernel, grid < most ? grid : most, 256, Shape::kLds, stream, a);
 }
 
 template <int MODE>
 ws_status run_product(const ProductArgs& a, hipStream_t stream) {
   const int64_t rows = MODE == kRowGroups ? ceil_div(a.M, a.groups) : a.M;
-  if (a.dtype != WS_OUT_F32 && rows > 64) {
-    if (rows > 512) return run_tiles<8, 8, MODE>(a, stream);
-    return run_tiles<4, 4, MODE>(a, stream);
+  if (rows > 64) {
+    if (a.dtype == WS_OUT_F32)
+      return rows > 512 ? run_tiles<8, 4, MODE, true>(a, stream) : run_tiles<4, 4, MODE, true>(a, stream);
+    return rows > 512 ? run_tiles<8, 8, MODE, false>(a, stream) : run_tiles<4, 4, MODE, false>(a, stream);
   }
   if (rows <= 16) return run_direct<1, 4, MODE>(a, stream);
   if (rows <= 32) return run_direct<2, 4, MODE>(a, stream);
