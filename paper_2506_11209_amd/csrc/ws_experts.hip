@@ -9,7 +9,8 @@ namespace {
 
 constexpr int kSortWaves = 8;
 constexpr int kSortThreads = 64 * kSortWaves;
-constexpr int64_t kSortChunk = 2048;   // slots of a workgroup: four steps a wave
+constexpr int kSortSteps = 4;          // steps of 64 slots whose ids a wave loads at once
+constexpr int64_t kSortChunk = kSortSteps * kSortThreads;  // slots of a workgroup
 constexpr int64_t kSortAlone = 4096;   // slots that one workgroup sorts by itself
 constexpr int64_t kSortBlocks = 256;   // chunks at the most; beyond, chunks grow
 
@@ -60,6 +61,11 @@ __device__ __forceinline__ int take_step(const SortArgs& a, int e, int32_t* mine
   return before;
 }
 
+__device__ __forceinline__ void load_steps(const SortArgs& a, int64_t s0, int64_t hi, int (&e)[kSortSteps]) {
+#pragma unroll
+  for (int i = 0; i < kSortSteps; ++i) e[i] = slot_expert(a, s0 + 64 * i + (threadIdx.x & 63), hi);
+}
+
 // counts[w][e] of this workgroup's waves, in LDS.
 __device__ __forceinline__ void count_slots(const SortArgs& a, int32_t* counts) {
   for (int i = threadIdx.x; i < kSortWaves * a.experts; i += kSortThreads) counts[i] = 0;
@@ -67,7 +73,12 @@ __device__ __forceinline__ void count_slots(const SortArgs& a, int32_t* counts) 
   int64_t lo, hi;
   wave_share(a, &lo, &hi);
   int32_t* mine = counts + (threadIdx.x >> 6) * a.experts;
-  for (int64_t s0 = lo; s0 < hi; s0 += 64) take_step(a, slot_expert(a, s0 + (threadIdx.x & 63), hi), mine);
+  for (int64_t s0 = lo; s0 < hi; s0 += 64 * kSortSteps) {
+    int e[kSortSteps];
+    load_steps(a, s0, hi, e);
+#pragma unroll
+    for (int i = 0; i < kSortSteps; ++i) take_step(a, e[i], mine);
+  }
   __syncthreads();
 }
 
@@ -96,10 +107,15 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortArgs a) {
   for (int e = tid; e < a.experts; e += kSortThreads) {
     int run = 0, all = 0;
     if constexpr (!ALONE)
-      for (int64_t b = 0; b < a.blocks; ++b) {
-        const int n = a.counts[b * a.experts + e];
-        if (b < (int64_t)blockIdx.x) run += n;
-        all += n;
+      for (int b0 = 0; b0 < (int)a.blocks; b0 += 16) {  // 16 loads at once
+        int n[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) n[i] = b0 + i < (int)a.blocks ? a.counts[(int64_t)(b0 + i) * a.experts + e] : 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          run += b0 + i < (int)blockIdx.x ? n[i] : 0;
+          all += n[i];
+        }
       }
     for (int w = 0; w < kSortWaves; ++w) {
       const int n = counts[w * a.experts + e];
@@ -135,16 +151,20 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortArgs a) {
   int64_t lo, hi;
   wave_share(a, &lo, &hi);
   int32_t* mine = counts + wave * a.experts;
-  for (int64_t s0 = lo; s0 < hi; s0 += 64) {
-    const int64_t s = s0 + lane;
-    const int e = slot_expert(a, s, hi);
-    const int before = take_step(a, e, mine);
-    if (e >= 0) {
-      const int row = first[e] + before;
-      a.place[s] = row;
-      a.token[row] = (int32_t)(s / a.k);
-    } else if (s < hi) {
-      a.place[s] = -1;
+  for (int64_t s0 = lo; s0 < hi; s0 += 64 * kSortSteps) {
+    int e[kSortSteps];
+    load_steps(a, s0, hi, e);
+#pragma unroll
+    for (int i = 0; i < kSortSteps; ++i) {
+      const int64_t s = s0 + 64 * i + lane;
+      const int before = take_step(a, e[i], mine);
+      if (e[i] >= 0) {
+        const int row = first[e[i]] + before;
+        a.place[s] = row;
+        a.token[row] = (int32_t)((uint32_t)s / (uint32_t)a.k);
+      } else if (s < hi) {
+        a.place[s] = -1;
+      }
     }
   }
 }

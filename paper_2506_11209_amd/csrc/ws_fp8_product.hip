@@ -677,7 +677,13 @@ ws_status run_tiles(ProductArgs a, hipStream_t stream) {
   if (a.tiles_m > kMaxGrid || tiles > kMaxGrid || grid > kMaxGrid) return WS_ERR_INVALID_ARG;
   const int64_t most = (int64_t)compute_units() * Shape::kWaves;
   const auto kernel = &tile_kernel<WM, WN, MODE, WIDE>;
-  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, Shape::kLds);
+  static std::atomic<uint64_t> allowed;  // devices on which the kernel may use this much LDS
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess && (dev >= 64 || !(allowed.load(std::memory_order_acquire) >> dev & 1))) {
+    e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, Shape::kLds);
+    if (e == hipSuccess && dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_acq_rel);
+  }
   if (e != hipSuccess) return hip_fail("hipFuncSetAttribute", e);
   return launch("fp8_product", kernel, grid < most ? grid : most, 256, Shape::kLds, stream, a);
 }

@@ -105,6 +105,27 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
   if (j < 4 && r0 + i < a.rows && (ct * 4 + j) * kBlock < a.cols) a.scales[(ct * 4 + j) * a.ld_scales + r0 + i] = sc[j][i];
 }
 
+// Eight elements as they lie in memory.  forget(): what was computed from them is
+// not kept in registers (widened, a thread's 64 would take two waves' registers).
+template <typename T>
+struct Raw8 {
+  uint32_t w[2 * sizeof(T)];
+  __device__ __forceinline__ float operator[](int j) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
+    const uint16_t h = (uint16_t)(w[j / 2] >> (j % 2 * 16));
+    return to_f32(__builtin_bit_cast(T, h));
+  }
+  __device__ __forceinline__ void forget() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (sizeof(T) == 2) asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
+#endif
+  }
+};
+template <>
+__device__ __forceinline__ float Raw8<float>::operator[](int j) const {
+  return __uint_as_float(w[j]);
+}
+
 // A 128 x 128 tile: row codes as above, and codes of the transpose by way of
 // LDS.  WEIGHT: one scale for the tile, else one for each row and, for the
 // transpose, for each column.  A thread holds 8 x 8 elements, so that eight
@@ -113,10 +134,10 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
 // 16 lanes of a row write 16 columns eight apart: one bank set without it), and
 // leave as whole 128-byte lines.  Bound: memory, one read and two writes.
 template <typename T, bool WEIGHT>
-__global__ __launch_bounds__(256) void quantize_tile_kernel(QuantArgs a) {
+__global__ __launch_bounds__(256, (WEIGHT || sizeof(T) == 2 ? 4 : 3)) void quantize_tile_kernel(QuantArgs a) {
   __shared__ uint8_t tile[kBlock * kBlock] __attribute__((aligned(16)));
   __shared__ uint32_t col_max[4][kBlock];
-  __shared__ uint8_t row_byte[kBlock], col_byte[kBlock];
+  __shared__ uint8_t row_byte[kBlock], col_byte[kBlock] __attribute__((aligned(16)));
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = tid >> 4, q = tid & 15;
   int64_t t = blockIdx.x;
   const int64_t cb = t % a.col_tiles;
@@ -141,27 +162,36 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantArgs a) {
   n = n > kBlock ? kBlock : n;
   const int64_t c0 = cb * kBlock, c = c0 + q * 8, end = (a.cols + 15) / 16 * 16;
 
-  T v[8][8];
+  Raw8<T> v[8];
+  if (there && n == kBlock && c0 + kBlock <= a.cols && !a.index) {  // all of it: no lane branches
+    const T* from = x + (r0 + 8 * g) * a.ld + c;
 #pragma unroll
-  for (int p = 0; p < 8; ++p) {
-    const int64_t r = r0 + 8 * g + p;
-    bool in = there && 8 * g + p < n;
-    int64_t src = r;
-    if (a.index && in) {
-      src = a.index[r];
-      in = src >= 0 && src < a.x_rows;
+    for (int p = 0; p < 8; ++p, from += a.ld) load_n<T, 8>(from, (T*)v[p].w);
+  } else {
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      const int64_t r = r0 + 8 * g + p;
+      bool in = there && 8 * g + p < n;
+      int64_t src = r;
+      if (a.index && in) {
+        src = a.index[r];
+        in = src >= 0 && src < a.x_rows;
+      }
+      T t[8];
+      load_row8<T>(x + src * a.ld, in, c, a.cols, t);
+      __builtin_memcpy(v[p].w, t, sizeof(t));
     }
-    load_row8<T>(x + src * a.ld, in, c, a.cols, v[p]);
   }
   uint32_t cm[8] = {0, 0, 0, 0, 0, 0, 0, 0}, rm[8];
 #pragma unroll
   for (int p = 0; p < 8; ++p) {
     rm[p] = 0;
     for (int j = 0; j < 8; ++j) {
-      const uint32_t b = finite_abs(to_f32(v[p][j]));
+      const uint32_t b = finite_abs(v[p][j]);
       rm[p] = max(rm[p], b);
       cm[j] = max(cm[j], b);
     }
+    v[p].forget();
   }
   uint32_t one = 0;  // WEIGHT: the tile's byte
   if constexpr (WEIGHT) {
@@ -181,30 +211,38 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantArgs a) {
     if (lane < 16)
       for (int j = 0; j < 8; ++j) col_max[wave][8 * q + j] = cm[j];
   }
+  uint8_t* to = codes + (r0 + 8 * g) * a.ld_codes + c;
 #pragma unroll
-  for (int p = 0; p < 8; ++p) {
+  for (int p = 0; p < 8; ++p, to += a.ld_codes) {
     const uint32_t byte = WEIGHT ? one : scale_byte(max16(rm[p]));
     const float by = inverse_scale(byte);
     float f[8];
-    for (int j = 0; j < 8; ++j) f[j] = scaled(to_f32(v[p][j]), by);
+    for (int j = 0; j < 8; ++j) f[j] = scaled(v[p][j], by);
+    v[p].forget();
     if (8 * g + p < n && c < end)
-      *(uint2*)(codes + (r0 + 8 * g + p) * a.ld_codes + c) =
-          make_uint2(codes4(f[0], f[1], f[2], f[3]), codes4(f[4], f[5], f[6], f[7]));
+      *(uint2*)to = make_uint2(codes4(f[0], f[1], f[2], f[3]), codes4(f[4], f[5], f[6], f[7]));
     if (!WEIGHT && q == 0) row_byte[8 * g + p] = (uint8_t)byte;
+    if (p % 2) __builtin_amdgcn_sched_barrier(0);  // two rows at a time: fewer registers
   }
-  if constexpr (!WEIGHT) __syncthreads();
+  uint32_t col_bytes[2] = {0, 0};
+  if constexpr (!WEIGHT) {
+    __syncthreads();
+    if (tid < kBlock)
+      col_byte[tid] = (uint8_t)scale_byte(max(max(col_max[0][tid], col_max[1][tid]), max(col_max[2][tid], col_max[3][tid])));
+    __syncthreads();
+    __builtin_memcpy(col_bytes, __builtin_assume_aligned(col_byte + 8 * q, 8), 8);
+  }
   if (codes_t) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int k = 8 * q + j;
-      uint32_t byte = one;
-      if constexpr (!WEIGHT) byte = scale_byte(max(max(col_max[0][k], col_max[1][k]), max(col_max[2][k], col_max[3][k])));
+      const uint32_t byte = WEIGHT ? one : col_bytes[j / 4] >> (j % 4 * 8) & 255u;
       const float by = inverse_scale(byte);
       float f[8];
-      for (int p = 0; p < 8; ++p) f[p] = scaled(to_f32(v[p][j]), by);
+      for (int p = 0; p < 8; ++p) f[p] = scaled(v[p][j], by);
       *(uint2*)(tile + k * kBlock + ((8 * g) ^ (16 * (q & 7)))) =
           make_uint2(codes4(f[0], f[1], f[2], f[3]), codes4(f[4], f[5], f[6], f[7]));
-      if (!WEIGHT && g == 0) col_byte[k] = (uint8_t)byte;
+      if (j % 2) __builtin_amdgcn_sched_barrier(0);
     }
   }
   __syncthreads();

@@ -17,7 +17,7 @@ import ctypes
 import torch
 
 from . import wsgemm as _w
-from .fp8 import _Call, _check, _index, _matrix, _mp, _need
+from .fp8 import _call, _check, _matrix, _mp, _need, _new_matrix
 
 MAX_EXPERTS = 1024
 
@@ -65,23 +65,24 @@ def sort(ids, experts: int, stream=None) -> Routes:
     if need < 0:
         raise ValueError("sort: 1 to %d experts, got %r, and at most 2^30 choices, got %d" % (MAX_EXPERTS, experts, ids.numel()))
     n, device = tokens * k, ids.device
-    with _Call(device, stream, (ids,)) as st:
-        # one allocation: offsets, token, place and the work memory
-        flat = torch.empty(experts + 1 + 2 * n + need // 4, dtype=torch.int32, device=device)
-        r = Routes(flat[: experts + 1], flat[experts + 1: experts + 1 + n],
-                   flat[experts + 1 + n: experts + 1 + 2 * n].view(tokens, k))
-        at = flat.data_ptr()
-        _check(_lib.ws_expert_sort(tokens, k, experts, ids.data_ptr(), ids.element_size(), at, at + 4 * (experts + 1),
-                                   at + 4 * (experts + 1 + n), at + 4 * (experts + 1 + 2 * n), need, st), "ws_expert_sort")
+    with _call(device, stream, ids) as st:
+        r = object.__new__(Routes)
+        r.offsets = offsets = torch.empty(experts + 1, dtype=torch.int32, device=device)
+        r.token = token = torch.empty(n, dtype=torch.int32, device=device)
+        r.place = place = torch.empty(tokens, k, dtype=torch.int32, device=device)
+        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        _check(_lib.ws_expert_sort(tokens, k, experts, ids.data_ptr(), ids.element_size(), offsets.data_ptr(), token.data_ptr(),
+                                   place.data_ptr(), work.data_ptr() if need else 0, need, st), "ws_expert_sort")
     return r
 
 
-def _out(out, what, shape, like):
+def _out(out, what, rows, cols, like):
+    """The result's tensor, new where none is given, and its descriptor."""
     if out is None:
-        return torch.empty(shape, dtype=like.dtype, device=like.device)
-    if tuple(out.shape) != tuple(shape) or out.dtype != like.dtype:
-        raise ValueError("%s: expected %s %s, got %s %s" % (what, tuple(shape), like.dtype, tuple(out.shape), out.dtype))
-    return out
+        return _new_matrix(rows, cols, like.dtype, like.device)
+    if tuple(out.shape) != (rows, cols) or out.dtype != like.dtype:
+        raise ValueError("%s: expected %s %s, got %s %s" % (what, (rows, cols), like.dtype, tuple(out.shape), out.dtype))
+    return out, _matrix(out, what, device=like.device)
 
 
 def _weights(weights, routes):
@@ -98,9 +99,9 @@ def gather(x, routes: Routes, out=None, stream=None):
     m = _matrix(x, "x", device=routes.token.device)
     if m.rows != routes.place.shape[0]:
         raise ValueError("x: %d rows for %d tokens" % (m.rows, routes.place.shape[0]))
-    with _Call(x.device, stream, (x, routes.token, out)) as st:
-        out = _out(out, "out", (routes.token.numel(), m.cols), x)
-        _check(_lib.ws_expert_gather(m, routes.token.data_ptr(), _matrix(out, "out", device=x.device), st), "ws_expert_gather")
+    with _call(x.device, stream, x, routes.token, out) as st:
+        out, mo = _out(out, "out", routes.token.numel(), m.cols, x)
+        _check(_lib.ws_expert_gather(m, routes.token.data_ptr(), mo, st), "ws_expert_gather")
     return out
 
 
@@ -111,10 +112,9 @@ def combine(h, routes: Routes, weights=None, out=None, stream=None):
     if m.rows != routes.token.numel():
         raise ValueError("h: %d rows for %d choices" % (m.rows, routes.token.numel()))
     w, (tokens, k) = _weights(weights, routes), routes.place.shape
-    with _Call(h.device, stream, (h, routes.place, weights, out)) as st:
-        out = _out(out, "out", (tokens, m.cols), h)
-        _check(_lib.ws_expert_combine(m, k, routes.place.data_ptr(), w, _matrix(out, "out", device=h.device), st),
-               "ws_expert_combine")
+    with _call(h.device, stream, h, routes.place, weights, out) as st:
+        out, mo = _out(out, "out", tokens, m.cols, h)
+        _check(_lib.ws_expert_combine(m, k, routes.place.data_ptr(), w, mo, st), "ws_expert_combine")
     return out
 
 
@@ -131,10 +131,10 @@ def combine_gradient(dy, h, routes: Routes, weights=None, dh=None, stream=None):
             raise ValueError("h: expected %s %s, got %s %s" % ((routes.token.numel(), m.cols), dy.dtype, tuple(h.shape), h.dtype))
     else:
         mh = None
-    with _Call(dy.device, stream, (dy, h, routes.offsets, routes.place, weights, dh)) as st:
-        dh = _out(dh, "dh", (routes.token.numel(), m.cols), dy)
+    with _call(dy.device, stream, dy, h, routes.offsets, routes.place, weights, dh) as st:
+        dh, mdh = _out(dh, "dh", routes.token.numel(), m.cols, dy)
         dw = torch.empty(tokens, k, dtype=torch.float32, device=dy.device) if weights is not None else None
         _check(_lib.ws_expert_combine_gradient(m, mh, k, routes.experts, routes.offsets.data_ptr(), routes.place.data_ptr(), w,
-                                               _matrix(dh, "dh", device=dy.device), dw.data_ptr() if dw is not None else 0, st),
+                                               mdh, dw.data_ptr() if dw is not None else 0, st),
                "ws_expert_combine_gradient")
     return dh, dw

@@ -60,6 +60,7 @@ for _name, _args, _res in (
         ("ws_fp8_grouped_gradient", [_qp, _qp, _i64, _i32, _p, _f32, _f32, _mp, _mp, _p], _i32)):
     getattr(_lib, _name).argtypes, getattr(_lib, _name).restype = _args, _res
 
+_ws_fp8_product, _ws_fp8_quantize_rows = _lib.ws_fp8_product, _lib.ws_fp8_quantize_rows
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _current_device = torch._C._cuda_getDevice
 
@@ -74,16 +75,12 @@ def _check(status: int, where: str) -> None:
 
 
 class _Call:
-    """The stream a call enqueues on, as a context in which results are made.
-    Costs nothing where that is the current stream of the current device."""
+    """The stream a call enqueues on, as a context in which results are made, for
+    calls that do not use the current stream of the current device."""
 
-    __slots__ = ("raw", "stream", "_stack")
+    __slots__ = ("raw", "_stack")
 
     def __init__(self, device: torch.device, stream, tensors):
-        self.stream, self._stack = stream, None
-        if stream is None and device.index == _current_device():
-            self.raw = _raw_stream(device.index)
-            return
         self._stack = contextlib.ExitStack()
         self._stack.enter_context(torch.cuda.device(device))
         if stream is None:
@@ -101,8 +98,29 @@ class _Call:
         return self.raw
 
     def __exit__(self, *exc):
-        if self._stack is not None:
-            self._stack.close()
+        self._stack.close()
+
+
+class _Here:
+    """The current stream of the current device: nothing to enter or leave."""
+
+    __slots__ = ("raw",)
+
+    def __init__(self, raw):
+        self.raw = raw
+
+    def __enter__(self):
+        return self.raw
+
+    def __exit__(self, *exc):
+        pass
+
+
+def _call(device: torch.device, stream, *tensors):
+    index = device.index
+    if stream is None and index == _current_device():
+        return _Here(_raw_stream(index))
+    return _Call(device, stream, tensors)
 
 
 def _need(t, what: str, dtypes, dims, device=None):
@@ -119,11 +137,17 @@ def _matrix(t, what: str, dims=(2,), device=None) -> ws_matrix:
     """Descriptor of a float tensor (batch x) rows x cols whose columns lie next to each other."""
     _need(t, what, _CODES, dims, device)
     shape, stride = t.shape, t.stride()
-    rows, cols = shape[-2:]
+    rows, cols = shape[-2], shape[-1]
     if cols > 1 and stride[-1] != 1 or rows > 1 and stride[-2] < cols:
         raise ValueError("%s: columns have to lie next to each other and rows may not overlap, got strides %s" % (what, stride))
     return ws_matrix(t.data_ptr(), rows, cols, stride[-2] if rows > 1 else cols, _CODES[t.dtype],
                      shape[0] if len(shape) == 3 else 1, stride[0] if len(shape) == 3 else 0)
+
+
+def _new_matrix(rows: int, cols: int, dtype: torch.dtype, device):
+    """A new dense tensor and its descriptor."""
+    t = torch.empty(rows, cols, dtype=dtype, device=device)
+    return t, ws_matrix(t.data_ptr(), rows, cols, cols, _CODES[dtype], 1, 0)
 
 
 def _index(t, what: str, n: int, device) -> int:
@@ -171,10 +195,20 @@ class Fp8Matrix:
 
     @classmethod
     def empty(cls, rows: int, cols: int, block_rows: int = 1, batch: int | None = None, device="cuda"):
-        lead = () if batch is None else (batch,)
-        codes = torch.empty(lead + (rows, _up(cols, 16)), dtype=E4M3, device=device)
-        scales = torch.empty(lead + (-(-cols // BLOCK), -(-rows // block_rows)), dtype=E8M0, device=device)
-        return cls(codes, scales, rows, cols, block_rows)
+        if block_rows not in (1, BLOCK) or rows < 0 or cols < 0:
+            raise ValueError("%d x %d with block_rows %r" % (rows, cols, block_rows))
+        pitch, blocks, per = _up(cols, 16), -(-cols // BLOCK), -(-rows // block_rows)
+        q = object.__new__(cls)
+        if batch is None:
+            q.codes = codes = torch.empty(rows, pitch, dtype=E4M3, device=device)
+            q.scales = scales = torch.empty(blocks, per, dtype=E8M0, device=device)
+        else:
+            q.codes = codes = torch.empty(batch, rows, pitch, dtype=E4M3, device=device)
+            q.scales = scales = torch.empty(batch, blocks, per, dtype=E8M0, device=device)
+        q.rows, q.cols, q.block_rows = rows, cols, block_rows
+        q._desc = ws_fp8_matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, pitch, per, block_rows, 1 if batch is None else batch,
+                                rows * pitch, blocks * per)
+        return q
 
     def dequantize(self) -> torch.Tensor:
         """The values in binary32 (for tests and inspection; plain torch)."""
@@ -196,9 +230,9 @@ def quantize_rows(x, index=None, out: Fp8Matrix | None = None, stream=None) -> F
     m = _matrix(x, "x")
     rows = m.rows if index is None else index.numel()
     at = _index(index, "index", rows, x.device)
-    with _Call(x.device, stream, (x, index) + ((out.codes, out.scales) if out is not None else ())) as st:
+    with _call(x.device, stream, x, index, *((out.codes, out.scales) if out is not None else ())) as st:
         q = Fp8Matrix.empty(rows, m.cols, device=x.device) if out is None else _fits(out, "out", rows, m.cols, 1, None, x.device)
-        _check(_lib.ws_fp8_quantize_rows(m, at, q._desc, st), "ws_fp8_quantize_rows")
+        _check(_ws_fp8_quantize_rows(m, at, q._desc, st), "ws_fp8_quantize_rows")
     return q
 
 
@@ -221,7 +255,7 @@ def quantize_both(x, index=None, offsets=None, out=None, stream=None):
     off = _index(offsets, "offsets", groups + 1, x.device)
     deep = padded_rows(rows, groups) if groups else rows
     used = () if out is None else (out[0].codes, out[0].scales, out[1].codes, out[1].scales)
-    with _Call(x.device, stream, (x, index, offsets) + used) as st:
+    with _call(x.device, stream, x, index, offsets, *used) as st:
         if out is None:
             q, t = Fp8Matrix.empty(rows, m.cols, device=x.device), Fp8Matrix.empty(m.cols, deep, device=x.device)
         else:
@@ -236,7 +270,7 @@ def quantize_weight(w, transposed: bool = True, out=None, stream=None):
     m = _matrix(w, "w", (2, 3))
     batch = m.batch if w.dim() == 3 else None
     used = () if out is None else tuple(t for q in out if q is not None for t in (q.codes, q.scales))
-    with _Call(w.device, stream, (w,) + used) as st:
+    with _call(w.device, stream, w, *used) as st:
         if out is None:
             q = Fp8Matrix.empty(m.rows, m.cols, BLOCK, batch, w.device)
             t = Fp8Matrix.empty(m.cols, m.rows, BLOCK, batch, w.device) if transposed else None
@@ -249,9 +283,12 @@ def quantize_weight(w, transposed: bool = True, out=None, stream=None):
 
 def _result(C, out_dtype: str, shape, device):
     if C is None:
-        if out_dtype not in _DTYPES:
+        dtype = _DTYPES.get(out_dtype)
+        if dtype is None:
             raise ValueError("out_dtype is one of %s, got %r" % (sorted(_DTYPES), out_dtype))
-        C = torch.empty(shape, dtype=_DTYPES[out_dtype], device=device)
+        if len(shape) == 2:
+            return _new_matrix(shape[0], shape[1], dtype, device)
+        C = torch.empty(shape, dtype=dtype, device=device)
     elif tuple(C.shape) != tuple(shape):
         raise ValueError("C: expected %s, got %s" % (tuple(shape), tuple(C.shape)))
     return C, _matrix(C, "C", (len(shape),), device)
@@ -275,14 +312,14 @@ def product(A: Fp8Matrix, B: Fp8Matrix, C=None, out_dtype: str = "bf16", alpha: 
     tensor of out_dtype ("f32", "bf16", "f16").  C0 may be C."""
     codes = A.codes
     device = codes.device
-    if A.batch is not None or B.batch is not None or B.codes.device != device:
+    if codes.dim() == 3 or B.codes.dim() == 3 or B.codes.device != device:
         raise ValueError("A and B have to be single matrices on one device")
     if A.cols != B.cols or A.block_rows != 1:
         raise ValueError("A (%d x %d) and B (%d x %d) have to have as many columns, A scales for single rows" % (
             A.rows, A.cols, B.rows, B.cols))
-    with _Call(device, stream, (codes, A.scales, B.codes, B.scales, C, C0)) as st:
+    with _call(device, stream, codes, A.scales, B.codes, B.scales, C, C0) as st:
         C, m = _result(C, out_dtype, (A.rows, B.rows), device)
-        _check(_lib.ws_fp8_product(A._desc, B._desc, alpha, beta, _old(C0, beta, C), m, st), "ws_fp8_product")
+        _check(_ws_fp8_product(A._desc, B._desc, alpha, beta, _old(C0, beta, C), m, st), "ws_fp8_product")
     return C
 
 
@@ -293,7 +330,7 @@ def grouped_product(A: Fp8Matrix, B: Fp8Matrix, offsets, C=None, out_dtype: str 
     if A.batch is not None or B.batch is None or A.cols != B.cols or A.block_rows != 1 or B.codes.device != device:
         raise ValueError("A has to be a single matrix with scales for single rows, B a batch of as many columns on its device")
     off = _index(offsets, "offsets", B.batch + 1, device)
-    with _Call(device, stream, (A.codes, A.scales, B.codes, B.scales, offsets, C)) as st:
+    with _call(device, stream, A.codes, A.scales, B.codes, B.scales, offsets, C) as st:
         C, m = _result(C, out_dtype, (A.rows, B.rows), device)
         _check(_lib.ws_fp8_grouped_product(A._desc, B._desc, B.batch, off, alpha, m, st), "ws_fp8_grouped_product")
     return C
@@ -312,7 +349,7 @@ def grouped_gradient(A: Fp8Matrix, B: Fp8Matrix, rows: int, offsets, C=None, out
         raise ValueError("A and B have to be single matrices with scales for single rows on one device")
     if groups < 1 or A.cols != B.cols or A.cols != padded_rows(rows, groups):
         raise ValueError("A and B have to hold the padded columns of %d rows in %d groups" % (rows, groups))
-    with _Call(device, stream, (A.codes, A.scales, B.codes, B.scales, offsets, C, C0)) as st:
+    with _call(device, stream, A.codes, A.scales, B.codes, B.scales, offsets, C, C0) as st:
         C, m = _result(C, out_dtype, (groups, A.rows, B.rows), device)
         _check(_lib.ws_fp8_grouped_gradient(A._desc, B._desc, rows, groups, off, alpha, beta, _old(C0, beta, C), m, st),
                "ws_fp8_grouped_gradient")
