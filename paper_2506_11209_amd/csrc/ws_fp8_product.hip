@@ -21,6 +21,8 @@
 // a wave covers 64 neighbouring bytes of every row.  The operands are passed in
 // exchanged order (B's rows first): a lane then ends up with four neighbouring
 // columns of one row of C.
+#include <math.h>
+
 #include <atomic>
 #include <type_traits>
 
@@ -263,23 +265,29 @@ __device__ __forceinline__ void load_to_lds(i32x4_t r, uint32_t at, uint32_t k, 
 #endif
 }
 
-// Waits for this wave's loads and LDS accesses, then for the workgroup.
+// Waits for this wave's LDS accesses and all but its last YOUNGER loads, then for
+// the workgroup.
+template <int YOUNGER = 0>
 __device__ __forceinline__ void drain_and_meet() {
+  static_assert(YOUNGER >= 0 && YOUNGER <= 63, "vmcnt");
 #if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(YOUNGER) : "memory");
 #endif
 }
 
-template <int WM, int WN>
+template <int WM, int WN, int STAGES>
 struct TileShape {
   static constexpr int TM = 32 * WM, TN = 32 * WN, kStage = (TM + TN) * kBlock;
-  static constexpr int kMine = (TM + TN + 255) / 256;  // a thread's rows of scales
-  // One wave a SIMD with sums in accumulation registers, or two with all in the others.
-  static constexpr int kWaves = WM * WN > 16 ? 1 : 2;
-  static constexpr bool kAgpr = kWaves == 1;
-  // LDS: two stages, two blocks of scales, and for every wave 16 rows of what it
-  // stores at a time, as many columns as fit
-  static constexpr int kStoreAt = 2 * kStage + 2 * (TM + TN), kStoreCols = kWaves == 1 ? 64 : 32, kStoreParts = 16 * WN / kStoreCols;
+  // One wave a SIMD with sums in accumulation registers, or more with all in the others.
+  static constexpr int kWaves = WM * WN > 16 || STAGES * kStage > 80 * 1024 ? 1 : 2;
+  static constexpr bool kAgpr = WM * WN > 16;
+  // Two stages: a thread brings the scales of its rows of the tile block by block;
+  // more: those of kDeep blocks at a time lie in LDS.
+  static constexpr int kMine = (TM + TN + 255) / 256, kDeep = STAGES == 2 ? 2 : 32;
+  // LDS: the stages, the scales, and for every wave 16 rows of what it stores at a
+  // time, as many columns as fit
+  static constexpr int kScalesAt = STAGES * kStage, kStoreAt = kScalesAt + kDeep * (TM + TN);
+  static constexpr int kStoreCols = kWaves == 1 && WN >= 4 ? 64 : 32, kStoreParts = 16 * WN / kStoreCols;
   static constexpr int kPitch = kStoreCols + 4;  // the pitch spreads rows over the banks
   static constexpr int kStoreBytes = 16 * kPitch * 4, kLds = kStoreAt + 4 * kStoreBytes;
   static_assert(kWaves * kLds <= 160 * 1024, "LDS of a CU");
@@ -307,10 +315,10 @@ __device__ __forceinline__ void settle(f32x4_t& acc) {
 // is added are rounded before LDS and leave in 16-byte pieces, at addresses that
 // differ by scalars only; others pass LDS in binary32.
 // rows, cols: of the tile, inside C.
-template <typename T, int WM, int WN>
+template <typename T, int WM, int WN, int STAGES>
 __device__ __forceinline__ void store_tile(const ProductArgs& a, const Part& p, f32x4_t (&acc)[WM][WN], uint8_t* own, int wm, int wn,
                                            int rows, int cols) {
-  typedef TileShape<WM, WN> Shape;
+  typedef TileShape<WM, WN, STAGES> Shape;
   constexpr int kCols = Shape::kStoreCols, kPitch = Shape::kPitch, kTiles = kCols / 16;
   constexpr int N = 16 / sizeof(T), kRow = kCols * (int)sizeof(T) + 16, kPieces = kCols / N, kAtOnce = 64 / kPieces;  // kRow: bytes
   static_assert(16 * kRow <= Shape::kStoreBytes && 64 % kPieces == 0 && 16 % kAtOnce == 0, "16 rows in whole stores");
@@ -426,16 +434,17 @@ __device__ __forceinline__ void settle_scales(uint32_t& s) {
 // so there is one barrier a block, no wait for memory that had less than a
 // block's time, and one set of registers for each operand.  Scales lie in LDS as
 // [row % 16][row / 16], so that a lane reads those of all its rows at once and
-// the instruction picks a byte.
+// the instruction picks a byte.  Small tiles have four stages, b + 4 being loaded
+// over b: their blocks are shorter than the way to memory.
 // WIDE: results in 32 bits.  A half's rows of A are widened at its start, a column
 // of B before its products, those of the next column between them.
 //
 // A workgroup takes every gridDim.x-th of an XCD's tiles.  It starts the loads of its
 // next tile before it stores the one it has, in LDS of their own, so that memory
 // is written and read while neither is waited for.
-template <int WM, int WN, int MODE, bool WIDE>
-__global__ __launch_bounds__(256, (TileShape<WM, WN>::kWaves)) void tile_kernel(ProductArgs a) {
-  typedef TileShape<WM, WN> Shape;
+template <int WM, int WN, int STAGES, int MODE, bool WIDE>
+__global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile_kernel(ProductArgs a) {
+  typedef TileShape<WM, WN, STAGES> Shape;
   constexpr int TM = Shape::TM, TN = Shape::TN, kStage = Shape::kStage, kRows = TM + TN, kHalf = WM / 2;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -464,7 +473,7 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN>::kWaves)) void tile_kernel(
   constexpr int kLoads = (TM + TN) / 32;  // of a wave and block, 1 KiB each
   const auto load = [&](int b, int from, int to) {
     const bool inside = b * kBlock + lc < t.K;  // else zeros: past the last column
-    const uint32_t ia = inside ? at_a : kOutside, ib = inside ? at_b : kOutside, lds = lds0 + (b & 1) * kStage;
+    const uint32_t ia = inside ? at_a : kOutside, ib = inside ? at_b : kOutside, lds = lds0 + b % STAGES * kStage;
 #pragma unroll
     for (int i = from; i < to; ++i) {
       if (i < TM / 32) load_to_lds(t.ra, ia + i * step_a, b * kBlock, lds + i * 4096);
@@ -472,20 +481,36 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN>::kWaves)) void tile_kernel(
     }
   };
   // scales of this thread's rows of the tile
-  uint8_t* scales = smem + 2 * kStage;
+  uint8_t* scales = smem + Shape::kScalesAt;
   typedef uint8_t bytes_t[Shape::kMine];
+  // where a row's scale lies: [row % 16][row / 16], A's rows first
+  const auto scale_place = [](int row) {
+    return row < TM ? row % 16 * (2 * WM) + row / 16 : TM + (row - TM) % 16 * (2 * WN) + (row - TM) / 16;
+  };
+  // Row i of this thread: every thread has one inside the tile, more than one thread
+  // the same where there are fewer rows than threads.
+  const auto my_row = [&](int i) { return kRows >= 256 ? min(tid + 256 * i, kRows - 1) : tid % kRows; };
   const auto fetch_scales = [&](int b, bytes_t& byte) {
 #pragma unroll
-    for (int i = 0; i < Shape::kMine; ++i)
-      byte[i] = t.scale_at[i][min(b, t.blocks - 1) * (tid + 256 * i < TM ? a.ldsa : a.ldsb)];
+    for (int i = 0; i < Shape::kMine; ++i) byte[i] = t.scale_at[i][min(b, t.blocks - 1) * (my_row(i) < TM ? a.ldsa : a.ldsb)];
   };
   const auto keep_scales = [&](int b, const bytes_t& byte) {
 #pragma unroll
-    for (int i = 0; i < Shape::kMine; ++i) {
-      const int row = tid + 256 * i;
-      if (kRows % 256 == 0 || row < kRows)
-        scales[(b & 1) * kRows + (row < TM ? row % 16 * (2 * WM) + row / 16 : TM + (row - TM) % 16 * (2 * WN) + (row - TM) / 16)] =
-            byte[i];
+    for (int i = 0; i < Shape::kMine; ++i) scales[(b & 1) * kRows + scale_place(my_row(i))] = byte[i];
+  };
+  // scales of kDeep blocks from b, by all threads
+  const auto fill_scales = [&](int b) {
+    constexpr int kAtOnce = 8;
+    static_assert(STAGES == 2 || 256 % kRows == 0, "whole blocks of scales at a time");
+    const int row = my_row(0);  // kRows divides 256
+    const uint8_t* from = t.scale_at[0];
+    const int64_t ld = row < TM ? a.ldsa : a.ldsb;
+    for (int k0 = tid / kRows; k0 < Shape::kDeep; k0 += kAtOnce * (256 / kRows)) {
+      uint8_t s[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) s[k] = from[min(b + k0 + k * (256 / kRows), t.blocks - 1) * ld];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) scales[(k0 + k * (256 / kRows)) * kRows + scale_place(row)] = s[k];
     }
   };
   bytes_t byte0, byte1, byte;
@@ -503,14 +528,16 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN>::kWaves)) void tile_kernel(
     t.rb = raw_buffer(t.p.B + t.p.n0 * a.ldb, (uint32_t)(t.cols * a.ldb));
 #pragma unroll
     for (int i = 0; i < Shape::kMine; ++i) {
-      const int row = tid + 256 * i;
+      const int row = my_row(i);
       t.scale_at[i] = row < TM ? t.p.sa + t.p.m0 + min(row, t.rows - 1) : t.p.sb + ((t.p.n0 + min(row - TM, t.cols - 1)) >> a.b_shift);
     }
-    fetch_scales(0, byte0);
-    fetch_scales(1, byte1);
-    fetch_scales(2, byte);
-    load(0, 0, kLoads);
-    load(1, 0, kLoads);
+    if constexpr (STAGES == 2) {
+      fetch_scales(0, byte0);
+      fetch_scales(1, byte1);
+      fetch_scales(2, byte);
+    }
+#pragma unroll
+    for (int b = 0; b < STAGES; ++b) load(b, 0, kLoads);
   };
 
   if (id < end) begin_tile();
@@ -529,12 +556,16 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN>::kWaves)) void tile_kernel(
         return join(*(const i32x4_t*)(f + c0), *(const i32x4_t*)(f + c1));
       };
       const auto read_scales = [&](int b, uint32_t* sa, uint32_t* sb) {
-        const uint8_t* s = scales + (b & 1) * kRows;
+        const uint8_t* s = scales + b % Shape::kDeep * kRows;
         __builtin_memcpy(sa, __builtin_assume_aligned(s + (2 * r + wm) * WM, WM), WM);
         __builtin_memcpy(sb, __builtin_assume_aligned(s + TM + (2 * r + wn) * WN, WN), WN);
       };
-      keep_scales(0, byte0);
-      keep_scales(1, byte1);
+      if constexpr (STAGES == 2) {
+        keep_scales(0, byte0);
+        keep_scales(1, byte1);
+      } else {
+        fill_scales(0);
+      }
       drain_and_meet();
       read_scales(0, sa, sb);
 #pragma unroll
@@ -543,7 +574,7 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN>::kWaves)) void tile_kernel(
       for (int i = 0; i < kHalf; ++i) fa[i] = frag(fa0 + i * 2048, 0);
       __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): in the loop the compiler then counts LDS reads only
       for (int b = 0; b < t.blocks; ++b) {
-        const int here = (b & 1) * kStage, next = kStage - here;
+        const int here = b % STAGES * kStage, next = (b + 1) % STAGES * kStage;
         if constexpr (WIDE) {
           Wide wa[kHalf], wb = widen_all(fb[0], sb[0], 0);
 #pragma unroll
@@ -572,10 +603,15 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN>::kWaves)) void tile_kernel(
             __builtin_amdgcn_sched_barrier(0);
           });
         }
-        drain_and_meet();
-        keep_scales(b + 2, byte);
-        __builtin_amdgcn_sched_barrier(0);
-        fetch_scales(b + 3, byte);
+        drain_and_meet<kLoads * (STAGES - 2)>();
+        if constexpr (STAGES == 2) {
+          keep_scales(b + 2, byte);
+          __builtin_amdgcn_sched_barrier(0);
+          fetch_scales(b + 3, byte);
+        } else if ((b + 1) % Shape::kDeep == 0 && b + 1 < t.blocks) {  // the next blocks' scales; every wave has read the last
+          fill_scales(b + 1);
+          drain_and_meet();
+        }
         uint32_t next_sa[(WM + 3) / 4], next_sb[(WN + 3) / 4];
         read_scales(b + 1, next_sa, next_sb);
         // loads one at a time between products: two at once hold up the products behind them
@@ -592,7 +628,7 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN>::kWaves)) void tile_kernel(
             for (int q = 0; q < 4; ++q) {
 #pragma unroll
               for (int i = 0; i < kHalf; ++i) multiply_wide<Shape::kAgpr>(acc[kHalf + i][j], wa[i].part[q], wb.part[q]);
-              load(b + 2, j * kPer + q * kPer / 4, j * kPer + (q + 1) * kPer / 4);
+              load(b + STAGES, j * kPer + q * kPer / 4, j * kPer + (q + 1) * kPer / 4);
             }
 #pragma unroll
             for (int k = j * kHalf / WN; k < (j + 1) * kHalf / WN; ++k) fa[k] = frag(fa0 + k * 2048, next);
@@ -606,7 +642,7 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN>::kWaves)) void tile_kernel(
             static_for<kHalf>([&](auto ic) {
               constexpr int i = decltype(ic)::value, row = kHalf + i;
               multiply<Shape::kAgpr, row % 4, j % 4>(acc[row][j], fa[row], fb[j], sa[row / 4], sb[j / 4]);
-              load(b + 2, j * kPer + i * kPer / kHalf, j * kPer + (i + 1) * kPer / kHalf);
+              load(b + STAGES, j * kPer + i * kPer / kHalf, j * kPer + (i + 1) * kPer / kHalf);
               if (i == 0) {
 #pragma unroll
                 for (int k = j * kHalf / WN; k < (j + 1) * kHalf / WN; ++k) fa[k] = frag(fa0 + k * 2048, next);
@@ -630,9 +666,9 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN>::kWaves)) void tile_kernel(
     id += stride;
     if (id < end) begin_tile();
     uint8_t* own = smem + Shape::kStoreAt + wave * Shape::kStoreBytes;
-    if constexpr (WIDE) store_tile<float, WM, WN>(a, p, acc, own, wm, wn, rows, cols);
-    else if (a.dtype == WS_OUT_BF16) store_tile<bf16_t, WM, WN>(a, p, acc, own, wm, wn, rows, cols);
-    else store_tile<f16_t, WM, WN>(a, p, acc, own, wm, wn, rows, cols);
+    if constexpr (WIDE) store_tile<float, WM, WN, STAGES>(a, p, acc, own, wm, wn, rows, cols);
+    else if (a.dtype == WS_OUT_BF16) store_tile<bf16_t, WM, WN, STAGES>(a, p, acc, own, wm, wn, rows, cols);
+    else store_tile<f16_t, WM, WN, STAGES>(a, p, acc, own, wm, wn, rows, cols);
   }
 }
 
@@ -667,16 +703,16 @@ ws_status run_direct(ProductArgs a, hipStream_t stream) {
   return launch("fp8_product", kernel, grid, 64 * waves, waves * MT * 1024, stream, a);
 }
 
-template <int WM, int WN, int MODE, bool WIDE>
+template <int WM, int WN, int STAGES, int MODE, bool WIDE>
 ws_status run_tiles(ProductArgs a, hipStream_t stream) {
-  typedef TileShape<WM, WN> Shape;
+  typedef TileShape<WM, WN, STAGES> Shape;
   constexpr int TM = Shape::TM, TN = Shape::TN;
   a.tiles_n = ceil_div(a.N, TN);
   a.tiles_m = MODE == kRowGroups ? group_tiles(a.M, a.groups, TM, true) : ceil_div(a.M, TM);
   const int64_t tiles = a.tiles_n * a.tiles_m, grid = tiles * (MODE == kDepthGroups ? a.groups : 1);
   if (a.tiles_m > kMaxGrid || tiles > kMaxGrid || grid > kMaxGrid) return WS_ERR_INVALID_ARG;
   const int64_t most = (int64_t)compute_units() * Shape::kWaves;
-  const auto kernel = &tile_kernel<WM, WN, MODE, WIDE>;
+  const auto kernel = &tile_kernel<WM, WN, STAGES, MODE, WIDE>;
   static std::atomic<uint64_t> allowed;  // devices on which the kernel may use this much LDS
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
@@ -688,17 +724,116 @@ ws_status run_tiles(ProductArgs a, hipStream_t stream) {
   return launch("fp8_product", kernel, grid < most ? grid : most, 256, Shape::kLds, stream, a);
 }
 
+// What a product costs by each kernel, in us (MI355X, 256 CUs; fitted to 23
+// products from 64 x 2048 x 2048 to 8192 x 8192 x 8192, most within 15 %).  A CU
+// has n tiles: their blocks of 128 columns take `alone` each where it has one,
+// n * `shared` otherwise, and every tile `tile` more.
+struct TileCost {
+  int rows, cols;  // of a tile
+  float fixed, alone, shared, tile;
+};
+//                                  16-bit results                     32-bit results
+constexpr TileCost kCost256 =      {256, 256, 4.0f, 1.30f, 1.50f, 7.0f};
+constexpr TileCost kCost256Wide =  {256, 128, 4.0f, 1.80f, 1.85f, 4.0f};
+constexpr TileCost kCost128[2] =  {{128, 128, 4.0f, 0.60f, 0.57f, 0.5f}, {128, 128, 4.0f, 1.05f, 1.02f, 0.7f}};
+constexpr TileCost kCost128Deep =  {128, 128, 4.5f, 0.50f, 0.55f, 2.6f};  // four stages
+constexpr TileCost kCost64[2] =   {{64, 64, 3.7f, 0.30f, 0.25f, 0.3f}, {64, 64, 3.7f, 0.50f, 0.37f, 0.3f}};
+constexpr TileCost kCost64Deep[2] = {{64, 64, 4.5f, 0.27f, 0.22f, 0.6f}, {64, 64, 4.5f, 0.48f, 0.35f, 0.6f}};
+
+enum Choice { kDirect16, kDirect32, kDirect64, kTile256, kTile128, kTile128Deep, kTile64, kTile64Deep };
+
+// `parts` products of on average rows x N, contracted over K columns each.
+struct Work {
+  double rows, parts;
+  int64_t N, K;
+};
+
+float tile_cost(const Work& w, const TileCost& c) {
+  // a part's last tile is partly filled: half of one on average, where there are several parts
+  const double tiles_m = w.parts > 1 ? w.parts * (w.rows / c.rows + 0.5) : (double)ceil_div((int64_t)w.rows, c.rows);
+  const double n = ceil(tiles_m * (double)ceil_div(w.N, c.cols) / compute_units());
+  const float blocks = (float)ceil_div(w.K, kBlock);
+  return c.fixed + blocks * (n <= 1 ? c.alone : c.shared * (float)n) + c.tile * (float)n;
+}
+
+// The direct kernel is bound by what its workgroups load, at 11 TB/s from the
+// caches, and for long contractions by the trips that a wave makes.
+float direct_cost(const Work& w, int rows) {
+  const double tiles_m = w.parts > 1 ? w.parts * (w.rows / rows + 0.5) : (double)ceil_div((int64_t)w.rows, rows);
+  return (float)(4.0 + tiles_m * (double)ceil_div(w.N, 16) * (rows + 16.0) * (double)w.K / 11e6 + 0.03 * (double)w.K / kBlock);
+}
+
+Choice choose(const Work& w, bool wide, float* cost) {
+  Choice best = kDirect16;
+  *cost = direct_cost(w, 16);
+  const auto consider = [&](Choice c, float t) {
+    if (t < *cost) {
+      *cost = t;
+      best = c;
+    }
+  };
+  consider(kDirect32, direct_cost(w, 32));
+  consider(kDirect64, direct_cost(w, 64));
+  consider(kTile64, tile_cost(w, kCost64[wide]));
+  consider(kTile64Deep, tile_cost(w, kCost64Deep[wide]));
+  consider(kTile128, tile_cost(w, kCost128[wide]));
+  if (!wide) consider(kTile128Deep, tile_cost(w, kCost128Deep));
+  consider(kTile256, tile_cost(w, wide ? kCost256Wide : kCost256));
+  return best;
+}
+
+template <int MODE>
+ws_status run_choice(Choice c, const ProductArgs& a, hipStream_t stream) {
+  const bool wide = a.dtype == WS_OUT_F32;
+  switch (c) {
+    case kDirect16: return run_direct<1, 4, MODE>(a, stream);
+    case kDirect32: return run_direct<2, 4, MODE>(a, stream);
+    case kDirect64: return run_direct<4, 2, MODE>(a, stream);
+    case kTile64: return wide ? run_tiles<2, 2, 2, MODE, true>(a, stream) : run_tiles<2, 2, 2, MODE, false>(a, stream);
+    case kTile64Deep: return wide ? run_tiles<2, 2, 4, MODE, true>(a, stream) : run_tiles<2, 2, 4, MODE, false>(a, stream);
+    case kTile128: return wide ? run_tiles<4, 4, 2, MODE, true>(a, stream) : run_tiles<4, 4, 2, MODE, false>(a, stream);
+    case kTile128Deep: return run_tiles<4, 4, 4, MODE, false>(a, stream);
+    default: return wide ? run_tiles<8, 4, 2, MODE, true>(a, stream) : run_tiles<8, 8, 2, MODE, false>(a, stream);
+  }
+}
+
 template <int MODE>
 ws_status run_product(const ProductArgs& a, hipStream_t stream) {
-  const int64_t rows = MODE == kRowGroups ? ceil_div(a.M, a.groups) : a.M;
-  if (rows > 64) {
-    if (a.dtype == WS_OUT_F32)
-      return rows > 512 ? run_tiles<8, 4, MODE, true>(a, stream) : run_tiles<4, 4, MODE, true>(a, stream);
-    return rows > 512 ? run_tiles<8, 8, MODE, false>(a, stream) : run_tiles<4, 4, MODE, false>(a, stream);
+  const bool wide = a.dtype == WS_OUT_F32;
+  Work w{(double)a.M, 1.0, a.N, a.K};
+  if (MODE == kRowGroups) {
+    w.parts = (double)(a.groups < a.M ? a.groups : a.M);
+    w.rows = (double)a.M / w.parts;
   }
-  if (rows <= 16) return run_direct<1, 4, MODE>(a, stream);
-  if (rows <= 32) return run_direct<2, 4, MODE>(a, stream);
-  return run_direct<4, 2, MODE>(a, stream);
+  if (MODE == kDepthGroups) {
+    w.parts = a.groups;
+    w.K = ceil_div(a.depth_rows, (int64_t)a.groups);
+  }
+  float cost;
+  const Choice c = choose(w, wide, &cost);
+  if (MODE == kDense && a.M > 128 && a.M % 64 != 0) {
+    // The last rows by themselves, where they would start tiles of their own that a
+    // round has no place for (4104 x 1000 x 4100: 33 x 8 tiles of 128 rows for 256
+    // CUs, of which the 8 rows past 4096 fill one row of tiles).
+    float main_cost, rest_cost;
+    Work top = w, rest = w;
+    top.rows = (double)(a.M / 128 * 128);
+    rest.rows = (double)(a.M % 128);
+    const Choice cm = choose(top, wide, &main_cost), cr = choose(rest, wide, &rest_cost);
+    if (rest.rows > 0 && main_cost + rest_cost < 0.95f * cost) {
+      ProductArgs m = a, r = a;
+      m.M = a.M / 128 * 128;
+      r.M = a.M - m.M;
+      const int size = elem_size(a.dtype);
+      r.A += m.M * a.lda;
+      r.sa += m.M;
+      r.C = (uint8_t*)a.C + m.M * a.ldc * size;
+      if (a.C0) r.C0 = (const uint8_t*)a.C0 + m.M * a.ldc0 * size;
+      const ws_status s = run_choice<MODE>(cm, m, stream);
+      return s != WS_OK ? s : run_choice<MODE>(cr, r, stream);
+    }
+  }
+  return run_choice<MODE>(c, a, stream);
 }
 
 // Operands of a contraction over K columns; b_batch: B's matrices.
