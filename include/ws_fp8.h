@@ -94,6 +94,21 @@ int64_t ws_fp8_padded_blocks(int64_t rows, int32_t groups);
 ws_status ws_fp8_quantize_weight(const ws_matrix* w, const ws_fp8_matrix* out,
                                  const ws_fp8_matrix* out_transposed, hipStream_t stream);
 
+/* A launch of a product: its tile and the stages of its ring of blocks of 128
+ * columns in LDS (0: operands go straight to registers), and the rows of the
+ * result it computes. */
+typedef struct {
+  int32_t tile_m, tile_n, stages;
+  int64_t rows;
+} ws_fp8_kernel_info;
+
+/* The launches of a product M x N x K with results of out_dtype, by rising rows
+ * (2 at the most).  groups > 0: of ws_fp8_grouped_product, or with depth != 0 of
+ * ws_fp8_grouped_gradient of K rows.  Host only; kernels are chosen by sizes and
+ * type alone, for the current device's compute units (256 without a device). */
+ws_status ws_fp8_plan(int64_t M, int64_t N, int64_t K, int32_t out_dtype, int32_t groups, int32_t depth,
+                      ws_fp8_kernel_info* out, int32_t* count);
+
 /* C <- alpha A B^T + beta C0: A is M x K (block_rows 1), B is N x K (block_rows
  * 1 or 128), C and C0 are M x N of the same type; accumulated in binary32,
  * rounded once.  C0 may be C itself, and NULL with beta == 0 (then it is not

@@ -797,43 +797,54 @@ ws_status run_choice(Choice c, const ProductArgs& a, hipStream_t stream) {
   }
 }
 
-template <int MODE>
-ws_status run_product(const ProductArgs& a, hipStream_t stream) {
-  const bool wide = a.dtype == WS_OUT_F32;
-  Work w{(double)a.M, 1.0, a.N, a.K};
-  if (MODE == kRowGroups) {
-    w.parts = (double)(a.groups < a.M ? a.groups : a.M);
-    w.rows = (double)a.M / w.parts;
+// One or two launches of a product: the first `split` rows by choice[0], the rest
+// by choice[1].
+struct Plan {
+  int count;
+  int64_t split;
+  Choice choice[2];
+};
+
+Plan plan_product(int mode, int64_t M, int64_t N, int64_t K, int64_t groups, bool wide) {
+  Work w{(double)M, 1.0, N, K};
+  if (mode == kRowGroups) {
+    w.parts = (double)(groups < M ? groups : M);
+    w.rows = (double)M / w.parts;
   }
-  if (MODE == kDepthGroups) {
-    w.parts = a.groups;
-    w.K = ceil_div(a.depth_rows, (int64_t)a.groups);
+  if (mode == kDepthGroups) {
+    w.parts = (double)groups;
+    w.K = ceil_div(K, groups);
   }
   float cost;
-  const Choice c = choose(w, wide, &cost);
-  if (MODE == kDense && a.M > 128 && a.M % 64 != 0) {
+  Plan plan{1, M, {choose(w, wide, &cost), kDirect16}};
+  if (mode == kDense && M > kBlock && M % kBlock != 0) {
     // The last rows by themselves, where they would start tiles of their own that a
     // round has no place for (4104 x 1000 x 4100: 33 x 8 tiles of 128 rows for 256
     // CUs, of which the 8 rows past 4096 fill one row of tiles).
     float main_cost, rest_cost;
     Work top = w, rest = w;
-    top.rows = (double)(a.M / 128 * 128);
-    rest.rows = (double)(a.M % 128);
+    top.rows = (double)(M / kBlock * kBlock);
+    rest.rows = (double)(M % kBlock);
     const Choice cm = choose(top, wide, &main_cost), cr = choose(rest, wide, &rest_cost);
-    if (rest.rows > 0 && main_cost + rest_cost < 0.95f * cost) {
-      ProductArgs m = a, r = a;
-      m.M = a.M / 128 * 128;
-      r.M = a.M - m.M;
-      const int size = elem_size(a.dtype);
-      r.A += m.M * a.lda;
-      r.sa += m.M;
-      r.C = (uint8_t*)a.C + m.M * a.ldc * size;
-      if (a.C0) r.C0 = (const uint8_t*)a.C0 + m.M * a.ldc0 * size;
-      const ws_status s = run_choice<MODE>(cm, m, stream);
-      return s != WS_OK ? s : run_choice<MODE>(cr, r, stream);
-    }
+    if (main_cost + rest_cost < 0.95f * cost) plan = Plan{2, M / kBlock * kBlock, {cm, cr}};
   }
-  return run_choice<MODE>(c, a, stream);
+  return plan;
+}
+
+template <int MODE>
+ws_status run_product(const ProductArgs& a, hipStream_t stream) {
+  const Plan plan = plan_product(MODE, a.M, a.N, MODE == kDepthGroups ? a.depth_rows : a.K, a.groups, a.dtype == WS_OUT_F32);
+  if (plan.count == 1) return run_choice<MODE>(plan.choice[0], a, stream);
+  ProductArgs m = a, r = a;
+  m.M = plan.split;
+  r.M = a.M - m.M;
+  const int size = elem_size(a.dtype);
+  r.A += m.M * a.lda;
+  r.sa += m.M;
+  r.C = (uint8_t*)a.C + m.M * a.ldc * size;
+  if (a.C0) r.C0 = (const uint8_t*)a.C0 + m.M * a.ldc0 * size;
+  const ws_status s = run_choice<MODE>(plan.choice[0], m, stream);
+  return s != WS_OK ? s : run_choice<MODE>(plan.choice[1], r, stream);
 }
 
 // Operands of a contraction over K columns; b_batch: B's matrices.
@@ -884,6 +895,34 @@ ProductArgs product_args(const ws_fp8_matrix* A, const ws_fp8_matrix* B, float a
 using namespace wsg;
 
 extern "C" {
+
+ws_status ws_fp8_plan(int64_t M, int64_t N, int64_t K, int32_t out_dtype, int32_t groups, int32_t depth,
+                      ws_fp8_kernel_info* out, int32_t* count) {
+  if (!out || !count || M < 0 || N < 0 || K < 0 || M > kMaxDim || N > kMaxDim || K > kMaxDim || !elem_size(out_dtype) || groups < 0 ||
+      groups > (1 << 20) || (groups == 0 && depth != 0))
+    return WS_ERR_INVALID_ARG;
+  *count = 0;
+  if (M == 0 || N == 0) return WS_OK;
+  const bool wide = out_dtype == WS_OUT_F32;
+  const Plan plan = plan_product(groups == 0 ? kDense : depth ? kDepthGroups : kRowGroups, M, N, K, groups, wide);
+  for (int i = 0; i < plan.count; ++i) {
+    ws_fp8_kernel_info k{};
+    switch (plan.choice[i]) {
+      case kDirect16: k = {16, 16, 0, 0}; break;
+      case kDirect32: k = {32, 16, 0, 0}; break;
+      case kDirect64: k = {64, 16, 0, 0}; break;
+      case kTile64: k = {64, 64, 2, 0}; break;
+      case kTile64Deep: k = {64, 64, 4, 0}; break;
+      case kTile128: k = {128, 128, 2, 0}; break;
+      case kTile128Deep: k = {128, 128, 4, 0}; break;
+      case kTile256: k = {256, wide ? 128 : 256, 2, 0}; break;
+    }
+    k.rows = i == 0 ? plan.split : M - plan.split;
+    out[i] = k;
+  }
+  *count = plan.count;
+  return WS_OK;
+}
 
 ws_status ws_fp8_product(const ws_fp8_matrix* A, const ws_fp8_matrix* B, float alpha, float beta, const ws_matrix* C0,
                          const ws_matrix* C, hipStream_t stream) {

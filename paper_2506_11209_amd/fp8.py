@@ -47,6 +47,10 @@ class ws_matrix(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("stride", ctypes.c_int64)]
 
 
+class ws_fp8_kernel_info(ctypes.Structure):
+    _fields_ = [("tile_m", ctypes.c_int32), ("tile_n", ctypes.c_int32), ("stages", ctypes.c_int32), ("rows", ctypes.c_int64)]
+
+
 _lib = _w.library()
 _p, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 _mp, _qp = ctypes.POINTER(ws_matrix), ctypes.POINTER(ws_fp8_matrix)
@@ -55,6 +59,7 @@ for _name, _args, _res in (
         ("ws_fp8_quantize_both", [_mp, _p, _i32, _p, _qp, _qp, _p], _i32),
         ("ws_fp8_padded_blocks", [_i64, _i32], _i64),
         ("ws_fp8_quantize_weight", [_mp, _qp, _qp, _p], _i32),
+        ("ws_fp8_plan", [_i64, _i64, _i64, _i32, _i32, _i32, ctypes.POINTER(ws_fp8_kernel_info), ctypes.POINTER(_i32)], _i32),
         ("ws_fp8_product", [_qp, _qp, _f32, _f32, _mp, _mp, _p], _i32),
         ("ws_fp8_grouped_product", [_qp, _qp, _i32, _p, _f32, _mp, _p], _i32),
         ("ws_fp8_grouped_gradient", [_qp, _qp, _i64, _i32, _p, _f32, _f32, _mp, _mp, _p], _i32)):
@@ -303,6 +308,16 @@ def _old(C0, beta: float, C):
     if C0.shape != C.shape or C0.dtype != C.dtype:
         raise ValueError("C0: expected %s %s, got %s %s" % (tuple(C.shape), C.dtype, tuple(C0.shape), C0.dtype))
     return _matrix(C0, "C0", (C.dim(),), C.device)
+
+
+def plan(M: int, N: int, K: int, out_dtype: str = "bf16", groups: int = 0, depth: bool = False) -> list:
+    """[(tile_m, tile_n, stages, rows)]: the launches of product (groups 0), of
+    grouped_product, or with depth of grouped_gradient over K rows."""
+    out, n = (ws_fp8_kernel_info * 2)(), _i32(0)
+    if out_dtype not in _DTYPES:
+        raise ValueError("out_dtype is one of %s, got %r" % (sorted(_DTYPES), out_dtype))
+    _check(_lib.ws_fp8_plan(M, N, K, _CODES[_DTYPES[out_dtype]], groups, int(depth), out, ctypes.byref(n)), "ws_fp8_plan")
+    return [(k.tile_m, k.tile_n, k.stages, k.rows) for k in out[: n.value]]
 
 
 def product(A: Fp8Matrix, B: Fp8Matrix, C=None, out_dtype: str = "bf16", alpha: float = 1.0, beta: float = 0.0, C0=None,
