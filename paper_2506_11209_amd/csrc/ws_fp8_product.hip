@@ -311,9 +311,10 @@ __device__ __forceinline__ void settle(f32x4_t& acc) {
 }
 
 // Writes a wave's part of a tile, 16 rows at a time by way of its own part of LDS,
-// so that a store covers whole stretches of a row.  Whole tiles to which nothing
-// is added are rounded before LDS and leave in 16-byte pieces, at addresses that
-// differ by scalars only; others pass LDS in binary32.
+// so that a store covers whole stretches of a row.  Where nothing is added, and the
+// columns are whole 16-byte pieces, the rows are rounded before LDS and leave in
+// such pieces, at addresses that differ by scalars only; else they pass LDS in
+// binary32.
 // rows, cols: of the tile, inside C.
 template <typename T, int WM, int WN, int STAGES>
 __device__ __forceinline__ void store_tile(const ProductArgs& a, const Part& p, f32x4_t (&acc)[WM][WN], uint8_t* own, int wm, int wn,
@@ -323,8 +324,13 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, const Part& p, 
   constexpr int N = 16 / sizeof(T), kRow = kCols * (int)sizeof(T) + 16, kPieces = kCols / N, kAtOnce = 64 / kPieces;  // kRow: bytes
   static_assert(16 * kRow <= Shape::kStoreBytes && 64 % kPieces == 0 && 16 % kAtOnce == 0, "16 rows in whole stores");
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const bool whole = a.beta == 0.0f && rows == Shape::TM && cols == Shape::TN && a.ldc <= (1 << 22);
-  const uint32_t ld = (uint32_t)a.ldc * (uint32_t)sizeof(T);  // bytes; used where whole
+  const bool plain = a.beta == 0.0f && a.ldc <= (1 << 22) && cols % N == 0;
+  const bool whole = rows == Shape::TM && cols == Shape::TN;
+  const int rows_left = rows - wm * 16 * WM - lane / kPieces;
+  bool in_cols[Shape::kStoreParts];
+#pragma unroll
+  for (int h = 0; h < Shape::kStoreParts; ++h) in_cols[h] = wn * 16 * WN + h * kCols + lane % kPieces * N < cols;
+  const uint32_t ld = (uint32_t)a.ldc * (uint32_t)sizeof(T);  // bytes; used where plain
   uint8_t* const to = (uint8_t*)a.C + uniform((p.c_at + (p.m0 + wm * 16 * WM) * a.ldc + p.n0 + wn * 16 * WN) * (int64_t)sizeof(T));
   const uint32_t mine = lane / kPieces * ld + lane % kPieces * 16;
   const uint8_t* const from = own + lane / kPieces * kRow + lane % kPieces * 16;
@@ -334,7 +340,7 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, const Part& p, 
     for (int h = 0; h < Shape::kStoreParts; ++h) {
 #pragma unroll
       for (int j = 0; j < kTiles; ++j) settle<Shape::kAgpr>(acc[i][h * kTiles + j]);
-      if (whole) {
+      if (plain) {
 #pragma unroll
         for (int j = 0; j < kTiles; ++j) {
           T t[4];
@@ -346,7 +352,9 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, const Part& p, 
         for (int e = 0; e < 16; e += kAtOnce) {
           T t[N];
           __builtin_memcpy(t, __builtin_assume_aligned(from + e * kRow, 16), 16);
-          store_n<T, N>((T*)(to + (uint64_t)(16 * i + e) * ld + h * kCols * sizeof(T) + mine), t);
+          T* c = (T*)(to + (uint64_t)(16 * i + e) * ld + h * kCols * sizeof(T) + mine);
+          if (whole) store_n<T, N>(c, t);
+          else if (in_cols[h] && 16 * i + e < rows_left) store_n<T, N>(c, t);
         }
       } else {
         float* f = (float*)own;
@@ -454,10 +462,15 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
   // of tiles at a time, so that those of one moment share operands in its L2.
   uint32_t tiles_m = (uint32_t)a.tiles_m;
   if (MODE == kRowGroups) tiles_m = (uint32_t)count_group_tiles(a.offsets, a.groups, a.M, TM);
+  // Groups of unlike depth are dealt out instead, every eighth tile to an XCD: with
+  // runs an XCD had two of 16 groups, and the one with the deepest took twice as long
+  // as the others (16 x 1024 x 2048 over 16384 rows: 146 us, dealt out 83 us).
   const uint32_t tiles_n = (uint32_t)a.tiles_n, plane = tiles_m * tiles_n, tiles = plane * (MODE == kDepthGroups ? a.groups : 1);
-  const uint32_t xcd = blockIdx.x % 8, share = tiles / 8, extra = tiles % 8, begin = xcd * share + min(xcd, extra),
-                 end = begin + share + (xcd < extra), stride = (gridDim.x + 7 - xcd) / 8;
-  uint32_t id = begin + blockIdx.x / 8;
+  const uint32_t xcd = blockIdx.x % 8, share = tiles / 8, extra = tiles % 8, turns = (gridDim.x + 7 - xcd) / 8;
+  const bool dealt = MODE == kDepthGroups;
+  const uint32_t begin = xcd * share + min(xcd, extra), end = dealt ? tiles : begin + share + (xcd < extra),
+                 stride = dealt ? 8 * turns : turns;
+  uint32_t id = dealt ? blockIdx.x : begin + blockIdx.x / 8;
 
   struct Tile {
     Part p;
