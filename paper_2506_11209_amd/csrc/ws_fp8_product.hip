@@ -281,6 +281,10 @@ struct TileShape {
   // One wave a SIMD with sums in accumulation registers, or more with all in the others.
   static constexpr int kWaves = WM * WN > 16 || STAGES * kStage > 80 * 1024 ? 1 : 2;
   static constexpr bool kAgpr = WM * WN > 16;
+  // Rows of products before a block's meeting point.  Few: the loads of the block
+  // after next, which keep the address unit busy for half a block of 256 x 256,
+  // spread over more products behind it.
+  static constexpr int kFirst = WM * WN > 32 ? 2 : WM / 2;
   // Two stages: a thread brings the scales of its rows of the tile block by block;
   // more: those of kDeep blocks at a time lie in LDS.
   static constexpr int kMine = (TM + TN + 255) / 256, kDeep = STAGES == 2 ? 2 : 32;
@@ -453,7 +457,7 @@ __device__ __forceinline__ void settle_scales(uint32_t& s) {
 template <int WM, int WN, int STAGES, int MODE, bool WIDE>
 __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile_kernel(ProductArgs a) {
   typedef TileShape<WM, WN, STAGES> Shape;
-  constexpr int TM = Shape::TM, TN = Shape::TN, kStage = Shape::kStage, kRows = TM + TN, kHalf = WM / 2;
+  constexpr int TM = Shape::TM, TN = Shape::TN, kStage = Shape::kStage, kRows = TM + TN, kFirst = Shape::kFirst, kRest = WM - kFirst;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
@@ -584,14 +588,18 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
 #pragma unroll
       for (int j = 0; j < WN; ++j) fb[j] = frag(fb0 + j * 2048, 0);
 #pragma unroll
-      for (int i = 0; i < kHalf; ++i) fa[i] = frag(fa0 + i * 2048, 0);
+      for (int i = 0; i < kFirst; ++i) fa[i] = frag(fa0 + i * 2048, 0);
+#pragma unroll
+      for (int i = 0; i < (WM + 3) / 4; ++i) settle_scales(sa[i]);
+#pragma unroll
+      for (int j = 0; j < (WN + 3) / 4; ++j) settle_scales(sb[j]);
       __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): in the loop the compiler then counts LDS reads only
       for (int b = 0; b < t.blocks; ++b) {
         const int here = b % STAGES * kStage, next = (b + 1) % STAGES * kStage;
         if constexpr (WIDE) {
-          Wide wa[kHalf], wb = widen_all(fb[0], sb[0], 0);
+          Wide wa[kFirst], wb = widen_all(fb[0], sb[0], 0);
 #pragma unroll
-          for (int i = 0; i < kHalf; ++i) wa[i] = widen_all(fa[i], sa[i / 4], i % 4);
+          for (int i = 0; i < kFirst; ++i) wa[i] = widen_all(fa[i], sa[i / 4], i % 4);
           static_for<WN>([&](auto jc) {
             constexpr int j = decltype(jc)::value;
             __builtin_amdgcn_sched_barrier(0);
@@ -599,40 +607,49 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
 #pragma unroll
             for (int q = 0; q < 4; ++q)  // a sum's next product comes after the other rows'
 #pragma unroll
-              for (int i = 0; i < kHalf; ++i) multiply_wide<Shape::kAgpr>(acc[i][j], wa[i].part[q], wb.part[q]);
+              for (int i = 0; i < kFirst; ++i) multiply_wide<Shape::kAgpr>(acc[i][j], wa[i].part[q], wb.part[q]);
 #pragma unroll
-            for (int k = j * kHalf / WN; k < (j + 1) * kHalf / WN; ++k) fa[kHalf + k] = frag(fa0 + (kHalf + k) * 2048, here);
+            for (int k = j * kRest / WN; k < (j + 1) * kRest / WN; ++k) fa[kFirst + k] = frag(fa0 + (kFirst + k) * 2048, here);
             if constexpr (j + 1 < WN) wb = widen_all(fb[j + 1], sb[(j + 1) / 4], (j + 1) % 4);
           });
           __builtin_amdgcn_sched_barrier(0);
         } else {
-          static_for<kHalf>([&](auto ic) {
+          static_for<kFirst>([&](auto ic) {
             constexpr int i = decltype(ic)::value;
             static_for<WN>([&](auto jc) {
-              constexpr int j = decltype(jc)::value;
-              if (j == 1) fa[kHalf + i] = frag(fa0 + (kHalf + i) * 2048, here);
+              constexpr int j = decltype(jc)::value, at = i * WN + j, all = kFirst * WN - 1;
               multiply<Shape::kAgpr, i % 4, j % 4>(acc[i][j], fa[i], fb[j], sa[i / 4], sb[j / 4]);
+#pragma unroll
+              for (int k = at * kRest / all; k < (at + 1) * kRest / all && at < all; ++k)
+                fa[kFirst + k] = frag(fa0 + (kFirst + k) * 2048, here);
             });
             __builtin_amdgcn_sched_barrier(0);
           });
         }
         drain_and_meet<kLoads * (STAGES - 2)>();
-        if constexpr (STAGES == 2) {
-          keep_scales(b + 2, byte);
-          __builtin_amdgcn_sched_barrier(0);
-          fetch_scales(b + 3, byte);
-        } else if ((b + 1) % Shape::kDeep == 0 && b + 1 < t.blocks) {  // the next blocks' scales; every wave has read the last
-          fill_scales(b + 1);
-          drain_and_meet();
-        }
         uint32_t next_sa[(WM + 3) / 4], next_sb[(WN + 3) / 4];
-        read_scales(b + 1, next_sa, next_sb);
-        // loads one at a time between products: two at once hold up the products behind them
-        constexpr int kPer = kLoads / WN;
+        // What else the block needs is done between its products: the scales first
+        // (before the loads, which their wait would wait for), then the loads, one at
+        // a time (two hold up the products behind them), and the next operands.
+        const auto scales_next = [&]() {
+          if constexpr (STAGES == 2) {
+            keep_scales(b + 2, byte);
+            fetch_scales(b + 3, byte);
+          }
+          read_scales(b + 1, next_sa, next_sb);
+        };
+        if constexpr (STAGES > 2)
+          if ((b + 1) % Shape::kDeep == 0 && b + 1 < t.blocks) {  // the next blocks' scales; every wave has read the last
+            fill_scales(b + 1);
+            drain_and_meet();
+          }
         if constexpr (WIDE) {
-          Wide wa[kHalf], wb = widen_all(fb[0], sb[0], 0);
+          constexpr int kPer = kLoads / WN;
+          scales_next();
+          __builtin_amdgcn_sched_barrier(0);
+          Wide wa[kRest], wb = widen_all(fb[0], sb[0], 0);
 #pragma unroll
-          for (int i = 0; i < kHalf; ++i) wa[i] = widen_all(fa[kHalf + i], sa[(kHalf + i) / 4], (kHalf + i) % 4);
+          for (int i = 0; i < kRest; ++i) wa[i] = widen_all(fa[kFirst + i], sa[(kFirst + i) / 4], (kFirst + i) % 4);
           static_for<WN>([&](auto jc) {
             constexpr int j = decltype(jc)::value;
             __builtin_amdgcn_sched_barrier(0);
@@ -640,25 +657,32 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
 #pragma unroll
-              for (int i = 0; i < kHalf; ++i) multiply_wide<Shape::kAgpr>(acc[kHalf + i][j], wa[i].part[q], wb.part[q]);
+              for (int i = 0; i < kRest; ++i) multiply_wide<Shape::kAgpr>(acc[kFirst + i][j], wa[i].part[q], wb.part[q]);
               load(b + STAGES, j * kPer + q * kPer / 4, j * kPer + (q + 1) * kPer / 4);
             }
 #pragma unroll
-            for (int k = j * kHalf / WN; k < (j + 1) * kHalf / WN; ++k) fa[k] = frag(fa0 + k * 2048, next);
+            for (int k = j * kFirst / WN; k < (j + 1) * kFirst / WN; ++k) fa[k] = frag(fa0 + k * 2048, next);
             fb[j] = frag(fb0 + j * 2048, next);
             if constexpr (j + 1 < WN) wb = widen_all(fb[j + 1], sb[(j + 1) / 4], (j + 1) % 4);
           });
           __builtin_amdgcn_sched_barrier(0);
         } else {
+          // loads follow the products of columns kFrom .. kTo - 1
+          constexpr int kFrom = WN > 2 ? 1 : 0, kTo = WN > 4 ? WN - 2 : WN, kSlots = (kTo - kFrom) * kRest;
           static_for<WN>([&](auto jc) {
             constexpr int j = decltype(jc)::value;
-            static_for<kHalf>([&](auto ic) {
-              constexpr int i = decltype(ic)::value, row = kHalf + i;
+            static_for<kRest>([&](auto ic) {
+              constexpr int i = decltype(ic)::value, row = kFirst + i, at = (j - kFrom) * kRest + i;
               multiply<Shape::kAgpr, row % 4, j % 4>(acc[row][j], fa[row], fb[j], sa[row / 4], sb[j / 4]);
-              load(b + STAGES, j * kPer + i * kPer / kHalf, j * kPer + (i + 1) * kPer / kHalf);
-              if (i == 0) {
+              if constexpr (j == 0 && i == 0) {
+                __builtin_amdgcn_sched_barrier(0);
+                scales_next();
+                __builtin_amdgcn_sched_barrier(0);
+              }
+              if constexpr (at >= 0 && at < kSlots) load(b + STAGES, at * kLoads / kSlots, (at + 1) * kLoads / kSlots);
+              if constexpr (i == 0) {
 #pragma unroll
-                for (int k = j * kHalf / WN; k < (j + 1) * kHalf / WN; ++k) fa[k] = frag(fa0 + k * 2048, next);
+                for (int k = j * kFirst / WN; k < (j + 1) * kFirst / WN; ++k) fa[k] = frag(fa0 + k * 2048, next);
                 if constexpr (j > 0) fb[j - 1] = frag(fb0 + (j - 1) * 2048, next);
               }
             });
