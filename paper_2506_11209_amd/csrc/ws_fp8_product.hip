@@ -284,7 +284,7 @@ struct TileShape {
   // Rows of products before a block's meeting point.  Few: the loads of the block
   // after next, which keep the address unit busy for half a block of 256 x 256,
   // spread over more products behind it.
-  static constexpr int kFirst = WM * WN > 32 ? 2 : WM / 2;
+  static constexpr int kFirst = WM * WN > 32 ? 3 : WM / 2;
   // Two stages: a thread brings the scales of its rows of the tile block by block;
   // more: those of kDeep blocks at a time lie in LDS.
   static constexpr int kMine = (TM + TN + 255) / 256, kDeep = STAGES == 2 ? 2 : 32;
@@ -617,7 +617,7 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
           static_for<kFirst>([&](auto ic) {
             constexpr int i = decltype(ic)::value;
             static_for<WN>([&](auto jc) {
-              constexpr int j = decltype(jc)::value, at = i * WN + j, all = kFirst * WN - 1;
+              constexpr int j = decltype(jc)::value, at = i * WN + j, all = (kFirst * WN - 1) / (kFirst > 2 ? 2 : 1);
               multiply<Shape::kAgpr, i % 4, j % 4>(acc[i][j], fa[i], fb[j], sa[i / 4], sb[j / 4]);
 #pragma unroll
               for (int k = at * kRest / all; k < (at + 1) * kRest / all && at < all; ++k)
@@ -668,7 +668,7 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
           __builtin_amdgcn_sched_barrier(0);
         } else {
           // loads follow the products of columns kFrom .. kTo - 1
-          constexpr int kFrom = WN > 2 ? 1 : 0, kTo = WN > 4 ? WN - 2 : WN, kSlots = (kTo - kFrom) * kRest;
+          constexpr int kFrom = WN > 2 ? 1 : 0, kTo = WN > 4 ? WN - 1 : WN, kSlots = (kTo - kFrom) * kRest;
           static_for<WN>([&](auto jc) {
             constexpr int j = decltype(jc)::value;
             static_for<kRest>([&](auto ic) {

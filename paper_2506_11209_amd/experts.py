@@ -17,7 +17,7 @@ import ctypes
 import torch
 
 from . import wsgemm as _w
-from .fp8 import _call, _check, _matrix, _mp, _need, _new_matrix
+from .fp8 import _Call, _check, _elsewhere, _matrix, _mp, _need, _new_matrix, _raw_stream
 
 MAX_EXPERTS = 1024
 
@@ -64,15 +64,17 @@ def sort(ids, experts: int, stream=None) -> Routes:
     need = _lib.ws_expert_sort_workspace(tokens, k, experts)
     if need < 0:
         raise ValueError("sort: 1 to %d experts, got %r, and at most 2^30 choices, got %d" % (MAX_EXPERTS, experts, ids.numel()))
+    if _elsewhere(ids, stream):
+        with _Call(ids.device, stream, [ids]):
+            return sort(ids, experts)
     n, device = tokens * k, ids.device
-    with _call(device, stream, ids) as st:
-        r = object.__new__(Routes)
-        r.offsets = offsets = torch.empty(experts + 1, dtype=torch.int32, device=device)
-        r.token = token = torch.empty(n, dtype=torch.int32, device=device)
-        r.place = place = torch.empty(tokens, k, dtype=torch.int32, device=device)
-        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        _check(_lib.ws_expert_sort(tokens, k, experts, ids.data_ptr(), ids.element_size(), offsets.data_ptr(), token.data_ptr(),
-                                   place.data_ptr(), work.data_ptr() if need else 0, need, st), "ws_expert_sort")
+    r = object.__new__(Routes)
+    r.offsets = offsets = torch.empty(experts + 1, dtype=torch.int32, device=device)
+    r.token = token = torch.empty(n, dtype=torch.int32, device=device)
+    r.place = place = torch.empty(tokens, k, dtype=torch.int32, device=device)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _check(_lib.ws_expert_sort(tokens, k, experts, ids.data_ptr(), ids.element_size(), offsets.data_ptr(), token.data_ptr(),
+                               place.data_ptr(), work.data_ptr() if need else 0, need, _raw_stream(device.index)), "ws_expert_sort")
     return r
 
 
@@ -99,9 +101,11 @@ def gather(x, routes: Routes, out=None, stream=None):
     m = _matrix(x, "x", device=routes.token.device)
     if m.rows != routes.place.shape[0]:
         raise ValueError("x: %d rows for %d tokens" % (m.rows, routes.place.shape[0]))
-    with _call(x.device, stream, x, routes.token, out) as st:
-        out, mo = _out(out, "out", routes.token.numel(), m.cols, x)
-        _check(_lib.ws_expert_gather(m, routes.token.data_ptr(), mo, st), "ws_expert_gather")
+    if _elsewhere(x, stream):
+        with _Call(x.device, stream, [x, routes.token, out]):
+            return gather(x, routes, out)
+    out, mo = _out(out, "out", routes.token.numel(), m.cols, x)
+    _check(_lib.ws_expert_gather(m, routes.token.data_ptr(), mo, _raw_stream(x.get_device())), "ws_expert_gather")
     return out
 
 
@@ -112,9 +116,11 @@ def combine(h, routes: Routes, weights=None, out=None, stream=None):
     if m.rows != routes.token.numel():
         raise ValueError("h: %d rows for %d choices" % (m.rows, routes.token.numel()))
     w, (tokens, k) = _weights(weights, routes), routes.place.shape
-    with _call(h.device, stream, h, routes.place, weights, out) as st:
-        out, mo = _out(out, "out", tokens, m.cols, h)
-        _check(_lib.ws_expert_combine(m, k, routes.place.data_ptr(), w, mo, st), "ws_expert_combine")
+    if _elsewhere(h, stream):
+        with _Call(h.device, stream, [h, routes.place, weights, out]):
+            return combine(h, routes, weights, out)
+    out, mo = _out(out, "out", tokens, m.cols, h)
+    _check(_lib.ws_expert_combine(m, k, routes.place.data_ptr(), w, mo, _raw_stream(h.get_device())), "ws_expert_combine")
     return out
 
 
@@ -131,10 +137,12 @@ def combine_gradient(dy, h, routes: Routes, weights=None, dh=None, stream=None):
             raise ValueError("h: expected %s %s, got %s %s" % ((routes.token.numel(), m.cols), dy.dtype, tuple(h.shape), h.dtype))
     else:
         mh = None
-    with _call(dy.device, stream, dy, h, routes.offsets, routes.place, weights, dh) as st:
-        dh, mdh = _out(dh, "dh", routes.token.numel(), m.cols, dy)
-        dw = torch.empty(tokens, k, dtype=torch.float32, device=dy.device) if weights is not None else None
-        _check(_lib.ws_expert_combine_gradient(m, mh, k, routes.experts, routes.offsets.data_ptr(), routes.place.data_ptr(), w,
-                                               mdh, dw.data_ptr() if dw is not None else 0, st),
-               "ws_expert_combine_gradient")
+    if _elsewhere(dy, stream):
+        with _Call(dy.device, stream, [dy, h, routes.offsets, routes.place, weights, dh]):
+            return combine_gradient(dy, h, routes, weights, dh)
+    dh, mdh = _out(dh, "dh", routes.token.numel(), m.cols, dy)
+    dw = torch.empty(tokens, k, dtype=torch.float32, device=dy.device) if weights is not None else None
+    _check(_lib.ws_expert_combine_gradient(m, mh, k, routes.experts, routes.offsets.data_ptr(), routes.place.data_ptr(), w, mdh,
+                                           dw.data_ptr() if dw is not None else 0, _raw_stream(dy.get_device())),
+           "ws_expert_combine_gradient")
     return dh, dw

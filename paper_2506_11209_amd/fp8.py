@@ -80,52 +80,34 @@ def _check(status: int, where: str) -> None:
 
 
 class _Call:
-    """The stream a call enqueues on, as a context in which results are made, for
-    calls that do not use the current stream of the current device."""
+    """Makes a call's stream and device the current ones, so that its results and
+    work memory belong to it, and marks tensors as in use by it."""
 
-    __slots__ = ("raw", "_stack")
+    __slots__ = ("_stack",)
 
     def __init__(self, device: torch.device, stream, tensors):
         self._stack = contextlib.ExitStack()
         self._stack.enter_context(torch.cuda.device(device))
         if stream is None:
-            self.raw = _raw_stream(device.index)
             return
         if stream.device != device:
             raise ValueError("the stream belongs to %s, the tensors to %s" % (stream.device, device))
         self._stack.enter_context(torch.cuda.stream(stream))
-        self.raw = stream.cuda_stream
         for t in tensors:
             if t is not None:
                 t.record_stream(stream)
 
     def __enter__(self):
-        return self.raw
+        return self
 
     def __exit__(self, *exc):
         self._stack.close()
 
 
-class _Here:
-    """The current stream of the current device: nothing to enter or leave."""
-
-    __slots__ = ("raw",)
-
-    def __init__(self, raw):
-        self.raw = raw
-
-    def __enter__(self):
-        return self.raw
-
-    def __exit__(self, *exc):
-        pass
-
-
-def _call(device: torch.device, stream, *tensors):
-    index = device.index
-    if stream is None and index == _current_device():
-        return _Here(_raw_stream(index))
-    return _Call(device, stream, tensors)
+def _elsewhere(t, stream):
+    """Whether a call on t does not use the current stream of t's device, or that is
+    not the current device: then it is made again inside a _Call."""
+    return stream is not None or t.get_device() != _current_device()
 
 
 def _need(t, what: str, dtypes, dims, device=None):
@@ -140,13 +122,22 @@ def _need(t, what: str, dtypes, dims, device=None):
 
 def _matrix(t, what: str, dims=(2,), device=None) -> ws_matrix:
     """Descriptor of a float tensor (batch x) rows x cols whose columns lie next to each other."""
-    _need(t, what, _CODES, dims, device)
+    code = _CODES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if code is None or not t.is_cuda or t.dim() not in dims or (device is not None and t.device != device):
+        _need(t, what, _CODES, dims, device)
     shape, stride = t.shape, t.stride()
-    rows, cols = shape[-2], shape[-1]
-    if cols > 1 and stride[-1] != 1 or rows > 1 and stride[-2] < cols:
+    if len(shape) == 2:
+        rows, cols = shape
+        ld = stride[0]
+        if rows <= 1:
+            ld = cols
+        if cols > 1 and stride[1] != 1 or ld < cols:
+            raise ValueError("%s: columns have to lie next to each other and rows may not overlap, got strides %s" % (what, stride))
+        return ws_matrix(t.data_ptr(), rows, cols, ld, code, 1, 0)
+    batch, rows, cols = shape
+    if cols > 1 and stride[2] != 1 or rows > 1 and stride[1] < cols:
         raise ValueError("%s: columns have to lie next to each other and rows may not overlap, got strides %s" % (what, stride))
-    return ws_matrix(t.data_ptr(), rows, cols, stride[-2] if rows > 1 else cols, _CODES[t.dtype],
-                     shape[0] if len(shape) == 3 else 1, stride[0] if len(shape) == 3 else 0)
+    return ws_matrix(t.data_ptr(), rows, cols, stride[1] if rows > 1 else cols, code, batch, stride[0])
 
 
 def _new_matrix(rows: int, cols: int, dtype: torch.dtype, device):
@@ -229,15 +220,22 @@ def _fits(q, what: str, rows: int, cols: int, block_rows: int, batch, device) ->
     return q
 
 
+def _both(*qs):
+    return [t for q in qs if q is not None for t in (q.codes, q.scales)]
+
+
 def quantize_rows(x, index=None, out: Fp8Matrix | None = None, stream=None) -> Fp8Matrix:
     """x (rows x cols; f32, bf16 or f16) with a scale for every 1 x 128 values.
     index (int32): the source row of each result row; out of range, zeros."""
     m = _matrix(x, "x")
+    if _elsewhere(x, stream):
+        with _Call(x.device, stream, [x, index] + _both(out)):
+            return quantize_rows(x, index, out)
+    device = x.device
     rows = m.rows if index is None else index.numel()
-    at = _index(index, "index", rows, x.device)
-    with _call(x.device, stream, x, index, *((out.codes, out.scales) if out is not None else ())) as st:
-        q = Fp8Matrix.empty(rows, m.cols, device=x.device) if out is None else _fits(out, "out", rows, m.cols, 1, None, x.device)
-        _check(_ws_fp8_quantize_rows(m, at, q._desc, st), "ws_fp8_quantize_rows")
+    at = 0 if index is None else _index(index, "index", rows, device)
+    q = Fp8Matrix.empty(rows, m.cols, device=device) if out is None else _fits(out, "out", rows, m.cols, 1, None, device)
+    _check(_ws_fp8_quantize_rows(m, at, q._desc, _raw_stream(device.index)), "ws_fp8_quantize_rows")
     return q
 
 
@@ -252,20 +250,22 @@ def quantize_both(x, index=None, offsets=None, out=None, stream=None):
     of each group, padded to 128 (see grouped_gradient), and rows in no group are
     zeros."""
     m = _matrix(x, "x")
+    if _elsewhere(x, stream):
+        with _Call(x.device, stream, [x, index, offsets] + _both(*(out or ()))):
+            return quantize_both(x, index, offsets, out)
+    device = x.device
     rows = m.rows if index is None else index.numel()
-    at = _index(index, "index", rows, x.device)
+    at = _index(index, "index", rows, device)
     groups = 0 if offsets is None else offsets.numel() - 1
     if offsets is not None and groups < 1:
         raise ValueError("offsets: expected one more than groups")
-    off = _index(offsets, "offsets", groups + 1, x.device)
+    off = _index(offsets, "offsets", groups + 1, device)
     deep = padded_rows(rows, groups) if groups else rows
-    used = () if out is None else (out[0].codes, out[0].scales, out[1].codes, out[1].scales)
-    with _call(x.device, stream, x, index, offsets, *used) as st:
-        if out is None:
-            q, t = Fp8Matrix.empty(rows, m.cols, device=x.device), Fp8Matrix.empty(m.cols, deep, device=x.device)
-        else:
-            q, t = _fits(out[0], "out[0]", rows, m.cols, 1, None, x.device), _fits(out[1], "out[1]", m.cols, deep, 1, None, x.device)
-        _check(_lib.ws_fp8_quantize_both(m, at, groups, off, q._desc, t._desc, st), "ws_fp8_quantize_both")
+    if out is None:
+        q, t = Fp8Matrix.empty(rows, m.cols, device=device), Fp8Matrix.empty(m.cols, deep, device=device)
+    else:
+        q, t = _fits(out[0], "out[0]", rows, m.cols, 1, None, device), _fits(out[1], "out[1]", m.cols, deep, 1, None, device)
+    _check(_lib.ws_fp8_quantize_both(m, at, groups, off, q._desc, t._desc, _raw_stream(device.index)), "ws_fp8_quantize_both")
     return q, t
 
 
@@ -273,16 +273,19 @@ def quantize_weight(w, transposed: bool = True, out=None, stream=None):
     """(w, its transpose) with a scale for every 128 x 128 values; w is out x in,
     or experts x out x in.  transposed=False: (w, None)."""
     m = _matrix(w, "w", (2, 3))
+    if _elsewhere(w, stream):
+        with _Call(w.device, stream, [w] + _both(*(out or ()))):
+            return quantize_weight(w, transposed, out)
+    device = w.device
     batch = m.batch if w.dim() == 3 else None
-    used = () if out is None else tuple(t for q in out if q is not None for t in (q.codes, q.scales))
-    with _call(w.device, stream, w, *used) as st:
-        if out is None:
-            q = Fp8Matrix.empty(m.rows, m.cols, BLOCK, batch, w.device)
-            t = Fp8Matrix.empty(m.cols, m.rows, BLOCK, batch, w.device) if transposed else None
-        else:
-            q = _fits(out[0], "out[0]", m.rows, m.cols, BLOCK, batch, w.device)
-            t = _fits(out[1], "out[1]", m.cols, m.rows, BLOCK, batch, w.device) if transposed else None
-        _check(_lib.ws_fp8_quantize_weight(m, q._desc, t._desc if t is not None else None, st), "ws_fp8_quantize_weight")
+    if out is None:
+        q = Fp8Matrix.empty(m.rows, m.cols, BLOCK, batch, device)
+        t = Fp8Matrix.empty(m.cols, m.rows, BLOCK, batch, device) if transposed else None
+    else:
+        q = _fits(out[0], "out[0]", m.rows, m.cols, BLOCK, batch, device)
+        t = _fits(out[1], "out[1]", m.cols, m.rows, BLOCK, batch, device) if transposed else None
+    _check(_lib.ws_fp8_quantize_weight(m, q._desc, t._desc if t is not None else None, _raw_stream(device.index)),
+           "ws_fp8_quantize_weight")
     return q, t
 
 
@@ -326,15 +329,17 @@ def product(A: Fp8Matrix, B: Fp8Matrix, C=None, out_dtype: str = "bf16", alpha: 
     scales for 1 or 128 rows.  Written to C (M x N; its type counts) or a new
     tensor of out_dtype ("f32", "bf16", "f16").  C0 may be C."""
     codes = A.codes
+    if _elsewhere(codes, stream):
+        with _Call(codes.device, stream, _both(A, B) + [C, C0]):
+            return product(A, B, C, out_dtype, alpha, beta, C0)
     device = codes.device
     if codes.dim() == 3 or B.codes.dim() == 3 or B.codes.device != device:
         raise ValueError("A and B have to be single matrices on one device")
     if A.cols != B.cols or A.block_rows != 1:
         raise ValueError("A (%d x %d) and B (%d x %d) have to have as many columns, A scales for single rows" % (
             A.rows, A.cols, B.rows, B.cols))
-    with _call(device, stream, codes, A.scales, B.codes, B.scales, C, C0) as st:
-        C, m = _result(C, out_dtype, (A.rows, B.rows), device)
-        _check(_ws_fp8_product(A._desc, B._desc, alpha, beta, _old(C0, beta, C), m, st), "ws_fp8_product")
+    C, m = _result(C, out_dtype, (A.rows, B.rows), device)
+    _check(_ws_fp8_product(A._desc, B._desc, alpha, beta, _old(C0, beta, C), m, _raw_stream(device.index)), "ws_fp8_product")
     return C
 
 
@@ -344,10 +349,12 @@ def grouped_product(A: Fp8Matrix, B: Fp8Matrix, offsets, C=None, out_dtype: str 
     device = A.codes.device
     if A.batch is not None or B.batch is None or A.cols != B.cols or A.block_rows != 1 or B.codes.device != device:
         raise ValueError("A has to be a single matrix with scales for single rows, B a batch of as many columns on its device")
+    if _elsewhere(A.codes, stream):
+        with _Call(device, stream, _both(A, B) + [offsets, C]):
+            return grouped_product(A, B, offsets, C, out_dtype, alpha)
     off = _index(offsets, "offsets", B.batch + 1, device)
-    with _call(device, stream, A.codes, A.scales, B.codes, B.scales, offsets, C) as st:
-        C, m = _result(C, out_dtype, (A.rows, B.rows), device)
-        _check(_lib.ws_fp8_grouped_product(A._desc, B._desc, B.batch, off, alpha, m, st), "ws_fp8_grouped_product")
+    C, m = _result(C, out_dtype, (A.rows, B.rows), device)
+    _check(_lib.ws_fp8_grouped_product(A._desc, B._desc, B.batch, off, alpha, m, _raw_stream(device.index)), "ws_fp8_grouped_product")
     return C
 
 
@@ -358,14 +365,16 @@ def grouped_gradient(A: Fp8Matrix, B: Fp8Matrix, rows: int, offsets, C=None, out
     the columns that quantize_both makes of ``rows`` rows under these offsets; the
     result is groups x M x N, zeros (beta C0) for an empty group."""
     device = A.codes.device
+    if _elsewhere(A.codes, stream):
+        with _Call(device, stream, _both(A, B) + [offsets, C, C0]):
+            return grouped_gradient(A, B, rows, offsets, C, out_dtype, alpha, beta, C0)
     groups = offsets.numel() - 1
     off = _index(offsets, "offsets", groups + 1, device)
     if A.batch is not None or B.batch is not None or A.block_rows != 1 or B.block_rows != 1 or B.codes.device != device:
         raise ValueError("A and B have to be single matrices with scales for single rows on one device")
     if groups < 1 or A.cols != B.cols or A.cols != padded_rows(rows, groups):
         raise ValueError("A and B have to hold the padded columns of %d rows in %d groups" % (rows, groups))
-    with _call(device, stream, A.codes, A.scales, B.codes, B.scales, offsets, C, C0) as st:
-        C, m = _result(C, out_dtype, (groups, A.rows, B.rows), device)
-        _check(_lib.ws_fp8_grouped_gradient(A._desc, B._desc, rows, groups, off, alpha, beta, _old(C0, beta, C), m, st),
-               "ws_fp8_grouped_gradient")
+    C, m = _result(C, out_dtype, (groups, A.rows, B.rows), device)
+    _check(_lib.ws_fp8_grouped_gradient(A._desc, B._desc, rows, groups, off, alpha, beta, _old(C0, beta, C), m,
+                                        _raw_stream(device.index)), "ws_fp8_grouped_gradient")
     return C
