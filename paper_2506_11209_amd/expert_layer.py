@@ -1,0 +1,133 @@
+"""A layer of experts in 8 bits, trained and served with this library's operators.
+
+Every token goes to k of E experts, y = sum over its choices of weight * W2 silu(W1
+x).  Forward: the choices are sorted by expert, the tokens' rows are quantised in
+that order (gathered on the way, both forms from one read), and the experts'
+products run as grouped products; the rows go back to their tokens with the
+router's weights.  Backward: the gradient of the way back, the input gradients as
+grouped products with the transposed weights, the weight gradients as products
+over each expert's rows in 32 bits.
+
+    python -m paper_2506_11209_amd.expert_layer [--tokens 4096] [--experts 16] ...
+
+times a training step and a decoding step on the GPU and prints a line for each.
+"""
+from __future__ import annotations
+
+import argparse
+import json
+import time
+
+import torch
+
+from . import experts, fp8
+
+
+class _Experts(torch.autograd.Function):
+    """y of x, the choices' weights (tokens x k, f32) and ids (tokens x k); w1 is E x
+    hidden x columns, w2 is E x columns x hidden."""
+
+    @staticmethod
+    def forward(ctx, x, weights, w1, w2, ids):
+        routes = experts.sort(ids, w1.shape[0])
+        xq, xt = fp8.quantize_both(x, index=routes.token, offsets=routes.offsets)
+        w1q, w1t = fp8.quantize_weight(w1)
+        h = fp8.grouped_product(xq, w1q, routes.offsets)
+        aq, at = fp8.quantize_both(torch.nn.functional.silu(h), offsets=routes.offsets)
+        w2q, w2t = fp8.quantize_weight(w2)
+        rows = fp8.grouped_product(aq, w2q, routes.offsets)
+        y = experts.combine(rows, routes, weights)
+        # quantised operands are kept, not the tensors they came from
+        ctx.save_for_backward(weights, h, rows)
+        ctx.routes, ctx.operands = routes, (xt, at, w1t, w2t)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        weights, h, rows = ctx.saved_tensors
+        routes, (xt, at, w1t, w2t) = ctx.routes, ctx.operands
+        off, n = routes.offsets, routes.token.numel()
+        drows, dweights = experts.combine_gradient(dy.contiguous(), rows, routes, weights)
+        gq, gt = fp8.quantize_both(drows, offsets=off)
+        dw2 = fp8.grouped_gradient(gt, at, n, off)
+        da = fp8.grouped_product(gq, w2t, off).float()
+        s = torch.sigmoid(h.float())
+        dh = (da * (s * (1.0 + h.float() * (1.0 - s)))).to(h.dtype)
+        hq, ht = fp8.quantize_both(dh, offsets=off)
+        dw1 = fp8.grouped_gradient(ht, xt, n, off)
+        dx = experts.combine(fp8.grouped_product(hq, w1t, off), routes)
+        return dx, dweights, dw1, dw2, None
+
+
+class ExpertLayer(torch.nn.Module):
+    """columns -> hidden -> columns by k of `count` experts; master weights in
+    binary32, activations in bf16."""
+
+    def __init__(self, columns: int, hidden: int, count: int, k: int, device="cuda", generator=None):
+        super().__init__()
+        make = lambda *s: torch.nn.Parameter(  # noqa: E731
+            torch.randn(*s, device=device, generator=generator) / s[-1] ** 0.5)
+        self.router, self.w1, self.w2 = make(count, columns), make(count, hidden, columns), make(count, columns, hidden)
+        self.k = k
+
+    def route(self, x):
+        """(weights, ids) of each token's k best experts."""
+        score, ids = (x.float() @ self.router.t()).topk(self.k, dim=1)
+        return score.softmax(1), ids
+
+    def forward(self, x):
+        weights, ids = self.route(x)
+        return _Experts.apply(x, weights, self.w1, self.w2, ids)
+
+    @torch.no_grad()
+    def serving_weights(self):
+        """The experts' weights in 8 bits, laid out once for serve."""
+        return fp8.quantize_weight(self.w1, transposed=False)[0], fp8.quantize_weight(self.w2, transposed=False)[0]
+
+    @torch.no_grad()
+    def serve(self, x, quantized):
+        """forward without what training keeps; quantized: serving_weights()."""
+        weights, ids = self.route(x)
+        routes = experts.sort(ids, self.w1.shape[0])
+        h = fp8.grouped_product(fp8.quantize_rows(x, index=routes.token), quantized[0], routes.offsets)
+        rows = fp8.grouped_product(fp8.quantize_rows(torch.nn.functional.silu(h)), quantized[1], routes.offsets)
+        return experts.combine(rows, routes, weights)
+
+
+def _time(step, steps: int) -> float:
+    for _ in range(3):
+        step()
+    torch.cuda.synchronize()
+    begin = time.perf_counter()
+    for _ in range(steps):
+        step()
+    torch.cuda.synchronize()
+    return (time.perf_counter() - begin) / steps
+
+
+def main(argv=None) -> None:
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    for name, value in (("tokens", 4096), ("decode", 32), ("columns", 2048), ("hidden", 4096), ("experts", 16), ("k", 2), ("steps", 20)):
+        ap.add_argument("--" + name, type=int, default=value)
+    a = ap.parse_args(argv)
+    g = torch.Generator(device="cuda").manual_seed(0)
+    layer = ExpertLayer(a.columns, a.hidden, a.experts, a.k, generator=g)
+    x = torch.randn(a.tokens, a.columns, device="cuda", generator=g).bfloat16().requires_grad_()
+    dy = torch.randn(a.tokens, a.columns, device="cuda", generator=g).bfloat16()
+    few = x.detach()[: a.decode].contiguous()
+    quantized = layer.serving_weights()
+
+    def train():
+        layer.zero_grad()
+        x.grad = None
+        layer(x).backward(dy)
+
+    flops = 6.0 * a.tokens * a.k * a.columns * a.hidden * 2
+    s = _time(train, a.steps)
+    print(json.dumps({"step": "training", "tokens": a.tokens, "us": round(s * 1e6, 1), "tflops": round(flops / s / 1e12, 1)}), flush=True)
+    s = _time(lambda: layer.serve(few, quantized), a.steps)
+    print(json.dumps({"step": "decoding", "tokens": few.shape[0], "us": round(s * 1e6, 1)}), flush=True)
+
+
+if __name__ == "__main__":
+    main()
