@@ -86,6 +86,13 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
+// The tile of workgroup `id` of n when each XCD (workgroups go round the eight in
+// turn) takes a run of neighbours: lines that two tiles share meet in one L2.
+__device__ __forceinline__ uint32_t xcd_run(uint32_t id, uint32_t n) {
+  const uint32_t share = n / 8, extra = n % 8, x = id % 8;
+  return x * share + min(x, extra) + id / 8;
+}
+
 struct GroupTile {
   int group;       // -1: none; `groups`: rows after the last group
   int64_t lo, hi;  // its rows

@@ -18,6 +18,7 @@ struct QuantArgs {
   int64_t padded;           // with groups: blocks of 128 of the column form
   int64_t stride_x, stride_codes, stride_scales, stride_codes_t, stride_scales_t;  // batch
   int64_t row_tiles, col_tiles;
+  int32_t runs;             // rows do not start at cache lines: neighbouring tiles on one XCD
 };
 
 // Bits of |x|, 0 for infinities and NaN: they order like the values.
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
   constexpr int kRows = 4 * UNROLL;  // rows of a workgroup
   __shared__ uint8_t sc[4][kRows];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t ct = blockIdx.x % a.col_tiles, r0 = blockIdx.x / a.col_tiles * kRows;
+  const int64_t id = a.runs ? xcd_run(blockIdx.x, gridDim.x) : blockIdx.x, ct = id % a.col_tiles, r0 = id / a.col_tiles * kRows;
   const int64_t c = ct * 512 + lane * 8, end = (a.cols + 15) / 16 * 16;
   T v[UNROLL][8];
 #pragma unroll
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(256, (WEIGHT || sizeof(T) == 2 ? 4 : 3)) void quant
   __shared__ uint32_t col_max[4][kBlock];
   __shared__ uint8_t row_byte[kBlock], col_byte[kBlock] __attribute__((aligned(16)));
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = tid >> 4, q = tid & 15;
-  int64_t t = blockIdx.x;
+  int64_t t = a.runs ? xcd_run(blockIdx.x, gridDim.x) : blockIdx.x;
   const int64_t cb = t % a.col_tiles;
   t /= a.col_tiles;
   const int64_t rb = t % a.row_tiles, batch = t / a.row_tiles;
@@ -301,6 +302,10 @@ QuantArgs base_args(const ws_matrix* x, const int32_t* index, const ws_fp8_matri
   a.scales = out->scales;
   a.ld_codes = out->ld;
   a.ld_scales = out->ld_scales;
+  // Rows that start inside a cache line share it with the next tile.  Runs of tiles
+  // per XCD then merge their parts (4100 x 4104 f32 with transpose: 28.0 us, in turn
+  // 30.5); where no line is shared, tiles in turn are better (8192 x 4096: 42.6, runs 45.6).
+  a.runs = x->ld * elem_size(x->dtype) % 128 != 0 || out->ld % 128 != 0;
   return a;
 }
 
@@ -309,6 +314,7 @@ void set_transposed(QuantArgs* a, const ws_fp8_matrix* t) {
   a->scales_t = t->scales;
   a->ld_codes_t = t->ld;
   a->ld_scales_t = t->ld_scales;
+  a->runs |= t->ld % 128 != 0;
 }
 
 // x against a row form of it.
