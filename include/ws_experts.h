@@ -36,9 +36,11 @@ ws_status ws_expert_sort(int64_t tokens, int32_t k, int32_t experts, const void*
                          int32_t* offsets, int32_t* token, int32_t* place, void* workspace,
                          int64_t workspace_bytes, hipStream_t stream);
 
-/* out[r] = x[token[r]], zeros for a token out of range.  x and out of one type. */
-ws_status ws_expert_gather(const ws_matrix* x, const int32_t* token, const ws_matrix* out,
-                           hipStream_t stream);
+/* out[place[t][j]] = x[t]: the tokens' rows in sorted order; rows past
+ * offsets[experts] are zeros, places out of range are left out.  x and out of one
+ * type; out does not overlap x. */
+ws_status ws_expert_gather(const ws_matrix* x, int32_t k, int32_t experts, const int32_t* offsets, const int32_t* place,
+                           const ws_matrix* out, hipStream_t stream);
 
 /* out[t] = sum over j of weights[t][j] h[place[t][j]] (weights NULL: 1), in
  * binary32 in the order of j, rounded once; places out of range are left out.

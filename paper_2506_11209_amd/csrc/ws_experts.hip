@@ -200,29 +200,35 @@ __device__ __forceinline__ void store_part(T* row, int64_t c, int64_t cols, cons
   }
 }
 
-// A wave copies 4 x 64 x 16 bytes of a row at a time.  Bound: memory.
+// A wave takes 4 x 64 x 16 bytes of a token's row and writes them to the rows of all
+// its choices: each token is read once, where a copy by sorted row reads it once
+// for every expert, on as many XCDs (8192 tokens of 2048 to 4 of 64 experts: 27 us,
+// by sorted row 39).  Bound: memory.
 template <typename T>
 __global__ __launch_bounds__(256) void gather_kernel(RowArgs a) {
   constexpr int N = 16 / sizeof(T), kSteps = 4;
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t r = item / a.parts, c0 = item % a.parts * (64 * N * kSteps) + (threadIdx.x & 63) * N;
-  if (r >= a.rows) return;
-  const int64_t src = a.index[r];
-  const bool there = src >= 0 && src < a.x_rows;
+  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t t = item / a.parts, c0 = item % a.parts * (64 * N * kSteps) + (threadIdx.x & 63) * N;
+  if (t >= a.x_rows) return;
   T v[kSteps][N];
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int64_t c = c0 + i * 64 * N;
-    if (there && c < a.cols) {
-      load_part<T, N>((const T*)a.x + src * a.ld_x, c, a.cols, v[i]);
-    } else {
-      for (int j = 0; j < N; ++j) v[i][j] = from_f32<T>(0.0f);
-    }
-  }
+  for (int i = 0; i < kSteps; ++i)
+    if (c0 + i * 64 * N < a.cols) load_part<T, N>((const T*)a.x + t * a.ld_x, c0 + i * 64 * N, a.cols, v[i]);
+  for (int j = 0; j < a.k; ++j) {
+    const int64_t r = a.index[t * a.k + j];
+    if (r < 0 || r >= a.rows) continue;
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int64_t c = c0 + i * 64 * N;
-    if (c < a.cols) store_part<T, N>((T*)a.out + r * a.ld_out, c, a.cols, v[i]);
+    for (int i = 0; i < kSteps; ++i)
+      if (c0 + i * 64 * N < a.cols) store_part<T, N>((T*)a.out + r * a.ld_out, c0 + i * 64 * N, a.cols, v[i]);
+  }
+  // rows of no slot
+  int64_t r = a.offsets[a.experts];
+  for (r = (r < 0 ? 0 : r) + t; r < a.rows; r += a.x_rows) {
+    T zero[N];
+    for (int j = 0; j < N; ++j) zero[j] = from_f32<T>(0.0f);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+      if (c0 + i * 64 * N < a.cols) store_part<T, N>((T*)a.out + r * a.ld_out, c0 + i * 64 * N, a.cols, zero);
   }
 }
 
@@ -376,21 +382,26 @@ ws_status ws_expert_sort(int64_t tokens, int32_t k, int32_t experts, const void*
   return s != WS_OK ? s : launch("expert_sort", &place_kernel<false>, a.blocks, kSortThreads, place_lds, stream, a);
 }
 
-ws_status ws_expert_gather(const ws_matrix* x, const int32_t* token, const ws_matrix* out, hipStream_t stream) {
-  if (!plain(x) || !plain(out) || x->cols != out->cols || x->dtype != out->dtype) return WS_ERR_INVALID_ARG;
+ws_status ws_expert_gather(const ws_matrix* x, int32_t k, int32_t experts, const int32_t* offsets, const int32_t* place,
+                           const ws_matrix* out, hipStream_t stream) {
+  if (!plain(x) || !plain(out) || x->cols != out->cols || x->dtype != out->dtype || k < 1 || experts < 1) return WS_ERR_INVALID_ARG;
+  if (x->rows == 0) return out->rows == 0 ? WS_OK : WS_ERR_INVALID_ARG;  // no tokens: no rows of theirs
   if (out->rows == 0 || out->cols == 0) return WS_OK;
-  if (!token || (uintptr_t)token % 4) return WS_ERR_INVALID_ARG;
+  if (!offsets || !place || (uintptr_t)offsets % 4 || (uintptr_t)place % 4) return WS_ERR_INVALID_ARG;
   RowArgs a{};
   a.x = x->data;
   a.out = out->data;
-  a.index = token;
+  a.index = place;
+  a.offsets = offsets;
   a.x_rows = x->rows;
   a.rows = out->rows;
   a.cols = out->cols;
   a.ld_x = x->ld;
   a.ld_out = out->ld;
+  a.k = k;
+  a.experts = experts;
   a.parts = (int32_t)ceil_div(a.cols * elem_size(x->dtype), 4096);
-  const int64_t grid = ceil_div(a.rows * a.parts, 4);
+  const int64_t grid = ceil_div(a.x_rows * a.parts, 4);
   if (grid > kMaxGrid) return WS_ERR_INVALID_ARG;
   return elem_size(x->dtype) == 4 ? launch("expert_gather", &gather_kernel<float>, grid, 256, 0, stream, a)
                                   : launch("expert_gather", &gather_kernel<bf16_t>, grid, 256, 0, stream, a);

@@ -26,7 +26,7 @@ _p, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
 for _name, _args, _res in (
         ("ws_expert_sort_workspace", [_i64, _i32, _i32], _i64),
         ("ws_expert_sort", [_i64, _i32, _i32, _p, _i32, _p, _p, _p, _p, _i64, _p], _i32),
-        ("ws_expert_gather", [_mp, _p, _mp, _p], _i32),
+        ("ws_expert_gather", [_mp, _i32, _i32, _p, _p, _mp, _p], _i32),
         ("ws_expert_combine", [_mp, _i32, _p, _p, _mp, _p], _i32),
         ("ws_expert_combine_gradient", [_mp, _mp, _i32, _i32, _p, _p, _p, _mp, _p, _p], _i32)):
     getattr(_lib, _name).argtypes, getattr(_lib, _name).restype = _args, _res
@@ -99,13 +99,15 @@ def _weights(weights, routes):
 def gather(x, routes: Routes, out=None, stream=None):
     """x (tokens x columns; f32, bf16 or f16) by sorted row; zeros for rows of no token."""
     m = _matrix(x, "x", device=routes.token.device)
-    if m.rows != routes.place.shape[0]:
-        raise ValueError("x: %d rows for %d tokens" % (m.rows, routes.place.shape[0]))
+    tokens, k = routes.place.shape
+    if m.rows != tokens:
+        raise ValueError("x: %d rows for %d tokens" % (m.rows, tokens))
     if _elsewhere(x, stream):
-        with _Call(x.device, stream, [x, routes.token, out]):
+        with _Call(x.device, stream, [x, routes.offsets, routes.place, out]):
             return gather(x, routes, out)
     out, mo = _out(out, "out", routes.token.numel(), m.cols, x)
-    _check(_lib.ws_expert_gather(m, routes.token.data_ptr(), mo, _raw_stream(x.get_device())), "ws_expert_gather")
+    _check(_lib.ws_expert_gather(m, k, routes.experts, routes.offsets.data_ptr(), routes.place.data_ptr(), mo,
+                                 _raw_stream(x.get_device())), "ws_expert_gather")
     return out
 
 

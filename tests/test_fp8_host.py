@@ -131,13 +131,14 @@ def test_rows_refuse():
     x, out = matrix(8, 64), matrix(16, 64)
     gather, combine, grad = lib.ws_expert_gather, lib.ws_expert_combine, lib.ws_expert_combine_gradient
     for m in BAD_MATRIX:
-        assert gather(m, AT, out, None) == w.WS_ERR_INVALID_ARG and gather(x, AT, m, None) == w.WS_ERR_INVALID_ARG
+        assert gather(m, 2, 4, AT, AT, out, None) == w.WS_ERR_INVALID_ARG and gather(x, 2, 4, AT, AT, m, None) == w.WS_ERR_INVALID_ARG
         assert combine(m, 2, AT, AT, x, None) == w.WS_ERR_INVALID_ARG and combine(out, 2, AT, AT, m, None) == w.WS_ERR_INVALID_ARG
         assert grad(m, out, 2, 4, AT, AT, AT, out, AT, None) == w.WS_ERR_INVALID_ARG
         assert grad(x, m, 2, 4, AT, AT, AT, out, AT, None) == w.WS_ERR_INVALID_ARG
-    assert gather(x, None, out, None) == w.WS_ERR_INVALID_ARG
-    assert gather(x, AT, matrix(16, 63), None) == w.WS_ERR_INVALID_ARG
-    assert gather(x, AT, matrix(16, 64, dtype=BF16), None) == w.WS_ERR_INVALID_ARG
+    assert gather(x, 2, 4, None, AT, out, None) == w.WS_ERR_INVALID_ARG and gather(x, 2, 4, AT, None, out, None) == w.WS_ERR_INVALID_ARG
+    assert gather(x, 0, 4, AT, AT, out, None) == w.WS_ERR_INVALID_ARG and gather(x, 2, 0, AT, AT, out, None) == w.WS_ERR_INVALID_ARG
+    assert gather(x, 2, 4, AT, AT, matrix(16, 63), None) == w.WS_ERR_INVALID_ARG
+    assert gather(x, 2, 4, AT, AT, matrix(16, 64, dtype=BF16), None) == w.WS_ERR_INVALID_ARG
     assert combine(out, 0, AT, AT, x, None) == w.WS_ERR_INVALID_ARG
     assert combine(out, 2, None, AT, x, None) == w.WS_ERR_INVALID_ARG
     assert combine(out, 2, AT, AT + 1, x, None) == w.WS_ERR_INVALID_ARG
@@ -153,7 +154,7 @@ def test_empty_calls_touch_nothing():
     assert lib.ws_fp8_quantize_rows(none, None, q0, None) == w.WS_OK
     assert lib.ws_fp8_quantize_both(none, None, 0, None, q0, coded(64, 0, codes=None, scales=None), None) == w.WS_OK
     assert lib.ws_fp8_product(q0, coded(32, 64), 1.0, 0.0, None, fp8.ws_matrix(None, 0, 32, 32, F32, 1, 0), None) == w.WS_OK
-    assert lib.ws_expert_gather(none, None, none, None) == w.WS_OK
+    assert lib.ws_expert_gather(none, 2, 4, None, None, none, None) == w.WS_OK
     assert lib.ws_expert_combine(none, 2, None, None, none, None) == w.WS_OK
 
 

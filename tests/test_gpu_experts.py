@@ -162,9 +162,10 @@ def test_indices_out_of_range_count_as_none():
     token = torch.tensor([0, 1, -1, 4, 1 << 30, 2, 3, -9], dtype=torch.int32, device="cuda")
     r = experts.Routes(torch.tensor([0, 3, 8], dtype=torch.int32, device="cuda"), token, place)
     x, h = torch.randn(T, C, device="cuda"), torch.randn(T * k, C, device="cuda")
-    xs = experts.gather(x, r)
     zero = torch.zeros(C, device="cuda")
-    assert torch.equal(xs, torch.stack([x[0], x[1], zero, zero, zero, x[2], x[3], zero]))
+    room = torch.full((T * k + 2, C), 7.0, device="cuda")  # places 0, 3 and 7; no row past the last offset
+    experts.gather(x, r, out=room[1:-1])
+    assert torch.equal(room[[0, 1, 4, 8, 9]], torch.stack([zero + 7, x[0], x[1], x[3], zero + 7]))
     assert torch.equal(experts.combine(h, r), torch.stack([h[0], h[3], zero, h[7]]))
     _, dw = experts.combine_gradient(x, h, r, torch.ones(T, k, device="cuda"))
     assert dw[0, 1] == 0 and dw[1, 0] == 0 and (dw[2] == 0).all() and dw[3, 1] == 0
