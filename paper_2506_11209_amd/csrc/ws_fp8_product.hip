@@ -149,6 +149,14 @@ __device__ __forceinline__ i32x8_t join(i32x4_t lo, i32x4_t hi) {
   return i32x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 }
 
+template <int N, typename F>
+__device__ __forceinline__ void static_for(const F& f) {
+  if constexpr (N > 0) {
+    static_for<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
+
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
@@ -297,13 +305,6 @@ struct TileShape {
   static_assert(kWaves * kLds <= 160 * 1024, "LDS of a CU");
 };
 
-// A column of B just widened, two wait states before its first product.
-__device__ __forceinline__ void settle_wide(i32x4_t& f) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("s_nop 1" : "+v"(f));
-#endif
-}
-
 // Keeps what reads acc behind the asm statements before, the wait for the last
 // products among them.
 template <bool AGPR>
@@ -378,14 +379,6 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, const Part& p, 
     }
 }
 
-template <int N, typename F>
-__device__ __forceinline__ void static_for(const F& f) {
-  if constexpr (N > 0) {
-    static_for<N - 1>(f);
-    f(std::integral_constant<int, N - 1>{});
-  }
-}
-
 // acc += A's 16 rows times B's 16 rows, each operand's scale in byte SA or SB of
 // its dword.  As asm with the sum in place: the compiler's own form of it moved
 // sums between registers (4 copies and a wait for each of a row's products), and
@@ -415,16 +408,58 @@ __device__ __forceinline__ void multiply_wide(f32x4_t& acc, const i32x4_t& fa, c
 #endif
 }
 
-// An operand's 128 columns in bf16, from its codes and byte `i` of its scales.
-struct Wide {
-  i32x4_t part[4];
-};
-__device__ __forceinline__ Wide widen_all(const i32x8_t& f, uint32_t scales, int i) {
-  const float s = scale_value((scales >> 8 * i) & 255u);
-  Wide w;
+// An operand just widened, two wait states before its first product.
+__device__ __forceinline__ void settle_wide(i32x4_t& f) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_nop 1" : "+v"(f));
+#endif
+}
+
+// A quarter of an operand's 128 columns in bf16.
+__device__ __forceinline__ i32x4_t widen_part(const i32x8_t& f, int q, float scale) {
+  return __builtin_bit_cast(i32x4_t, widen(f[2 * q], f[2 * q + 1], scale));
+}
+// Byte i of packed scales.
+__device__ __forceinline__ float scale_of(const uint32_t* scales, int i) { return scale_value(scales[i / 4] >> i % 4 * 8 & 255u); }
+
+// Rows FROM .. FROM + N - 1 of a block's products in bf16.  Operands are widened a
+// quarter at a time between the products of the quarter before: A's along with the
+// first column of B, each column of B during the one before.  (All of a column's
+// at once kept the matrix unit waiting: 8192 x 8192 x 8192 in 910 us, so 875.)
+// between(j, q, i) is called behind every product.
+template <bool AGPR, int FROM, int N, int WM, int WN, typename F>
+__device__ __forceinline__ void multiply_rows_wide(f32x4_t (&acc)[WM][WN], const i32x8_t (&fa)[WM], const i32x8_t (&fb)[WN],
+                                                   const uint32_t* sa, const uint32_t* sb, const F& between) {
+  i32x4_t wa[N][4], wb[2][4];
+  float by[N];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) w.part[q] = __builtin_bit_cast(i32x4_t, widen(f[2 * q], f[2 * q + 1], s));
-  return w;
+  for (int i = 0; i < N; ++i) by[i] = scale_of(sa, FROM + i);
+  wb[0][0] = widen_part(fb[0], 0, scale_of(sb, 0));
+#pragma unroll
+  for (int i = 0; i < N; ++i) wa[i][0] = widen_part(fa[FROM + i], 0, by[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) settle_wide(wa[i][0]);
+  __builtin_amdgcn_sched_barrier(0);
+  static_for<WN * 4>([&](auto sc) {
+    constexpr int j = decltype(sc)::value / 4, q = decltype(sc)::value % 4;
+    static_for<N>([&](auto ic) {
+      constexpr int i = decltype(ic)::value;
+      multiply_wide<AGPR>(acc[FROM + i][j], wa[i][q], wb[j & 1][q]);
+      if constexpr (j == 0 && q < 3) {
+        wa[i][q + 1] = widen_part(fa[FROM + i], q + 1, by[i]);
+        if constexpr (i == 0) wb[0][q + 1] = widen_part(fb[0], q + 1, scale_of(sb, 0));
+      }
+      if constexpr (i == N / 2 && j + 1 < WN) wb[(j + 1) & 1][q] = widen_part(fb[j + 1], q, scale_of(sb, j + 1));
+      between(std::integral_constant<int, j>{}, std::integral_constant<int, q>{}, ic);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (j == 0 && q < 3) {
+      settle_wide(wa[N - 1][q + 1]);
+      settle_wide(wb[0][q + 1]);
+    } else if constexpr (q == 3 && j + 1 < WN) {
+      settle_wide(wb[(j + 1) & 1][3]);
+    }
+  });
 }
 
 // Scales just moved, two wait states before their first product.
@@ -448,8 +483,7 @@ __device__ __forceinline__ void settle_scales(uint32_t& s) {
 // [row % 16][row / 16], so that a lane reads those of all its rows at once and
 // the instruction picks a byte.  Small tiles have four stages, b + 4 being loaded
 // over b: their blocks are shorter than the way to memory.
-// WIDE: results in 32 bits.  A half's rows of A are widened at its start, a column
-// of B before its products, those of the next column between them.
+// WIDE: results in 32 bits, the same halves (multiply_rows_wide).
 //
 // A workgroup takes every gridDim.x-th of an XCD's tiles.  It starts the loads of its
 // next tile before it stores the one it has, in LDS of their own, so that memory
@@ -468,7 +502,7 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
   if (MODE == kRowGroups) tiles_m = (uint32_t)count_group_tiles(a.offsets, a.groups, a.M, TM);
   // Groups of unlike depth are dealt out instead, every eighth tile to an XCD: with
   // runs an XCD had two of 16 groups, and the one with the deepest took twice as long
-  // as the others (16 x 1024 x 2048 over 16384 rows: 146 us, dealt out 83 us).
+  // as the others (16 x 1024 x 2048 over 16384 rows: 146 us, dealt out 96 us).
   const uint32_t tiles_n = (uint32_t)a.tiles_n, plane = tiles_m * tiles_n, tiles = plane * (MODE == kDepthGroups ? a.groups : 1);
   const uint32_t xcd = blockIdx.x % 8, share = tiles / 8, extra = tiles % 8, turns = (gridDim.x + 7 - xcd) / 8;
   const bool dealt = MODE == kDepthGroups;
@@ -597,22 +631,12 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
       for (int b = 0; b < t.blocks; ++b) {
         const int here = b % STAGES * kStage, next = (b + 1) % STAGES * kStage;
         if constexpr (WIDE) {
-          Wide wa[kFirst], wb = widen_all(fb[0], sb[0], 0);
+          multiply_rows_wide<Shape::kAgpr, 0, kFirst>(acc, fa, fb, sa, sb, [&](auto jc, auto qc, auto ic) {
+            constexpr int at = (decltype(jc)::value * 4 + decltype(qc)::value) * kFirst + decltype(ic)::value, all = WN * 2 * kFirst;
 #pragma unroll
-          for (int i = 0; i < kFirst; ++i) wa[i] = widen_all(fa[i], sa[i / 4], i % 4);
-          static_for<WN>([&](auto jc) {
-            constexpr int j = decltype(jc)::value;
-            __builtin_amdgcn_sched_barrier(0);
-            settle_wide(wb.part[0]);
-#pragma unroll
-            for (int q = 0; q < 4; ++q)  // a sum's next product comes after the other rows'
-#pragma unroll
-              for (int i = 0; i < kFirst; ++i) multiply_wide<Shape::kAgpr>(acc[i][j], wa[i].part[q], wb.part[q]);
-#pragma unroll
-            for (int k = j * kRest / WN; k < (j + 1) * kRest / WN; ++k) fa[kFirst + k] = frag(fa0 + (kFirst + k) * 2048, here);
-            if constexpr (j + 1 < WN) wb = widen_all(fb[j + 1], sb[(j + 1) / 4], (j + 1) % 4);
+            for (int k = at * kRest / all; k < (at + 1) * kRest / all && at < all; ++k)
+              fa[kFirst + k] = frag(fa0 + (kFirst + k) * 2048, here);
           });
-          __builtin_amdgcn_sched_barrier(0);
         } else {
           static_for<kFirst>([&](auto ic) {
             constexpr int i = decltype(ic)::value;
@@ -644,28 +668,20 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
             drain_and_meet();
           }
         if constexpr (WIDE) {
-          constexpr int kPer = kLoads / WN;
           scales_next();
           __builtin_amdgcn_sched_barrier(0);
-          Wide wa[kRest], wb = widen_all(fb[0], sb[0], 0);
+          multiply_rows_wide<Shape::kAgpr, kFirst, kRest>(acc, fa, fb, sa, sb, [&](auto jc, auto qc, auto ic) {
+            constexpr int j = decltype(jc)::value, q = decltype(qc)::value, i = decltype(ic)::value;
+            constexpr int at = (j * 4 + q) * kRest + i, all = WN * 4 * kRest;
+            load(b + STAGES, at * kLoads / all, (at + 1) * kLoads / all);
+            if constexpr (q == 3 && i == kRest - 1) {
 #pragma unroll
-          for (int i = 0; i < kRest; ++i) wa[i] = widen_all(fa[kFirst + i], sa[(kFirst + i) / 4], (kFirst + i) % 4);
-          static_for<WN>([&](auto jc) {
-            constexpr int j = decltype(jc)::value;
-            __builtin_amdgcn_sched_barrier(0);
-            settle_wide(wb.part[0]);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-#pragma unroll
-              for (int i = 0; i < kRest; ++i) multiply_wide<Shape::kAgpr>(acc[kFirst + i][j], wa[i].part[q], wb.part[q]);
-              load(b + STAGES, j * kPer + q * kPer / 4, j * kPer + (q + 1) * kPer / 4);
+              for (int k = j * kFirst / WN; k < (j + 1) * kFirst / WN; ++k) fa[k] = frag(fa0 + k * 2048, next);
             }
-#pragma unroll
-            for (int k = j * kFirst / WN; k < (j + 1) * kFirst / WN; ++k) fa[k] = frag(fa0 + k * 2048, next);
-            fb[j] = frag(fb0 + j * 2048, next);
-            if constexpr (j + 1 < WN) wb = widen_all(fb[j + 1], sb[(j + 1) / 4], (j + 1) % 4);
+            // column j is widened during column j - 1
+            if constexpr (q == 0 && i == 0 && j > 0) fb[j] = frag(fb0 + j * 2048, next);
+            if constexpr (j == 0 && q == 3 && i == 0) fb[0] = frag(fb0, next);
           });
-          __builtin_amdgcn_sched_barrier(0);
         } else {
           // loads follow the products of columns kFrom .. kTo - 1
           constexpr int kFrom = WN > 2 ? 1 : 0, kTo = WN > 4 ? WN - 1 : WN, kSlots = (kTo - kFrom) * kRest;
