@@ -102,7 +102,7 @@ typedef struct {
   int64_t rows;
 } ws_fp8_kernel_info;
 
-/* The launches of a product M x N x K with results of out_dtype, by rising rows
+/* The parts of a product M x N x K with results of out_dtype, by rising rows
  * (2 at the most).  groups > 0: of ws_fp8_grouped_product, or with depth != 0 of
  * ws_fp8_grouped_gradient of K rows.  Host only; kernels are chosen by sizes and
  * type alone, for the current device's compute units (256 without a device). */

@@ -47,6 +47,8 @@ struct ProductArgs {
   int32_t groups;
   int64_t depth_rows;  // kDepthGroups: rows that the groups cut
   int64_t tiles_m, tiles_n;
+  int32_t tile_groups;  // workgroups that take tiles of a tile kernel; those behind them
+  int64_t rest_end;     // take rows M .. rest_end - 1, 16 x 16 each (dense products)
 };
 
 // What one workgroup computes: rows m0 .. m_end - 1 (at most a tile) of its
@@ -178,16 +180,10 @@ __device__ __forceinline__ bf16x8_t widen(int lo, int hi, float scale) {
 // of the contraction and add up their parts through LDS in a fixed order.
 // Operands go from memory straight to registers, U blocks at a time.  For few
 // rows: bound by reading B once.
-template <int MT, int U, int MODE, bool WIDE>
-__global__ __launch_bounds__(512) void direct_kernel(ProductArgs a) {
-  extern __shared__ float lds[];
+template <int MT, int U, bool WIDE, bool AGPR = false>
+__device__ __forceinline__ void direct_part(const ProductArgs& a, const Part& p, float* lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int waves = blockDim.x >> 6, r = lane & 15, g = lane >> 4;
-  const int64_t tn = blockIdx.x % a.tiles_n, t = blockIdx.x / a.tiles_n;
-  Part p;
-  if (!find_part<MODE>(a, MODE == kDepthGroups ? t % a.tiles_m : t, tn, MODE == kDepthGroups ? t / a.tiles_m : 0, 16 * MT,
-                       16, &p))
-    return;
   const int rows = (int)min(p.m_end - p.m0, (int64_t)16 * MT), cols = (int)min(a.N - p.n0, (int64_t)16);
   f32x4_t acc[MT];
   for (int i = 0; i < MT; ++i) acc[i] = f32x4_t{0, 0, 0, 0};
@@ -227,6 +223,14 @@ __global__ __launch_bounds__(512) void direct_kernel(ProductArgs a) {
         acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(join(vb[u][0], vb[u][1]), join(va[u][i][0], va[u][i][1]),
                                                                   acc[i], 0, 0, 0, sbv[u], 0, sav[u][i]);
     }
+    // Inside the tile kernels sums stay in one kind of register, and keep the longest
+    // wait before anything else reads them, as those of their products in asm do.
+#if defined(__HIP_DEVICE_COMPILE__)
+    for (int i = 0; i < MT; ++i) {
+      if constexpr (AGPR) asm volatile("s_nop 15\n\ts_nop 2" : "+a"(acc[i]));
+      else asm volatile("s_nop 15\n\ts_nop 2" : "+v"(acc[i]));
+    }
+#endif
   }
   // lane: row l % 16 of C's tile, columns 4 (l / 16) ..
   f32x4_t* part = (f32x4_t*)lds;
@@ -239,6 +243,15 @@ __global__ __launch_bounds__(512) void direct_kernel(ProductArgs a) {
     float v[4] = {sum[0], sum[1], sum[2], sum[3]};
     if (row < rows && 4 * col < cols) store_out(a, p, p.m0 + row, p.n0 + 4 * col, v);
   }
+}
+
+template <int MT, int U, int MODE, bool WIDE>
+__global__ __launch_bounds__(512) void direct_kernel(ProductArgs a) {
+  extern __shared__ float lds[];
+  const int64_t tn = blockIdx.x % a.tiles_n, t = blockIdx.x / a.tiles_n;
+  Part p;
+  if (find_part<MODE>(a, MODE == kDepthGroups ? t % a.tiles_m : t, tn, MODE == kDepthGroups ? t / a.tiles_m : 0, 16 * MT, 16, &p))
+    direct_part<MT, U, WIDE>(a, p, lds);
 }
 
 // -- tiles -----------------------------------------------------------------------
@@ -485,7 +498,7 @@ __device__ __forceinline__ void settle_scales(uint32_t& s) {
 // over b: their blocks are shorter than the way to memory.
 // WIDE: results in 32 bits, the same halves (multiply_rows_wide).
 //
-// A workgroup takes every gridDim.x-th of an XCD's tiles.  It starts the loads of its
+// A workgroup takes every tile_groups-th of an XCD's tiles.  It starts the loads of its
 // next tile before it stores the one it has, in LDS of their own, so that memory
 // is written and read while neither is waited for.
 template <int WM, int WN, int STAGES, int MODE, bool WIDE>
@@ -493,6 +506,12 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
   typedef TileShape<WM, WN, STAGES> Shape;
   constexpr int TM = Shape::TM, TN = Shape::TN, kStage = Shape::kStage, kRows = TM + TN, kFirst = Shape::kFirst, kRest = WM - kFirst;
   extern __shared__ __align__(1024) uint8_t smem[];
+  if constexpr (MODE == kDense)
+    if (blockIdx.x >= (uint32_t)a.tile_groups) {
+      const uint32_t t = blockIdx.x - a.tile_groups, across = (uint32_t)((a.N + 15) / 16);
+      const Part p{a.A, a.B, a.sa, a.sb, a.M + t / across * 16, a.rest_end, t % across * 16, a.K, 0, 0, false};
+      return direct_part<1, 4, WIDE, Shape::kWaves == 1>(a, p, (float*)smem);
+    }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
 
@@ -504,7 +523,7 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
   // runs an XCD had two of 16 groups, and the one with the deepest took twice as long
   // as the others (16 x 1024 x 2048 over 16384 rows: 146 us, dealt out 96 us).
   const uint32_t tiles_n = (uint32_t)a.tiles_n, plane = tiles_m * tiles_n, tiles = plane * (MODE == kDepthGroups ? a.groups : 1);
-  const uint32_t xcd = blockIdx.x % 8, share = tiles / 8, extra = tiles % 8, turns = (gridDim.x + 7 - xcd) / 8;
+  const uint32_t xcd = blockIdx.x % 8, share = tiles / 8, extra = tiles % 8, turns = (a.tile_groups + 7 - xcd) / 8;
   const bool dealt = MODE == kDepthGroups;
   const uint32_t begin = xcd * share + min(xcd, extra), end = dealt ? tiles : begin + share + (xcd < extra),
                  stride = dealt ? 8 * turns : turns;
@@ -765,6 +784,8 @@ ws_status run_tiles(ProductArgs a, hipStream_t stream) {
   const int64_t tiles = a.tiles_n * a.tiles_m, grid = tiles * (MODE == kDepthGroups ? a.groups : 1);
   if (a.tiles_m > kMaxGrid || tiles > kMaxGrid || grid > kMaxGrid) return WS_ERR_INVALID_ARG;
   const int64_t most = (int64_t)compute_units() * Shape::kWaves;
+  a.tile_groups = (int32_t)(grid < most ? grid : most);
+  const int64_t rest = a.rest_end > a.M ? ceil_div(a.rest_end - a.M, 16) * ceil_div(a.N, 16) : 0;
   const auto kernel = &tile_kernel<WM, WN, STAGES, MODE, WIDE>;
   static std::atomic<uint64_t> allowed;  // devices on which the kernel may use this much LDS
   int dev = 0;
@@ -774,7 +795,7 @@ ws_status run_tiles(ProductArgs a, hipStream_t stream) {
     if (e == hipSuccess && dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_acq_rel);
   }
   if (e != hipSuccess) return hip_fail("hipFuncSetAttribute", e);
-  return launch("fp8_product", kernel, grid < most ? grid : most, 256, Shape::kLds, stream, a);
+  return launch("fp8_product", kernel, a.tile_groups + rest, 256, Shape::kLds, stream, a);
 }
 
 // What a product costs by each kernel, in us (MI355X, 256 CUs; fitted to 23
@@ -850,7 +871,7 @@ ws_status run_choice(Choice c, const ProductArgs& a, hipStream_t stream) {
   }
 }
 
-// One or two launches of a product: the first `split` rows by choice[0], the rest
+// One or two parts of a product: the first `split` rows by choice[0], the rest
 // by choice[1].
 struct Plan {
   int count;
@@ -891,6 +912,15 @@ ws_status run_product(const ProductArgs& a, hipStream_t stream) {
   ProductArgs m = a, r = a;
   m.M = plan.split;
   r.M = a.M - m.M;
+  // The last rows in the launch of the tiles, by workgroups of 16 rows: beside the
+  // tiles where a CU has room for two (4216 x 1000 x 4100 in 32 bits: 55 us, so 45),
+  // else behind them, where they are few (4104 x 1000 x 4100: 33.0 us, so 31.8, but
+  // 4160 x 4096 x 4096: 68, by itself with 64 rows a workgroup, 75).
+  const bool beside = plan.choice[0] == kTile128 || plan.choice[0] == kTile64;
+  if (plan.choice[0] >= kTile256 && plan.choice[1] < kTile256 && (beside || r.M <= 16) && a.N <= kMaxGrid) {
+    m.rest_end = a.M;
+    return run_choice<MODE>(plan.choice[0], m, stream);
+  }
   const int size = elem_size(a.dtype);
   r.A += m.M * a.lda;
   r.sa += m.M;

@@ -314,7 +314,7 @@ def _old(C0, beta: float, C):
 
 
 def plan(M: int, N: int, K: int, out_dtype: str = "bf16", groups: int = 0, depth: bool = False) -> list:
-    """[(tile_m, tile_n, stages, rows)]: the launches of product (groups 0), of
+    """[(tile_m, tile_n, stages, rows)]: the parts of product (groups 0), of
     grouped_product, or with depth of grouped_gradient over K rows."""
     out, n = (ws_fp8_kernel_info * 2)(), _i32(0)
     if out_dtype not in _DTYPES:

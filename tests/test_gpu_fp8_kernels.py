@@ -42,6 +42,17 @@ DEPTH = [
     ((4104, 520, 4104, 5, "bf16"), [T256]), ((1030, 1030, 8200, 5, "f32"), [T256W]),
 ]
 
+# Last rows by kernels of their own: in the launch of the tiles, or behind it.
+SPLIT = [
+    ((2314, 417, 4601, "bf16"), [T64, D16]), ((8219, 104, 4315, "bf16"), [T64, D32]), ((773, 1334, 5271, "f16"), [T64D, D16]),
+    ((2102, 474, 6647, "bf16"), [T64D, D64]), ((1543, 2612, 1278, "f16"), [T128, D16]), ((2065, 1994, 1286, "bf16"), [T128, D32]),
+    ((2216, 1872, 1328, "bf16"), [T128, D64]), ((1643, 2520, 2705, "bf16"), [T128, T64]), ((1936, 2066, 3344, "bf16"), [T128D, D16]),
+    ((1557, 2505, 3362, "f16"), [T128D, D32]), ((3341, 4854, 800, "bf16"), [T256, D16]), ((3603, 4509, 920, "bf16"), [T256, D32]),
+    ((1162, 858, 3272, "f32"), [T64, D16]), ((1064, 984, 4347, "f32"), [T64, D64]), ((1168, 837, 7327, "f32"), [T64D, D16]),
+    ((1665, 2402, 655, "f32"), [T128, D16]), ((1971, 2142, 939, "f32"), [T128, D64]), ((3080, 2580, 1332, "f32"), [T256W, D16]),
+    ((5402, 1469, 1283, "f32"), [T256W, D32]),
+]
+
 
 def launches(*args, **kw):
     return [k[:3] for k in fp8.plan(*args, **kw)]
@@ -60,6 +71,12 @@ def test_sizes_reach_every_kernel():
             everything = {D16, D32, D64, T64, T64D, T128} | ({T256W} if wide else {T128D, T256})
             assert everything - seen <= {D16, D32, D64}, (cases[0], wide, everything - seen)
     assert fp8.plan(0, 5, 5) == [] and sum(k[3] for k in fp8.plan(4104, 1000, 4100, "f32")) == 4104
+
+
+def test_last_rows_by_themselves():
+    for (M, N, K, t), want in SPLIT:
+        assert launches(M, N, K, t) == want, (M, N, K, t)
+        assert [k[3] for k in fp8.plan(M, N, K, t)] == [M // 128 * 128, M % 128]
 
 
 def test_plan_refuses():
@@ -111,7 +128,7 @@ def check(got, a, b, alpha=1.0, c0=None, beta=0.0, what=""):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("case", [c for c, _ in DENSE], ids=lambda c: "x".join(map(str, c)))
+@pytest.mark.parametrize("case", [c for c, _ in DENSE + SPLIT], ids=lambda c: "x".join(map(str, c)))
 def test_dense(case):
     M, N, K, t = case
     log("case dense %dx%dx%d %s" % case)
