@@ -436,43 +436,51 @@ __device__ __forceinline__ i32x4_t widen_part(const i32x8_t& f, int q, float sca
 __device__ __forceinline__ float scale_of(const uint32_t* scales, int i) { return scale_value(scales[i / 4] >> i % 4 * 8 & 255u); }
 
 // Rows FROM .. FROM + N - 1 of a block's products in bf16.  Operands are widened a
-// quarter at a time between the products of the quarter before: A's along with the
-// first column of B, each column of B during the one before.  (All of a column's
-// at once kept the matrix unit waiting: 8192 x 8192 x 8192 in 910 us, so 875.)
+// quarter at a time between products: A's rows along with the first column of B, a
+// column of B, for all of the block, during the one before (FROM = 0), the first
+// quarters of the NEXT rows of A during the last.  (All of a column's at once, by
+// each half of the rows again, kept the matrix unit waiting: 8192 x 8192 x 8192 in
+// 910 us, so 870.)
 // between(j, q, i) is called behind every product.
-template <bool AGPR, int FROM, int N, int WM, int WN, typename F>
+template <bool AGPR, int FROM, int N, int NEXT, int WM, int WN, typename F>
 __device__ __forceinline__ void multiply_rows_wide(f32x4_t (&acc)[WM][WN], const i32x8_t (&fa)[WM], const i32x8_t (&fb)[WN],
-                                                   const uint32_t* sa, const uint32_t* sb, const F& between) {
-  i32x4_t wa[N][4], wb[2][4];
-  float by[N];
+                                                   i32x4_t (&wa)[WM][4], i32x4_t (&wb)[WN][4], const uint32_t* sa,
+                                                   const uint32_t* sb, const F& between) {
+  constexpr bool kFresh = FROM == 0;  // B, and the first quarters of A, are still to be widened
+  if constexpr (kFresh) {
+    wb[0][0] = widen_part(fb[0], 0, scale_of(sb, 0));
 #pragma unroll
-  for (int i = 0; i < N; ++i) by[i] = scale_of(sa, FROM + i);
-  wb[0][0] = widen_part(fb[0], 0, scale_of(sb, 0));
+    for (int i = 0; i < N; ++i) wa[i][0] = widen_part(fa[i], 0, scale_of(sa, i));
 #pragma unroll
-  for (int i = 0; i < N; ++i) wa[i][0] = widen_part(fa[FROM + i], 0, by[i]);
-#pragma unroll
-  for (int i = 0; i < N; ++i) settle_wide(wa[i][0]);
+    for (int i = 0; i < N; ++i) settle_wide(wa[i][0]);
+    settle_wide(wb[0][0]);
+  }
   __builtin_amdgcn_sched_barrier(0);
   static_for<WN * 4>([&](auto sc) {
     constexpr int j = decltype(sc)::value / 4, q = decltype(sc)::value % 4;
     static_for<N>([&](auto ic) {
-      constexpr int i = decltype(ic)::value;
-      multiply_wide<AGPR>(acc[FROM + i][j], wa[i][q], wb[j & 1][q]);
-      if constexpr (j == 0 && q < 3) {
-        wa[i][q + 1] = widen_part(fa[FROM + i], q + 1, by[i]);
-        if constexpr (i == 0) wb[0][q + 1] = widen_part(fb[0], q + 1, scale_of(sb, 0));
+      constexpr int i = decltype(ic)::value, row = FROM + i;
+      multiply_wide<AGPR>(acc[row][j], wa[row][q], wb[j][q]);
+      if constexpr (j == 0 && q < 3) wa[row][q + 1] = widen_part(fa[row], q + 1, scale_of(sa, row));
+      if constexpr (kFresh && j == 0 && q < 3 && i == 0) wb[0][q + 1] = widen_part(fb[0], q + 1, scale_of(sb, 0));
+      if constexpr (kFresh && i == N / 2 && j + 1 < WN) wb[j + 1][q] = widen_part(fb[j + 1], q, scale_of(sb, j + 1));
+      if constexpr (j == WN - 1) {
+#pragma unroll
+        for (int k = (q * N + i) * NEXT / (4 * N); k < (q * N + i + 1) * NEXT / (4 * N); ++k)
+          wa[FROM + N + k][0] = widen_part(fa[FROM + N + k], 0, scale_of(sa, FROM + N + k));
       }
-      if constexpr (i == N / 2 && j + 1 < WN) wb[(j + 1) & 1][q] = widen_part(fb[j + 1], q, scale_of(sb, j + 1));
       between(std::integral_constant<int, j>{}, std::integral_constant<int, q>{}, ic);
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (j == 0 && q < 3) {
-      settle_wide(wa[N - 1][q + 1]);
-      settle_wide(wb[0][q + 1]);
-    } else if constexpr (q == 3 && j + 1 < WN) {
-      settle_wide(wb[(j + 1) & 1][3]);
+      settle_wide(wa[FROM + N - 1][q + 1]);
+      if constexpr (kFresh) settle_wide(wb[0][q + 1]);
+    } else if constexpr (kFresh && q == 3 && j + 1 < WN) {
+      settle_wide(wb[j + 1][3]);
     }
   });
+#pragma unroll
+  for (int k = 0; k < NEXT; ++k) settle_wide(wa[FROM + N + k][0]);
 }
 
 // Scales just moved, two wait states before their first product.
@@ -620,6 +628,7 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
     if (t.blocks > 0) {
       const int fa0 = (wm * WM * 16 + r) * kBlock, fb0 = (TM + wn * WN * 16 + r) * kBlock, c0 = chunk_at(r, g), c1 = chunk_at(r, g + 4);
       i32x8_t fa[WM], fb[WN];
+      i32x4_t wa[WM][4], wb[WN][4];  // WIDE: operands in bf16
       uint32_t sa[(WM + 3) / 4], sb[(WN + 3) / 4];
       const auto frag = [&](int row, int stage) {
         const uint8_t* f = smem + stage + row;
@@ -650,7 +659,7 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
       for (int b = 0; b < t.blocks; ++b) {
         const int here = b % STAGES * kStage, next = (b + 1) % STAGES * kStage;
         if constexpr (WIDE) {
-          multiply_rows_wide<Shape::kAgpr, 0, kFirst>(acc, fa, fb, sa, sb, [&](auto jc, auto qc, auto ic) {
+          multiply_rows_wide<Shape::kAgpr, 0, kFirst, kRest>(acc, fa, fb, wa, wb, sa, sb, [&](auto jc, auto qc, auto ic) {
             constexpr int at = (decltype(jc)::value * 4 + decltype(qc)::value) * kFirst + decltype(ic)::value, all = WN * 2 * kFirst;
 #pragma unroll
             for (int k = at * kRest / all; k < (at + 1) * kRest / all && at < all; ++k)
@@ -689,7 +698,7 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
         if constexpr (WIDE) {
           scales_next();
           __builtin_amdgcn_sched_barrier(0);
-          multiply_rows_wide<Shape::kAgpr, kFirst, kRest>(acc, fa, fb, sa, sb, [&](auto jc, auto qc, auto ic) {
+          multiply_rows_wide<Shape::kAgpr, kFirst, kRest, 0>(acc, fa, fb, wa, wb, sa, sb, [&](auto jc, auto qc, auto ic) {
             constexpr int j = decltype(jc)::value, q = decltype(qc)::value, i = decltype(ic)::value;
             constexpr int at = (j * 4 + q) * kRest + i, all = WN * 4 * kRest;
             load(b + STAGES, at * kLoads / all, (at + 1) * kLoads / all);
