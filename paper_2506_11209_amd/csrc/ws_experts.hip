@@ -82,7 +82,9 @@ __device__ __forceinline__ void count_slots(const SortArgs& a, int32_t* counts) 
   __syncthreads();
 }
 
-// First of two launches: how many slots of each expert a chunk has.
+// First of two launches: how many slots of each expert a chunk has.  Bound, both:
+// latency, a chain of loads, ballots and meetings (8192 x 4 slots of 64 experts: 4 to
+// 5 us, and 7.4 to 8 for place_kernel).
 __global__ __launch_bounds__(kSortThreads) void count_kernel(SortArgs a) {
   extern __shared__ int32_t lds[];
   count_slots(a, lds);
@@ -203,7 +205,7 @@ __device__ __forceinline__ void store_part(T* row, int64_t c, int64_t cols, cons
 // A wave takes 4 x 64 x 16 bytes of a token's row and writes them to the rows of all
 // its choices: each token is read once, where a copy by sorted row reads it once
 // for every expert, on as many XCDs (8192 tokens of 2048 to 4 of 64 experts: 27 us,
-// by sorted row 39).  Bound: memory.
+// by sorted row 39).  Bound: memory, 168 MB at 6.2 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void gather_kernel(RowArgs a) {
   constexpr int N = 16 / sizeof(T), kSteps = 4;
@@ -234,7 +236,8 @@ __global__ __launch_bounds__(256) void gather_kernel(RowArgs a) {
 
 constexpr int kRowsAtOnce = 4;  // rows of h in flight
 
-// A wave sums 512 columns of a token.  Bound: memory.
+// A wave sums 512 columns of a token.  Bound: memory (8192 tokens of 4 times 2048
+// columns: 32.6 us, 5.2 TB/s; 32 tokens 3.5 us, which is the launch and two trips).
 template <typename T>
 __global__ __launch_bounds__(256) void combine_kernel(RowArgs a) {
   const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -266,7 +269,8 @@ __global__ __launch_bounds__(256) void combine_kernel(RowArgs a) {
 // A workgroup takes a token: its gradient row is read once for four of its
 // experts at a time, scaled into their rows, and multiplied with what they had
 // given.  Dot products: a lane's columns, then the lanes by a tree, then the
-// waves in order; always the same order.  Bound: memory.
+// waves in order; always the same order.  Bound: memory (8192 tokens of 4 times 2048
+// columns: 302 MB in 51 us back to back, 5.9 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void combine_gradient_kernel(RowArgs a) {
   __shared__ float part[4][kRowsAtOnce];
