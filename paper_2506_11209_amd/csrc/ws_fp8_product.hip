@@ -494,9 +494,9 @@ __device__ __forceinline__ void settle_scales(uint32_t& s) {
 // each.  Blocks of 128 columns are double-buffered in LDS, and a block's products
 // come in two halves:
 //
-//   rows 0 .. WM / 2 - 1, row by row: the rest of A of block b is read
+//   the first kFirst rows, row by row: the rest of A of block b is read
 //   meet: b + 1 has landed everywhere, b has been read everywhere
-//   rows WM / 2 .., column by column: b + 2 is loaded over b; the first rows of A
+//   the other rows, column by column: b + 2 is loaded over b; the first rows of A
 //   of b + 1 are read, and every column of B of b + 1 once that of b is done
 //
 // so there is one barrier a block, no wait for memory that had less than a
@@ -509,6 +509,12 @@ __device__ __forceinline__ void settle_scales(uint32_t& s) {
 // A workgroup takes every tile_groups-th of an XCD's tiles.  It starts the loads of its
 // next tile before it stores the one it has, in LDS of their own, so that memory
 // is written and read while neither is waited for.
+//
+// Bound: the matrix unit at the clock that its power leaves; 8192 x 8192 x 8192 in
+// 370 to 430 us in 16 bits (256 x 256; 3.0 to 2.6 PFLOP/s by the operands' bits), in
+// 875 in 32 bits (256 x 128).  Short contractions: the way to the first block and of
+// the last sums to memory, 8 us a tile of 256 x 256 where all are written at once
+// (8192 x 2 rows for 16 experts of 4096 x 2048: 163 us; without its stores 134).
 template <int WM, int WN, int STAGES, int MODE, bool WIDE>
 __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile_kernel(ProductArgs a) {
   typedef TileShape<WM, WN, STAGES> Shape;
