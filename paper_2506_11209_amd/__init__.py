@@ -9,6 +9,10 @@ The compute path is the C-ABI library ``libwsgemm.so`` (``include/ws_gemm.h``);
 ``paper_2506_11209_amd.wsgemm`` is its ctypes binding.  Importing this package
 does not load the library; importing ``paper_2506_11209_amd.wsgemm`` does, and
 raises if it has not been built.
+
+``fp8`` and ``experts`` are operators of layers of experts in 8 bits over torch
+tensors, from the same library (``include/ws_fp8.h``, ``include/ws_experts.h``);
+``expert_layer`` is a layer that uses them.
 """
 
 __all__ = ["inputs", "workloads"]

@@ -17,9 +17,9 @@ Codes are torch.float8_e4m3fn, scales torch.float8_e8m0fnu (powers of two) for
 Calls enqueue on ``stream`` (default: the current stream of the operands'
 device) and return at once.  Results and work memory made here belong to that
 stream, and tensors handed in are marked as in use by it, so that their memory
-is not given out again before the work is done.  Codes and scales may be wrong
-silently only if a caller writes wrong ones: sizes, types, devices and strides
-are checked and raise ValueError; a status of the library raises WsGemmError.
+is not given out again before the work is done.  Sizes, types, devices and
+strides are checked and raise ValueError, a status of the library raises
+WsGemmError; the contents of codes, scales and offsets are not looked at.
 """
 from __future__ import annotations
 
