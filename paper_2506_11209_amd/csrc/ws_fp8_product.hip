@@ -835,21 +835,31 @@ enum Choice { kDirect16, kDirect32, kDirect64, kTile256, kTile128, kTile128Deep,
 struct Work {
   double rows, parts;
   int64_t N, K;
+  int size;  // bytes of a result
 };
+
+// Bytes of results per us, and a tile's way from its first load to its last store
+// where two workgroups of a CU go it in turn: what tiles of few blocks take.
+constexpr float kStoreRate = 5.1e6f, kTrip = 1.5f;
 
 float tile_cost(const Work& w, const TileCost& c) {
   // a part's last tile is partly filled: half of one on average, where there are several parts
   const double tiles_m = w.parts > 1 ? w.parts * (w.rows / c.rows + 0.5) : (double)ceil_div((int64_t)w.rows, c.rows);
   const double n = ceil(tiles_m * (double)ceil_div(w.N, c.cols) / compute_units());
   const float blocks = (float)ceil_div(w.K, kBlock);
-  return c.fixed + blocks * (n <= 1 ? c.alone : c.shared * (float)n) + c.tile * (float)n;
+  if (n <= 1) return c.fixed + blocks * c.alone + c.tile * (float)n;
+  const float store = (float)c.rows * c.cols * w.size * compute_units() / kStoreRate;
+  return c.fixed + (float)n * fmaxf(blocks * c.shared + c.tile, fmaxf(store, kTrip));
 }
 
 // The direct kernel is bound by what its workgroups load, at 11 TB/s from the
-// caches, and for long contractions by the trips that a wave makes.
+// caches, where there are many by starting and ending them (0.7 to 1.2 ns each), and for
+// long contractions by the trips that a wave makes.
 float direct_cost(const Work& w, int rows) {
   const double tiles_m = w.parts > 1 ? w.parts * (w.rows / rows + 0.5) : (double)ceil_div((int64_t)w.rows, rows);
-  return (float)(4.0 + tiles_m * (double)ceil_div(w.N, 16) * (rows + 16.0) * (double)w.K / 11e6 + 0.03 * (double)w.K / kBlock);
+  const double groups = tiles_m * (double)ceil_div(w.N, 16);
+  return (float)(4.0 + groups * (rows + 16.0) * (double)w.K / 11e6 + fmax(groups - 4096.0, 0.0) * (0.55 + 0.01 * rows) / 1e3 +
+                 0.03 * (double)w.K / kBlock);
 }
 
 Choice choose(const Work& w, bool wide, float* cost) {
@@ -895,14 +905,14 @@ struct Plan {
 };
 
 Plan plan_product(int mode, int64_t M, int64_t N, int64_t K, int64_t groups, bool wide) {
-  Work w{(double)M, 1.0, N, K};
+  Work w{(double)M, 1.0, N, K, wide ? 4 : 2};
   if (mode == kRowGroups) {
     w.parts = (double)(groups < M ? groups : M);
     w.rows = (double)M / w.parts;
   }
   if (mode == kDepthGroups) {
     w.parts = (double)groups;
-    w.K = ceil_div(K, groups);
+    w.K = ceil_div(ceil_div(K, groups), kBlock) * kBlock;
   }
   float cost;
   Plan plan{1, M, {choose(w, wide, &cost), kDirect16}};

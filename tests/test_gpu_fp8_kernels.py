@@ -53,6 +53,12 @@ SPLIT = [
     ((5402, 1469, 1283, "f32"), [T256W, D32]),
 ]
 
+# Few rows in many groups, most of them empty: bound by the results.
+SHORT = [
+    ((1000, 400, 50, 20, "f32"), [T128]), ((300, 300, 20, 8, "f32"), [T64]), ((1030, 700, 24, 20, "bf16"), [T128]),
+    ((390, 520, 1000, 40, "f32"), [T128]), ((260, 1290, 64, 16, "f16"), [T128]),
+]
+
 
 def launches(*args, **kw):
     return [k[:3] for k in fp8.plan(*args, **kw)]
@@ -71,6 +77,11 @@ def test_sizes_reach_every_kernel():
             everything = {D16, D32, D64, T64, T64D, T128} | ({T256W} if wide else {T128D, T256})
             assert everything - seen <= {D16, D32, D64}, (cases[0], wide, everything - seen)
     assert fp8.plan(0, 5, 5) == [] and sum(k[3] for k in fp8.plan(4104, 1000, 4100, "f32")) == 4104
+
+
+def test_few_rows_in_many_groups_run_as_tiles():
+    for (M, N, R, g, t), want in SHORT:
+        assert launches(M, N, R, t, g, True) == want, (M, N, R, g, t)
 
 
 def test_last_rows_by_themselves():
@@ -180,7 +191,7 @@ def test_row_groups(case):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("case", [c for c, _ in DEPTH], ids=lambda c: "x".join(map(str, c)))
+@pytest.mark.parametrize("case", [c for c, _ in DEPTH + SHORT], ids=lambda c: "x".join(map(str, c)))
 def test_depth_groups(case):
     M, N, R, G, t = case
     log("case depth %dx%d over %d rows in %d %s" % case)
