@@ -186,6 +186,49 @@ def test_strided_rows_and_another_stream():
     assert torch.equal(y, experts.combine(xs, r))
 
 
+def test_rows_past_32_bits():
+    """Rows so far apart that offsets pass 2^32."""
+    log("case rows far apart")
+    T, k, E, C, ld = 70, 4, 6, 264, 1 << 24
+    r = experts.sort(make_ids(T, k, E, 3).cuda(), E)
+    x, w = torch.randn(T, C, device="cuda").bfloat16(), torch.rand(T, k, device="cuda")
+    room = torch.empty(T * k * ld, dtype=torch.bfloat16, device="cuda").view(T * k, ld)
+    far = room[:, :C]
+    xs = experts.gather(x, r)
+    assert torch.equal(experts.gather(x, r, out=far), xs) and torch.equal(experts.combine(far, r, w), experts.combine(xs, r, w))
+    dh, dw = experts.combine_gradient(x, xs, r, w)
+    assert torch.equal(experts.combine_gradient(x, far, r, w)[1], dw)
+    far_dh, far_dw = experts.combine_gradient(x, xs, r, w, dh=far)
+    assert torch.equal(far_dh, dh) and torch.equal(far_dw, dw)
+
+
+def test_captured_and_replayed():
+    """Sort, gather, combine and its gradient in a graph, replayed on new choices with
+    eager work between."""
+    log("case rows graph")
+    for T in (40, 3000):  # one workgroup sorts, several do
+        k, E, C = 2, 9, 136
+        ids, x, w = make_ids(T, k, E, 1).cuda(), torch.randn(T, C, device="cuda").bfloat16(), torch.rand(T, k, device="cuda")
+
+        def step():
+            r = experts.sort(ids, E)
+            xs = experts.gather(x, r)
+            return (r.offsets, r.token, r.place, xs, experts.combine(xs, r, w)) + experts.combine_gradient(x, xs, r, w)
+
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            kept = step()
+        for seed in range(4):
+            ids.copy_(make_ids(T, k, E, 10 + seed, skew=seed % 2 == 1).cuda())
+            x.copy_(torch.randn(T, C, device="cuda"))
+            graph.replay()
+            torch.cuda.synchronize()
+            for a, b in zip(kept, step()):
+                assert torch.equal(a, b)
+
+
 def test_refusals():
     log("case rows refusals")
     ids = torch.zeros(6, 2, dtype=torch.int32, device="cuda")

@@ -244,6 +244,28 @@ def test_long_rows_far_apart():
     ref.assert_within(ref.f64(fp8.product(B, A, out_dtype="f32")), want.T, ref.product_bound(bn, an, want.T, torch.float32))
 
 
+def test_operands_past_32_bits():
+    """Rows to quantise, and matrices of a batch, at offsets past 2^32: the same bits
+    as close together."""
+    log("case far operands")
+    x = values(70, 300, torch.bfloat16, 1).cuda()
+    far = torch.empty(70 << 26, dtype=torch.bfloat16, device="cuda").view(70, 1 << 26)[:, :300]
+    far.copy_(x)
+    for got, want in zip((fp8.quantize_rows(far),) + fp8.quantize_both(far) + fp8.quantize_weight(far),
+                         (fp8.quantize_rows(x),) + fp8.quantize_both(x) + fp8.quantize_weight(x)):
+        assert torch.equal(got.codes.view(torch.uint8), want.codes.view(torch.uint8))
+        assert torch.equal(got.scales.view(torch.uint8), want.scales.view(torch.uint8))
+    E, N, K = 3, 200, 384
+    W, _ = fp8.quantize_weight(values(E * N, K, torch.float32, 2).cuda().view(E, N, K), transposed=False)
+    room = torch.empty(E, 1 << 32, dtype=torch.uint8, device="cuda")
+    codes = room.as_strided((E, N, K), (1 << 32, K, 1)).view(torch.float8_e4m3fn)
+    codes.view(torch.uint8).copy_(W.codes.view(torch.uint8))
+    A = fp8.quantize_rows(values(300, K, torch.bfloat16, 3).cuda())
+    offsets = torch.tensor([0, 120, 121, 290], dtype=torch.int32, device="cuda")
+    got = fp8.grouped_product(A, fp8.Fp8Matrix(codes, W.scales, N, K, 128), offsets)
+    assert torch.equal(got, fp8.grouped_product(A, W, offsets))
+
+
 def test_another_stream_and_a_graph():
     """Enqueued on a stream of the caller's; captured and replayed on new data."""
     log("case stream and graph")

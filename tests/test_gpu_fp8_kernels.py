@@ -229,3 +229,20 @@ def test_offsets_out_of_order_stay_inside():
         fp8.quantize_both(torch.randn(R, 50, device="cuda"), offsets=off)
         torch.cuda.synchronize()
         assert (room[0] == 3).all() and (room[-1] == 3).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case,ld", [((4104, 1000, 4100, "f32"), 1 << 20), ((1543, 2612, 1278, "f16"), 1 << 22),
+                                     ((3341, 4854, 800, "bf16"), 1 << 20), ((9, 300, 520, "bf16"), 1 << 29)], ids=str)
+def test_results_past_32_bits(case, ld):
+    """Rows of C so far apart that offsets pass 2^32: the same bits as dense."""
+    M, N, K, t = case
+    log("case far results %s %d" % (case, ld))
+    A, B = codes(M, K, 1)[0], codes(N, K, 2)[0]
+    room = torch.empty(M * ld, dtype=TYPES[t], device="cuda").view(M, ld)
+    room[:, N:N + 8] = 3.0
+    C = fp8.product(A, B, C=room[:, :N], alpha=2.0 ** -9)
+    assert torch.equal(C, fp8.product(A, B, out_dtype=t, alpha=2.0 ** -9)) and (room[:, N:N + 8] == 3.0).all()
+    if t == "f32":
+        fp8.product(A, B, C=C, alpha=2.0 ** -9, beta=-1.0, C0=C)  # in place: the same sums, so exactly zero
+        assert (C == 0).all()
