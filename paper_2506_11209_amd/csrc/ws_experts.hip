@@ -11,7 +11,9 @@ constexpr int kSortWaves = 8;
 constexpr int kSortThreads = 64 * kSortWaves;
 constexpr int kSortSteps = 4;          // steps of 64 slots whose ids a wave loads at once
 constexpr int64_t kSortChunk = kSortSteps * kSortThreads;  // slots of a workgroup
-constexpr int64_t kSortAlone = 4096;   // slots that one workgroup sorts by itself
+// Slots that one workgroup sorts by itself (4096: 11.5 us, where two launches of
+// several take 7.5 and one launch more of the caller's time; 1024: 5.1 and 7.4).
+constexpr int64_t kSortAlone = 4096;
 constexpr int64_t kSortBlocks = 256;   // chunks at the most; beyond, chunks grow
 
 struct SortArgs {
@@ -77,14 +79,15 @@ __device__ __forceinline__ void count_slots(const SortArgs& a, int32_t* counts) 
     int e[kSortSteps];
     load_steps(a, s0, hi, e);
 #pragma unroll
-    for (int i = 0; i < kSortSteps; ++i) take_step(a, e[i], mine);
+    for (int i = 0; i < kSortSteps; ++i)
+      if (s0 + 64 * i < hi) take_step(a, e[i], mine);
   }
   __syncthreads();
 }
 
 // First of two launches: how many slots of each expert a chunk has.  Bound, both:
-// latency, a chain of loads, ballots and meetings (8192 x 4 slots of 64 experts: 4 to
-// 5 us, and 7.4 to 8 for place_kernel).
+// latency, a chain of loads, ballots and meetings (8192 x 4 slots of 64 experts: 2.2 to
+// 3.6 us, and 7.2 for place_kernel).
 __global__ __launch_bounds__(kSortThreads) void count_kernel(SortArgs a) {
   extern __shared__ int32_t lds[];
   count_slots(a, lds);
@@ -158,6 +161,7 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortArgs a) {
     load_steps(a, s0, hi, e);
 #pragma unroll
     for (int i = 0; i < kSortSteps; ++i) {
+      if (s0 + 64 * i >= hi) break;
       const int64_t s = s0 + 64 * i + lane;
       const int before = take_step(a, e[i], mine);
       if (e[i] >= 0) {
@@ -337,10 +341,15 @@ bool sort_sizes(int64_t tokens, int32_t k, int32_t experts) {
   return tokens >= 0 && k >= 1 && experts >= 1 && experts <= WS_MAX_EXPERTS && tokens <= kMaxDim && tokens * k <= kMaxDim;
 }
 
+// Slots of a workgroup.  Beyond what one sorts alone, small chunks for short kernels
+// (32768 slots of 64 experts as 64 chunks: 9.5 us, as 16: 11.5), but not so many that
+// summing their counts takes longer (131072 slots of 1024 experts as 64 chunks: 21
+// us, as 256: 34); then whole rounds of loads, and at last kSortBlocks of what it takes.
 int64_t sort_chunk(int64_t slots) {
-  if (slots <= kSortAlone) return kSortAlone;
-  const int64_t even = ceil_div(ceil_div(slots, kSortBlocks), kSortThreads) * kSortThreads;
-  return even > kSortChunk ? even : kSortChunk;
+  const auto chunk = [&](int64_t blocks) { return ceil_div(ceil_div(slots, blocks), kSortThreads) * kSortThreads; };
+  if (slots <= kSortAlone) return chunk(1);
+  const int64_t few = chunk(64), most = chunk(kSortBlocks);
+  return most > kSortChunk ? most : few < kSortChunk ? few : kSortChunk;
 }
 
 bool plain(const ws_matrix* m) { return valid(m) && m->batch <= 1; }
