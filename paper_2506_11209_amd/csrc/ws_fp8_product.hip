@@ -201,7 +201,7 @@ __device__ __forceinline__ bf16x8_t widen(int lo, int hi, float scale) {
 // A workgroup computes 16 MT rows of 16 columns; its waves share out the blocks
 // of the contraction and add up their parts through LDS in a fixed order.
 // Operands go from memory straight to registers, U blocks at a time.  For few
-// rows: bound by reading B once (1 x 8192 x 8192: 13 to 14 us, 5 TB/s).
+// rows: bound by reading B once (1 x 8192 x 8192: 13 to 15 us, 5 TB/s).
 template <int MT, int U, bool WIDE, bool AGPR = false>
 __device__ __forceinline__ void direct_part(const ProductArgs& a, const Part& p, float* lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -66,7 +66,7 @@ __device__ __forceinline__ void load_row8(const T* row, bool there, int64_t c, i
 // wave takes four blocks of a row (1 KiB of codes and elements in 16 bits).  A
 // workgroup's rows are `rows_per_wg` deep so that the scales, which lie along
 // the rows, are written in runs and not byte by byte.  Bound: memory; 8192 x 4096
-// bf16 in 24.2 us (4.2 TB/s), 16 x 4096 in 2.6, which is the launch.
+// bf16 in 24.2 us (4.2 TB/s), 16 x 4096 in 2.7, which is the launch.
 template <typename T, int UNROLL>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantArgs a) {
   constexpr int kRows = 4 * UNROLL;  // rows of a workgroup
@@ -135,7 +135,7 @@ __device__ __forceinline__ float Raw8<float>::operator[](int j) const {
 // to LDS in 8-byte pieces at a place that the column's upper bits permute (the
 // 16 lanes of a row write 16 columns eight apart: one bank set without it), and
 // leave as whole 128-byte lines.  Bound: memory, one read and two writes: 8192 x
-// 4096 bf16 in 28.9 us (4.7 TB/s), a 4100 x 4104 f32 weight in 19.9 (5.1 TB/s).
+// 4096 bf16 in 28.9 us (4.7 TB/s), a 4100 x 4104 f32 weight in 20 to 21 (5 TB/s).
 template <typename T, bool WEIGHT>
 __global__ __launch_bounds__(256, (WEIGHT || sizeof(T) == 2 ? 4 : 3)) void quantize_tile_kernel(QuantArgs a) {
   __shared__ uint8_t tile[kBlock * kBlock] __attribute__((aligned(16)));
