@@ -80,7 +80,8 @@ ws_status ws_fp8_quantize_rows(const ws_matrix* x, const int32_t* index, const w
  * a multiple of 128 in out_columns: those of group g at the sum of the earlier
  * groups' row counts, each rounded up to 128.  out_columns->cols ==
  * 128 * ws_fp8_padded_blocks(rows, groups); codes of no row are zero, their
- * scales 1.  Rows in no group are zeros in out_rows. */
+ * scales 1.  Rows in no group, before the first or after the last, are zeros in
+ * out_rows. */
 ws_status ws_fp8_quantize_both(const ws_matrix* x, const int32_t* index, int32_t groups,
                                const int32_t* offsets, const ws_fp8_matrix* out_rows,
                                const ws_fp8_matrix* out_columns, hipStream_t stream);
@@ -130,7 +131,8 @@ ws_status ws_fp8_product(const ws_fp8_matrix* A, const ws_fp8_matrix* B, float a
                          const ws_matrix* C0, const ws_matrix* C, hipStream_t stream);
 
 /* Rows by group: row r of C is row r of A times B_g^T, for the group g whose
- * rows offsets[g] .. offsets[g + 1] - 1 hold r; rows in no group become zeros.
+ * rows offsets[g] .. offsets[g + 1] - 1 hold r; rows in no group, before the first
+ * or after the last, become zeros.
  * B is a batch of `groups` matrices; offsets as above.  C <- alpha A B^T. */
 ws_status ws_fp8_grouped_product(const ws_fp8_matrix* A, const ws_fp8_matrix* B, int32_t groups,
                                  const int32_t* offsets, float alpha, const ws_matrix* C,

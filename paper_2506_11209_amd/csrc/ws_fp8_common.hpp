@@ -70,11 +70,12 @@ __device__ __forceinline__ uint32_t max16(uint32_t x) {
   return x;
 }
 
-// The rows of group i of `groups` among `rows`; i == groups: the rows after
-// the last group.  Offsets that decrease or leave the rows are cut to them.
+// The rows of group i of `groups` among `rows`; i == groups: the rows after the
+// last group, i == groups + 1: those before the first.  Offsets that decrease or
+// leave the rows are cut to them.
 __device__ __forceinline__ void group_rows(const int32_t* offsets, int groups, int64_t rows, int i, int64_t* lo,
                                            int64_t* hi) {
-  int64_t a = offsets[i], b = i < groups ? (int64_t)offsets[i + 1] : rows;
+  int64_t a = i <= groups ? offsets[i] : 0, b = i == groups ? rows : (int64_t)offsets[i < groups ? i + 1 : 0];
   a = a < 0 ? 0 : a > rows ? rows : a;
   *lo = a;
   *hi = b < a ? a : b > rows ? rows : b;
@@ -94,18 +95,19 @@ __device__ __forceinline__ uint32_t xcd_run(uint32_t id, uint32_t n) {
 }
 
 struct GroupTile {
-  int group;       // -1: none; `groups`: rows after the last group
+  int group;       // -1: none; `groups` and more: rows of no group
   int64_t lo, hi;  // its rows
   int64_t index;   // the tile's number inside the group
   int64_t before;  // tiles of the groups before it
 };
 
 // Which group tile `t` belongs to when every group, and then the rows after the
-// last one, is cut into tiles of `size` rows.  Called by whole waves; the answer
-// is the same in all lanes.  Sums of 64 groups' tiles at a time.
+// last and those before the first, are cut into tiles of `size` rows.  Called by
+// whole waves; the answer is the same in all lanes.  Sums of 64 groups' tiles at a
+// time.
 __device__ __forceinline__ GroupTile find_group_tile(const int32_t* offsets, int groups, int64_t rows, int size,
-                                                     int64_t t, bool with_tail) {
-  const int lane = threadIdx.x & 63, n = groups + (with_tail ? 1 : 0);
+                                                     int64_t t) {
+  const int lane = threadIdx.x & 63, n = groups + 2;
   int64_t before = 0;
   for (int first = 0; first < n; first += 64) {
     const int i = first + lane;
@@ -134,9 +136,9 @@ __device__ __forceinline__ GroupTile find_group_tile(const int32_t* offsets, int
   return GroupTile{-1, 0, 0, 0, before};
 }
 
-// All tiles of the groups and of the rows after the last one.
+// All tiles of the groups and of the rows in none.
 __device__ __forceinline__ int64_t count_group_tiles(const int32_t* offsets, int groups, int64_t rows, int size) {
-  const GroupTile g = find_group_tile(offsets, groups, rows, size, (int64_t)1 << 60, true);
+  const GroupTile g = find_group_tile(offsets, groups, rows, size, (int64_t)1 << 60);
   return uniform(g.before);
 }
 
@@ -144,10 +146,10 @@ __device__ __forceinline__ int64_t count_group_tiles(const int32_t* offsets, int
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Tiles of `size` rows that hold `rows` rows in `groups` groups and, with
-// tail, the rows after them, whatever the offsets.
-inline int64_t group_tiles(int64_t rows, int64_t groups, int size, bool tail) {
-  const int64_t parts = groups + (tail ? 1 : 0);
+// Tiles of `size` rows that hold `rows` rows in `groups` groups and, with `outside`,
+// the rows before and after them, whatever the offsets.
+inline int64_t group_tiles(int64_t rows, int64_t groups, int size, bool outside) {
+  const int64_t parts = groups + (outside ? 2 : 0);
   return (rows + (size - 1) * (parts < rows ? parts : rows)) / size;
 }
 

@@ -63,11 +63,11 @@ template <int MODE>
 __device__ __forceinline__ bool find_part(const ProductArgs& a, int64_t tm, int64_t tn, int64_t group, int TM, int TN, Part* p) {
   *p = Part{a.A, a.B, a.sa, a.sb, tm * TM, a.M, tn * TN, a.K, 0, 0, false};
   if constexpr (MODE == kRowGroups) {
-    const GroupTile gt = find_group_tile(a.offsets, a.groups, a.M, TM, tm, true);
+    const GroupTile gt = find_group_tile(a.offsets, a.groups, a.M, TM, tm);
     if (gt.group < 0) return false;
     p->m0 = gt.lo + gt.index * TM;
     p->m_end = gt.hi;
-    p->zero = gt.group == a.groups;
+    p->zero = gt.group >= a.groups;
     if (!p->zero) {
       p->B += gt.group * a.stride_b;
       p->sb += gt.group * a.stride_sb;

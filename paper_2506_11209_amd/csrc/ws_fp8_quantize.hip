@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256, (WEIGHT || sizeof(T) == 2 ? 4 : 3)) void quant
   int64_t r0 = rb * kBlock, n = a.rows - r0;
   bool there = true;
   if (a.offsets) {
-    const GroupTile gt = find_group_tile(a.offsets, a.groups, a.rows, kBlock, rb, true);
+    const GroupTile gt = find_group_tile(a.offsets, a.groups, a.rows, kBlock, rb);
     r0 = gt.lo + gt.index * kBlock;
     n = gt.group < 0 ? 0 : gt.hi - r0;
     there = gt.group >= 0 && gt.group < a.groups;
