@@ -38,7 +38,8 @@ extern "C" {
 
 /* A matrix in 8 bits (see above).  With `batch` above 1, `batch` matrices of
  * the same size, stride_codes and stride_scales bytes apart (weights of
- * experts). */
+ * experts).  A call on single matrices takes 0 as 1; where a batch is taken, 0 is
+ * an empty one. */
 typedef struct {
   void* codes;            /* 16-byte aligned */
   uint8_t* scales;

@@ -161,17 +161,18 @@ inline int elem_size(int32_t dtype) {
   return dtype == WS_OUT_F32 ? 4 : dtype == WS_OUT_BF16 || dtype == WS_OUT_F16 ? 2 : 0;
 }
 
-// A dense operand: sizes, type, and data where it has elements.
-inline bool valid(const ws_matrix* m, bool need_data = true) {
+// A dense operand: sizes, type, and data where it has elements.  `batched`: the call
+// takes a batch, so that 0 matrices have none; elsewhere batch 0 is a single matrix.
+inline bool valid(const ws_matrix* m, bool batched = false) {
   if (!m || m->rows < 0 || m->cols < 0 || m->rows > kMaxDim || m->cols > kMaxDim || m->batch < 0) return false;
   const int size = elem_size(m->dtype);
   if (!size || m->ld < m->cols || m->ld > kMaxDim) return false;
   if (m->batch > 1 && m->rows > 0 && m->cols > 0 && m->stride < (m->rows - 1) * m->ld + m->cols) return false;
-  if (m->rows == 0 || m->cols == 0 || m->batch == 0) return true;
-  return !need_data || (m->data && (uintptr_t)m->data % size == 0);
+  if (m->rows == 0 || m->cols == 0 || (batched && m->batch == 0)) return true;
+  return m->data && (uintptr_t)m->data % size == 0;
 }
 
-inline bool valid(const ws_fp8_matrix* m) {
+inline bool valid(const ws_fp8_matrix* m, bool batched = false) {
   if (!m || m->rows < 0 || m->cols < 0 || m->rows > kMaxDim || m->cols > kMaxDim || m->batch < 0) return false;
   if (m->block_rows != 1 && m->block_rows != kBlock) return false;
   if (m->ld % 16 || m->ld < ceil_div(m->cols, 16) * 16 || m->ld > kMaxDim) return false;
@@ -180,7 +181,7 @@ inline bool valid(const ws_fp8_matrix* m) {
       (m->stride_codes % 16 || m->stride_codes < (m->rows - 1) * m->ld + ceil_div(m->cols, 16) * 16 ||
        m->stride_scales < (ceil_div(m->cols, kBlock) - 1) * m->ld_scales + ceil_div(m->rows, m->block_rows)))
     return false;
-  if (m->rows == 0 || m->cols == 0 || m->batch == 0) return true;
+  if (m->rows == 0 || m->cols == 0 || (batched && m->batch == 0)) return true;
   return m->codes && m->scales && (uintptr_t)m->codes % 16 == 0;
 }
 

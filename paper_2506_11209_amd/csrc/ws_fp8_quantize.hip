@@ -368,11 +368,11 @@ ws_status ws_fp8_quantize_both(const ws_matrix* x, const int32_t* index, int32_t
 
 ws_status ws_fp8_quantize_weight(const ws_matrix* w, const ws_fp8_matrix* out, const ws_fp8_matrix* out_transposed,
                                  hipStream_t stream) {
-  if (!valid(w) || !valid(out) || out->block_rows != kBlock || out->rows != w->rows || out->cols != w->cols ||
+  if (!valid(w, true) || !valid(out, true) || out->block_rows != kBlock || out->rows != w->rows || out->cols != w->cols ||
       out->batch != w->batch)
     return WS_ERR_INVALID_ARG;
   const ws_fp8_matrix* t = out_transposed;
-  if (t && (!valid(t) || t->block_rows != kBlock || t->rows != w->cols || t->cols != w->rows || t->batch != w->batch))
+  if (t && (!valid(t, true) || t->block_rows != kBlock || t->rows != w->cols || t->cols != w->rows || t->batch != w->batch))
     return WS_ERR_INVALID_ARG;
   if (w->rows == 0 || w->cols == 0 || w->batch == 0) return WS_OK;
   QuantArgs a = base_args(w, nullptr, out);
