@@ -81,23 +81,25 @@ def _check(status: int, where: str) -> None:
 
 class _Call:
     """Makes a call's stream and device the current ones, so that its results and
-    work memory belong to it, and marks tensors as in use by it."""
+    work memory belong to it, and marks tensors of the device as in use by it (what
+    else was handed in is refused by the call's own checks)."""
 
-    __slots__ = ("_stack",)
+    __slots__ = ("_device", "_stream", "_tensors", "_stack")
 
     def __init__(self, device: torch.device, stream, tensors):
-        self._stack = contextlib.ExitStack()
-        self._stack.enter_context(torch.cuda.device(device))
-        if stream is None:
-            return
-        if stream.device != device:
+        if stream is not None and stream.device != device:
             raise ValueError("the stream belongs to %s, the tensors to %s" % (stream.device, device))
-        self._stack.enter_context(torch.cuda.stream(stream))
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+        self._device, self._stream, self._tensors = device, stream, tensors
 
     def __enter__(self):
+        with contextlib.ExitStack() as stack:  # left again where something fails
+            stack.enter_context(torch.cuda.device(self._device))
+            if self._stream is not None:
+                stack.enter_context(torch.cuda.stream(self._stream))
+                for t in self._tensors:
+                    if isinstance(t, torch.Tensor) and t.is_cuda and t.device == self._device:
+                        t.record_stream(self._stream)
+            self._stack = stack.pop_all()
         return self
 
     def __exit__(self, *exc):
