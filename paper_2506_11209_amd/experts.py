@@ -8,13 +8,17 @@ include/ws_experts.h; computed by the HIP kernels of libwsgemm.so).
     dh, dweights = combine_gradient(dy, h, routes, weights)
     dx = combine(dxs, routes)                      # gradient of gather
 
-Streams and errors as in ``fp8``.
+Streams and errors as in ``fp8``.  gather and combine are recorded by autograd
+(once: their gradients are not differentiated again), so that the last two lines
+are what their results' backward does; results in memory of the caller's (``out``)
+cannot be, and ask for torch.no_grad() where an input requires a gradient.
 """
 from __future__ import annotations
 
 import ctypes
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import wsgemm as _w
 from .fp8 import _Call, _check, _elsewhere, _matrix, _mp, _need, _new_matrix, _raw_stream
@@ -96,6 +100,42 @@ def _weights(weights, routes):
     return weights.data_ptr()
 
 
+def _recorded(out, *inputs) -> bool:
+    """Whether autograd has to know of a call on these inputs."""
+    if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in inputs):
+        return False
+    if out is not None:
+        raise ValueError("out: a result in the caller's memory is not recorded for gradients; call it under torch.no_grad()")
+    return True
+
+
+class _Gather(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, routes):
+        ctx.save_for_backward(routes.offsets, routes.token, routes.place)
+        return gather(x, routes)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dxs):
+        return combine(dxs.contiguous(), Routes(*ctx.saved_tensors)), None
+
+
+class _Combine(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, h, weights, routes):
+        of_weights = ctx.needs_input_grad[1]
+        ctx.save_for_backward(h if of_weights else None, weights, routes.offsets, routes.token, routes.place)
+        return combine(h, routes, weights)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        h, weights, *routes = ctx.saved_tensors
+        dh, dweights = _gradient(dy.contiguous(), h, Routes(*routes), weights, None, ctx.needs_input_grad[1])
+        return dh if ctx.needs_input_grad[0] else None, dweights, None
+
+
 def gather(x, routes: Routes, out=None, stream=None):
     """x (tokens x columns; f32, bf16 or f16) by sorted row; zeros for rows of no token."""
     m = _matrix(x, "x", device=routes.token.device)
@@ -105,6 +145,8 @@ def gather(x, routes: Routes, out=None, stream=None):
     if _elsewhere(x, stream):
         with _Call(x.device, stream, [x, routes.offsets, routes.place, out]):
             return gather(x, routes, out)
+    if _recorded(out, x):
+        return _Gather.apply(x, routes)
     out, mo = _out(out, "out", routes.token.numel(), m.cols, x)
     _check(_lib.ws_expert_gather(m, k, routes.experts, routes.offsets.data_ptr(), routes.place.data_ptr(), mo,
                                  _raw_stream(x.get_device())), "ws_expert_gather")
@@ -121,6 +163,8 @@ def combine(h, routes: Routes, weights=None, out=None, stream=None):
     if _elsewhere(h, stream):
         with _Call(h.device, stream, [h, routes.place, weights, out]):
             return combine(h, routes, weights, out)
+    if _recorded(out, h, weights):
+        return _Combine.apply(h, weights, routes)
     out, mo = _out(out, "out", tokens, m.cols, h)
     _check(_lib.ws_expert_combine(m, k, routes.place.data_ptr(), w, mo, _raw_stream(h.get_device())), "ws_expert_combine")
     return out
@@ -128,12 +172,18 @@ def combine(h, routes: Routes, weights=None, out=None, stream=None):
 
 def combine_gradient(dy, h, routes: Routes, weights=None, dh=None, stream=None):
     """(dh, dweights) of combine: dh like h, rows without a token zero; dweights
-    tokens x k in binary32, None where weights is None (then h may be None)."""
+    tokens x k in binary32, None where weights is None (then h may be None).  Not
+    recorded by autograd."""
+    return _gradient(dy, h, routes, weights, dh, weights is not None, stream)
+
+
+def _gradient(dy, h, routes, weights, dh, of_weights, stream=None):
+    """of_weights: dweights is wanted (else None, and h is not looked at)."""
     m = _matrix(dy, "dy", device=routes.token.device)
     w, (tokens, k) = _weights(weights, routes), routes.place.shape
     if m.rows != tokens:
         raise ValueError("dy: %d rows for %d tokens" % (m.rows, tokens))
-    if weights is not None:
+    if of_weights:
         mh = _matrix(h, "h", device=dy.device)
         if (mh.rows, mh.cols) != (routes.token.numel(), m.cols) or h.dtype != dy.dtype:
             raise ValueError("h: expected %s %s, got %s %s" % ((routes.token.numel(), m.cols), dy.dtype, tuple(h.shape), h.dtype))
@@ -141,9 +191,9 @@ def combine_gradient(dy, h, routes: Routes, weights=None, dh=None, stream=None):
         mh = None
     if _elsewhere(dy, stream):
         with _Call(dy.device, stream, [dy, h, routes.offsets, routes.place, weights, dh]):
-            return combine_gradient(dy, h, routes, weights, dh)
+            return _gradient(dy, h, routes, weights, dh, of_weights)
     dh, mdh = _out(dh, "dh", routes.token.numel(), m.cols, dy)
-    dw = torch.empty(tokens, k, dtype=torch.float32, device=dy.device) if weights is not None else None
+    dw = torch.empty(tokens, k, dtype=torch.float32, device=dy.device) if of_weights else None
     _check(_lib.ws_expert_combine_gradient(m, mh, k, routes.experts, routes.offsets.data_ptr(), routes.place.data_ptr(), w, mdh,
                                            dw.data_ptr() if dw is not None else 0, _raw_stream(dy.get_device())),
            "ws_expert_combine_gradient")

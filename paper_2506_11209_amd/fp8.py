@@ -20,6 +20,8 @@ stream, and tensors handed in are marked as in use by it, so that their memory
 is not given out again before the work is done.  Sizes, types, devices and
 strides are checked and raise ValueError, a status of the library raises
 WsGemmError; the contents of codes, scales and offsets are not looked at.
+Nothing here is recorded by autograd: a layer's backward makes the gradients with
+the calls above.
 """
 from __future__ import annotations
 
