@@ -19,6 +19,7 @@ import json
 import time
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import experts, fp8
 
@@ -43,6 +44,7 @@ class _Experts(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         weights, h, rows = ctx.saved_tensors
         routes, (xt, at, w1t, w2t) = ctx.routes, ctx.operands

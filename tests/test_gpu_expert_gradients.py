@@ -134,3 +134,26 @@ def test_second_derivatives_are_refused():
         d, = torch.autograd.grad(y.sum(), x, create_graph=True)
         with pytest.raises(RuntimeError):
             d.square().sum().backward()
+
+
+def make_layer(seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    layer = expert_layer.ExpertLayer(136, 200, 5, 3, generator=g)
+    x = torch.randn(33, 136, device="cuda", generator=g).bfloat16()
+    return layer, x, torch.randn(33, 136, device="cuda", generator=g).bfloat16()
+
+
+def grads(layer, x, dy):
+    layer.zero_grad()
+    xd = x.clone().requires_grad_()
+    layer(xd).backward(dy)
+    return {"x": xd.grad, "router": layer.router.grad, "w1": layer.w1.grad, "w2": layer.w2.grad}
+
+
+def test_layer_refuses_second_derivatives():
+    log("case second derivatives of the layer")
+    layer, x, _ = make_layer()
+    x.requires_grad_()
+    d, = torch.autograd.grad(layer(x).float().square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        d.float().square().sum().backward()
