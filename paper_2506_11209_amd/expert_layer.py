@@ -26,39 +26,57 @@ from . import experts, fp8
 
 class _Experts(torch.autograd.Function):
     """y of x, the choices' weights (tokens x k, f32) and ids (tokens x k); w1 is E x
-    hidden x columns, w2 is E x columns x hidden."""
+    hidden x columns, w2 is E x columns x hidden.  Only what the gradients that are
+    asked for need is quantised, kept and computed."""
 
     @staticmethod
     def forward(ctx, x, weights, w1, w2, ids):
+        of_x, of_weights, of_w1, of_w2, _ = ctx.needs_input_grad
+        of_h = of_x or of_w1  # of the first product
         routes = experts.sort(ids, w1.shape[0])
-        xq, xt = fp8.quantize_both(x, index=routes.token, offsets=routes.offsets)
-        w1q, w1t = fp8.quantize_weight(w1)
+        xq, xt = _operand(x, routes, of_w1, index=routes.token)
+        w1q, w1t = fp8.quantize_weight(w1, transposed=of_x)
         h = fp8.grouped_product(xq, w1q, routes.offsets)
-        aq, at = fp8.quantize_both(torch.nn.functional.silu(h), offsets=routes.offsets)
-        w2q, w2t = fp8.quantize_weight(w2)
+        aq, at = _operand(torch.nn.functional.silu(h), routes, of_w2)
+        w2q, w2t = fp8.quantize_weight(w2, transposed=of_h)
         rows = fp8.grouped_product(aq, w2q, routes.offsets)
         y = experts.combine(rows, routes, weights)
         # quantised operands are kept, not the tensors they came from
-        ctx.save_for_backward(weights, h, rows)
+        ctx.save_for_backward(weights, h if of_h else None, rows if of_weights else None)
         ctx.routes, ctx.operands = routes, (xt, at, w1t, w2t)
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
+        of_x, of_weights, of_w1, of_w2, _ = ctx.needs_input_grad
         weights, h, rows = ctx.saved_tensors
         routes, (xt, at, w1t, w2t) = ctx.routes, ctx.operands
         off, n = routes.offsets, routes.token.numel()
-        drows, dweights = experts.combine_gradient(dy.contiguous(), rows, routes, weights)
-        gq, gt = fp8.quantize_both(drows, offsets=off)
-        dw2 = fp8.grouped_gradient(gt, at, n, off)
-        da = fp8.grouped_product(gq, w2t, off).float()
-        s = torch.sigmoid(h.float())
-        dh = (da * (s * (1.0 + h.float() * (1.0 - s)))).to(h.dtype)
-        hq, ht = fp8.quantize_both(dh, offsets=off)
-        dw1 = fp8.grouped_gradient(ht, xt, n, off)
-        dx = experts.combine(fp8.grouped_product(hq, w1t, off), routes)
+        dx = dw1 = dw2 = None
+        drows, dweights = experts._gradient(dy.contiguous(), rows, routes, weights, None, of_weights)
+        if of_x or of_w1 or of_w2:
+            gq, gt = _operand(drows, routes, of_w2)
+        if of_w2:
+            dw2 = fp8.grouped_gradient(gt, at, n, off)
+        if of_x or of_w1:
+            da = fp8.grouped_product(gq, w2t, off).float()
+            s = torch.sigmoid(h.float())
+            dh = (da * (s * (1.0 + h.float() * (1.0 - s)))).to(h.dtype)
+            hq, ht = _operand(dh, routes, of_w1)
+        if of_w1:
+            dw1 = fp8.grouped_gradient(ht, xt, n, off)
+        if of_x:
+            dx = experts.combine(fp8.grouped_product(hq, w1t, off), routes)
         return dx, dweights, dw1, dw2, None
+
+
+def _operand(x, routes, columns: bool, index=None):
+    """x, one row for each choice, for a grouped product, and its columns where a
+    weight gradient contracts over them."""
+    if columns:
+        return fp8.quantize_both(x, index=index, offsets=routes.offsets)
+    return fp8.quantize_rows(x, index=index), None
 
 
 class ExpertLayer(torch.nn.Module):

@@ -157,3 +157,34 @@ def test_layer_refuses_second_derivatives():
     d, = torch.autograd.grad(layer(x).float().square().sum(), x, create_graph=True)
     with pytest.raises(RuntimeError):
         d.float().square().sum().backward()
+
+
+def test_layer_computes_what_is_asked_for(monkeypatch):
+    log("case layer frozen weights")
+    layer, x, dy = make_layer()
+    want = grads(layer, x, dy)
+    calls = []
+    for name in ("grouped_gradient", "grouped_product", "quantize_both"):
+        f = getattr(fp8, name)
+        monkeypatch.setattr(fp8, name, lambda *a, _f=f, _n=name, **kw: (calls.append(_n), _f(*a, **kw))[1])
+
+    def count():
+        c = [calls.count(n) for n in ("grouped_gradient", "grouped_product", "quantize_both")]
+        calls.clear()
+        return c
+
+    grads(layer, x, dy)
+    assert count() == [2, 4, 4]  # weight gradients; products forward and back; operands in both forms
+    for frozen in (("w1",), ("w2",), ("w1", "w2")):
+        for name in ("w1", "w2"):
+            getattr(layer, name).requires_grad_(name not in frozen)
+        got = grads(layer, x, dy)
+        assert count()[0] == 2 - len(frozen)
+        for name, value in got.items():
+            assert value is None if name in frozen else torch.equal(value, want[name])
+    layer.zero_grad()
+    for name in ("w1", "w2"):
+        getattr(layer, name).requires_grad_(False)
+    layer(x).backward(dy)  # only the router learns
+    assert count() == [0, 2, 0] and torch.equal(layer.router.grad, want["router"])
+    assert torch.equal(layer(x).detach(), layer.serve(x, layer.serving_weights()))
