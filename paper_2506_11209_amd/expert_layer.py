@@ -42,17 +42,19 @@ class _Experts(torch.autograd.Function):
         rows = fp8.grouped_product(aq, w2q, routes.offsets)
         y = experts.combine(rows, routes, weights)
         # quantised operands are kept, not the tensors they came from
-        ctx.save_for_backward(weights, h if of_h else None, rows if of_weights else None)
-        ctx.routes, ctx.operands = routes, (xt, at, w1t, w2t)
+        operands = (xt, at, w1t, w2t)
+        ctx.shapes = [q and (q.rows, q.cols, q.block_rows) for q in operands]
+        ctx.save_for_backward(weights, h if of_h else None, rows if of_weights else None, routes.offsets, routes.token, routes.place,
+                              *(t for q in operands for t in ((q.codes, q.scales) if q else (None, None))))
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         of_x, of_weights, of_w1, of_w2, _ = ctx.needs_input_grad
-        weights, h, rows = ctx.saved_tensors
-        routes, (xt, at, w1t, w2t) = ctx.routes, ctx.operands
-        off, n = routes.offsets, routes.token.numel()
+        weights, h, rows, off, token, place, *kept = ctx.saved_tensors
+        xt, at, w1t, w2t = (s and fp8.Fp8Matrix(*kept[2 * i:2 * i + 2], *s) for i, s in enumerate(ctx.shapes))
+        routes, n = experts.Routes(off, token, place), token.numel()
         dx = dw1 = dw2 = None
         drows, dweights = experts._gradient(dy.contiguous(), rows, routes, weights, None, of_weights)
         if of_x or of_w1 or of_w2:

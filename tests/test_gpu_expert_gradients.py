@@ -188,3 +188,34 @@ def test_layer_computes_what_is_asked_for(monkeypatch):
     layer(x).backward(dy)  # only the router learns
     assert count() == [0, 2, 0] and torch.equal(layer.router.grad, want["router"])
     assert torch.equal(layer(x).detach(), layer.serve(x, layer.serving_weights()))
+
+
+def test_layer_keeps_its_operands_as_saved_tensors():
+    log("case layer saved tensors")
+    layer, x, dy = make_layer()
+    want, kept = grads(layer, x, dy), []
+
+    def pack(t):
+        kept.append(t.numel() * t.element_size())
+        return t.cpu()
+
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t.cuda()):
+        got = grads(layer, x, dy)
+    for name in want:
+        assert torch.equal(got[name], want[name])
+    # the transposed weights' codes, of 136 and of 200 columns padded to 16, and the rows' of 99 choices
+    weights = 5 * (136 * 208 + 200 * 144)
+    assert sum(kept) >= weights + 99 * (136 + 200)
+    y = layer(x.clone().requires_grad_())
+    y.backward(dy)
+    with pytest.raises(RuntimeError):  # they are gone
+        y.backward(dy)
+
+
+def test_layer_of_no_tokens():
+    log("case layer of nothing")
+    layer, x, dy = make_layer()
+    got = grads(layer, x[:0], dy[:0])
+    assert got["x"].shape == (0, 136)
+    for name in ("router", "w1", "w2"):
+        assert torch.equal(got[name], torch.zeros_like(getattr(layer, name)))
