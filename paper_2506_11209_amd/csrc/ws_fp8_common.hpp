@@ -154,8 +154,9 @@ inline int64_t group_tiles(int64_t rows, int64_t groups, int size, bool outside)
 }
 
 constexpr int64_t kMaxDim = 1ll << 30;
-// Workgroups of one launch: the runtime counts threads of a dimension in 32 bits.
 constexpr int64_t kMaxGrid = (1ll << 32) / 1024 - 1;
+// Workgroups of `block` threads in one launch: the runtime counts threads of a dimension in 32 bits.
+constexpr int64_t max_workgroups(int block) { return ((1ll << 32) - 1) / block; }
 
 inline int elem_size(int32_t dtype) {
   return dtype == WS_OUT_F32 ? 4 : dtype == WS_OUT_BF16 || dtype == WS_OUT_F16 ? 2 : 0;

@@ -268,7 +268,7 @@ __device__ __forceinline__ void direct_part(const ProductArgs& a, const Part& p,
 }
 
 template <int MT, int U, int MODE, bool WIDE>
-__global__ __launch_bounds__(512) void direct_kernel(ProductArgs a) {
+__global__ __launch_bounds__(512) void direct_kernel(ProductArgs a) {  // kDirectThreads
   extern __shared__ float lds[];
   const int64_t tn = blockIdx.x % a.tiles_n, t = blockIdx.x / a.tiles_n;
   Part p;
@@ -811,12 +811,28 @@ int compute_units() {
 // Bytes between rows so that a tile's offsets stay below kOutside.
 constexpr int64_t kMaxLd = 1 << 22;
 
+constexpr int kDirectThreads = 512;  // of a workgroup of the direct kernel, at the most
+// Tiles of a tile kernel, whose workgroups take any number: their numbers, counted
+// two rounds of workgroups past the end, fit 32 bits.
+constexpr int64_t kMaxTiles = 1ll << 31;
+
+int64_t tiles_of_rows(int mode, int64_t M, int64_t groups, int rows) {
+  return mode == kRowGroups ? group_tiles(M, groups, rows, true) : ceil_div(M, rows);
+}
+// Tiles of rows x cols that cover a product, or `most` + 1 for more than `most`.
+int64_t tiles_of(int mode, int64_t M, int64_t N, int64_t groups, int rows, int cols, int64_t most) {
+  const int64_t plane = tiles_of_rows(mode, M, groups, rows) * ceil_div(N, cols);
+  if (plane > most) return most + 1;
+  const int64_t all = plane * (mode == kDepthGroups ? groups : 1);
+  return all > most ? most + 1 : all;
+}
+
 template <int MT, int U, int MODE>
 ws_status run_direct(ProductArgs a, hipStream_t stream) {
   a.tiles_n = ceil_div(a.N, 16);
-  a.tiles_m = MODE == kRowGroups ? group_tiles(a.M, a.groups, 16 * MT, true) : ceil_div(a.M, 16 * MT);
-  const int64_t grid = a.tiles_n * a.tiles_m * (MODE == kDepthGroups ? a.groups : 1);
-  if (a.tiles_m > kMaxGrid || grid > kMaxGrid) return WS_ERR_INVALID_ARG;
+  a.tiles_m = tiles_of_rows(MODE, a.M, a.groups, 16 * MT);
+  const int64_t most = max_workgroups(kDirectThreads), grid = tiles_of(MODE, a.M, a.N, a.groups, 16 * MT, 16, most);
+  if (grid > most) return WS_ERR_INVALID_ARG;
   // Waves that share a contraction: as many as give the card 4096 or one block each.
   int waves = 1;
   while (waves < 8 && grid * waves < 4096 && waves * kBlock < a.K) waves *= 2;
@@ -829,11 +845,11 @@ ws_status run_tiles(ProductArgs a, hipStream_t stream) {
   typedef TileShape<WM, WN, STAGES> Shape;
   constexpr int TM = Shape::TM, TN = Shape::TN;
   a.tiles_n = ceil_div(a.N, TN);
-  a.tiles_m = MODE == kRowGroups ? group_tiles(a.M, a.groups, TM, true) : ceil_div(a.M, TM);
-  const int64_t tiles = a.tiles_n * a.tiles_m, grid = tiles * (MODE == kDepthGroups ? a.groups : 1);
-  if (a.tiles_m > kMaxGrid || tiles > kMaxGrid || grid > kMaxGrid) return WS_ERR_INVALID_ARG;
+  a.tiles_m = tiles_of_rows(MODE, a.M, a.groups, TM);
+  const int64_t tiles = tiles_of(MODE, a.M, a.N, a.groups, TM, TN, kMaxTiles);
+  if (tiles > kMaxTiles) return WS_ERR_INVALID_ARG;
   const int64_t most = (int64_t)compute_units() * Shape::kWaves;
-  a.tile_groups = (int32_t)(grid < most ? grid : most);
+  a.tile_groups = (int32_t)(tiles < most ? tiles : most);
   const int64_t rest = a.rest_end > a.M ? ceil_div(a.rest_end - a.M, 16) * ceil_div(a.N, 16) : 0;
   const auto kernel = &tile_kernel<WM, WN, STAGES, MODE, WIDE>;
   static std::atomic<uint64_t> allowed;  // devices on which the kernel may use this much LDS
@@ -896,15 +912,34 @@ float direct_cost(const Work& w, int rows) {
                  0.03 * (double)w.K / kBlock);
 }
 
-Choice choose(const Work& w, bool wide, float* cost) {
+// A kernel's tile and the stages of its ring.
+ws_fp8_kernel_info kernel_of(Choice c, bool wide) {
+  switch (c) {
+    case kDirect16: return {16, 16, 0, 0};
+    case kDirect32: return {32, 16, 0, 0};
+    case kDirect64: return {64, 16, 0, 0};
+    case kTile64: return {64, 64, 2, 0};
+    case kTile64Deep: return {64, 64, 4, 0};
+    case kTile128: return {128, 128, 2, 0};
+    case kTile128Deep: return {128, 128, 4, 0};
+    default: return {256, wide ? 128 : 256, 2, 0};
+  }
+}
+
+// The cheapest kernel of those that one launch can run on all of a product's tiles;
+// *cost is infinite where there is none.
+Choice choose(const Work& w, int mode, int64_t M, int64_t groups, bool wide, float* cost) {
   Choice best = kDirect16;
-  *cost = direct_cost(w, 16);
+  *cost = INFINITY;
   const auto consider = [&](Choice c, float t) {
-    if (t < *cost) {
+    const ws_fp8_kernel_info k = kernel_of(c, wide);
+    const int64_t most = k.stages == 0 ? max_workgroups(kDirectThreads) : kMaxTiles;
+    if (t < *cost && tiles_of(mode, M, w.N, groups, k.tile_m, k.tile_n, most) <= most) {
       *cost = t;
       best = c;
     }
   };
+  consider(kDirect16, direct_cost(w, 16));
   consider(kDirect32, direct_cost(w, 32));
   consider(kDirect64, direct_cost(w, 64));
   consider(kTile64, tile_cost(w, kCost64[wide]));
@@ -931,7 +966,7 @@ ws_status run_choice(Choice c, const ProductArgs& a, hipStream_t stream) {
 }
 
 // One or two parts of a product: the first `split` rows by choice[0], the rest
-// by choice[1].
+// by choice[1].  No part: no kernel's launch holds it.
 struct Plan {
   int count;
   int64_t split;
@@ -949,7 +984,8 @@ Plan plan_product(int mode, int64_t M, int64_t N, int64_t K, int64_t groups, boo
     w.K = ceil_div(ceil_div(K, groups), kBlock) * kBlock;
   }
   float cost;
-  Plan plan{1, M, {choose(w, wide, &cost), kDirect16}};
+  Plan plan{1, M, {choose(w, mode, M, groups, wide, &cost), kDirect16}};
+  if (isinf(cost)) plan.count = 0;
   if (mode == kDense && M > kBlock && M % kBlock != 0) {
     // The last rows by themselves, where they would start tiles of their own that a
     // round has no place for (4104 x 1000 x 4100: 33 x 8 tiles of 128 rows for 256
@@ -958,7 +994,8 @@ Plan plan_product(int mode, int64_t M, int64_t N, int64_t K, int64_t groups, boo
     Work top = w, rest = w;
     top.rows = (double)(M / kBlock * kBlock);
     rest.rows = (double)(M % kBlock);
-    const Choice cm = choose(top, wide, &main_cost), cr = choose(rest, wide, &rest_cost);
+    const Choice cm = choose(top, mode, M / kBlock * kBlock, groups, wide, &main_cost);
+    const Choice cr = choose(rest, mode, M % kBlock, groups, wide, &rest_cost);
     if (main_cost + rest_cost < 0.95f * cost) plan = Plan{2, M / kBlock * kBlock, {cm, cr}};
   }
   return plan;
@@ -967,6 +1004,7 @@ Plan plan_product(int mode, int64_t M, int64_t N, int64_t K, int64_t groups, boo
 template <int MODE>
 ws_status run_product(const ProductArgs& a, hipStream_t stream) {
   const Plan plan = plan_product(MODE, a.M, a.N, MODE == kDepthGroups ? a.depth_rows : a.K, a.groups, a.dtype == WS_OUT_F32);
+  if (plan.count == 0) return WS_ERR_INVALID_ARG;
   if (plan.count == 1) return run_choice<MODE>(plan.choice[0], a, stream);
   ProductArgs m = a, r = a;
   m.M = plan.split;
@@ -976,7 +1014,8 @@ ws_status run_product(const ProductArgs& a, hipStream_t stream) {
   // else behind them, where they are few (4104 x 1000 x 4100: 33.0 us, so 31.8, but
   // 4160 x 4096 x 4096: 68, by itself with 64 rows a workgroup, 75).
   const bool beside = plan.choice[0] == kTile128 || plan.choice[0] == kTile64;
-  if (plan.choice[0] >= kTile256 && plan.choice[1] < kTile256 && (beside || r.M <= 16) && a.N <= kMaxGrid) {
+  if (plan.choice[0] >= kTile256 && plan.choice[1] < kTile256 && (beside || r.M <= 16) &&
+      ceil_div(r.M, 16) * ceil_div(a.N, 16) <= max_workgroups(256) - 2 * compute_units()) {
     m.rest_end = a.M;
     return run_choice<MODE>(plan.choice[0], m, stream);
   }
@@ -1047,18 +1086,9 @@ ws_status ws_fp8_plan(int64_t M, int64_t N, int64_t K, int32_t out_dtype, int32_
   if (M == 0 || N == 0) return WS_OK;
   const bool wide = out_dtype == WS_OUT_F32;
   const Plan plan = plan_product(groups == 0 ? kDense : depth ? kDepthGroups : kRowGroups, M, N, K, groups, wide);
+  if (plan.count == 0) return WS_ERR_INVALID_ARG;
   for (int i = 0; i < plan.count; ++i) {
-    ws_fp8_kernel_info k{};
-    switch (plan.choice[i]) {
-      case kDirect16: k = {16, 16, 0, 0}; break;
-      case kDirect32: k = {32, 16, 0, 0}; break;
-      case kDirect64: k = {64, 16, 0, 0}; break;
-      case kTile64: k = {64, 64, 2, 0}; break;
-      case kTile64Deep: k = {64, 64, 4, 0}; break;
-      case kTile128: k = {128, 128, 2, 0}; break;
-      case kTile128Deep: k = {128, 128, 4, 0}; break;
-      case kTile256: k = {256, wide ? 128 : 256, 2, 0}; break;
-    }
+    ws_fp8_kernel_info k = kernel_of(plan.choice[i], wide);
     k.rows = i == 0 ? plan.split : M - plan.split;
     out[i] = k;
   }
