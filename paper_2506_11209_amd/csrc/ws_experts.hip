@@ -184,6 +184,7 @@ struct RowArgs {
   const float* weights;
   float* dweights;
   int64_t x_rows, rows, cols, ld_x, ld_dy, ld_out;
+  int64_t first;  // token of this launch
   int32_t k, experts, parts;
 };
 
@@ -214,7 +215,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void gather_kernel(RowArgs a) {
   constexpr int N = 16 / sizeof(T), kSteps = 4;
   const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t t = item / a.parts, c0 = item % a.parts * (64 * N * kSteps) + (threadIdx.x & 63) * N;
+  const int64_t t = a.first + item / a.parts, c0 = item % a.parts * (64 * N * kSteps) + (threadIdx.x & 63) * N;
   if (t >= a.x_rows) return;
   T v[kSteps][N];
 #pragma unroll
@@ -245,7 +246,7 @@ constexpr int kRowsAtOnce = 4;  // rows of h in flight
 template <typename T>
 __global__ __launch_bounds__(256) void combine_kernel(RowArgs a) {
   const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t t = item / a.parts, c = item % a.parts * 512 + (threadIdx.x & 63) * 8;
+  const int64_t t = a.first + item / a.parts, c = item % a.parts * 512 + (threadIdx.x & 63) * 8;
   if (t >= a.rows || c >= a.cols) return;
   float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   for (int j0 = 0; j0 < a.k; j0 += kRowsAtOnce) {
@@ -279,7 +280,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void combine_gradient_kernel(RowArgs a) {
   __shared__ float part[4][kRowsAtOnce];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
-  const int64_t t = blockIdx.x;
+  const int64_t t = a.first + blockIdx.x;
   const T* dy = (const T*)a.dy + t * a.ld_dy;
   for (int j0 = 0; j0 < a.k; j0 += kRowsAtOnce) {
     int64_t p[kRowsAtOnce];
@@ -332,10 +333,21 @@ __global__ __launch_bounds__(256) void combine_gradient_kernel(RowArgs a) {
     for (int64_t c = tid * 8; c < a.cols; c += blockDim.x * 8) store_part<T, 8>((T*)a.out + r * a.ld_out, c, a.cols, zero);
 }
 
-#define WSG_BY_TYPE(dtype, what, kernel, grid, block, args)                                          \
-  ((dtype) == WS_OUT_F32    ? launch(what, &kernel<float>, grid, block, 0, stream, args)             \
-   : (dtype) == WS_OUT_BF16 ? launch(what, &kernel<bf16_t>, grid, block, 0, stream, args)            \
-                            : launch(what, &kernel<f16_t>, grid, block, 0, stream, args))
+#define WSG_BY_TYPE(dtype, kernel) \
+  ((dtype) == WS_OUT_F32 ? &kernel<float> : (dtype) == WS_OUT_BF16 ? &kernel<bf16_t> : &kernel<f16_t>)
+
+// Launches kernel(a) for all tokens, each of which has `parts` items; a workgroup of
+// `block` threads takes `items` of them.  What one launch does not hold, in turn.
+ws_status launch_tokens(const char* what, void (*kernel)(RowArgs), int64_t tokens, int64_t parts, int items, int block,
+                        hipStream_t stream, RowArgs a) {
+  const int64_t most = max_workgroups(block) / parts * items;  // whole workgroups
+  for (a.first = 0; a.first < tokens; a.first += most) {
+    const int64_t n = tokens - a.first < most ? tokens - a.first : most;
+    const ws_status s = launch(what, kernel, ceil_div(n * parts, items), block, 0, stream, a);
+    if (s != WS_OK) return s;
+  }
+  return WS_OK;
+}
 
 bool sort_sizes(int64_t tokens, int32_t k, int32_t experts) {
   return tokens >= 0 && k >= 1 && experts >= 1 && experts <= WS_MAX_EXPERTS && tokens <= kMaxDim && tokens * k <= kMaxDim;
@@ -414,10 +426,8 @@ ws_status ws_expert_gather(const ws_matrix* x, int32_t k, int32_t experts, const
   a.k = k;
   a.experts = experts;
   a.parts = (int32_t)ceil_div(a.cols * elem_size(x->dtype), 4096);
-  const int64_t grid = ceil_div(a.x_rows * a.parts, 4);
-  if (grid > kMaxGrid) return WS_ERR_INVALID_ARG;
-  return elem_size(x->dtype) == 4 ? launch("expert_gather", &gather_kernel<float>, grid, 256, 0, stream, a)
-                                  : launch("expert_gather", &gather_kernel<bf16_t>, grid, 256, 0, stream, a);
+  return launch_tokens("expert_gather", elem_size(x->dtype) == 4 ? &gather_kernel<float> : &gather_kernel<bf16_t>, a.x_rows, a.parts, 4,
+                       256, stream, a);
 }
 
 ws_status ws_expert_combine(const ws_matrix* h, int32_t k, const int32_t* place, const float* weights,
@@ -438,9 +448,7 @@ ws_status ws_expert_combine(const ws_matrix* h, int32_t k, const int32_t* place,
   a.ld_out = out->ld;
   a.k = k;
   a.parts = (int32_t)ceil_div(a.cols, 512);
-  const int64_t grid = ceil_div(a.rows * a.parts, 4);
-  if (grid > kMaxGrid) return WS_ERR_INVALID_ARG;
-  return WSG_BY_TYPE(h->dtype, "expert_combine", combine_kernel, grid, 256, a);
+  return launch_tokens("expert_combine", WSG_BY_TYPE(h->dtype, combine_kernel), a.rows, a.parts, 4, 256, stream, a);
 }
 
 ws_status ws_expert_combine_gradient(const ws_matrix* dy, const ws_matrix* h, int32_t k, int32_t experts,
@@ -472,9 +480,8 @@ ws_status ws_expert_combine_gradient(const ws_matrix* dy, const ws_matrix* h, in
   a.ld_out = dh->ld;
   a.k = k;
   a.experts = experts;
-  if (a.rows > kMaxGrid) return WS_ERR_INVALID_ARG;
   const int block = a.cols <= 512 ? 64 : a.cols <= 1024 ? 128 : 256;
-  return WSG_BY_TYPE(dy->dtype, "expert_combine_gradient", combine_gradient_kernel, a.rows, block, a);
+  return launch_tokens("expert_combine_gradient", WSG_BY_TYPE(dy->dtype, combine_gradient_kernel), a.rows, 1, 1, block, stream, a);
 }
 
 }  // extern "C"

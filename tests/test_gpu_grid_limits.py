@@ -36,3 +36,28 @@ def test_product(M, N, K, out):
     for at in (0, max(M, N) // 2 - 77, max(M, N) - 3000):
         part = lambda q, s: q.codes[at:at + 3000].float().double() if s else q.codes.float().double()  # noqa: E731
         check(C.narrow(side, at, 3000), part(A, side == 0), part(B, side == 1), 2.0 ** -9, what="from %d" % at)
+
+
+@pytest.mark.parametrize("T,C", [(5000000, 8), ((1 << 26) + 5000, 1), (9000000, 514)])
+def test_routing_of_many_tokens(T, C):
+    """More tokens than a launch of a workgroup for each, or for four of them, holds."""
+    experts = pytest.importorskip("paper_2506_11209_amd.experts")
+    log("case many tokens %d x %d" % (T, C))
+    E = 3
+    g = torch.Generator(device="cuda").manual_seed(T)
+    ids = torch.randint(-1, E, (T, 1), generator=g, device="cuda", dtype=torch.int32)
+    r = experts.sort(ids, E)
+    n, place = int(r.offsets[-1]), r.place.flatten().long()
+    there = place >= 0
+    assert n == int(there.sum()) and torch.equal(there, ids.flatten() >= 0)
+    x = torch.randn(T, C, generator=g, device="cuda").bfloat16()
+    w = torch.randint(1, 5, (T, 1), generator=g, device="cuda").float()
+    xs = experts.gather(x, r)
+    assert torch.equal(xs[place[there]], x[there]) and (xs[n:] == 0).all()
+    y = experts.combine(xs, r, w)
+    scaled = (x.float() * w).bfloat16()
+    assert torch.equal(y[there], scaled[there]) and (y[~there] == 0).all()
+    dh, dw = experts.combine_gradient(x, xs, r, w)
+    assert torch.equal(dh[place[there]], scaled[there]) and (dh[n:] == 0).all()
+    want = torch.where(there, x.double().square().sum(1), 0.0)
+    assert ((dw.flatten().double() - want).abs() <= (C + 1) * 2.0 ** -24 * want).all()
