@@ -154,7 +154,6 @@ inline int64_t group_tiles(int64_t rows, int64_t groups, int size, bool outside)
 }
 
 constexpr int64_t kMaxDim = 1ll << 30;
-constexpr int64_t kMaxGrid = (1ll << 32) / 1024 - 1;
 // Workgroups of `block` threads in one launch: the runtime counts threads of a dimension in 32 bits.
 constexpr int64_t max_workgroups(int block) { return ((1ll << 32) - 1) / block; }
 

@@ -275,16 +275,25 @@ ws_status run_rows(const QuantArgs& in, hipStream_t stream) {
   // shallow ones spread few rows over the CUs (rows x columns below one round
   // of deep ones).
   const bool deep = ceil_div(a.rows, 32) * a.col_tiles >= 1024;
-  const int64_t grid = ceil_div(a.rows, deep ? 32 : 4) * a.col_tiles;
-  if (grid > kMaxGrid) return WS_ERR_INVALID_ARG;
-  return deep ? launch("quantize_rows", &quantize_rows_kernel<T, 8>, grid, 256, 0, stream, a)
-              : launch("quantize_rows", &quantize_rows_kernel<T, 1>, grid, 256, 0, stream, a);
+  const int depth = deep ? 32 : 4;
+  const auto kernel = deep ? &quantize_rows_kernel<T, 8> : &quantize_rows_kernel<T, 1>;
+  const int64_t most = max_workgroups(256) / a.col_tiles * depth;  // rows of one launch: any width has some
+  for (int64_t left = a.rows; left > 0; left -= most) {
+    a.rows = left < most ? left : most;
+    const ws_status s = launch("quantize_rows", kernel, ceil_div(a.rows, depth) * a.col_tiles, 256, 0, stream, a);
+    if (s != WS_OK) return s;
+    if (a.index) a.index += most;
+    else a.x = (const T*)a.x + most * a.ld;
+    a.codes += most * a.ld_codes;
+    a.scales += most;
+  }
+  return WS_OK;
 }
 
 template <bool WEIGHT>
 ws_status run_tiles(const QuantArgs& a, int32_t dtype, int64_t batch, hipStream_t stream) {
   const int64_t grid = a.row_tiles * a.col_tiles;
-  if (grid > kMaxGrid || grid * batch > kMaxGrid) return WS_ERR_INVALID_ARG;
+  if (grid > max_workgroups(256) || grid * batch > max_workgroups(256)) return WS_ERR_INVALID_ARG;
   switch (dtype) {
     case WS_OUT_F32: return launch("quantize_tile", &quantize_tile_kernel<float, WEIGHT>, grid * batch, 256, 0, stream, a);
     case WS_OUT_BF16: return launch("quantize_tile", &quantize_tile_kernel<bf16_t, WEIGHT>, grid * batch, 256, 0, stream, a);

@@ -61,3 +61,24 @@ def test_routing_of_many_tokens(T, C):
     assert torch.equal(dh[place[there]], scaled[there]) and (dh[n:] == 0).all()
     want = torch.where(there, x.double().square().sum(1), 0.0)
     assert ((dw.flatten().double() - want).abs() <= (C + 1) * 2.0 ** -24 * want).all()
+
+
+@pytest.mark.parametrize("gathered", (False, True))
+def test_quantize_many_rows(gathered):
+    """More rows than one launch holds, 32 a workgroup: the same as a part of them by
+    itself."""
+    R, C = (1 << 29) + 70000, 16
+    log("case quantize %d x %d %s" % (R, C, gathered))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(1000 if gathered else R, C, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    index = torch.randint(-1, 1000, (R,), generator=g, device="cuda", dtype=torch.int32) if gathered else None
+    q = fp8.Fp8Matrix.empty(R, C)
+    q.codes.view(torch.uint8).fill_(0x7f)
+    q.scales.view(torch.uint8).fill_(0xff)
+    assert fp8.quantize_rows(x, index=index, out=q) is q
+    assert not (q.codes.view(torch.uint8) == 0x7f).any() and not (q.scales.view(torch.uint8) == 0xff).any()  # all of it is written
+    for at in (0, (1 << 29) - 33000, R - 70000):
+        part = slice(at, at + 70000)
+        want = fp8.quantize_rows(x, index=index[part].contiguous()) if gathered else fp8.quantize_rows(x[part])
+        assert torch.equal(q.codes[part].view(torch.uint8), want.codes.view(torch.uint8))
+        assert torch.equal(q.scales[:, part].view(torch.uint8), want.scales.view(torch.uint8))
