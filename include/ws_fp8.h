@@ -96,11 +96,11 @@ int64_t ws_fp8_padded_blocks(int64_t rows, int32_t groups);
 ws_status ws_fp8_quantize_weight(const ws_matrix* w, const ws_fp8_matrix* out,
                                  const ws_fp8_matrix* out_transposed, hipStream_t stream);
 
-/* A launch of a product: its tile and the stages of its ring of blocks of 128
- * columns in LDS (0: operands go straight to registers), and the rows of the
- * result it computes. */
+/* A part of a product: the tile it is computed in and the stages of its ring of
+ * blocks of 128 columns in LDS (0: operands go straight to registers), the launch
+ * that computes it (0, or 1 for a second one behind it), and the rows of the result. */
 typedef struct {
-  int32_t tile_m, tile_n, stages;
+  int32_t tile_m, tile_n, stages, launch;
   int64_t rows;
 } ws_fp8_kernel_info;
 

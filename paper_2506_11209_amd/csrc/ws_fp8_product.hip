@@ -48,7 +48,8 @@ struct ProductArgs {
   int64_t depth_rows;  // kDepthGroups: rows that the groups cut
   int64_t tiles_m, tiles_n;
   int32_t tile_groups;  // workgroups that take tiles of a tile kernel; those behind them
-  int64_t rest_end;     // take rows M .. rest_end - 1, 16 x 16 each (dense products)
+  int32_t rest_rows;    // take rows M .. rest_end - 1, rest_rows x 16 each (dense products)
+  int64_t rest_end;
 };
 
 // What one workgroup computes: rows m0 .. m_end - 1 (at most a tile) of its
@@ -196,13 +197,23 @@ __device__ __forceinline__ bf16x8_t widen(int lo, int hi, float scale) {
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// acc += A's 16 rows times B's 16 rows, where the sum is, and two wait states after
+// what widened the operands: the compiler's own form leaves sums on their way in
+// registers that it uses again right behind a product.
+__device__ __forceinline__ void multiply_in_place(f32x4_t& acc, const bf16x8_t& fa, const bf16x8_t& fb) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(fb), "v"(fa));
+#endif
+}
+
 // -- few rows --------------------------------------------------------------------
 
 // A workgroup computes 16 MT rows of 16 columns; its waves share out the blocks
 // of the contraction and add up their parts through LDS in a fixed order.
 // Operands go from memory straight to registers, U blocks at a time.  For few
 // rows: bound by reading B once (1 x 8192 x 8192: 13 to 15 us, 5 TB/s).
-template <int MT, int U, bool WIDE, bool AGPR = false>
+// IN_TILE: more than 16 rows inside a tile kernel.
+template <int MT, int U, bool WIDE, bool AGPR = false, bool IN_TILE = false>
 __device__ __forceinline__ void direct_part(const ProductArgs& a, const Part& p, float* lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int waves = blockDim.x >> 6, r = lane & 15, g = lane >> 4;
@@ -235,9 +246,11 @@ __device__ __forceinline__ void direct_part(const ProductArgs& a, const Part& p,
         for (int h = 0; h < 2; ++h)
           for (int q = 0; q < 4; q += 2) {
             const bf16x8_t wb = widen(vb[u][h][q], vb[u][h][q + 1], scale_value(sbv[u]));
-            for (int i = 0; i < MT; ++i)
-              acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                  wb, widen(va[u][i][h][q], va[u][i][h][q + 1], scale_value(sav[u][i])), acc[i], 0, 0, 0);
+            for (int i = 0; i < MT; ++i) {
+              const bf16x8_t wa = widen(va[u][i][h][q], va[u][i][h][q + 1], scale_value(sav[u][i]));
+              if constexpr (IN_TILE) multiply_in_place(acc[i], wa, wb);
+              else acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, wa, acc[i], 0, 0, 0);
+            }
           }
         continue;
       }
@@ -324,6 +337,8 @@ struct TileShape {
   // One wave a SIMD with sums in accumulation registers, or more with all in the others.
   static constexpr int kWaves = WM * WN > 16 || STAGES * kStage > 80 * 1024 ? 1 : 2;
   static constexpr bool kAgpr = WM * WN > 16;
+  // Last rows of a product beside the tiles, more than 16 of them to a workgroup.
+  static constexpr bool kDeepRest = STAGES == 2 && kWaves == 2;
   // Rows of products before a block's meeting point.  Few: the loads of the block
   // after next, which keep the address unit busy for half a block of 256 x 256,
   // spread over more products behind it.
@@ -545,7 +560,11 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
   if constexpr (MODE == kDense)
     if (blockIdx.x >= (uint32_t)a.tile_groups) {
       const uint32_t t = blockIdx.x - a.tile_groups, across = (uint32_t)((a.N + 15) / 16);
-      const Part p{a.A, a.B, a.sa, a.sb, a.M + t / across * 16, a.rest_end, t % across * 16, a.K, 0, 0, false};
+      const Part p{a.A, a.B, a.sa, a.sb, a.M + (int64_t)(t / across) * a.rest_rows, a.rest_end, t % across * 16, a.K, 0, 0, false};
+      if constexpr (Shape::kDeepRest) {
+        if (a.rest_rows == 64) return direct_part<4, 2, WIDE, false, true>(a, p, (float*)smem);
+        if (a.rest_rows == 32) return direct_part<2, 4, WIDE, false, true>(a, p, (float*)smem);
+      }
       return direct_part<1, 4, WIDE, Shape::kWaves == 1>(a, p, (float*)smem);
     }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -850,7 +869,7 @@ ws_status run_tiles(ProductArgs a, hipStream_t stream) {
   if (tiles > kMaxTiles) return WS_ERR_INVALID_ARG;
   const int64_t most = (int64_t)compute_units() * Shape::kWaves;
   a.tile_groups = (int32_t)(tiles < most ? tiles : most);
-  const int64_t rest = a.rest_end > a.M ? ceil_div(a.rest_end - a.M, 16) * ceil_div(a.N, 16) : 0;
+  const int64_t rest = a.rest_end > a.M ? ceil_div(a.rest_end - a.M, a.rest_rows) * ceil_div(a.N, 16) : 0;
   const auto kernel = &tile_kernel<WM, WN, STAGES, MODE, WIDE>;
   static std::atomic<uint64_t> allowed;  // devices on which the kernel may use this much LDS
   int dev = 0;
@@ -966,11 +985,12 @@ ws_status run_choice(Choice c, const ProductArgs& a, hipStream_t stream) {
 }
 
 // One or two parts of a product: the first `split` rows by choice[0], the rest
-// by choice[1].  No part: no kernel's launch holds it.
+// by choice[1], `together` in one launch.  No part: no kernel's launch holds it.
 struct Plan {
   int count;
   int64_t split;
   Choice choice[2];
+  bool together;
 };
 
 Plan plan_product(int mode, int64_t M, int64_t N, int64_t K, int64_t groups, bool wide) {
@@ -984,7 +1004,7 @@ Plan plan_product(int mode, int64_t M, int64_t N, int64_t K, int64_t groups, boo
     w.K = ceil_div(ceil_div(K, groups), kBlock) * kBlock;
   }
   float cost;
-  Plan plan{1, M, {choose(w, mode, M, groups, wide, &cost), kDirect16}};
+  Plan plan{1, M, {choose(w, mode, M, groups, wide, &cost), kDirect16}, false};
   if (isinf(cost)) plan.count = 0;
   if (mode == kDense && M > kBlock && M % kBlock != 0) {
     // The last rows by themselves, where they would start tiles of their own that a
@@ -996,7 +1016,18 @@ Plan plan_product(int mode, int64_t M, int64_t N, int64_t K, int64_t groups, boo
     rest.rows = (double)(M % kBlock);
     const Choice cm = choose(top, mode, M / kBlock * kBlock, groups, wide, &main_cost);
     const Choice cr = choose(rest, mode, M % kBlock, groups, wide, &rest_cost);
-    if (main_cost + rest_cost < 0.95f * cost) plan = Plan{2, M / kBlock * kBlock, {cm, cr}};
+    if (main_cost + rest_cost < 0.95f * cost) {
+      // The last rows in the launch of the tiles, by workgroups of the direct kernel's
+      // rows: beside the tiles where a CU has room for two (4216 x 1000 x 4100 in 32
+      // bits: 55 us, so 45), else behind them, where they are few (4104 x 1000 x 4100:
+      // 33.0 us, so 31.8, but 4160 x 4096 x 4096: 68, by itself with 64 rows a
+      // workgroup, 75).
+      const bool beside = cm == kTile128 || cm == kTile64;
+      const ws_fp8_kernel_info last = kernel_of(cr, wide);
+      const bool together = cm >= kTile256 && last.stages == 0 && (beside || M % kBlock <= 16) &&
+                            ceil_div(M % kBlock, last.tile_m) * ceil_div(N, 16) <= max_workgroups(256) - 2 * compute_units();
+      plan = Plan{2, M / kBlock * kBlock, {cm, cr}, together};
+    }
   }
   return plan;
 }
@@ -1009,14 +1040,9 @@ ws_status run_product(const ProductArgs& a, hipStream_t stream) {
   ProductArgs m = a, r = a;
   m.M = plan.split;
   r.M = a.M - m.M;
-  // The last rows in the launch of the tiles, by workgroups of 16 rows: beside the
-  // tiles where a CU has room for two (4216 x 1000 x 4100 in 32 bits: 55 us, so 45),
-  // else behind them, where they are few (4104 x 1000 x 4100: 33.0 us, so 31.8, but
-  // 4160 x 4096 x 4096: 68, by itself with 64 rows a workgroup, 75).
-  const bool beside = plan.choice[0] == kTile128 || plan.choice[0] == kTile64;
-  if (plan.choice[0] >= kTile256 && plan.choice[1] < kTile256 && (beside || r.M <= 16) &&
-      ceil_div(r.M, 16) * ceil_div(a.N, 16) <= max_workgroups(256) - 2 * compute_units()) {
+  if (plan.together) {
     m.rest_end = a.M;
+    m.rest_rows = kernel_of(plan.choice[1], false).tile_m;
     return run_choice<MODE>(plan.choice[0], m, stream);
   }
   const int size = elem_size(a.dtype);
@@ -1090,6 +1116,7 @@ ws_status ws_fp8_plan(int64_t M, int64_t N, int64_t K, int32_t out_dtype, int32_
   for (int i = 0; i < plan.count; ++i) {
     ws_fp8_kernel_info k = kernel_of(plan.choice[i], wide);
     k.rows = i == 0 ? plan.split : M - plan.split;
+    k.launch = plan.together ? 0 : i;
     out[i] = k;
   }
   *count = plan.count;

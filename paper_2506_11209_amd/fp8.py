@@ -50,7 +50,8 @@ class ws_matrix(ctypes.Structure):
 
 
 class ws_fp8_kernel_info(ctypes.Structure):
-    _fields_ = [("tile_m", ctypes.c_int32), ("tile_n", ctypes.c_int32), ("stages", ctypes.c_int32), ("rows", ctypes.c_int64)]
+    _fields_ = [("tile_m", ctypes.c_int32), ("tile_n", ctypes.c_int32), ("stages", ctypes.c_int32), ("launch", ctypes.c_int32),
+                ("rows", ctypes.c_int64)]
 
 
 _lib = _w.library()
@@ -318,13 +319,13 @@ def _old(C0, beta: float, C):
 
 
 def plan(M: int, N: int, K: int, out_dtype: str = "bf16", groups: int = 0, depth: bool = False) -> list:
-    """[(tile_m, tile_n, stages, rows)]: the parts of product (groups 0), of
+    """[(tile_m, tile_n, stages, rows, launch)]: the parts of product (groups 0), of
     grouped_product, or with depth of grouped_gradient over K rows."""
     out, n = (ws_fp8_kernel_info * 2)(), _i32(0)
     if out_dtype not in _DTYPES:
         raise ValueError("out_dtype is one of %s, got %r" % (sorted(_DTYPES), out_dtype))
     _check(_lib.ws_fp8_plan(M, N, K, _CODES[_DTYPES[out_dtype]], groups, int(depth), out, ctypes.byref(n)), "ws_fp8_plan")
-    return [(k.tile_m, k.tile_n, k.stages, k.rows) for k in out[: n.value]]
+    return [(k.tile_m, k.tile_n, k.stages, k.rows, k.launch) for k in out[: n.value]]
 
 
 def product(A: Fp8Matrix, B: Fp8Matrix, C=None, out_dtype: str = "bf16", alpha: float = 1.0, beta: float = 0.0, C0=None,

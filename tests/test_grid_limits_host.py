@@ -23,7 +23,7 @@ def launched(M, N, tile_m, tile_n, stages, groups=0, depth=False):
 def test_a_kernel_that_fits(M, N, K, groups, depth, out):
     parts = fp8.plan(M, N, K, out, groups, depth)
     assert sum(p[3] for p in parts) == M
-    for tile_m, tile_n, stages, rows in parts:
+    for tile_m, tile_n, stages, rows in (p[:4] for p in parts):
         assert launched(rows, N, tile_m, tile_n, stages, groups, depth) <= (TILES if stages else WORKGROUPS)
 
 
