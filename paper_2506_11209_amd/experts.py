@@ -65,7 +65,7 @@ def sort(ids, experts: int, stream=None) -> Routes:
     if not ids.is_contiguous() or ids.shape[1] < 1:
         raise ValueError("ids: expected contiguous tokens x k, k at least 1, got %s of strides %s" % (tuple(ids.shape), ids.stride()))
     tokens, k = ids.shape
-    need = _lib.ws_expert_sort_workspace(tokens, k, experts)
+    need = _lib.ws_expert_sort_workspace(tokens, k, experts) if 0 < experts <= MAX_EXPERTS else -1
     if need < 0:
         raise ValueError("sort: 1 to %d experts, got %r, and at most 2^30 choices, got %d" % (MAX_EXPERTS, experts, ids.numel()))
     if _elsewhere(ids, stream):

@@ -34,6 +34,7 @@ from . import wsgemm as _w
 
 BLOCK = 128
 E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+_MOST = 1 << 30  # rows or columns that the library takes; counts have to fit before ctypes cuts them
 _DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 _CODES = {torch.float32: _w.WS_OUT_F32, torch.bfloat16: _w.WS_OUT_BF16, torch.float16: _w.WS_OUT_F16}
 
@@ -246,6 +247,8 @@ def quantize_rows(x, index=None, out: Fp8Matrix | None = None, stream=None) -> F
 
 def padded_rows(rows: int, groups: int) -> int:
     """Columns of the transposed form of ``rows`` rows in ``groups`` groups."""
+    if not (0 <= rows <= _MOST and 0 <= groups <= _MOST):
+        raise ValueError("padded_rows: %r rows in %r groups" % (rows, groups))
     return BLOCK * _lib.ws_fp8_padded_blocks(rows, groups)
 
 
@@ -324,6 +327,8 @@ def plan(M: int, N: int, K: int, out_dtype: str = "bf16", groups: int = 0, depth
     out, n = (ws_fp8_kernel_info * 2)(), _i32(0)
     if out_dtype not in _DTYPES:
         raise ValueError("out_dtype is one of %s, got %r" % (sorted(_DTYPES), out_dtype))
+    if not all(0 <= n <= _MOST for n in (M, N, K, groups)):
+        raise _w.WsGemmError("ws_fp8_plan", _w.WS_ERR_INVALID_ARG)
     _check(_lib.ws_fp8_plan(M, N, K, _CODES[_DTYPES[out_dtype]], groups, int(depth), out, ctypes.byref(n)), "ws_fp8_plan")
     return [(k.tile_m, k.tile_n, k.stages, k.rows, k.launch) for k in out[: n.value]]
 
