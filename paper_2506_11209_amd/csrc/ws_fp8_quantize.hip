@@ -331,7 +331,7 @@ void set_transposed(QuantArgs* a, const ws_fp8_matrix* t) {
 // x against a row form of it.
 bool rows_fit(const ws_matrix* x, const int32_t* index, const ws_fp8_matrix* out) {
   return valid(x) && valid(out) && x->batch <= 1 && out->batch <= 1 && out->block_rows == 1 && out->cols == x->cols &&
-         (index || out->rows == x->rows);
+         (index || out->rows == x->rows) && (uintptr_t)index % 4 == 0;
 }
 
 }  // namespace
@@ -360,7 +360,7 @@ ws_status ws_fp8_quantize_rows(const ws_matrix* x, const int32_t* index, const w
 ws_status ws_fp8_quantize_both(const ws_matrix* x, const int32_t* index, int32_t groups, const int32_t* offsets,
                                const ws_fp8_matrix* out_rows, const ws_fp8_matrix* out_columns, hipStream_t stream) {
   if (!rows_fit(x, index, out_rows) || !valid(out_columns) || out_columns->batch > 1 || out_columns->block_rows != 1 ||
-      out_columns->rows != out_rows->cols || groups < 0 || groups > (1 << 20) || (groups > 0 && !offsets))
+      out_columns->rows != out_rows->cols || groups < 0 || groups > (1 << 20) || (groups > 0 && (!offsets || (uintptr_t)offsets % 4)))
     return WS_ERR_INVALID_ARG;
   const int64_t padded = ws_fp8_padded_blocks(out_rows->rows, groups);
   if (out_columns->cols != (groups ? padded * kBlock : out_rows->rows)) return WS_ERR_INVALID_ARG;

@@ -71,3 +71,11 @@ def test_an_empty_batch_of_weights_does_nothing():
     assert lib.ws_fp8_quantize_weight(none, q, t, None) == w.WS_OK
     assert lib.ws_fp8_quantize_weight(none, coded(64, 256, block_rows=128), None, None) == INVALID
     assert lib.ws_fp8_quantize_weight(matrix(64, 256), q, None, None) == INVALID
+
+
+def test_misaligned_indices():
+    x, q, t = matrix(64, 256), coded(64, 256), coded(256, 64)
+    for at in (AT + 1, AT + 2):
+        assert lib.ws_fp8_quantize_rows(x, at, q, None) == INVALID
+        assert lib.ws_fp8_quantize_both(x, at, 0, None, q, t, None) == INVALID
+        assert lib.ws_fp8_quantize_both(x, None, 3, at, q, coded(256, 384), None) == INVALID
