@@ -49,7 +49,7 @@ typedef struct {
                              at least ceil(rows / block_rows) */
   int32_t block_rows;     /* rows that share a scale: 1 or 128 */
   int32_t batch;
-  int64_t stride_codes;   /* a multiple of 16 */
+  int64_t stride_codes;   /* a multiple of 16; matrices do not overlap */
   int64_t stride_scales;
 } ws_fp8_matrix;
 
@@ -61,7 +61,7 @@ typedef struct {
   int64_t rows, cols, ld;
   int32_t dtype;
   int32_t batch;
-  int64_t stride;         /* elements between matrices of a batch */
+  int64_t stride;         /* elements between matrices of a batch, which do not overlap */
 } ws_matrix;
 
 /* Scales of 1 x 128.  out has x's columns and out->rows rows: row r is row

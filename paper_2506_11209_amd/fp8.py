@@ -141,9 +141,10 @@ def _matrix(t, what: str, dims=(2,), device=None) -> ws_matrix:
             raise ValueError("%s: columns have to lie next to each other and rows may not overlap, got strides %s" % (what, stride))
         return ws_matrix(t.data_ptr(), rows, cols, ld, code, 1, 0)
     batch, rows, cols = shape
-    if cols > 1 and stride[2] != 1 or rows > 1 and stride[1] < cols:
-        raise ValueError("%s: columns have to lie next to each other and rows may not overlap, got strides %s" % (what, stride))
-    return ws_matrix(t.data_ptr(), rows, cols, stride[1] if rows > 1 else cols, code, batch, stride[0])
+    ld = stride[1] if rows > 1 else cols
+    if cols > 1 and stride[2] != 1 or ld < cols or (batch > 1 and rows > 0 and stride[0] < (rows - 1) * ld + cols):
+        raise ValueError("%s: columns have to lie next to each other, rows and matrices may not overlap, got strides %s" % (what, stride))
+    return ws_matrix(t.data_ptr(), rows, cols, ld, code, batch, stride[0])
 
 
 def _new_matrix(rows: int, cols: int, dtype: torch.dtype, device):
@@ -185,9 +186,13 @@ class Fp8Matrix:
         ld = cs[-2] if rows > 1 and shape[-1] > 0 else _up(shape[-1], 16)
         if ld % 16 or codes.data_ptr() % 16 or (batch > 1 and cs[0] % 16):
             raise ValueError("codes: rows have to start at multiples of 16 bytes, got strides %s" % (cs,))
+        ld_scales = ss[-2] if blocks > 1 else per
+        if rows > 0 and cols > 0 and (ld < _up(cols, 16) or ld_scales < per or (batch > 1 and (
+                cs[0] < (rows - 1) * ld + _up(cols, 16) or ss[0] < (blocks - 1) * ld_scales + per))):
+            raise ValueError("rows and matrices may not overlap, got strides %s of codes and %s of scales" % (cs, ss))
         self.codes, self.scales, self.rows, self.cols, self.block_rows = codes, scales, rows, cols, block_rows
         self._desc = ws_fp8_matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld,
-                                   ss[-2] if blocks > 1 else per, block_rows, batch,
+                                   ld_scales, block_rows, batch,
                                    cs[0] if len(shape) == 3 else 0, ss[0] if len(shape) == 3 else 0)
 
     @property
