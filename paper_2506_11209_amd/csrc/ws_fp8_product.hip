@@ -109,9 +109,12 @@ __device__ __forceinline__ bool find_part(const ProductArgs& a, int64_t tm, int6
   return true;
 }
 
-// Up to so many groups are put in order of their depths (64 groups of 512 x 512: 29.8
-// us in their own order, 31.5 in that of their depths).
-constexpr int kRanked = 32;
+// Up to so many groups, one for each lane of a wave, are put in order of their depths.
+// 16384 rows, on average over six draws of the depths, us in the groups' own order and
+// in that of their depths: 1024 x 2048 in 16 groups 97.6 and 89.2, in 32 134.8 and
+// 133.2, in 64 217 and 212; 512 x 512, where the order costs as much as it saves, 28.3
+// and 25.2, 25.9 and 26.1, 29.6 and 30.6.
+constexpr int kRanked = 64;
 
 // How many groups are deeper than this lane's, or as deep and before it; -1 for a lane
 // without a group.
@@ -1019,9 +1022,9 @@ Plan plan_product(int mode, int64_t M, int64_t N, int64_t K, int64_t groups, boo
     if (main_cost + rest_cost < 0.95f * cost) {
       // The last rows in the launch of the tiles, by workgroups of the direct kernel's
       // rows: beside the tiles where a CU has room for two (4216 x 1000 x 4100 in 32
-      // bits: 55 us, so 45), else behind them, where they are few (4104 x 1000 x 4100:
-      // 33.0 us, so 31.8, but 4160 x 4096 x 4096: 68, by itself with 64 rows a
-      // workgroup, 75).
+      // bits: 41 us, in a launch of their own 51), else behind them, where they are few
+      // (4104 x 1000 x 4100 in bf16: 30.3 and 31.6; but 4160 x 4096 x 4096 in bf16,
+      // 16 rows a workgroup: 73, in a launch of their own 66).
       const bool beside = cm == kTile128 || cm == kTile64;
       const ws_fp8_kernel_info last = kernel_of(cr, wide);
       const bool together = cm >= kTile256 && last.stages == 0 && (beside || M % kBlock <= 16) &&

@@ -74,3 +74,21 @@ def test_depth_groups(case):
         n = ref.up(hi - lo, 128)
         same(got[g], a[:, at:at + n].contiguous(), b[:, at:at + n].contiguous(), "group %d" % g)
         at += n
+
+
+@pytest.mark.parametrize("G", (1, 2, 31, 32, 33, 63, 64, 65, 130))
+def test_groups_around_a_wave(G):
+    """As many groups as a wave has lanes, one fewer and one more, of like and unlike
+    depth: by the order of their depths up to 64, else by their own."""
+    M, N, R = 1000, 1000, 40 * G + 700
+    log("case exact depth of %d groups" % G)
+    assert all(p[2] > 0 for p in fp8.plan(M, N, R, "f32", G, True))
+    deep = fp8.padded_rows(R, G)
+    A, B = integers(M, deep, 1), integers(N, deep, 2)
+    a, b = value(A), value(B)
+    for offsets in (split(R, G, G), [R // G * g for g in range(G + 1)], [0] * G + [R]):
+        got, at = fp8.grouped_gradient(A, B, R, torch.tensor(offsets, dtype=torch.int32, device="cuda")), 0
+        for g, (lo, hi) in enumerate(ref.segments(offsets, R)):
+            n = ref.up(hi - lo, 128)
+            same(got[g], a[:, at:at + n].contiguous(), b[:, at:at + n].contiguous(), "group %d" % g)
+            at += n
