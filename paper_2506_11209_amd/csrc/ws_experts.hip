@@ -11,8 +11,11 @@ constexpr int kSortWaves = 8;
 constexpr int kSortThreads = 64 * kSortWaves;
 constexpr int kSortSteps = 4;          // steps of 64 slots whose ids a wave loads at once
 constexpr int64_t kSortChunk = kSortSteps * kSortThreads;  // slots of a workgroup
-// Slots that one workgroup sorts by itself (4096: 11.5 us, where two launches of
-// several take 7.5 and one launch more of the caller's time; 1024: 5.1 and 7.4).
+// Slots that one workgroup sorts by itself, where two launches of several take less of
+// the GPU but more of the caller.  us of one workgroup and of several, for 64 experts:
+// calls back to back from Python 8.9 and 13.3 (2048 slots), 11.3 and 13.5 (4096), 15.7
+// and 13.4 (6144); one call waited for 23.1 and 25.5, 27.4 and 25.5, 32.3 and 25.5; in
+// a captured graph 7.1 and 7.1, 11.5 and 7.3, 16.0 and 7.4.
 constexpr int64_t kSortAlone = 4096;
 constexpr int64_t kSortBlocks = 256;   // chunks at the most; beyond, chunks grow
 
