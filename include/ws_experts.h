@@ -38,7 +38,8 @@ ws_status ws_expert_sort(int64_t tokens, int32_t k, int32_t experts, const void*
 
 /* out[place[t][j]] = x[t]: the tokens' rows in sorted order; rows past
  * offsets[experts] are zeros, places out of range are left out.  x and out of one
- * type; out does not overlap x. */
+ * type; out does not overlap x.  place as ws_expert_sort leaves it: below
+ * offsets[experts], no row twice. */
 ws_status ws_expert_gather(const ws_matrix* x, int32_t k, int32_t experts, const int32_t* offsets, const int32_t* place,
                            const ws_matrix* out, hipStream_t stream);
 
@@ -53,7 +54,7 @@ ws_status ws_expert_combine(const ws_matrix* h, int32_t k, const int32_t* place,
  * past offsets[experts] zero, and dweights[t][j] = dot(dy[t], h[place[t][j]])
  * in binary32, 0 for a place out of range.  weights NULL: 1; dweights NULL: not
  * computed (then h may be NULL).  dy, h and dh of one type; dh may not overlap
- * h or dy.  place as ws_expert_sort leaves it: no row twice. */
+ * h or dy.  place as ws_expert_sort leaves it. */
 ws_status ws_expert_combine_gradient(const ws_matrix* dy, const ws_matrix* h, int32_t k, int32_t experts,
                                      const int32_t* offsets, const int32_t* place, const float* weights,
                                      const ws_matrix* dh, float* dweights, hipStream_t stream);

@@ -16,8 +16,9 @@ Codes are torch.float8_e4m3fn, scales torch.float8_e8m0fnu (powers of two) for
 
 Calls enqueue on ``stream`` (default: the current stream of the operands'
 device) and return at once.  Results and work memory made here belong to that
-stream, and tensors handed in are marked as in use by it, so that their memory
-is not given out again before the work is done.  Sizes, types, devices and
+stream; tensors handed in with a ``stream`` are marked as in use by it, so that
+their memory is not given out again before the work is done (on the current
+stream that is the caller's, as for torch's own operations).  Sizes, types, devices and
 strides are checked and raise ValueError, a status of the library raises
 WsGemmError; the contents of codes, scales and offsets are not looked at.
 Nothing here is recorded by autograd: a layer's backward makes the gradients with
@@ -342,7 +343,12 @@ def product(A: Fp8Matrix, B: Fp8Matrix, C=None, out_dtype: str = "bf16", alpha: 
             stream=None):
     """alpha A B^T + beta C0: A is M x K with scales for single rows, B is N x K with
     scales for 1 or 128 rows.  Written to C (M x N; its type counts) or a new
-    tensor of out_dtype ("f32", "bf16", "f16").  C0 may be C."""
+    tensor of out_dtype ("f32", "bf16", "f16").  C0 may be C.
+
+    Results in 32 bits have binary32 sums.  Those in 16 bits come from the 8-bit
+    matrix instruction at twice the rate, whose sums hold fewer bits: 1.5e-5 to
+    5e-5 of the result before it is rounded (see ws_fp8.h); for binary32 sums in
+    16 bits take out_dtype="f32" and round."""
     codes = A.codes
     if _elsewhere(codes, stream):
         with _Call(codes.device, stream, _both(A, B) + [C, C0]):
@@ -359,8 +365,9 @@ def product(A: Fp8Matrix, B: Fp8Matrix, C=None, out_dtype: str = "bf16", alpha: 
 
 
 def grouped_product(A: Fp8Matrix, B: Fp8Matrix, offsets, C=None, out_dtype: str = "bf16", alpha: float = 1.0, stream=None):
-    """Rows offsets[g] .. offsets[g + 1] - 1 of A times B[g]^T; rows in no group
-    become zeros.  offsets: int32 on the device, not decreasing."""
+    """Rows offsets[g] .. offsets[g + 1] - 1 of A times B[g]^T; rows in no group,
+    before the first or after the last, become zeros.  offsets: int32 on the
+    device, not decreasing.  Sums as in product."""
     device = A.codes.device
     if A.batch is not None or B.batch is None or A.cols != B.cols or A.block_rows != 1 or B.codes.device != device:
         raise ValueError("A has to be a single matrix with scales for single rows, B a batch of as many columns on its device")
