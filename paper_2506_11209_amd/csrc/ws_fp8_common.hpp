@@ -75,7 +75,10 @@ __device__ __forceinline__ uint32_t max16(uint32_t x) {
 // leave the rows are cut to them.
 __device__ __forceinline__ void group_rows(const int32_t* offsets, int groups, int64_t rows, int i, int64_t* lo,
                                            int64_t* hi) {
-  int64_t a = i <= groups ? offsets[i] : 0, b = i == groups ? rows : (int64_t)offsets[i < groups ? i + 1 : 0];
+  // both loads at once and for every i; then what they mean at the ends
+  int64_t a = offsets[i < groups ? i : groups], b = offsets[i < groups ? i + 1 : 0];
+  if (i > groups) a = 0;
+  if (i == groups) b = rows;
   a = a < 0 ? 0 : a > rows ? rows : a;
   *lo = a;
   *hi = b < a ? a : b > rows ? rows : b;
