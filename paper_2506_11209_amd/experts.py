@@ -100,9 +100,9 @@ def _weights(weights, routes):
     return weights.data_ptr()
 
 
-def _recorded(out, *inputs) -> bool:
-    """Whether autograd has to know of a call on these inputs."""
-    if not torch.is_grad_enabled() or not any(t is not None and t.requires_grad for t in inputs):
+def _recorded(out) -> bool:
+    """Whether autograd has to know of a call on inputs that require a gradient."""
+    if not torch.is_grad_enabled():
         return False
     if out is not None:
         raise ValueError("out: a result in the caller's memory is not recorded for gradients; call it under torch.no_grad()")
@@ -145,7 +145,7 @@ def gather(x, routes: Routes, out=None, stream=None):
     if _elsewhere(x, stream):
         with _Call(x.device, stream, [x, routes.offsets, routes.place, out]):
             return gather(x, routes, out)
-    if _recorded(out, x):
+    if x.requires_grad and _recorded(out):
         return _Gather.apply(x, routes)
     out, mo = _out(out, "out", routes.token.numel(), m.cols, x)
     _check(_lib.ws_expert_gather(m, k, routes.experts, routes.offsets.data_ptr(), routes.place.data_ptr(), mo,
@@ -163,7 +163,7 @@ def combine(h, routes: Routes, weights=None, out=None, stream=None):
     if _elsewhere(h, stream):
         with _Call(h.device, stream, [h, routes.place, weights, out]):
             return combine(h, routes, weights, out)
-    if _recorded(out, h, weights):
+    if (h.requires_grad or (weights is not None and weights.requires_grad)) and _recorded(out):
         return _Combine.apply(h, weights, routes)
     out, mo = _out(out, "out", tokens, m.cols, h)
     _check(_lib.ws_expert_combine(m, k, routes.place.data_ptr(), w, mo, _raw_stream(h.get_device())), "ws_expert_combine")
