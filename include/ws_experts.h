@@ -23,6 +23,40 @@ extern "C" {
 #endif
 
 #define WS_MAX_EXPERTS 1024
+#define WS_MAX_CHOICES 64
+
+/* Bytes of device memory that ws_expert_choose needs (0: none, then workspace may
+ * be NULL); -1 for sizes that it refuses. */
+int64_t ws_expert_choose_workspace(int64_t tokens, int32_t experts, int32_t k);
+
+/* A router's choice for logits l (tokens x experts), with p its softmax over the
+ * experts:
+ *   ids[t][j]      the token's k largest logits, the largest first, the lowest
+ *                  index first among equals (both zeros are equal, NaN is the
+ *                  largest); a logit of -inf is not chosen: -1 where none is left
+ *   weights[t][j]  softmax over the token's choices, 0 for a place without one
+ *   counts[e]      choices of expert e; counts[experts]: tokens with a choice
+ *   loss           experts * sum over e of counts[e] / choices * mean of p[t][e],
+ *                  the mean over tokens with a choice; 0 without any: 1 where the
+ *                  experts are chosen alike, up to experts where one is
+ * A NaN among a token's logits makes its weights, and so the loss, NaN; so does
+ * +inf.  k up to experts and WS_MAX_CHOICES, experts up to WS_MAX_EXPERTS, at most
+ * 2^30 choices.  weights and ids: tokens * k, dense; counts: experts + 1; all
+ * 4-byte aligned.  Exponentials and sums in binary32 or more; results do not depend
+ * on anything but logits and sizes.  The workspace (4-byte aligned) is written
+ * before it is read; calls on other streams need another. */
+ws_status ws_expert_choose(const ws_matrix* logits, int32_t k, float* weights, int32_t* ids, int32_t* counts,
+                           float* loss, void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/* Its gradient, from those of weights (dense; NULL: zeros, then weights and ids may
+ * be NULL) and of loss (one value; NULL: zero), counts taken for constants:
+ *   dlogits[t][e] = w[j] (dw[j] - sum over i of w[i] dw[i])  where e is choice j of t
+ *     + dloss experts / (choices tokens_with_one) p[t][e] (counts[e] - sum over i of counts[i] p[t][i])
+ * rounded once to the type of logits; dlogits may be logits.  weights, ids and counts
+ * as ws_expert_choose leaves them; an id out of range counts as none. */
+ws_status ws_expert_choose_gradient(const ws_matrix* logits, int32_t k, const float* dweights, const float* dloss,
+                                    const float* weights, const int32_t* ids, const int32_t* counts,
+                                    const ws_matrix* dlogits, hipStream_t stream);
 
 /* Bytes of device memory that ws_expert_sort needs (0: none, then workspace may
  * be NULL); -1 for sizes that it refuses. */

@@ -1,0 +1,523 @@
+// The router's choice of experts, its balance loss and its gradient (definitions:
+// ws_experts.h).
+#include <math.h>
+
+#include "ws_experts.h"
+#include "ws_fp8_common.hpp"
+
+namespace wsg {
+namespace {
+
+struct ChooseArgs {
+  const void* logits;
+  void* dlogits;
+  float *weights, *loss, *sums;  // sums: blocks x (experts + 1), of probabilities; null for one workgroup alone
+  int32_t *ids, *counts, *parts;  // parts: blocks x (experts + 1), counts
+  const float *dweights, *dloss;
+  int64_t tokens, ld, ld_d;
+  int32_t experts, k, blocks;
+};
+
+template <int CTRL>
+__device__ __forceinline__ float rotated(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+// Sum over L lanes (16 or 64), the same bits in all of them.
+template <int L>
+__device__ __forceinline__ float sum_lanes(float x) {
+  x += rotated<0x128>(x);  // row_ror:8
+  x += rotated<0x124>(x);
+  x += rotated<0x122>(x);
+  x += rotated<0x121>(x);
+  if constexpr (L == 64) {
+    x += __shfl_xor(x, 16);
+    x += __shfl_xor(x, 32);
+  }
+  return x;
+}
+template <int L>
+__device__ __forceinline__ float largest(float x) {
+  x = fmaxf(x, rotated<0x128>(x));
+  x = fmaxf(x, rotated<0x124>(x));
+  x = fmaxf(x, rotated<0x122>(x));
+  x = fmaxf(x, rotated<0x121>(x));
+  if constexpr (L == 64) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    x = fmaxf(x, __shfl_xor(x, 32));
+  }
+  return x;
+}
+template <int L>
+__device__ __forceinline__ uint32_t max_lanes(uint32_t x) {
+  x = max16(x);
+  if constexpr (L == 64) {
+    x = max(x, (uint32_t)__shfl_xor((int)x, 16));
+    x = max(x, (uint32_t)__shfl_xor((int)x, 32));
+  }
+  return x;
+}
+
+// Logits in the order in which they are chosen: larger is earlier, NaN first of all,
+// both zeros the same, 0 for -inf, which is not chosen.
+__device__ __forceinline__ uint32_t rank_of(float x) {
+  const uint32_t b = __float_as_uint(x + 0.0f);
+  const uint32_t key = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+  return x != x ? 0xffffffffu : x == -INFINITY ? 0u : key;
+}
+__device__ __forceinline__ float logit_of(uint32_t key) {
+  return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+
+// A row of up to L V logits on L lanes: lane i holds elements W i .. W i + W - 1 of
+// every W L, W as many as 16 bytes hold.
+template <typename T, int L, int V>
+struct Row {
+  static constexpr int kWide = 16 / (int)sizeof(T), W = V < kWide ? V : kWide;
+  static __device__ __forceinline__ int element(int sub, int v) { return v / W * (L * W) + sub * W + v % W; }
+  static __device__ __forceinline__ void load(const T* row, int sub, int n, T (&x)[V]) {
+#pragma unroll
+    for (int v = 0; v < V; v += W) {
+      const int e = element(sub, v);
+      if constexpr (W * sizeof(T) >= 4) {
+        if (e + W <= n) {
+          load_n<T, W>(row + e, x + v);
+          continue;
+        }
+      }
+#pragma unroll
+      for (int w = 0; w < W; ++w) x[v + w] = e + w < n ? row[e + w] : from_f32<T>(-INFINITY);
+    }
+  }
+  static __device__ __forceinline__ void store(T* row, int sub, int n, const T (&x)[V]) {
+#pragma unroll
+    for (int v = 0; v < V; v += W) {
+      const int e = element(sub, v);
+      if constexpr (W * sizeof(T) >= 4) {
+        if (e + W <= n) {
+          store_n<T, W>(row + e, x + v);
+          continue;
+        }
+      }
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+        if (e + w < n) row[e + w] = x[v + w];
+    }
+  }
+};
+
+// Waves of a workgroup: the sums of a wave's tokens pass LDS.
+template <int L>
+constexpr int choose_waves() { return L == 16 ? 16 : 8; }
+
+// What the sums of probabilities and the counts give; by one workgroup, S_e and c_e in LDS.
+__device__ __forceinline__ void finish(const ChooseArgs& a, const float* sums, const int32_t* counts, double* scratch) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
+  double dot = 0.0, all = 0.0;
+  for (int e = tid; e < a.experts; e += blockDim.x) {
+    dot += (double)counts[e] * (double)sums[e];
+    all += (double)counts[e];
+    a.counts[e] = counts[e];
+  }
+  for (int d = 32; d; d /= 2) {
+    dot += __shfl_xor(dot, d);
+    all += __shfl_xor(all, d);
+  }
+  if (lane == 0) {
+    scratch[2 * wave] = dot;
+    scratch[2 * wave + 1] = all;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < waves; ++w) {
+      dot += scratch[2 * w];
+      all += scratch[2 * w + 1];
+    }
+    const double n = (double)counts[a.experts];
+    a.counts[a.experts] = counts[a.experts];
+    *a.loss = n > 0.0 ? (float)((double)a.experts * dot / (all * n)) : 0.0f;
+  }
+}
+
+// L lanes take a token: its row stays in registers, the choices are k searches for the
+// largest (and lowest) left, the first of which is the softmax's maximum too.  Sums of
+// probabilities and counts stay in the lanes over a workgroup's tokens and pass LDS at
+// the end, in a fixed order.  ALONE: one workgroup.
+template <typename T, int L, int V, bool ALONE>
+__global__ __launch_bounds__(64 * choose_waves<L>()) void choose_kernel(ChooseArgs a) {
+  typedef Row<T, L, V> R;
+  constexpr int kWaves = choose_waves<L>(), kGroups = kWaves * 64 / L, kMine = (WS_MAX_CHOICES + L - 1) / L;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int n = a.experts + 1;  // the last: tokens with a choice
+  float* lds_sums = (float*)smem;                    // waves x n
+  int32_t* lds_counts = (int32_t*)(lds_sums + kWaves * n);  // waves x n
+  __shared__ double scratch[2 * kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = tid % L;
+  float sums[V];
+  int32_t counts[V], with = 0;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    sums[v] = 0.0f;
+    counts[v] = 0;
+  }
+  const int64_t step = (int64_t)a.blocks * kGroups;
+  for (int64_t t = (int64_t)blockIdx.x * kGroups + tid / L; t < a.tokens; t += step) {
+    T raw[V];
+    R::load((const T*)a.logits + t * a.ld, sub, a.experts, raw);
+    uint32_t key[V], best = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      key[v] = R::element(sub, v) < a.experts ? rank_of(to_f32(raw[v])) : 0;
+      best = max(best, key[v]);
+    }
+    best = max_lanes<L>(best);
+    const bool some = best != 0;
+    const float top = logit_of(best);
+    if (some) {
+      float p[V], sum = 0.0f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        p[v] = R::element(sub, v) < a.experts ? expf(to_f32(raw[v]) - top) : 0.0f;
+        sum += p[v];
+      }
+      const float by = 1.0f / sum_lanes<L>(sum);
+#pragma unroll
+      for (int v = 0; v < V; ++v) sums[v] = fmaf(p[v], by, sums[v]);
+    }
+    int32_t id[kMine];
+    float w[kMine], all = 0.0f;
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+      id[q] = -1;
+      w[q] = 0.0f;
+      for (int j = q * L; j < a.k && j < (q + 1) * L; ++j) {
+        if (j > 0) {
+          best = 0;
+#pragma unroll
+          for (int v = 0; v < V; ++v) best = max(best, key[v]);
+          best = max_lanes<L>(best);
+        }
+        if (best == 0) break;
+        uint32_t low = 0;  // the lowest element with it, as a large number
+#pragma unroll
+        for (int v = V - 1; v >= 0; --v) low = key[v] == best ? ~(uint32_t)R::element(sub, v) : low;
+        const int e = (int)~max_lanes<L>(low);
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = R::element(sub, v) == e ? 0 : key[v];
+        const float x = expf(logit_of(best) - top);
+        all += x;
+        if (j - q * L == sub) {
+          id[q] = e;
+          w[q] = x;
+        }
+      }
+    }
+    const float by = 1.0f / all;
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+      const int j = q * L + sub;
+      if (j < a.k) {
+        a.ids[t * a.k + j] = id[q];
+        a.weights[t * a.k + j] = id[q] >= 0 ? w[q] * by : 0.0f;
+      }
+    }
+    // what has no rank left, but had one
+#pragma unroll
+    for (int v = 0; v < V; ++v) counts[v] += key[v] == 0 && to_f32(raw[v]) != -INFINITY;
+    with += some;
+  }
+  // the wave's tokens, then the workgroup's
+  const auto add_groups = [](auto x) {
+    if constexpr (L == 16) {
+      x += __shfl_xor(x, 16);
+      x += __shfl_xor(x, 32);
+    }
+    return x;
+  };
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    sums[v] = add_groups(sums[v]);
+    counts[v] = add_groups(counts[v]);
+    const int e = R::element(sub, v);
+    if (lane < L && e < a.experts) {
+      lds_sums[wave * n + e] = sums[v];
+      lds_counts[wave * n + e] = counts[v];
+    }
+  }
+  with = add_groups(with);
+  if (lane == 0) {
+    lds_sums[wave * n + a.experts] = 0.0f;
+    lds_counts[wave * n + a.experts] = with;
+  }
+  __syncthreads();
+  for (int e = tid; e < n; e += 64 * kWaves) {
+    float s = lds_sums[e];
+    int32_t c = lds_counts[e];
+    for (int w = 1; w < kWaves; ++w) {
+      s += lds_sums[w * n + e];
+      c += lds_counts[w * n + e];
+    }
+    if constexpr (ALONE) {
+      lds_sums[e] = s;
+      lds_counts[e] = c;
+    } else {
+      a.sums[(int64_t)blockIdx.x * n + e] = s;
+      a.parts[(int64_t)blockIdx.x * n + e] = c;
+    }
+  }
+  if constexpr (ALONE) {
+    __syncthreads();
+    finish(a, lds_sums, lds_counts, scratch);
+  }
+}
+
+constexpr int kFinishThreads = 1024;
+
+// Adds up what the workgroups left, every expert's in a fixed order.
+__global__ __launch_bounds__(kFinishThreads) void choose_finish_kernel(ChooseArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ double scratch[kFinishThreads / 32];
+  const int n = a.experts + 1, slices = kFinishThreads / n > 0 ? kFinishThreads / n : 1;
+  float* sums = (float*)smem;                 // slices x n
+  int32_t* counts = (int32_t*)(sums + slices * n);
+  for (int i = threadIdx.x; i < slices * n; i += kFinishThreads) {
+    const int e = i % n, slice = i / n;
+    float s = 0.0f;
+    int32_t c = 0;
+    for (int b0 = slice; b0 < a.blocks; b0 += 8 * slices) {  // 16 loads at once
+      float x[8];
+      int32_t y[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int b = b0 + u * slices;
+        x[u] = b < a.blocks ? a.sums[(int64_t)b * n + e] : 0.0f;
+        y[u] = b < a.blocks ? a.parts[(int64_t)b * n + e] : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        s += x[u];
+        c += y[u];
+      }
+    }
+    sums[slice * n + e] = s;
+    counts[slice * n + e] = c;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < n; e += kFinishThreads)
+    for (int i = 1; i < slices; ++i) {
+      sums[e] += sums[i * n + e];
+      counts[e] += counts[i * n + e];
+    }
+  __syncthreads();
+  finish(a, sums, counts, scratch);
+}
+
+// L lanes take a token: its softmax again from its logits, what its weights ask of its
+// choices by way of a row in LDS, and one write.  Bound: memory.
+template <typename T, int L, int V>
+__global__ __launch_bounds__(256) void choose_gradient_kernel(ChooseArgs a) {
+  typedef Row<T, L, V> R;
+  constexpr int kGroups = 256 / L, kMine = (WS_MAX_CHOICES + L - 1) / L;
+  __shared__ float rows[kGroups][L * V];
+  const int tid = threadIdx.x, sub = tid % L;
+  float* row = rows[tid / L];
+  // counts, and what of the loss belongs to one choice of one token
+  float c[V], all = 0.0f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int e = R::element(sub, v);
+    c[v] = e < a.experts ? (float)a.counts[e] : 0.0f;
+    all += c[v];
+    row[e] = 0.0f;
+  }
+  const float n = (float)a.counts[a.experts];
+  all = sum_lanes<L>(all);
+  const float scale = a.dloss && all > 0.0f && n > 0.0f ? *a.dloss * (float)a.experts / all / n : 0.0f;
+  __builtin_amdgcn_wave_barrier();
+  const int64_t step = (int64_t)gridDim.x * kGroups;
+  for (int64_t t = (int64_t)blockIdx.x * kGroups + tid / L; t < a.tokens; t += step) {
+    T raw[V];
+    R::load((const T*)a.logits + t * a.ld, sub, a.experts, raw);
+    int32_t id[kMine];
+    float w[kMine], dw[kMine], dot = 0.0f;
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+      const int j = q * L + sub;
+      id[q] = -1;
+      w[q] = dw[q] = 0.0f;
+      if (a.dweights && j < a.k) {
+        id[q] = a.ids[t * a.k + j];
+        if ((uint32_t)id[q] < (uint32_t)a.experts) {
+          w[q] = a.weights[t * a.k + j];
+          dw[q] = a.dweights[t * a.k + j];
+        } else {
+          id[q] = -1;
+        }
+      }
+      dot = fmaf(w[q], dw[q], dot);
+    }
+    // the largest that is no NaN: a NaN makes the sum one
+    float x[V], top = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      x[v] = to_f32(raw[v]);  // -inf past the last expert
+      top = fmaxf(top, x[v]);
+    }
+    top = largest<L>(top);
+    const float from = top == -INFINITY ? 0.0f : top;  // a masked token's exponentials are zeros
+    float sum = 0.0f, of_counts = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      x[v] = expf(x[v] - from);
+      sum += x[v];
+      of_counts = fmaf(c[v], x[v], of_counts);
+    }
+    sum = sum_lanes<L>(sum);
+    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+    of_counts = sum_lanes<L>(of_counts) * by;
+    dot = sum_lanes<L>(dot);
+    // what a choice is asked, added up where an id comes twice: the same for all its places
+    float asked[kMine];
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) asked[q] = 0.0f;
+    if (a.dweights) {
+#pragma unroll
+      for (int o = 0; o < kMine; ++o)
+        for (int j = 0; j < L && o * L + j < a.k; ++j) {
+          const int other = __shfl(id[o], j, L);
+          const float of = __shfl(w[o] * (dw[o] - dot), j, L);
+#pragma unroll
+          for (int q = 0; q < kMine; ++q) asked[q] += other == id[q] ? of : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < kMine; ++q)
+      if (id[q] >= 0) row[id[q]] = asked[q];
+    __builtin_amdgcn_wave_barrier();  // a wave's LDS accesses keep their order
+    T d[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) d[v] = from_f32<T>(fmaf(scale * (x[v] * by), c[v] - of_counts, row[R::element(sub, v)]));
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int q = 0; q < kMine; ++q)
+      if (id[q] >= 0) row[id[q]] = 0.0f;
+    __builtin_amdgcn_wave_barrier();
+    R::store((T*)a.dlogits + t * a.ld_d, sub, a.experts, d);
+  }
+}
+
+// -- host ---------------------------------------------------------------------
+
+constexpr int kMostBlocks = 256;
+// Tokens that one workgroup takes by itself.
+constexpr int64_t kAloneTokens = 256;
+
+bool choose_sizes(int64_t tokens, int32_t experts, int32_t k) {
+  return tokens >= 0 && experts >= 1 && experts <= WS_MAX_EXPERTS && k >= 1 && k <= experts && k <= WS_MAX_CHOICES &&
+         tokens <= kMaxDim && tokens * k <= kMaxDim;
+}
+
+int lanes_of(int experts) { return experts <= 256 ? 16 : 64; }
+
+int choose_blocks(int64_t tokens, int experts) {
+  if (tokens <= kAloneTokens) return 1;
+  const int64_t groups = experts <= 256 ? choose_waves<16>() * 4 : choose_waves<64>(), n = ceil_div(tokens, groups);
+  return (int)(n < kMostBlocks ? n : kMostBlocks);
+}
+
+// f(type, lanes, elements a lane) of the smallest that holds a row.
+template <typename T, typename F>
+ws_status by_experts(int experts, const F& f) {
+  typedef std::integral_constant<int, 16> L16;
+  typedef std::integral_constant<int, 64> L64;
+  if (experts <= 16) return f(T{}, L16{}, std::integral_constant<int, 1>{});
+  if (experts <= 64) return f(T{}, L16{}, std::integral_constant<int, 4>{});
+  if (experts <= 128) return f(T{}, L16{}, std::integral_constant<int, 8>{});
+  if (experts <= 256) return f(T{}, L16{}, std::integral_constant<int, 16>{});
+  if (experts <= 512) return f(T{}, L64{}, std::integral_constant<int, 8>{});
+  return f(T{}, L64{}, std::integral_constant<int, 16>{});
+}
+template <typename F>
+ws_status by_type(int32_t dtype, int experts, const F& f) {
+  if (dtype == WS_OUT_F32) return by_experts<float>(experts, f);
+  if (dtype == WS_OUT_BF16) return by_experts<bf16_t>(experts, f);
+  return by_experts<f16_t>(experts, f);
+}
+
+bool aligned4(const void* p) { return p && (uintptr_t)p % 4 == 0; }
+
+}  // namespace
+}  // namespace wsg
+
+using namespace wsg;
+
+extern "C" {
+
+int64_t ws_expert_choose_workspace(int64_t tokens, int32_t experts, int32_t k) {
+  if (!choose_sizes(tokens, experts, k)) return -1;
+  const int blocks = choose_blocks(tokens, experts);
+  return blocks == 1 ? 0 : (int64_t)blocks * (experts + 1) * 8;
+}
+
+ws_status ws_expert_choose(const ws_matrix* logits, int32_t k, float* weights, int32_t* ids, int32_t* counts, float* loss,
+                           void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+  if (!valid(logits) || logits->batch > 1 || logits->cols > WS_MAX_EXPERTS) return WS_ERR_INVALID_ARG;
+  const int64_t need = ws_expert_choose_workspace(logits->rows, (int32_t)logits->cols, k);
+  if (need < 0 || workspace_bytes < need || (need > 0 && !aligned4(workspace)) || !aligned4(counts) || !aligned4(loss) ||
+      (logits->rows > 0 && (!aligned4(weights) || !aligned4(ids))))
+    return WS_ERR_INVALID_ARG;
+  ChooseArgs a{};
+  a.logits = logits->data;
+  a.weights = weights;
+  a.loss = loss;
+  a.ids = ids;
+  a.counts = counts;
+  a.tokens = logits->rows;
+  a.ld = logits->ld;
+  a.experts = (int32_t)logits->cols;
+  a.k = k;
+  a.blocks = choose_blocks(a.tokens, a.experts);
+  a.sums = (float*)workspace;
+  a.parts = (int32_t*)workspace + (int64_t)a.blocks * (a.experts + 1);
+  const ws_status s = by_type(logits->dtype, a.experts, [&](auto type, auto lanes, auto each) {
+    typedef decltype(type) T;
+    constexpr int L = decltype(lanes)::value, V = decltype(each)::value, waves = choose_waves<L>();
+    const int lds = waves * (a.experts + 1) * 8;
+    if (a.blocks == 1) return launch("expert_choose", &choose_kernel<T, L, V, true>, 1, 64 * waves, lds, stream, a);
+    return launch("expert_choose", &choose_kernel<T, L, V, false>, a.blocks, 64 * waves, lds, stream, a);
+  });
+  if (s != WS_OK || a.blocks == 1) return s;
+  const int n = a.experts + 1, slices = kFinishThreads / n > 0 ? kFinishThreads / n : 1;
+  return launch("expert_choose", &choose_finish_kernel, 1, kFinishThreads, slices * n * 8, stream, a);
+}
+
+ws_status ws_expert_choose_gradient(const ws_matrix* logits, int32_t k, const float* dweights, const float* dloss,
+                                    const float* weights, const int32_t* ids, const int32_t* counts, const ws_matrix* dlogits,
+                                    hipStream_t stream) {
+  if (!valid(logits) || logits->batch > 1 || !valid(dlogits) || dlogits->batch > 1 || logits->rows != dlogits->rows ||
+      logits->cols != dlogits->cols || logits->dtype != dlogits->dtype || logits->cols > WS_MAX_EXPERTS ||
+      !choose_sizes(logits->rows, (int32_t)logits->cols, k))
+    return WS_ERR_INVALID_ARG;
+  if (logits->rows == 0) return WS_OK;
+  if (!aligned4(counts) || (dloss && (uintptr_t)dloss % 4) || (dweights && (!aligned4(dweights) || !aligned4(weights) || !aligned4(ids))))
+    return WS_ERR_INVALID_ARG;
+  ChooseArgs a{};
+  a.logits = logits->data;
+  a.dlogits = dlogits->data;
+  a.weights = const_cast<float*>(weights);
+  a.ids = const_cast<int32_t*>(ids);
+  a.counts = const_cast<int32_t*>(counts);
+  a.dweights = dweights;
+  a.dloss = dloss;
+  a.tokens = logits->rows;
+  a.ld = logits->ld;
+  a.ld_d = dlogits->ld;
+  a.experts = (int32_t)logits->cols;
+  a.k = k;
+  const int64_t most = 2048, n = ceil_div(a.tokens, 256 / lanes_of(a.experts));
+  return by_type(logits->dtype, a.experts, [&](auto type, auto lanes, auto each) {
+    return launch("expert_choose_gradient", &choose_gradient_kernel<decltype(type), decltype(lanes)::value, decltype(each)::value>,
+                  n < most ? n : most, 256, 0, stream, a);
+  });
+}
+
+}  // extern "C"

@@ -1,17 +1,20 @@
 """Routing of tokens to experts and back over torch tensors (declared in
 include/ws_experts.h; computed by the HIP kernels of libwsgemm.so).
 
+    weights, ids, counts, loss = choose(logits, k) # logits: tokens x experts
     routes = sort(ids, experts)                    # ids: tokens x k
     xs = gather(x, routes)                         # rows by expert
     h = ...                                        # the experts' work on their rows
     y = combine(h, routes, weights)                # tokens x columns
     dh, dweights = combine_gradient(dy, h, routes, weights)
     dx = combine(dxs, routes)                      # gradient of gather
+    dlogits = choose_gradient(dweights, dloss, logits, weights, ids, counts)
 
-Streams and errors as in ``fp8``.  gather and combine are recorded by autograd
-(once: their gradients are not differentiated again), so that the last two lines
-are what their results' backward does; results in memory of the caller's (``out``)
-cannot be, and ask for torch.no_grad() where an input requires a gradient.
+Streams and errors as in ``fp8``.  choose, gather and combine are recorded by
+autograd (once: their gradients are not differentiated again), so that the last
+three lines are what their results' backward does; results in memory of the
+caller's (``out``) cannot be, and ask for torch.no_grad() where an input requires a
+gradient.
 """
 from __future__ import annotations
 
@@ -24,10 +27,14 @@ from . import wsgemm as _w
 from .fp8 import _Call, _check, _elsewhere, _matrix, _mp, _need, _new_matrix, _raw_stream
 
 MAX_EXPERTS = 1024
+MAX_CHOICES = 64
 
 _lib = _w.library()
 _p, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
 for _name, _args, _res in (
+        ("ws_expert_choose_workspace", [_i64, _i32, _i32], _i64),
+        ("ws_expert_choose", [_mp, _i32, _p, _p, _p, _p, _p, _i64, _p], _i32),
+        ("ws_expert_choose_gradient", [_mp, _i32, _p, _p, _p, _p, _p, _mp, _p], _i32),
         ("ws_expert_sort_workspace", [_i64, _i32, _i32], _i64),
         ("ws_expert_sort", [_i64, _i32, _i32, _p, _i32, _p, _p, _p, _p, _i64, _p], _i32),
         ("ws_expert_gather", [_mp, _i32, _i32, _p, _p, _mp, _p], _i32),
@@ -56,6 +63,97 @@ class Routes:
     @property
     def experts(self) -> int:
         return self.offsets.numel() - 1
+
+
+class _Choose(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, k):
+        weights, ids, counts, loss = choose(logits, k)
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(ids, counts)
+        ctx.save_for_backward(logits, weights, ids, counts)
+        return weights, ids, counts, loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dweights, _ids, _counts, dloss):
+        if dweights is None and dloss is None:
+            return None, None
+        if dweights is not None:
+            dweights = dweights.contiguous()
+        return choose_gradient(dweights, dloss, *ctx.saved_tensors), None
+
+
+def _logits(logits):
+    m = _matrix(logits, "logits")
+    if m.cols > MAX_EXPERTS:
+        raise ValueError("logits: at most %d experts, got %d" % (MAX_EXPERTS, m.cols))
+    return m
+
+
+def choose(logits, k: int, stream=None):
+    """(weights, ids, counts, loss) of a router's logits (tokens x experts; f32, bf16
+    or f16).  ids (tokens x k, int32): each token's k largest logits, the largest
+    first, the lowest index first among equals; -inf is not chosen, -1 stands where
+    none is left (a masked token is a row of -inf).  weights (tokens x k, f32): the
+    softmax over a token's choices.  counts (experts + 1, int32): the choices of each
+    expert, and at last the tokens that have any.  loss (f32, no dimensions): experts
+    * sum over the experts of their share of the choices * the mean of their softmax
+    probability over the tokens with a choice.  Gradients flow from weights and loss."""
+    m = _logits(logits)
+    tokens, experts = m.rows, m.cols
+    need = _lib.ws_expert_choose_workspace(tokens, experts, k) if 0 < k <= min(experts, MAX_CHOICES) else -1
+    if need < 0:
+        raise ValueError("choose: 1 to %d of the %d experts and at most 2^30 choices, got k = %r for %d tokens" % (
+            MAX_CHOICES, experts, k, tokens))
+    if _elsewhere(logits, stream):
+        with _Call(logits.device, stream, [logits]):
+            return choose(logits, k)
+    if logits.requires_grad and torch.is_grad_enabled():
+        return _Choose.apply(logits, k)
+    device = logits.device
+    weights = torch.empty(tokens, k, dtype=torch.float32, device=device)
+    ids = torch.empty(tokens, k, dtype=torch.int32, device=device)
+    counts = torch.empty(experts + 1, dtype=torch.int32, device=device)
+    loss = torch.empty((), dtype=torch.float32, device=device)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _check(_lib.ws_expert_choose(m, k, weights.data_ptr(), ids.data_ptr(), counts.data_ptr(), loss.data_ptr(),
+                                 work.data_ptr() if need else 0, need, _raw_stream(device.index)), "ws_expert_choose")
+    return weights, ids, counts, loss
+
+
+def choose_gradient(dweights, dloss, logits, weights, ids, counts, out=None, stream=None):
+    """dlogits (like logits) of choose, from the gradients of its weights (tokens x k)
+    and its loss (one value); each may be None, which is zero.  logits and the rest as
+    choose took and gave them; an id out of range counts as none.  Not recorded by
+    autograd."""
+    m = _logits(logits)
+    device = logits.device
+    _need(ids, "ids", (torch.int32,), (2,), device)
+    tokens, k = ids.shape
+    if tokens != m.rows or not 0 < k <= min(m.cols, MAX_CHOICES) or not ids.is_contiguous():
+        raise ValueError("ids: expected contiguous %d x k, k up to %d, got %s" % (m.rows, min(m.cols, MAX_CHOICES), tuple(ids.shape)))
+    for t, what in ((weights, "weights"), (dweights, "dweights")):
+        if t is None and what == "dweights":
+            continue
+        _need(t, what, (torch.float32,), (2,), device)
+        if t.shape != ids.shape or not t.is_contiguous():
+            raise ValueError("%s: expected contiguous %s, got %s" % (what, tuple(ids.shape), tuple(t.shape)))
+    _need(counts, "counts", (torch.int32,), (1,), device)
+    if counts.numel() != m.cols + 1 or not counts.is_contiguous():
+        raise ValueError("counts: expected %d contiguous values, got %s" % (m.cols + 1, tuple(counts.shape)))
+    if dloss is not None:
+        _need(dloss, "dloss", (torch.float32,), (0, 1), device)
+        if dloss.numel() != 1:
+            raise ValueError("dloss: expected one value, got %s" % (tuple(dloss.shape),))
+    if _elsewhere(logits, stream):
+        with _Call(device, stream, [dweights, dloss, logits, weights, ids, counts, out]):
+            return choose_gradient(dweights, dloss, logits, weights, ids, counts, out)
+    out, mo = _out(out, "out", m.rows, m.cols, logits)
+    _check(_lib.ws_expert_choose_gradient(m, k, dweights.data_ptr() if dweights is not None else 0,
+                                          dloss.data_ptr() if dloss is not None else 0, weights.data_ptr(), ids.data_ptr(),
+                                          counts.data_ptr(), mo, _raw_stream(device.index)), "ws_expert_choose_gradient")
+    return out
 
 
 def sort(ids, experts: int, stream=None) -> Routes:
