@@ -1,0 +1,74 @@
+/*
+ * ws_fp4.h -- C ABI of weights in 4 bits for AMD MI355X (gfx950): rounding by
+ * blocks, the way back, and products of a few rows with such weights.
+ *
+ * Format: codes are OCP e2m1 (1 sign, 2 exponent, 1 fraction bit: 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6 and their negatives).  A scale is a power of two in 8 bits (E8M0: byte
+ * b stands for 2^(b - 127), 255 for NaN) and belongs to 32 neighbouring columns of a
+ * row.  Powers of two, as in ws_fp8.h: scaling by them rounds nothing, and gfx950
+ * widens codes to bf16 with the scale in one instruction, exactly.
+ *
+ * A matrix in 4 bits (ws_fp4_matrix) has columns padded with zero codes to a multiple
+ * of 128.  128 columns of a row are 64 bytes: byte 16 g + 4 i + b holds columns
+ * 32 i + 8 g + 2 b (low half) and 32 i + 8 g + 2 b + 1 (high half), g, i and b from 0
+ * to 3, so that a lane's 16 bytes are its operands of four matrix instructions.
+ * The scale of columns 32 j .. 32 j + 31 of row r is scales[r * ld_scales + j]; those
+ * of padding are 1.
+ *
+ * Rounding of a block: amax is its largest |x|, the scale is the smallest power of two s
+ * with amax <= 6 s (1 for amax = 0; at least 2^-127; at most 2^125, whose multiples
+ * binary32 holds), and a code is x / s rounded to nearest, ties to the code with an
+ * even last bit, above 6 to 6.  A block with an infinity or NaN
+ * gets a NaN scale: its values are gone.
+ *
+ * Calls, pointers, sizes and errors as in ws_fp8.h.
+ */
+#ifndef WS_FP4_H
+#define WS_FP4_H
+
+#include "ws_fp8.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define WS_FP4_BLOCK 32
+
+typedef struct {
+  void* codes;            /* 16-byte aligned */
+  uint8_t* scales;        /* 4-byte aligned */
+  int64_t rows, cols;
+  int64_t ld;             /* bytes between rows: a multiple of 16, at least 64 ceil(cols / 128) */
+  int64_t ld_scales;      /* bytes between the scales of rows: a multiple of 4, at least 4 ceil(cols / 128) */
+  int32_t batch;          /* matrices of one size (weights of experts); 0 as in ws_fp8_matrix */
+  int64_t stride_codes;   /* between them: a multiple of 16; they do not overlap */
+  int64_t stride_scales;  /* a multiple of 4 */
+} ws_fp4_matrix;
+
+/* out <- w (f32, bf16 or f16; (a batch of) rows x cols, of the same sizes). */
+ws_status ws_fp4_quantize(const ws_matrix* w, const ws_fp4_matrix* out, hipStream_t stream);
+
+/* out (f32 or bf16) <- the values of q, exactly (bf16: from 2^-126 up). */
+ws_status ws_fp4_dequantize(const ws_fp4_matrix* q, const ws_matrix* out, hipStream_t stream);
+
+/* C <- A B^T: B is N x K in 4 bits; C (f32, bf16 or f16) is M x N; its row m is row
+ * index[m] of A (a negative or too large index: a row of zeros), or row m for index
+ * NULL (then A has M rows).  A is bf16 or f16, K columns.  Products and sums in
+ * binary32, rounded once (bf16: operand values below 2^-126 count as 0).  Made for
+ * the rows of a decoding step: the weights are read once for every 64 rows.  Results
+ * depend on the operands and sizes only: no atomics. */
+ws_status ws_fp4_product(const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, const ws_matrix* C,
+                         hipStream_t stream);
+
+/* The same by group: row r of C is its row of A times B_g^T, for the group g whose
+ * rows offsets[g] .. offsets[g + 1] - 1 hold r (int32 on the device, not decreasing);
+ * rows in no group, before the first or after the last, become zeros.  B is a batch of
+ * `groups` matrices. */
+ws_status ws_fp4_grouped_product(const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, int32_t groups,
+                                 const int32_t* offsets, const ws_matrix* C, hipStream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* WS_FP4_H */

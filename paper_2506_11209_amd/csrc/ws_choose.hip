@@ -2,6 +2,8 @@
 // ws_experts.h).
 #include <math.h>
 
+#include <type_traits>
+
 #include "ws_experts.h"
 #include "ws_fp8_common.hpp"
 

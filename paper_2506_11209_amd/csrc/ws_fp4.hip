@@ -1,0 +1,409 @@
+// Weights in 4 bits: rounding, widening and products of a few rows (definitions:
+// ws_fp4.h).
+#include <math.h>
+
+#include <type_traits>
+
+#include "ws_fp4.h"
+#include "ws_fp8_common.hpp"
+
+namespace wsg {
+namespace {
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+
+// 2^(byte - 127); 2^-127 is subnormal, 255 is NaN.
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+  return __uint_as_float(byte == 0 ? 1u << 22 : byte == 255 ? 0x7fc00000u : byte << 23);
+}
+
+// -- rounding and widening -------------------------------------------------------
+
+struct Fp4CastArgs {
+  const void* w;
+  void* out;
+  uint8_t *codes, *scales;
+  int64_t rows, cols, ld_w, ld, ld_scales, stride_w, stride_codes, stride_scales;
+  int64_t units, per_row;  // 128 columns of a row are a unit
+};
+
+// Largest over the 4 lanes of a quad, in all of them.
+__device__ __forceinline__ uint32_t max_quad(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, true));  // quad_perm 1 0 3 2
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, true));  // quad_perm 2 3 0 1
+  return x;
+}
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, float (&v)[8]) {
+  if (c + 8 <= cols) {
+    T t[8];
+    if constexpr (sizeof(T) == 4) {
+      load_n<T, 4>(row + c, t);
+      load_n<T, 4>(row + c + 4, t + 4);
+    } else {
+      load_n<T, 8>(row + c, t);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = to_f32(t[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? to_f32(row[c + j]) : 0.0f;
+  }
+}
+
+// A quad of lanes takes 128 columns of a row, 8 of every 32 a lane.  Bound: memory.
+template <typename T>
+__global__ __launch_bounds__(256) void fp4_quantize_kernel(Fp4CastArgs a) {
+  const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 2;
+  const int g = threadIdx.x & 3;
+  if (unit >= a.units) return;  // whole quads
+  const int64_t line = unit / a.per_row, b = unit % a.per_row, m = line / a.rows, r = line % a.rows;
+  const T* row = (const T*)a.w + m * a.stride_w + r * a.ld_w;
+  float v[4][8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) load8<T>(row, 128 * b + 32 * i + 8 * g, a.cols, v[i]);
+  uint32_t code[4], scale = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t amax = 0;  // of the magnitudes' bits, which are in their order; NaN above infinity
+#pragma unroll
+    for (int j = 0; j < 8; ++j) amax = max(amax, __float_as_uint(v[i][j]) & 0x7fffffffu);
+    amax = max_quad(amax);
+    // amax = f 2^e, 1 <= f < 2: 2^(e - 2) where f <= 1.5, else 2^(e - 1)
+    const int e = (int)(amax >> 23) - ((amax & 0x7fffffu) <= 0x400000u ? 2 : 1);
+    const int byte = amax >= 0x7f800000u ? 255 : amax == 0 ? kScaleOne : min(max(e, 0), 252);
+    scale |= (uint32_t)byte << (8 * i);
+    uint32_t c = 0;
+    if (byte != 255) {
+      float y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = ldexpf(v[i][j], kScaleOne - byte);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[0], y[1], 1.0f, 0);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[2], y[3], 1.0f, 1);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[4], y[5], 1.0f, 2);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, y[6], y[7], 1.0f, 3);
+    }
+    code[i] = c;
+  }
+  *(i32x4_t*)(a.codes + m * a.stride_codes + r * a.ld + 64 * b + 16 * g) =
+      i32x4_t{(int)code[0], (int)code[1], (int)code[2], (int)code[3]};
+  if (g == 0) *(uint32_t*)(a.scales + m * a.stride_scales + r * a.ld_scales + 4 * b) = scale;
+}
+
+// Eight codes of a dword times a scale, exactly.
+__device__ __forceinline__ bf16x8_t widen_bf16(uint32_t c, float scale) {
+  const bf16x2_t p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
+  const bf16x2_t r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2), s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
+  return bf16x8_t{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
+__device__ __forceinline__ f16x8_t widen_f16(uint32_t c) {
+  const f16x2_t p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.0f, 0), q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.0f, 1);
+  const f16x2_t r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.0f, 2), s = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, 1.0f, 3);
+  return f16x8_t{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
+
+// As fp4_quantize_kernel, the other way.  T: float or bf16_t.
+template <typename T>
+__global__ __launch_bounds__(256) void fp4_dequantize_kernel(Fp4CastArgs a) {
+  const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 2;
+  const int g = threadIdx.x & 3;
+  if (unit >= a.units) return;
+  const int64_t line = unit / a.per_row, b = unit % a.per_row, m = line / a.rows, r = line % a.rows;
+  const i32x4_t code = *(const i32x4_t*)(a.codes + m * a.stride_codes + r * a.ld + 64 * b + 16 * g);
+  const uint32_t scale = *(const uint32_t*)(a.scales + m * a.stride_scales + r * a.ld_scales + 4 * b);
+  T* row = (T*)a.out + m * a.stride_w + r * a.ld_w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float by = scale_value(scale >> (8 * i) & 255u);
+    const f16x8_t h = widen_f16((uint32_t)code[i]);
+    const int64_t c = 128 * b + 32 * i + 8 * g;
+    T t[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = from_f32<T>((float)h[j] * by);
+    if (c + 8 <= a.cols) {
+      if constexpr (sizeof(T) == 4) {
+        store_n<T, 4>(row + c, t);
+        store_n<T, 4>(row + c + 4, t + 4);
+      } else {
+        store_n<T, 8>(row + c, t);
+      }
+    } else {
+      for (int j = 0; j < 8; ++j)
+        if (c + j < a.cols) row[c + j] = t[j];
+    }
+  }
+}
+
+// -- products --------------------------------------------------------------------
+
+struct Fp4Args {
+  const void* x;
+  const uint8_t *codes, *scales;
+  void* C;
+  const int32_t *index, *offsets;
+  int64_t ldx, ld, ld_scales, stride_codes, stride_scales, ldc;
+  int64_t M, x_rows, N, K;
+  int64_t tiles_m, strips;
+  int32_t groups, dtype;
+};
+
+__device__ __forceinline__ f32x4_t multiply(bf16x8_t x, bf16x8_t w, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4_t multiply(f16x8_t x, f16x8_t w, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w, c, 0, 0, 0);
+}
+
+// Eight of a row's columns from k, zeros past its end and for no row.
+template <typename T>
+__device__ __forceinline__ i32x4_t load_row(const T* row, bool valid, int64_t k, int64_t K) {
+  i32x4_t v = {0, 0, 0, 0};
+  if (valid) {
+    if (k + 8 <= K) {
+      load_n<T, 8>(row + k, (T*)&v);
+    } else {
+      T t[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[j] = k + j < K ? row[k + j] : from_f32<T>(0.0f);
+      __builtin_memcpy(&v, t, 16);
+    }
+  }
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_value(void* C, int64_t at, float v) {
+  ((T*)C)[at] = from_f32<T>(v);
+}
+
+// A workgroup computes 16 MT rows of 16 NT columns; its W waves share out the
+// contraction, 256 columns at a time, and add up their parts through LDS in a fixed
+// order.  Operands go from memory straight to registers.  Bound: reading the weights.
+template <typename X, int MT, int NT, int W, bool GROUPED>
+__global__ __launch_bounds__(64 * W) void fp4_product_kernel(Fp4Args a) {
+  constexpr bool kBf16 = sizeof(X) == sizeof(bf16_t) && std::is_same<X, bf16_t>::value;
+  __shared__ f32x4_t part[W * MT * NT * 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+  // strips of columns go round the XCDs, the tiles of rows of one strip follow each other on one
+  const int64_t turn = 8 * a.tiles_m, strip = blockIdx.x / turn * 8 + blockIdx.x % 8, tm = blockIdx.x % turn / 8;
+  if (strip >= a.strips) return;
+  int64_t m0 = tm * 16 * MT, m_end = a.M;
+  const uint8_t *codes = a.codes, *scales = a.scales;
+  bool zero = false;
+  if constexpr (GROUPED) {
+    const GroupTile gt = find_group_tile(a.offsets, a.groups, a.M, 16 * MT, tm);
+    if (gt.group < 0) return;
+    m0 = gt.lo + gt.index * 16 * MT;
+    m_end = gt.hi;
+    zero = gt.group >= a.groups;
+    if (!zero) {
+      codes += gt.group * a.stride_codes;
+      scales += gt.group * a.stride_scales;
+    }
+  }
+  const int64_t n0 = strip * 16 * NT;
+  const X* x[MT];
+  bool valid[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t m = m0 + 16 * i + r;
+    valid[i] = m < m_end && !zero;
+    int64_t from = valid[i] && a.index ? a.index[m] : m;
+    valid[i] = valid[i] && from >= 0 && from < a.x_rows;
+    x[i] = (const X*)a.x + (valid[i] ? from : 0) * a.ldx;
+  }
+  const uint8_t *code_row[NT], *scale_row[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int64_t n = min(n0 + 16 * t + r, a.N - 1);  // past the last column: computed and not stored
+    code_row[t] = codes + n * a.ld + 16 * g;
+    scale_row[t] = scales + n * a.ld_scales;
+  }
+  f32x4_t acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[i][t] = f32x4_t{0, 0, 0, 0};
+  const int64_t blocks = zero ? 0 : (a.K + 127) / 128;
+  for (int64_t b0 = 2 * wave; b0 < blocks; b0 += 2 * W) {
+    i32x4_t code[2][NT];
+    uint32_t scale[2][NT];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int64_t b = min(b0 + u, blocks - 1);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        code[u][t] = *(const i32x4_t*)(code_row[t] + 64 * b);
+        scale[u][t] = *(const uint32_t*)(scale_row[t] + 4 * b);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if (b0 + u >= blocks) break;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        i32x4_t xv[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xv[i] = load_row<X>(x[i], valid[i], 128 * (b0 + u) + 32 * q + 8 * g, a.K);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float by = scale_value(scale[u][t] >> (8 * q) & 255u);
+          if constexpr (kBf16) {
+            const bf16x8_t w = widen_bf16((uint32_t)code[u][t][q], by);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) acc[i][t] = multiply(__builtin_bit_cast(bf16x8_t, xv[i]), w, acc[i][t]);
+          } else {  // binary16 does not reach as far as scales do: they are applied to the sums
+            const f16x8_t w = widen_f16((uint32_t)code[u][t][q]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              const f32x4_t p = multiply(__builtin_bit_cast(f16x8_t, xv[i]), w, f32x4_t{0, 0, 0, 0});
+#pragma unroll
+              for (int j = 0; j < 4; ++j) acc[i][t][j] = fmaf(by, p[j], acc[i][t][j]);
+            }
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) part[((wave * MT + i) * NT + t) * 64 + lane] = acc[i][t];
+  __syncthreads();
+  // lane l of a piece: rows 4 (l / 16) .., column l % 16
+  for (int j = tid; j < MT * NT * 64; j += 64 * W) {
+    f32x4_t sum = part[j];
+    for (int w = 1; w < W; ++w) sum += part[w * MT * NT * 64 + j];
+    const int64_t m = m0 + j / (NT * 64) * 16 + (j & 63) / 16 * 4, n = n0 + j / 64 % NT * 16 + (j & 15);
+    if (n >= a.N) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (m + e >= m_end) break;
+      const int64_t at = (m + e) * a.ldc + n;
+      switch (a.dtype) {  // the same for the whole launch
+        case WS_OUT_F32: store_value<float>(a.C, at, sum[e]); break;
+        case WS_OUT_BF16: store_value<bf16_t>(a.C, at, sum[e]); break;
+        default: store_value<f16_t>(a.C, at, sum[e]);
+      }
+    }
+  }
+}
+
+// -- host ---------------------------------------------------------------------
+
+bool valid_fp4(const ws_fp4_matrix* q, bool batched) {
+  if (!q || q->rows < 0 || q->cols < 0 || q->rows > kMaxDim || q->cols > kMaxDim || q->batch < 0) return false;
+  const int64_t units = ceil_div(q->cols, 128);
+  if (q->ld % 16 || q->ld < 64 * units || q->ld > kMaxDim || q->ld_scales % 4 || q->ld_scales < 4 * units || q->ld_scales > kMaxDim)
+    return false;
+  if (q->rows == 0 || q->cols == 0 || (batched && q->batch == 0)) return true;
+  if (q->batch > 1 && (q->stride_codes % 16 || q->stride_scales % 4 || q->stride_codes < (q->rows - 1) * q->ld + 64 * units ||
+                       q->stride_scales < (q->rows - 1) * q->ld_scales + 4 * units))
+    return false;
+  return q->codes && (uintptr_t)q->codes % 16 == 0 && q->scales && (uintptr_t)q->scales % 4 == 0;
+}
+
+ws_status cast(const char* what, const ws_matrix* w, const ws_fp4_matrix* q, bool out, hipStream_t stream) {
+  if (!valid(w, true) || !valid_fp4(q, true) || w->rows != q->rows || w->cols != q->cols) return WS_ERR_INVALID_ARG;
+  if (w->batch != q->batch) return WS_ERR_INVALID_ARG;
+  if (!out && w->dtype == WS_OUT_F16) return WS_ERR_INVALID_ARG;  // values of 2^17 and more
+  if (w->rows == 0 || w->cols == 0 || w->batch == 0) return WS_OK;
+  Fp4CastArgs a{};
+  a.w = w->data;
+  a.out = w->data;
+  a.codes = (uint8_t*)q->codes;
+  a.scales = q->scales;
+  a.rows = w->rows;
+  a.cols = w->cols;
+  a.ld_w = w->ld;
+  a.stride_w = w->stride;
+  a.ld = q->ld;
+  a.ld_scales = q->ld_scales;
+  a.stride_codes = q->stride_codes;
+  a.stride_scales = q->stride_scales;
+  a.per_row = ceil_div(w->cols, 128);
+  a.units = a.per_row * w->rows * w->batch;
+  const int64_t grid = ceil_div(a.units, 64);
+  if (grid > max_workgroups(256)) return WS_ERR_INVALID_ARG;
+  if (out)
+    return launch(what, w->dtype == WS_OUT_F32 ? &fp4_quantize_kernel<float> : w->dtype == WS_OUT_BF16 ? &fp4_quantize_kernel<bf16_t>
+                                                                                                          : &fp4_quantize_kernel<f16_t>,
+                  grid, 256, 0, stream, a);
+  return launch(what, w->dtype == WS_OUT_F32 ? &fp4_dequantize_kernel<float> : &fp4_dequantize_kernel<bf16_t>, grid, 256, 0, stream, a);
+}
+
+template <int MT, int NT, int W>
+ws_status launch_product(const char* what, bool bf16, bool grouped, hipStream_t stream, Fp4Args a) {
+  a.strips = ceil_div(a.N, 16 * NT);
+  a.tiles_m = grouped ? group_tiles(a.M, a.groups, 16 * MT, true) : ceil_div(a.M, 16 * MT);
+  const int64_t grid = ceil_div(a.strips, 8) * 8 * a.tiles_m;
+  if (grid > max_workgroups(64 * W)) return WS_ERR_INVALID_ARG;
+  void (*kernel)(Fp4Args) = bf16 ? (grouped ? &fp4_product_kernel<bf16_t, MT, NT, W, true> : &fp4_product_kernel<bf16_t, MT, NT, W, false>)
+                                 : (grouped ? &fp4_product_kernel<f16_t, MT, NT, W, true> : &fp4_product_kernel<f16_t, MT, NT, W, false>);
+  return launch(what, kernel, grid, 64 * W, 0, stream, a);
+}
+
+ws_status product(const char* what, const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, int32_t groups,
+                  const int32_t* offsets, const ws_matrix* C, hipStream_t stream) {
+  const bool grouped = groups >= 0;
+  if (!valid(A) || A->batch > 1 || !valid(C) || C->batch > 1 || !valid_fp4(B, grouped)) return WS_ERR_INVALID_ARG;
+  if (A->dtype == WS_OUT_F32 || A->cols != B->cols || C->cols != B->rows || (!index && A->rows != C->rows) || (uintptr_t)index % 4)
+    return WS_ERR_INVALID_ARG;
+  if (grouped ? B->batch != groups || groups > 1 << 20 || !offsets || (uintptr_t)offsets % 4 : B->batch > 1) return WS_ERR_INVALID_ARG;
+  if (C->rows == 0 || C->cols == 0) return WS_OK;
+  Fp4Args a{};
+  a.x = A->data;
+  a.codes = (const uint8_t*)B->codes;
+  a.scales = B->scales;
+  a.C = C->data;
+  a.index = index;
+  a.offsets = offsets;
+  a.ldx = A->ld;
+  a.ld = B->ld;
+  a.ld_scales = B->ld_scales;
+  a.stride_codes = B->stride_codes;
+  a.stride_scales = B->stride_scales;
+  a.ldc = C->ld;
+  a.M = C->rows;
+  a.x_rows = A->rows;
+  a.N = C->cols;
+  a.K = A->cols;
+  a.groups = groups;
+  a.dtype = C->dtype;
+  const bool bf16 = A->dtype == WS_OUT_BF16;
+  const int64_t rows = grouped ? (groups ? ceil_div(a.M, groups) : a.M) : a.M;  // of a group, on average
+  if (rows <= 16) return launch_product<1, 2, 4>(what, bf16, grouped, stream, a);
+  if (rows <= 32) return launch_product<2, 2, 4>(what, bf16, grouped, stream, a);
+  return launch_product<4, 2, 4>(what, bf16, grouped, stream, a);
+}
+
+}  // namespace
+}  // namespace wsg
+
+using namespace wsg;
+
+extern "C" {
+
+ws_status ws_fp4_quantize(const ws_matrix* w, const ws_fp4_matrix* out, hipStream_t stream) {
+  return cast("fp4_quantize", w, out, true, stream);
+}
+
+ws_status ws_fp4_dequantize(const ws_fp4_matrix* q, const ws_matrix* out, hipStream_t stream) {
+  return cast("fp4_dequantize", out, q, false, stream);
+}
+
+ws_status ws_fp4_product(const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, const ws_matrix* C, hipStream_t stream) {
+  return product("fp4_product", A, index, B, -1, nullptr, C, stream);
+}
+
+ws_status ws_fp4_grouped_product(const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, int32_t groups,
+                                 const int32_t* offsets, const ws_matrix* C, hipStream_t stream) {
+  if (groups < 0) return WS_ERR_INVALID_ARG;
+  return product("fp4_grouped_product", A, index, B, groups, offsets, C, stream);
+}
+
+}  // extern "C"
