@@ -24,10 +24,7 @@
 // columns of one row of C.
 #include <math.h>
 
-#include <atomic>
-#include <type_traits>
-
-#include "ws_fp8_common.hpp"
+#include "ws_tile.hpp"
 
 namespace wsg {
 namespace {
@@ -166,8 +163,6 @@ __device__ __forceinline__ void store_out(const ProductArgs& a, const Part& p, i
   }
 }
 
-constexpr uint32_t kOutside = 0x80000000u;  // an offset past every buffer: reads zeros
-
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const uint8_t* base, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), (short)0, (int)bytes, 0x00027000);
 }
@@ -176,14 +171,6 @@ __device__ __forceinline__ i32x4_t load16(__amdgpu_buffer_rsrc_t r, uint32_t at)
 }
 __device__ __forceinline__ i32x8_t join(i32x4_t lo, i32x4_t hi) {
   return i32x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-}
-
-template <int N, typename F>
-__device__ __forceinline__ void static_for(const F& f) {
-  if constexpr (N > 0) {
-    static_for<N - 1>(f);
-    f(std::integral_constant<int, N - 1>{});
-  }
 }
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -295,46 +282,6 @@ __global__ __launch_bounds__(512) void direct_kernel(ProductArgs a) {  // kDirec
 
 // -- tiles -----------------------------------------------------------------------
 
-#define WSG_LDS __attribute__((address_space(3)))
-
-// Byte position, in a row of 128, of 16-byte chunk c of tile row r.  The operand
-// read (lane l: row l % 16, chunk l / 16 or four more) is free of bank conflicts
-// so; with (r ^ r / 8 % 2) % 8, which suits reads of 32 rows, it took twice as long
-// (SQ_LDS_BANK_CONFLICT).  The choice depends on r % 16 only, which is fixed for
-// a lane.
-__device__ __forceinline__ int chunk_at(int r, int c) { return (c ^ (r & 7)) * 16; }
-
-// A buffer descriptor as four scalars, for asm.
-__device__ __forceinline__ i32x4_t raw_buffer(const uint8_t* base, uint32_t bytes) {
-  const uint64_t at = (uint64_t)base;
-  return i32x4_t{(int)__builtin_amdgcn_readfirstlane((uint32_t)at), (int)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)),
-                 (int)__builtin_amdgcn_readfirstlane(bytes), 0x00027000};
-}
-
-// 64 lanes' 16 bytes from buffer offsets `at` + k straight to 1 KiB of LDS at
-// `to` (zeros where `at` is outside).  As asm, so that the compiler does not wait
-// for it before LDS reads of other addresses; whoever reads what it brings waits
-// for vmcnt himself.  Nothing else in these kernels uses m0.
-__device__ __forceinline__ void load_to_lds(i32x4_t r, uint32_t at, uint32_t k, uint32_t to) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile(
-      "s_mov_b32 m0, %3\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(at),
-      "s"(r), "s"(__builtin_amdgcn_readfirstlane(k)), "s"(__builtin_amdgcn_readfirstlane(to)));
-#endif
-}
-
-// Waits for this wave's LDS accesses and all but its last YOUNGER loads, then for
-// the workgroup.
-template <int YOUNGER = 0>
-__device__ __forceinline__ void drain_and_meet() {
-  static_assert(YOUNGER >= 0 && YOUNGER <= 63, "vmcnt");
-#if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(YOUNGER) : "memory");
-#endif
-}
-
 template <int WM, int WN, int STAGES>
 struct TileShape {
   static constexpr int TM = 32 * WM, TN = 32 * WN, kStage = (TM + TN) * kBlock;
@@ -358,16 +305,6 @@ struct TileShape {
   static constexpr int kStoreBytes = 16 * kPitch * 4, kLds = kStoreAt + 4 * kStoreBytes;
   static_assert(kWaves * kLds <= 160 * 1024, "LDS of a CU");
 };
-
-// Keeps what reads acc behind the asm statements before, the wait for the last
-// products among them.
-template <bool AGPR>
-__device__ __forceinline__ void settle(f32x4_t& acc) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  if constexpr (AGPR) asm volatile("" : "+a"(acc));
-  else asm volatile("" : "+v"(acc));
-#endif
-}
 
 // Writes a wave's part of a tile, 16 rows at a time by way of its own part of LDS,
 // so that a store covers whole stretches of a row.  Where nothing is added, and the
@@ -817,19 +754,6 @@ __global__ __launch_bounds__(256, (TileShape<WM, WN, STAGES>::kWaves)) void tile
 }
 
 // -- host --------------------------------------------------------------------------
-
-// Compute units of the current device, asked for once (256 where it does not say).
-int compute_units() {
-  static std::atomic<int> known[64];
-  int dev = 0, n = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
-  n = known[dev].load(std::memory_order_relaxed);
-  if (n == 0) {
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
-    known[dev].store(n, std::memory_order_relaxed);
-  }
-  return n;
-}
 
 // Bytes between rows so that a tile's offsets stay below kOutside.
 constexpr int64_t kMaxLd = 1 << 22;

@@ -1,0 +1,597 @@
+// Orthogonalised updates (definitions: ws_orthogonal.h).
+//
+// X (n x m, n the shorter side of G) and its transpose Y lie in binary16, scaled by
+// 2^14 (entries of X stay below 1.3, and those of a large matrix are small), with what
+// that leaves of every entry, times 2^11 more, in a third matrix.  A step is three
+// launches of one tile kernel, every operand's contraction along its rows:
+//
+//   S  <- X X^T             off the diagonal, which goes to dA in binary32
+//   T  <- b A + c A^2       likewise, dB = a + b A_ii + c (A^2)_ii, with
+//                           A^2 = S^2 + (dA_i + dA_j) S + dA_i^2 on the diagonal
+//   Y' <- Y T + dB_j Y      and X' its transpose
+//
+// S and T are symmetric: tiles below their diagonal are computed and written twice.
+// Why diagonals are kept apart: once singular values are near 1, A and T are near
+// multiples of the identity, and rounding these to binary16 cost most of the error
+// (1.0e-3 to 2.3e-3 of the result so, 1e-4 to 1e-3 apart).  Why X is two values: where a
+// few directions dominate G, rounding X alone cost 6e-3 in the others.
+#include <math.h>
+
+#include "ws_orthogonal.h"
+#include "ws_tile.hpp"
+
+namespace wsg {
+namespace {
+
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr float kUnit = 16384.0f, kPerUnit = 1.0f / kUnit;  // of X, S and T
+constexpr float kRest = 2048.0f;                            // of the rest of X, beyond
+constexpr int kPad = 64;                                    // sides in the workspace are multiples of it
+
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
+
+enum Kind { kGram, kSquare, kApply, kLast };
+
+struct OrthArgs {
+  const _Float16 *A, *B;         // operands, `batch` of them
+  int64_t stride_a, stride_b;    // elements between them
+  int32_t M, N, K;               // multiples of kPad; rows of K elements
+  int32_t batch, tile_groups, tiles_m, tiles_n;
+  uint32_t plane;                // tiles of one matrix
+  _Float16 *to, *mirror;         // S; T; Y' and X'
+  int64_t stride_to, stride_mirror;
+  const float* d_in;             // kSquare: dA; kApply: dB
+  float* d_out;                  // kGram: dA; kSquare: dB
+  int64_t stride_d;
+  _Float16* rest;                // of Y
+  // kLast
+  uint16_t* out;
+  int64_t ld_out, stride_out;
+  int32_t rows, cols, transposed;  // of out; transposed: it is X, not Y
+};
+
+template <int WM, int WN>
+struct OrthShape {
+  static constexpr int TM = 32 * WM, TN = 32 * WN, kStage = (TM + TN) * 128;
+  static constexpr bool kAgpr = WM * WN > 16;
+  static constexpr int kWaves = kAgpr ? 1 : 2;
+  static constexpr int kFirst = WM > 4 ? 3 : WM / 2;
+  // a wave's way to memory: 64 x 32 results
+  static constexpr int kStoreBytes = 64 * 32 * 2;
+  static constexpr int kStoreAt = 2 * kStage, kLds = kStoreAt + 4 * kStoreBytes;
+  static_assert(kWaves * kLds <= 160 * 1024, "LDS of a CU");
+};
+
+// acc += A's 16 rows times B's 16 rows over 32 columns; see ws_fp8_product.hip's.
+template <bool AGPR>
+__device__ __forceinline__ void multiply_f16(f32x4_t& acc, const i32x4_t& fa, const i32x4_t& fb) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (AGPR) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(fb), "v"(fa));
+  else asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(acc) : "v"(fb), "v"(fa));
+#endif
+}
+
+__device__ __forceinline__ uint32_t pack(_Float16 a, _Float16 b) { return __builtin_bit_cast(uint32_t, f16x2_t{a, b}); }
+__device__ __forceinline__ uint32_t pack(bf16_t a, bf16_t b) { return a.bits | (uint32_t)b.bits << 16; }
+
+// Writes 64 x 32 values of a wave, of which lane (r, g) has columns 16 j + 4 g .. of
+// rows 16 i + r, two to a word, by way of its part of LDS.  put(row, column, piece)
+// takes 8 neighbours of a row, or with TURNED of a column.  Pieces of 16 bytes change
+// places within a line, by the line's number, against bank conflicts.
+template <bool TURNED, typename F>
+__device__ __forceinline__ void hand_out(const uint32_t (&v)[4][2][2], uint8_t* own, const F& put) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  constexpr int kPieces = TURNED ? 8 : 4;  // of a line
+  const auto place = [](int line, int piece) { return (line * kPieces + (piece ^ (TURNED ? line & 7 : line >> 1 & 3))) * 16; };
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if constexpr (!TURNED) {
+        *(uint64_t*)(own + place(16 * i + r, 2 * j + g / 2) + g % 2 * 8) = (uint64_t)v[i][j][1] << 32 | v[i][j][0];
+      } else {
+        // with the neighbouring row's: even lanes take columns 0 and 2, odd ones 1 and 3
+        const uint32_t sel = lane & 1 ? 0x03020706u : 0x05040100u;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v[i][j][k], 0xb1, 0xf, 0xf, true);  // quad_perm 1 0 3 2
+          // even: low halves of mine and the other's; odd: high halves of the other's and mine
+          const uint32_t both = __builtin_amdgcn_perm(other, v[i][j][k], sel);
+          *(uint32_t*)(own + place(16 * j + 4 * g + 2 * k + (lane & 1), 2 * i + r / 8) + (r & 6) * 2) = both;
+        }
+      }
+    }
+  __builtin_amdgcn_wave_barrier();  // a wave's LDS accesses keep their order
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int line = e * (64 / kPieces) + lane / kPieces, at = lane % kPieces;
+    put(line, 8 * at, *(const i32x4_t*)(own + place(line, at)));
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// 64 x 32 results of a wave from row m and column n of the product: what the kind of
+// launch makes of the sums, written where they belong.
+template <int KIND>
+__device__ __forceinline__ void finish_part(const OrthArgs& a, f32x4_t* (&acc)[4][2], int64_t matrix, int m, int n, bool twice,
+                                            uint8_t* own) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  uint32_t v[4][2][2];
+  const float* d_in = a.d_in + matrix * a.stride_d;
+  float* d_out = a.d_out + matrix * a.stride_d;
+  const _Float16* old = a.A + matrix * a.stride_a;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int col = n + 16 * j + 4 * g;
+    f32x4_t dn = {0, 0, 0, 0};
+    if constexpr (KIND != kGram) dn = *(const f32x4_t*)(d_in + col);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = m + 16 * i + r;
+      const f32x4_t s = *acc[i][j];
+      float x[4];
+      if constexpr (KIND == kGram) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          x[k] = s[k] * kPerUnit;
+          if (row == col + k) {
+            d_out[row] = x[k] * kPerUnit;
+            x[k] = 0.0f;
+          }
+        }
+      } else if constexpr (KIND == kSquare) {
+        const f16x4_t o = *(const f16x4_t*)(old + (int64_t)row * a.K + col);
+        const float dm = d_in[row];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          // in units of kUnit
+          const float square = fmaf(dm + dn[k], (float)o[k], s[k] * kPerUnit);
+          x[k] = fmaf(kC, square, kB * (float)o[k]);
+          if (row == col + k) {
+            d_out[row] = fmaf(kC, fmaf(dm, dm, square * kPerUnit), fmaf(kB, dm, kA));
+            x[k] = 0.0f;
+          }
+        }
+      } else {
+        const int64_t at = (int64_t)row * a.N + col;
+        _Float16* rest = a.rest + matrix * a.stride_a + at;
+        const f16x4_t hi = *(const f16x4_t*)(old + at), lo = *(const f16x4_t*)rest;
+        f16x4_t left;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          x[k] = fmaf(dn[k], fmaf((float)lo[k], 1.0f / kRest, (float)hi[k]), s[k] * kPerUnit);
+          if constexpr (KIND == kApply) left[k] = (_Float16)((x[k] - (float)(_Float16)x[k]) * kRest);
+        }
+        if constexpr (KIND == kApply) *(f16x4_t*)rest = left;
+      }
+      if constexpr (KIND == kLast) {
+        v[i][j][0] = pack(from_f32<bf16_t>(x[0] * kPerUnit), from_f32<bf16_t>(x[1] * kPerUnit));
+        v[i][j][1] = pack(from_f32<bf16_t>(x[2] * kPerUnit), from_f32<bf16_t>(x[3] * kPerUnit));
+      } else {
+        v[i][j][0] = pack((_Float16)x[0], (_Float16)x[1]);
+        v[i][j][1] = pack((_Float16)x[2], (_Float16)x[3]);
+      }
+    }
+  }
+  if constexpr (KIND == kLast) {
+    uint16_t* out = a.out + matrix * a.stride_out;
+    const auto put = [&](int row, int col, i32x4_t piece) {
+      if (row >= a.rows) return;
+      uint16_t* to = out + (int64_t)row * a.ld_out + col;
+      if (col + 8 <= a.cols) {
+        store_n<bf16_t, 8>((bf16_t*)to, (const bf16_t*)&piece);
+      } else {
+        for (int e = 0; e < 8; ++e)
+          if (col + e < a.cols) to[e] = ((const uint16_t*)&piece)[e];
+      }
+    };
+    if (a.transposed) hand_out<true>(v, own, [&](int line, int at, i32x4_t piece) { put(n + line, m + at, piece); });
+    else hand_out<false>(v, own, [&](int line, int at, i32x4_t piece) { put(m + line, n + at, piece); });
+  } else {
+    _Float16* to = a.to + matrix * a.stride_to;
+    hand_out<false>(v, own, [&](int line, int at, i32x4_t piece) { *(i32x4_t*)(to + (int64_t)(m + line) * a.N + n + at) = piece; });
+    if (twice) {
+      _Float16* mirror = a.mirror + matrix * a.stride_mirror;
+      hand_out<true>(v, own, [&](int line, int at, i32x4_t piece) { *(i32x4_t*)(mirror + (int64_t)(n + line) * a.M + m + at) = piece; });
+    }
+  }
+}
+
+// A tile of 32 WM x 32 WN by four waves, 2 x 2.  Blocks of 64 columns are double-buffered
+// in LDS, and a block's products come in two halves, as in ws_fp8_product.hip:
+//
+//   the first kFirst rows, row by row: the rest of A of block b is read
+//   meet: b + 1 has landed everywhere, b has been read everywhere
+//   the other rows, column by column: b + 2 is loaded over b; the first rows of A
+//   of b + 1 are read, and every column of B of b + 1 once that of b is done
+//
+// The loads of a workgroup's next tile start before the tile it has is written.
+template <int WM, int WN, int KIND>
+__global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_kernel(OrthArgs a) {
+  typedef OrthShape<WM, WN> Shape;
+  constexpr int TM = Shape::TM, TN = Shape::TN, kStage = Shape::kStage, kFirst = Shape::kFirst, kRows = WM - kFirst;
+  constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
+  static_assert(!kSymmetric || TM == TN, "tiles of the lower triangle");
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
+  // an XCD (workgroups go round them in turn) has a run of the tiles
+  const uint32_t tiles = a.plane * (uint32_t)a.batch, xcd = blockIdx.x % 8, share = tiles / 8, extra = tiles % 8;
+  const uint32_t turns = (a.tile_groups + 7 - xcd) / 8, end = xcd * share + min(xcd, extra) + share + (xcd < extra);
+  uint32_t id = xcd * share + min(xcd, extra) + blockIdx.x / 8;
+
+  const uint32_t ld = (uint32_t)a.K * 2;  // bytes between rows of both operands
+  const int lr = 8 * wave + (lane >> 3), lc = chunk_at(lr, lane & 7);
+  const uint32_t at = (uint32_t)lr * ld + lc, step = 32 * ld;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(WSG_LDS uint8_t*)smem + wave * 1024;
+  const int blocks = a.K / 64;
+  constexpr int kLoads = (TM + TN) / 32;  // of a wave and block, 1 KiB each
+  struct Tile {
+    int64_t matrix;
+    int m0, n0;
+    i32x4_t ra, rb;
+  } t;
+  const auto load = [&](int b, int from, int to) {
+    const uint32_t in = b < blocks ? at : kOutside, lds = lds0 + (b & 1) * kStage;  // else zeros
+#pragma unroll
+    for (int i = from; i < to; ++i) {
+      if (i < TM / 32) load_to_lds(t.ra, in + i * step, b * 128, lds + i * 4096);
+      else load_to_lds(t.rb, in + (i - TM / 32) * step, b * 128, lds + i * 4096);
+    }
+  };
+  // Finds tile `id` and starts on its first two blocks.
+  const auto begin_tile = [&]() {
+    const uint32_t matrix = id / a.plane, in = id % a.plane;
+    uint32_t tm, tn;
+    if constexpr (kSymmetric) {  // row after row of the lower triangle
+      tm = (uint32_t)((sqrtf(8.0f * (float)in + 1.0f) - 1.0f) * 0.5f);
+      while (tm * (tm + 1) / 2 > in) --tm;
+      while ((tm + 1) * (tm + 2) / 2 <= in) ++tm;
+      tn = in - tm * (tm + 1) / 2;
+    } else {  // eight rows of tiles at a time
+      const uint32_t wide = 8 * a.tiles_n, first = in / wide * 8, high = min(8u, a.tiles_m - first);
+      tm = first + in % wide % high;
+      tn = in % wide / high;
+    }
+    t.matrix = matrix;
+    t.m0 = __builtin_amdgcn_readfirstlane((int)tm * TM);
+    t.n0 = __builtin_amdgcn_readfirstlane((int)tn * TN);
+    t.ra = raw_buffer((const uint8_t*)(a.A + matrix * a.stride_a + (int64_t)t.m0 * a.K), (uint32_t)min(a.M - t.m0, TM) * ld);
+    t.rb = raw_buffer((const uint8_t*)(a.B + matrix * a.stride_b + (int64_t)t.n0 * a.K), (uint32_t)min(a.N - t.n0, TN) * ld);
+    load(0, 0, kLoads);
+    load(1, 0, kLoads);
+  };
+
+  if (id < end) begin_tile();
+  while (id < end) {
+    f32x4_t acc[WM][WN];
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+      for (int j = 0; j < WN; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
+    const int fa0 = (wm * WM * 16 + r) * 128, fb0 = (TM + wn * WN * 16 + r) * 128, c0 = chunk_at(r, g), c1 = chunk_at(r, g + 4);
+    i32x4_t fa[WM][2], fb[WN][2];
+    const auto frag = [&](i32x4_t (&f)[2], int row, int stage) {
+      const uint8_t* from = smem + stage + row;
+      f[0] = *(const i32x4_t*)(from + c0);
+      f[1] = *(const i32x4_t*)(from + c1);
+    };
+    drain_and_meet();
+#pragma unroll
+    for (int j = 0; j < WN; ++j) frag(fb[j], fb0 + j * 2048, 0);
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i) frag(fa[i], fa0 + i * 2048, 0);
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): in the loop the compiler then counts LDS reads only
+    for (int b = 0; b < blocks; ++b) {
+      const int here = (b & 1) * kStage, next = kStage - here;
+      static_for<kFirst>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        static_for<2 * WN>([&](auto jc) {
+          constexpr int q = decltype(jc)::value / WN, j = decltype(jc)::value % WN, n = i * 2 * WN + decltype(jc)::value;
+          constexpr int all = kFirst * WN;  // slots: the first half of these products
+          multiply_f16<Shape::kAgpr>(acc[i][j], fa[i][q], fb[j][q]);
+          if constexpr (n < all) {
+#pragma unroll
+            for (int k = n * kRows / all; k < (n + 1) * kRows / all; ++k) frag(fa[kFirst + k], fa0 + (kFirst + k) * 2048, here);
+          }
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      drain_and_meet();
+      static_for<WN>([&](auto jc) {
+        constexpr int j = decltype(jc)::value;
+        static_for<2 * kRows>([&](auto ic) {
+          constexpr int q = decltype(ic)::value / kRows, i = kFirst + decltype(ic)::value % kRows;
+          constexpr int n = j * 2 * kRows + decltype(ic)::value, all = 2 * kRows * (WN > 2 ? WN - 1 : WN);
+          multiply_f16<Shape::kAgpr>(acc[i][j], fa[i][q], fb[j][q]);
+          if constexpr (n < all) load(b + 2, n * kLoads / all, (n + 1) * kLoads / all);
+          if constexpr (decltype(ic)::value == 0) {
+#pragma unroll
+            for (int k = j * kFirst / WN; k < (j + 1) * kFirst / WN; ++k) frag(fa[k], fa0 + k * 2048, next);
+            if constexpr (j > 0) frag(fb[j - 1], fb0 + (j - 1) * 2048, next);
+          }
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      frag(fb[WN - 1], fb0 + (WN - 1) * 2048, next);
+    }
+    asm volatile("s_nop 15\n\ts_nop 15");  // the last sums, before anything may move them
+    drain_and_meet();                      // no load of this tile lands, and no wave reads, after this
+    const int64_t matrix = t.matrix;
+    const int m0 = t.m0, n0 = t.n0;
+    id += turns;
+    if (id < end) begin_tile();
+    uint8_t* own = smem + Shape::kStoreAt + wave * Shape::kStoreBytes;
+#pragma unroll
+    for (int ih = 0; ih < WM / 4; ++ih)
+#pragma unroll
+      for (int jh = 0; jh < WN / 2; ++jh) {
+        f32x4_t* part[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            settle<Shape::kAgpr>(acc[4 * ih + i][2 * jh + j]);
+            part[i][j] = &acc[4 * ih + i][2 * jh + j];
+          }
+        const int m = m0 + (wm * WM + 4 * ih) * 16, n = n0 + (wn * WN + 2 * jh) * 16;
+        if (m < a.M && n < a.N)  // sides are multiples of 64
+          finish_part<KIND>(a, part, matrix, m, n, !kSymmetric || m0 != n0, own);
+      }
+  }
+}
+
+// -- the start -------------------------------------------------------------------
+
+struct OrthStartArgs {
+  const void* G;
+  int64_t rows, cols, ld, stride;
+  double* sums;
+  int32_t parts, transposed;  // transposed: Y is G^T, X is G
+  _Float16 *X, *Y, *rest;
+  int64_t n, m;               // padded sides
+};
+
+constexpr int kSumThreads = 256, kMostParts = 64;
+
+__device__ __forceinline__ double sum_of_wave(double x) {
+  for (int d = 32; d; d /= 2) x += __shfl_xor(x, d);
+  return x;
+}
+
+// The sum of squares of a part of a matrix, in binary64: it neither overflows nor loses
+// small gradients.
+template <typename T>
+__global__ __launch_bounds__(kSumThreads) void orth_sum_kernel(OrthStartArgs a) {
+  __shared__ double part[kSumThreads / 64];
+  const int64_t matrix = blockIdx.x / a.parts, p = blockIdx.x % a.parts;
+  const T* G = (const T*)a.G + matrix * a.stride;
+  double sum = 0.0;
+  const int64_t chunks = (a.cols + 7) / 8, all = chunks * a.rows;
+  for (int64_t i = p * kSumThreads + threadIdx.x; i < all; i += (int64_t)a.parts * kSumThreads) {
+    const int64_t c = i % chunks * 8;
+    const T* row = G + i / chunks * a.ld;
+    float v[8];
+    if (c + 8 <= a.cols) {
+      T t[8];
+      if constexpr (sizeof(T) == 4) {
+        load_n<T, 4>(row + c, t);
+        load_n<T, 4>(row + c + 4, t + 4);
+      } else {
+        load_n<T, 8>(row + c, t);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = to_f32(t[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = c + k < a.cols ? to_f32(row[c + k]) : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum = fma((double)v[k], (double)v[k], sum);
+  }
+  sum = sum_of_wave(sum);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kSumThreads / 64; ++w) sum += part[w];
+    a.sums[blockIdx.x] = sum;
+  }
+}
+
+// 64 x 64 values of G, normalised, to X, Y and what they leave; zeros around.
+template <typename T>
+__global__ __launch_bounds__(256) void orth_start_kernel(OrthStartArgs a) {
+  __shared__ float tile[64][65];
+  const int64_t rows = a.transposed ? a.n : a.m, cols = a.transposed ? a.m : a.n;  // padded sides of G
+  const int64_t across = cols / 64, plane = rows / 64 * across, matrix = blockIdx.x / plane, in = blockIdx.x % plane;
+  const int64_t r0 = in / across * 64, c0 = in % across * 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  double sum = lane < a.parts ? a.sums[matrix * a.parts + lane] : 0.0;  // every wave by itself, in the same order
+  sum = sum_of_wave(sum);
+  const double by = sum == 0.0 ? 0.0 : sum > 1.7e308 || sum != sum ? (double)NAN : (double)kUnit / sqrt(sum);
+  const T* G = (const T*)a.G + matrix * a.stride;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int64_t r = r0 + 4 * i + wave, c = c0 + lane;
+    tile[4 * i + wave][lane] = r < a.rows && c < a.cols ? (float)((double)to_f32(G[r * a.ld + c]) * by) : 0.0f;
+  }
+  __syncthreads();
+  _Float16 *X = a.X + matrix * a.n * a.m, *Y = a.Y + matrix * a.n * a.m, *rest = a.rest + matrix * a.n * a.m;
+  // as G lies: Y (with its rest) where G is tall, else X
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = 32 * i + tid / 8, c = tid % 8 * 8;
+    _Float16 hi[8], lo[8], thi[8], tlo[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float x = tile[row][c + k], y = tile[c + k][row];
+      hi[k] = (_Float16)x;
+      lo[k] = (_Float16)((x - (float)hi[k]) * kRest);
+      thi[k] = (_Float16)y;
+      tlo[k] = (_Float16)((y - (float)thi[k]) * kRest);
+    }
+    const int64_t straight = (r0 + row) * cols + c0 + c, turned = (c0 + row) * rows + r0 + c;
+    if (a.transposed) {
+      *(i32x4_t*)(X + straight) = *(const i32x4_t*)hi;
+      *(i32x4_t*)(Y + turned) = *(const i32x4_t*)thi;
+      *(i32x4_t*)(rest + turned) = *(const i32x4_t*)tlo;
+    } else {
+      *(i32x4_t*)(Y + straight) = *(const i32x4_t*)hi;
+      *(i32x4_t*)(rest + straight) = *(const i32x4_t*)lo;
+      *(i32x4_t*)(X + turned) = *(const i32x4_t*)thi;
+    }
+  }
+}
+
+// -- host ---------------------------------------------------------------------
+
+constexpr int64_t kMaxTiles = 1ll << 30;
+
+struct Layout {
+  int64_t n, m;  // padded sides
+  int64_t sums, X, Y0, Y1, rest, S, T, dA, dB, all;
+};
+
+Layout layout(int64_t rows, int64_t cols, int64_t batch) {
+  Layout l{};
+  l.n = ceil_div(rows < cols ? rows : cols, kPad) * kPad;
+  l.m = ceil_div(rows < cols ? cols : rows, kPad) * kPad;
+  const auto take = [&](int64_t bytes) {
+    const int64_t at = l.all;
+    l.all += ceil_div(bytes, 256) * 256;
+    return at;
+  };
+  l.sums = take(batch * kMostParts * 8);
+  l.X = take(batch * l.n * l.m * 2);
+  l.Y0 = take(batch * l.n * l.m * 2);
+  l.Y1 = take(batch * l.n * l.m * 2);
+  l.rest = take(batch * l.n * l.m * 2);
+  l.S = take(batch * l.n * l.n * 2);
+  l.T = take(batch * l.n * l.n * 2);
+  l.dA = take(batch * l.n * 4);
+  l.dB = take(batch * l.n * 4);
+  return l;
+}
+
+bool orth_sizes(int64_t rows, int64_t cols, int64_t batch) {
+  return rows >= 0 && cols >= 0 && batch >= 0 && rows <= WS_ORTHOGONAL_SIDE && cols <= WS_ORTHOGONAL_SIDE && batch <= 1 << 20 &&
+         (rows == 0 || cols == 0 || batch <= kMaxTiles / (ceil_div(rows, 64) * ceil_div(cols, 64)));
+}
+
+template <int WM, int WN, int KIND>
+ws_status run_tiles(OrthArgs a, hipStream_t stream) {
+  typedef OrthShape<WM, WN> Shape;
+  a.tiles_m = (int32_t)ceil_div(a.M, Shape::TM);
+  a.tiles_n = (int32_t)ceil_div(a.N, Shape::TN);
+  a.plane = KIND == kGram || KIND == kSquare ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
+  const int64_t tiles = (int64_t)a.plane * a.batch, most = (int64_t)compute_units() * Shape::kWaves;
+  a.tile_groups = (int32_t)(tiles < most ? tiles : most);
+  const auto kernel = &orth_step_kernel<WM, WN, KIND>;
+  static std::atomic<uint64_t> allowed;  // devices on which the kernel may use this much LDS
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess && (dev >= 64 || !(allowed.load(std::memory_order_acquire) >> dev & 1))) {
+    e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, Shape::kLds);
+    if (e == hipSuccess && dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_acq_rel);
+  }
+  if (e != hipSuccess) return hip_fail("hipFuncSetAttribute", e);
+  return launch("orthogonalize", kernel, a.tile_groups, 256, Shape::kLds, stream, a);
+}
+
+template <int KIND>
+ws_status run_tiles(const OrthArgs& a, hipStream_t stream) {
+  const int64_t big = KIND == kGram || KIND == kSquare ? ceil_div(a.M, 256) * (ceil_div(a.M, 256) + 1) / 2
+                                                       : ceil_div(a.M, 256) * ceil_div(a.N, 256);
+  if (big * a.batch >= 256) return run_tiles<8, 8, KIND>(a, stream);
+  return run_tiles<4, 4, KIND>(a, stream);
+}
+
+}  // namespace
+}  // namespace wsg
+
+using namespace wsg;
+
+extern "C" {
+
+int64_t ws_orthogonal_workspace(int64_t rows, int64_t cols, int32_t batch) {
+  if (!orth_sizes(rows, cols, batch)) return -1;
+  return rows == 0 || cols == 0 || batch == 0 ? 0 : layout(rows, cols, batch).all;
+}
+
+ws_status ws_orthogonalize(const ws_matrix* G, int32_t steps, const ws_matrix* out, void* workspace, int64_t workspace_bytes,
+                           hipStream_t stream) {
+  if (!valid(G, true) || !valid(out, true) || G->rows != out->rows || G->cols != out->cols || G->batch != out->batch ||
+      out->dtype != WS_OUT_BF16 || steps < 1 || steps > WS_ORTHOGONAL_STEPS)
+    return WS_ERR_INVALID_ARG;
+  const int64_t need = ws_orthogonal_workspace(G->rows, G->cols, G->batch);
+  if (need < 0 || workspace_bytes < need || (need > 0 && (!workspace || (uintptr_t)workspace % 256))) return WS_ERR_INVALID_ARG;
+  if (need == 0) return WS_OK;
+  const Layout l = layout(G->rows, G->cols, G->batch);
+  uint8_t* w = (uint8_t*)workspace;
+  OrthStartArgs s{};
+  s.G = G->data;
+  s.rows = G->rows;
+  s.cols = G->cols;
+  s.ld = G->ld;
+  s.stride = G->stride;
+  s.sums = (double*)(w + l.sums);
+  s.transposed = G->rows <= G->cols;
+  s.X = (_Float16*)(w + l.X);
+  s.Y = (_Float16*)(w + l.Y0);
+  s.rest = (_Float16*)(w + l.rest);
+  s.n = l.n;
+  s.m = l.m;
+  const int64_t parts = ceil_div(G->rows * G->cols, 8 * kSumThreads * 4);
+  s.parts = (int32_t)(parts < kMostParts ? parts : kMostParts);
+  const int64_t grid = l.n / 64 * (l.m / 64) * G->batch;
+  if (grid > max_workgroups(256)) return WS_ERR_INVALID_ARG;
+  ws_status st = launch("orthogonalize", G->dtype == WS_OUT_F32 ? &orth_sum_kernel<float> : G->dtype == WS_OUT_BF16 ? &orth_sum_kernel<bf16_t>
+                                                                                                                   : &orth_sum_kernel<f16_t>,
+                        (int64_t)s.parts * G->batch, kSumThreads, 0, stream, s);
+  if (st == WS_OK)
+    st = launch("orthogonalize", G->dtype == WS_OUT_F32 ? &orth_start_kernel<float> : G->dtype == WS_OUT_BF16 ? &orth_start_kernel<bf16_t>
+                                                                                                               : &orth_start_kernel<f16_t>,
+                grid, 256, 0, stream, s);
+  OrthArgs gram{}, square{}, apply{};
+  gram.batch = square.batch = apply.batch = G->batch;
+  gram.A = gram.B = (const _Float16*)(w + l.X);
+  gram.stride_a = gram.stride_b = l.n * l.m;
+  gram.M = gram.N = (int32_t)l.n;
+  gram.K = (int32_t)l.m;
+  gram.to = gram.mirror = (_Float16*)(w + l.S);
+  gram.stride_to = gram.stride_mirror = l.n * l.n;
+  gram.d_out = (float*)(w + l.dA);
+  gram.stride_d = square.stride_d = apply.stride_d = l.n;
+  square.A = square.B = (const _Float16*)(w + l.S);
+  square.stride_a = square.stride_b = l.n * l.n;
+  square.M = square.N = square.K = (int32_t)l.n;
+  square.to = square.mirror = (_Float16*)(w + l.T);
+  square.stride_to = square.stride_mirror = l.n * l.n;
+  square.d_in = (const float*)(w + l.dA);
+  square.d_out = (float*)(w + l.dB);
+  apply.B = (const _Float16*)(w + l.T);
+  apply.stride_a = apply.stride_to = apply.stride_mirror = l.n * l.m;
+  apply.stride_b = l.n * l.n;
+  apply.M = (int32_t)l.m;
+  apply.N = apply.K = (int32_t)l.n;
+  apply.mirror = (_Float16*)(w + l.X);
+  apply.d_in = (const float*)(w + l.dB);
+  apply.rest = (_Float16*)(w + l.rest);
+  apply.out = (uint16_t*)out->data;
+  apply.ld_out = out->ld;
+  apply.stride_out = out->stride;
+  apply.rows = (int32_t)out->rows;
+  apply.cols = (int32_t)out->cols;
+  apply.transposed = s.transposed;
+  for (int i = 0; i < steps && st == WS_OK; ++i) {
+    st = run_tiles<kGram>(gram, stream);
+    if (st == WS_OK) st = run_tiles<kSquare>(square, stream);
+    apply.A = (const _Float16*)(w + (i & 1 ? l.Y1 : l.Y0));
+    apply.to = (_Float16*)(w + (i & 1 ? l.Y0 : l.Y1));
+    if (st == WS_OK) st = i + 1 < steps ? run_tiles<kApply>(apply, stream) : run_tiles<kLast>(apply, stream);
+  }
+  return st;
+}
+
+}  // extern "C"

@@ -1,0 +1,22 @@
+"""Wait states around the hand-placed matrix instructions of the orthogonalised
+update's kernels, read from the built library's machine code (CPU only)."""
+import os
+
+import pytest
+
+from tests.test_product_isa import check
+from tests.test_signal_waits_isa import LIB, OBJDUMP, library_code  # noqa: F401  (a fixture)
+
+
+@pytest.mark.skipif(not os.path.exists(LIB), reason="library not built")
+@pytest.mark.skipif(not os.path.exists(OBJDUMP), reason="llvm-objdump not found")
+def test_step_kernels_keep_their_wait_states(library_code):  # noqa: F811
+    kernels, problems = 0, []
+    for name, start, ins in library_code:
+        if "orth_step_kernel" not in name:
+            continue
+        kernels += 1
+        assert sum(mn == "v_mfma_f32_16x16x32_f16" for _, mn, _, _ in ins) >= 16
+        problems += [(name[-40:],) + b for b in check(start, ins)]
+    assert kernels >= 8
+    assert not problems, problems[:20]
