@@ -26,10 +26,9 @@ namespace {
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kUnit = 16384.0f, kPerUnit = 1.0f / kUnit;  // of X, S and T
 constexpr float kRest = 2048.0f;                            // of the rest of X, beyond
-constexpr int kPad = 64;                                    // sides in the workspace are multiples of it
+constexpr int kPad = 128;                                    // sides in the workspace are multiples of it: blocks of 64 columns are even in number
 
-typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 enum Kind { kGram, kSquare, kApply, kLast };
 
@@ -59,9 +58,31 @@ struct OrthShape {
   static constexpr int kFirst = WM > 4 ? 3 : WM / 2;
   // a wave's way to memory: 64 x 32 results
   static constexpr int kStoreBytes = 64 * 32 * 2;
-  static constexpr int kStoreAt = 2 * kStage, kLds = kStoreAt + 4 * kStoreBytes;
+  // Lines of later blocks are asked for ahead by loads that end here, 256 bytes a wave.
+  static constexpr bool kAhead = kWaves == 1;
+  static constexpr int kStoreAt = 2 * kStage, kAheadAt = kStoreAt + 4 * kStoreBytes, kLds = kAheadAt + (kAhead ? 4 * 256 : 0);
   static_assert(kWaves * kLds <= 160 * 1024, "LDS of a CU");
 };
+
+// One of two descriptors, as scalars.
+__device__ __forceinline__ i32x4_t select(bool first, const i32x4_t& a, const i32x4_t& b) {
+  i32x4_t r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(first ? a[i] : b[i]);
+  return r;
+}
+
+// Loads 4 bytes a lane from buffer offsets `at` + k to LDS at `to`, for what that leaves
+// in the L2; see load_to_lds.
+__device__ __forceinline__ void touch(i32x4_t r, uint32_t at, uint32_t k, uint32_t to) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile(
+      "s_mov_b32 m0, %3\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dword %0, %1, %2 offen lds" ::"v"(at),
+      "s"(r), "s"(__builtin_amdgcn_readfirstlane(k)), "s"(__builtin_amdgcn_readfirstlane(to)));
+#endif
+}
 
 // acc += A's 16 rows times B's 16 rows over 32 columns; see ws_fp8_product.hip's.
 template <bool AGPR>
@@ -72,108 +93,127 @@ __device__ __forceinline__ void multiply_f16(f32x4_t& acc, const i32x4_t& fa, co
 #endif
 }
 
-__device__ __forceinline__ uint32_t pack(_Float16 a, _Float16 b) { return __builtin_bit_cast(uint32_t, f16x2_t{a, b}); }
-__device__ __forceinline__ uint32_t pack(bf16_t a, bf16_t b) { return a.bits | (uint32_t)b.bits << 16; }
+// Byte position, in a row of 128, of chunk c of row r of B's half of a stage.  B's rows
+// are read in an order that gives a lane eight neighbouring columns of the product
+// (row_of_b); the position follows that order against bank conflicts.
+__device__ __forceinline__ int chunk_of_b(int r, int c) { return (c ^ (r & 3 | (r >> 3 & 1) << 2)) * 16; }
+// Row, of 32, that lane r % 16 has of the j-th of two fragments of B: the lanes 4 g ..
+// 4 g + 3 of both hold rows 8 g .. 8 g + 7.
+__device__ __forceinline__ int row_of_b(int r, int j) { return 8 * (r >> 2) + 4 * j + (r & 3); }
 
-// Writes 64 x 32 values of a wave, of which lane (r, g) has columns 16 j + 4 g .. of
-// rows 16 i + r, two to a word, by way of its part of LDS.  put(row, column, piece)
-// takes 8 neighbours of a row, or with TURNED of a column.  Pieces of 16 bytes change
-// places within a line, by the line's number, against bank conflicts.
-template <bool TURNED, typename F>
-__device__ __forceinline__ void hand_out(const uint32_t (&v)[4][2][2], uint8_t* own, const F& put) {
+// Writes 64 x 32 values of a wave, of which lane (r, g) has columns 8 g .. of rows 16 i
+// + r, two to a word, turned round by way of its part of LDS: put(column, row, piece)
+// takes 8 neighbours of a column.  Pieces of 16 bytes change places within a line, by
+// the line's number, against bank conflicts.
+template <typename F>
+__device__ __forceinline__ void turn_round(const i32x4_t (&v)[4], uint8_t* own, const F& put) {
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  constexpr int kPieces = TURNED ? 8 : 4;  // of a line
-  const auto place = [](int line, int piece) { return (line * kPieces + (piece ^ (TURNED ? line & 7 : line >> 1 & 3))) * 16; };
+  const auto place = [](int line, int piece) { return (line * 8 + (piece ^ (line & 7))) * 16; };
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      if constexpr (!TURNED) {
-        *(uint64_t*)(own + place(16 * i + r, 2 * j + g / 2) + g % 2 * 8) = (uint64_t)v[i][j][1] << 32 | v[i][j][0];
-      } else {
-        // with the neighbouring row's: even lanes take columns 0 and 2, odd ones 1 and 3
-        const uint32_t sel = lane & 1 ? 0x03020706u : 0x05040100u;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v[i][j][k], 0xb1, 0xf, 0xf, true);  // quad_perm 1 0 3 2
-          // even: low halves of mine and the other's; odd: high halves of the other's and mine
-          const uint32_t both = __builtin_amdgcn_perm(other, v[i][j][k], sel);
-          *(uint32_t*)(own + place(16 * j + 4 * g + 2 * k + (lane & 1), 2 * i + r / 8) + (r & 6) * 2) = both;
-        }
-      }
+    for (int k = 0; k < 4; ++k) {
+      // with the neighbouring row's: even lanes take the first column of a word, odd ones the second
+      const uint32_t mine = (uint32_t)v[i][k], other = (uint32_t)__builtin_amdgcn_update_dpp(0, v[i][k], 0xb1, 0xf, 0xf, true);  // quad_perm 1 0 3 2
+      const uint32_t both = __builtin_amdgcn_perm(other, mine, lane & 1 ? 0x03020706u : 0x05040100u);
+      *(uint32_t*)(own + place(8 * g + 2 * k + (lane & 1), 2 * i + r / 8) + (r & 6) * 2) = both;
     }
   __builtin_amdgcn_wave_barrier();  // a wave's LDS accesses keep their order
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const int line = e * (64 / kPieces) + lane / kPieces, at = lane % kPieces;
+    const int line = 8 * e + lane / 8, at = lane % 8;
     put(line, 8 * at, *(const i32x4_t*)(own + place(line, at)));
   }
   __builtin_amdgcn_wave_barrier();
 }
 
-// 64 x 32 results of a wave from row m and column n of the product: what the kind of
-// launch makes of the sums, written where they belong.
+// What half a part of a tile's results needs from memory: 32 x 32 values from row m and
+// column n, lane (r, g) columns 8 g .. of rows 16 i + r.
 template <int KIND>
-__device__ __forceinline__ void finish_part(const OrthArgs& a, f32x4_t* (&acc)[4][2], int64_t matrix, int m, int n, bool twice,
-                                            uint8_t* own) {
-  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  uint32_t v[4][2][2];
-  const float* d_in = a.d_in + matrix * a.stride_d;
-  float* d_out = a.d_out + matrix * a.stride_d;
-  const _Float16* old = a.A + matrix * a.stride_a;
+struct Old {
+  f16x8_t value[2], rest[2];  // kSquare: S; kApply, kLast: Y
+  f32x4_t dn[2];
+  float dm[2];
+};
+template <int KIND>
+__device__ __forceinline__ void fetch(const OrthArgs& a, int64_t matrix, int m, int n, Old<KIND>& o) {
+  const int lane = threadIdx.x & 63, row = m + (lane & 15), col = n + 8 * (lane >> 4);
+  if constexpr (KIND != kGram) {
+    const float* d_in = a.d_in + matrix * a.stride_d;
+    o.dn[0] = *(const f32x4_t*)(d_in + col);
+    o.dn[1] = *(const f32x4_t*)(d_in + col + 4);
+    const int64_t at = matrix * a.stride_a + (int64_t)row * a.K + col;  // kApply, kLast: N == K
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int col = n + 16 * j + 4 * g;
-    f32x4_t dn = {0, 0, 0, 0};
-    if constexpr (KIND != kGram) dn = *(const f32x4_t*)(d_in + col);
+    for (int i = 0; i < 2; ++i) {
+      o.value[i] = *(const f16x8_t*)(a.A + at + 16 * i * a.K);
+      if constexpr (KIND == kSquare) o.dm[i] = d_in[row + 16 * i];
+      else o.rest[i] = *(const f16x8_t*)(a.rest + at + 16 * i * a.K);
+    }
+  }
+}
+
+// What the kind of launch makes of the sums of 32 x 32 results from row m and column n;
+// the rest of X is written at once.
+template <int KIND>
+__device__ __forceinline__ void convert(const OrthArgs& a, const f32x4_t* (&acc)[2][2], const Old<KIND>& o, int64_t matrix, int m,
+                                        int n, i32x4_t* v) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, col = n + 8 * g;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = m + 16 * i + r;
-      const f32x4_t s = *acc[i][j];
-      float x[4];
+  for (int i = 0; i < 2; ++i) {
+    const int row = m + 16 * i + r;
+    float x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float s = (*acc[i][k / 4])[k % 4] * kPerUnit;
       if constexpr (KIND == kGram) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          x[k] = s[k] * kPerUnit;
-          if (row == col + k) {
-            d_out[row] = x[k] * kPerUnit;
-            x[k] = 0.0f;
-          }
-        }
-      } else if constexpr (KIND == kSquare) {
-        const f16x4_t o = *(const f16x4_t*)(old + (int64_t)row * a.K + col);
-        const float dm = d_in[row];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          // in units of kUnit
-          const float square = fmaf(dm + dn[k], (float)o[k], s[k] * kPerUnit);
-          x[k] = fmaf(kC, square, kB * (float)o[k]);
-          if (row == col + k) {
-            d_out[row] = fmaf(kC, fmaf(dm, dm, square * kPerUnit), fmaf(kB, dm, kA));
-            x[k] = 0.0f;
-          }
-        }
+        x[k] = s;
+      } else if constexpr (KIND == kSquare) {  // in units of kUnit
+        const float square = fmaf(o.dm[i] + o.dn[k / 4][k % 4], (float)o.value[i][k], s);
+        x[k] = fmaf(kC, square, kB * (float)o.value[i][k]);
       } else {
-        const int64_t at = (int64_t)row * a.N + col;
-        _Float16* rest = a.rest + matrix * a.stride_a + at;
-        const f16x4_t hi = *(const f16x4_t*)(old + at), lo = *(const f16x4_t*)rest;
-        f16x4_t left;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          x[k] = fmaf(dn[k], fmaf((float)lo[k], 1.0f / kRest, (float)hi[k]), s[k] * kPerUnit);
-          if constexpr (KIND == kApply) left[k] = (_Float16)((x[k] - (float)(_Float16)x[k]) * kRest);
-        }
-        if constexpr (KIND == kApply) *(f16x4_t*)rest = left;
+        x[k] = fmaf(o.dn[k / 4][k % 4], fmaf((float)o.rest[i][k], 1.0f / kRest, (float)o.value[i][k]), s);
       }
-      if constexpr (KIND == kLast) {
-        v[i][j][0] = pack(from_f32<bf16_t>(x[0] * kPerUnit), from_f32<bf16_t>(x[1] * kPerUnit));
-        v[i][j][1] = pack(from_f32<bf16_t>(x[2] * kPerUnit), from_f32<bf16_t>(x[3] * kPerUnit));
-      } else {
-        v[i][j][0] = pack((_Float16)x[0], (_Float16)x[1]);
-        v[i][j][1] = pack((_Float16)x[2], (_Float16)x[3]);
+    }
+    if constexpr (KIND == kGram || KIND == kSquare) {
+      if (m + 32 > n && n + 32 > m) {  // the diagonal is near
+        float* d_out = a.d_out + matrix * a.stride_d;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (row == col + k) {
+            if constexpr (KIND == kGram) {
+              d_out[row] = x[k] * kPerUnit;
+            } else {  // S is zero there
+              d_out[row] = fmaf(kC, fmaf(o.dm[i], o.dm[i], (*acc[i][k / 4])[k % 4] * (kPerUnit * kPerUnit)), fmaf(kB, o.dm[i], kA));
+            }
+            x[k] = 0.0f;
+          }
+      }
+    }
+    if constexpr (KIND == kLast) {
+      bf16_t t[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) t[k] = from_f32<bf16_t>(x[k] * kPerUnit);
+      __builtin_memcpy(&v[i], t, 16);
+    } else {
+      f16x8_t t;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) t[k] = (_Float16)x[k];
+      v[i] = __builtin_bit_cast(i32x4_t, t);
+      if constexpr (KIND == kApply) {
+        f16x8_t left;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) left[k] = (_Float16)((x[k] - (float)t[k]) * kRest);
+        *(f16x8_t*)(a.rest + matrix * a.stride_a + (int64_t)row * a.N + col) = left;
       }
     }
   }
+}
+
+// Writes 64 x 32 converted results of a wave from row m and column n where they belong.
+template <int KIND>
+__device__ __forceinline__ void write_part(const OrthArgs& a, const i32x4_t (&v)[4], int64_t matrix, int m, int n, bool twice,
+                                           uint8_t* own) {
+  const int lane = threadIdx.x & 63, r = lane & 15, col = n + 8 * (lane >> 4);
   if constexpr (KIND == kLast) {
     uint16_t* out = a.out + matrix * a.stride_out;
     const auto put = [&](int row, int col, i32x4_t piece) {
@@ -186,14 +226,19 @@ __device__ __forceinline__ void finish_part(const OrthArgs& a, f32x4_t* (&acc)[4
           if (col + e < a.cols) to[e] = ((const uint16_t*)&piece)[e];
       }
     };
-    if (a.transposed) hand_out<true>(v, own, [&](int line, int at, i32x4_t piece) { put(n + line, m + at, piece); });
-    else hand_out<false>(v, own, [&](int line, int at, i32x4_t piece) { put(m + line, n + at, piece); });
+    if (a.transposed) {
+      turn_round(v, own, [&](int line, int at, i32x4_t piece) { put(n + line, m + at, piece); });
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) put(m + 16 * i + r, col, v[i]);
+    }
   } else {
-    _Float16* to = a.to + matrix * a.stride_to;
-    hand_out<false>(v, own, [&](int line, int at, i32x4_t piece) { *(i32x4_t*)(to + (int64_t)(m + line) * a.N + n + at) = piece; });
+    _Float16* to = a.to + matrix * a.stride_to + (int64_t)(m + r) * a.N + col;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *(i32x4_t*)(to + 16 * i * (int64_t)a.N) = v[i];
     if (twice) {
       _Float16* mirror = a.mirror + matrix * a.stride_mirror;
-      hand_out<true>(v, own, [&](int line, int at, i32x4_t piece) { *(i32x4_t*)(mirror + (int64_t)(n + line) * a.M + m + at) = piece; });
+      turn_round(v, own, [&](int line, int at, i32x4_t piece) { *(i32x4_t*)(mirror + (int64_t)(n + line) * a.M + m + at) = piece; });
     }
   }
 }
@@ -206,7 +251,8 @@ __device__ __forceinline__ void finish_part(const OrthArgs& a, f32x4_t* (&acc)[4
 //   the other rows, column by column: b + 2 is loaded over b; the first rows of A
 //   of b + 1 are read, and every column of B of b + 1 once that of b is done
 //
-// The loads of a workgroup's next tile start before the tile it has is written.
+// Loads go on into a workgroup's next tile, whose first two blocks are there when the
+// tile it has is written.
 template <int WM, int WN, int KIND>
 __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_kernel(OrthArgs a) {
   typedef OrthShape<WM, WN> Shape;
@@ -222,26 +268,19 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
   uint32_t id = xcd * share + min(xcd, extra) + blockIdx.x / 8;
 
   const uint32_t ld = (uint32_t)a.K * 2;  // bytes between rows of both operands
-  const int lr = 8 * wave + (lane >> 3), lc = chunk_at(lr, lane & 7);
-  const uint32_t at = (uint32_t)lr * ld + lc, step = 32 * ld;
+  const int lr = 8 * wave + (lane >> 3);  // chunk_at and chunk_of_b are their own inverses
+  const uint32_t at_a = (uint32_t)lr * ld + chunk_at(lr, lane & 7), at_b = (uint32_t)lr * ld + chunk_of_b(lr, lane & 7), step = 32 * ld;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(WSG_LDS uint8_t*)smem + wave * 1024;
-  const int blocks = a.K / 64;
+  const int blocks = a.K / 64;  // even
   constexpr int kLoads = (TM + TN) / 32;  // of a wave and block, 1 KiB each
   struct Tile {
     int64_t matrix;
     int m0, n0;
     i32x4_t ra, rb;
-  } t;
-  const auto load = [&](int b, int from, int to) {
-    const uint32_t in = b < blocks ? at : kOutside, lds = lds0 + (b & 1) * kStage;  // else zeros
-#pragma unroll
-    for (int i = from; i < to; ++i) {
-      if (i < TM / 32) load_to_lds(t.ra, in + i * step, b * 128, lds + i * 4096);
-      else load_to_lds(t.rb, in + (i - TM / 32) * step, b * 128, lds + i * 4096);
-    }
-  };
-  // Finds tile `id` and starts on its first two blocks.
-  const auto begin_tile = [&]() {
+    uint32_t ahead_a, ahead_b;  // rows of the tile that this workgroup asks for ahead
+  } t, later;
+  // Where tile `id` lies; past the last one: nowhere, which reads zeros.
+  const auto find_tile = [&](Tile& t, uint32_t id) {
     const uint32_t matrix = id / a.plane, in = id % a.plane;
     uint32_t tm, tn;
     if constexpr (kSymmetric) {  // row after row of the lower triangle
@@ -254,34 +293,65 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
       tm = first + in % wide % high;
       tn = in % wide / high;
     }
-    t.matrix = matrix;
-    t.m0 = __builtin_amdgcn_readfirstlane((int)tm * TM);
-    t.n0 = __builtin_amdgcn_readfirstlane((int)tn * TN);
-    t.ra = raw_buffer((const uint8_t*)(a.A + matrix * a.stride_a + (int64_t)t.m0 * a.K), (uint32_t)min(a.M - t.m0, TM) * ld);
-    t.rb = raw_buffer((const uint8_t*)(a.B + matrix * a.stride_b + (int64_t)t.n0 * a.K), (uint32_t)min(a.N - t.n0, TN) * ld);
-    load(0, 0, kLoads);
-    load(1, 0, kLoads);
+    const bool there = id < end;
+    t.matrix = there ? matrix : 0;
+    t.m0 = __builtin_amdgcn_readfirstlane(there ? (int)tm * TM : 0);
+    t.n0 = __builtin_amdgcn_readfirstlane(there ? (int)tn * TN : 0);
+    t.ra = raw_buffer((const uint8_t*)(a.A + t.matrix * a.stride_a + (int64_t)t.m0 * a.K), there ? (uint32_t)min(a.M - t.m0, TM) * ld : 0);
+    t.rb = raw_buffer((const uint8_t*)(a.B + t.matrix * a.stride_b + (int64_t)t.n0 * a.K), there ? (uint32_t)min(a.N - t.n0, TN) * ld : 0);
+    t.ahead_a = tn % 4 * 64;
+    t.ahead_b = tm % 8 * 32;
+  };
+  // Loads `from` .. `to` of a block, which may be one of the next tile's first.
+  const auto load = [&](int b, int from, int to) {
+    const bool here = b < blocks;
+    const int k = (here ? b : b - blocks) * 128;
+    const uint32_t lds = lds0 + (b & 1) * kStage;
+    const i32x4_t ra = select(here, t.ra, later.ra), rb = select(here, t.rb, later.rb);
+#pragma unroll
+    for (int i = from; i < to; ++i) {
+      if (i < TM / 32) load_to_lds(ra, at_a + i * step, k, lds + i * 4096);
+      else load_to_lds(rb, at_b + (i - TM / 32) * step, k, lds + i * 4096);
+    }
+  };
+  // Asks for lines of a block, so that they are in the L2 when they are loaded: 32 rows
+  // a wave of those that the tiles beside this one share, waves 0 and 1 of A, 2 of B.
+  const auto ask_ahead = [&](int b) {
+    const bool here = b < blocks;
+    const int k = (here ? b : b - blocks) * 128;
+    const uint32_t row = wave < 2 ? (here ? t.ahead_a : later.ahead_a) + 32 * wave + lane : (here ? t.ahead_b : later.ahead_b) + lane;
+    const i32x4_t ra = select(here, t.ra, later.ra), rb = select(here, t.rb, later.rb);
+    touch(select(wave < 2, ra, rb), lane < 32 && wave < 3 && b < 2 * blocks ? row * ld : kOutside, k,
+          (uint32_t)(uintptr_t)(WSG_LDS uint8_t*)smem + Shape::kAheadAt + wave * 256);
   };
 
-  if (id < end) begin_tile();
-  while (id < end) {
+  if (id >= end) return;
+  find_tile(t, id);
+  load(0, 0, kLoads);
+  load(1, 0, kLoads);
+  drain_and_meet();
+  for (; id < end; id += turns) {
+    find_tile(later, id + turns);
     f32x4_t acc[WM][WN];
 #pragma unroll
     for (int i = 0; i < WM; ++i)
 #pragma unroll
       for (int j = 0; j < WN; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
-    const int fa0 = (wm * WM * 16 + r) * 128, fb0 = (TM + wn * WN * 16 + r) * 128, c0 = chunk_at(r, g), c1 = chunk_at(r, g + 4);
+    const int fa0 = (wm * WM * 16 + r) * 128, a0 = fa0 + chunk_at(r, g), a1 = fa0 + chunk_at(r, g + 4);
+    const int fb0 = (TM + wn * WN * 16 + row_of_b(r, 0)) * 128, b0 = fb0 + chunk_of_b(row_of_b(r, 0), g), b1 = fb0 + chunk_of_b(row_of_b(r, 0), g + 4);
     i32x4_t fa[WM][2], fb[WN][2];
-    const auto frag = [&](i32x4_t (&f)[2], int row, int stage) {
-      const uint8_t* from = smem + stage + row;
-      f[0] = *(const i32x4_t*)(from + c0);
-      f[1] = *(const i32x4_t*)(from + c1);
+    const auto frag_a = [&](int i, int stage) {
+      fa[i][0] = *(const i32x4_t*)(smem + stage + a0 + i * 2048);
+      fa[i][1] = *(const i32x4_t*)(smem + stage + a1 + i * 2048);
     };
-    drain_and_meet();
+    const auto frag_b = [&](int j, int stage) {
+      fb[j][0] = *(const i32x4_t*)(smem + stage + b0 + j / 2 * 4096 + j % 2 * 512);
+      fb[j][1] = *(const i32x4_t*)(smem + stage + b1 + j / 2 * 4096 + j % 2 * 512);
+    };
 #pragma unroll
-    for (int j = 0; j < WN; ++j) frag(fb[j], fb0 + j * 2048, 0);
+    for (int j = 0; j < WN; ++j) frag_b(j, 0);
 #pragma unroll
-    for (int i = 0; i < kFirst; ++i) frag(fa[i], fa0 + i * 2048, 0);
+    for (int i = 0; i < kFirst; ++i) frag_a(i, 0);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): in the loop the compiler then counts LDS reads only
     for (int b = 0; b < blocks; ++b) {
       const int here = (b & 1) * kStage, next = kStage - here;
@@ -293,12 +363,12 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
           multiply_f16<Shape::kAgpr>(acc[i][j], fa[i][q], fb[j][q]);
           if constexpr (n < all) {
 #pragma unroll
-            for (int k = n * kRows / all; k < (n + 1) * kRows / all; ++k) frag(fa[kFirst + k], fa0 + (kFirst + k) * 2048, here);
+            for (int k = n * kRows / all; k < (n + 1) * kRows / all; ++k) frag_a(kFirst + k, here);
           }
         });
         __builtin_amdgcn_sched_barrier(0);
       });
-      drain_and_meet();
+      drain_and_meet<Shape::kAhead ? 1 : 0>();  // all but the lines asked for
       static_for<WN>([&](auto jc) {
         constexpr int j = decltype(jc)::value;
         static_for<2 * kRows>([&](auto ic) {
@@ -308,37 +378,50 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
           if constexpr (n < all) load(b + 2, n * kLoads / all, (n + 1) * kLoads / all);
           if constexpr (decltype(ic)::value == 0) {
 #pragma unroll
-            for (int k = j * kFirst / WN; k < (j + 1) * kFirst / WN; ++k) frag(fa[k], fa0 + k * 2048, next);
-            if constexpr (j > 0) frag(fb[j - 1], fb0 + (j - 1) * 2048, next);
+            for (int k = j * kFirst / WN; k < (j + 1) * kFirst / WN; ++k) frag_a(k, next);
+            if constexpr (j > 0) frag_b(j - 1, next);
           }
         });
         __builtin_amdgcn_sched_barrier(0);
       });
-      frag(fb[WN - 1], fb0 + (WN - 1) * 2048, next);
+      frag_b(WN - 1, next);
+      if constexpr (Shape::kAhead) ask_ahead(b + 4);
     }
     asm volatile("s_nop 15\n\ts_nop 15");  // the last sums, before anything may move them
-    drain_and_meet();                      // no load of this tile lands, and no wave reads, after this
     const int64_t matrix = t.matrix;
     const int m0 = t.m0, n0 = t.n0;
-    id += turns;
-    if (id < end) begin_tile();
+    t = later;
     uint8_t* own = smem + Shape::kStoreAt + wave * Shape::kStoreBytes;
+    // parts of 64 x 32; what the next half of one needs is fetched before a half is converted
+    constexpr int kParts = WM / 4 * (WN / 2);
+    const auto place = [&](int p, int* m, int* n) {
+      *m = m0 + (wm * WM + p / (WN / 2) * 4) * 16;
+      *n = n0 + (wn * WN + p % (WN / 2) * 2) * 16;
+      return *m < a.M && *n < a.N;  // sides are multiples of 64
+    };
+    Old<KIND> old[2];
+    i32x4_t v[4];
+    int m, n;
+    if (place(0, &m, &n)) fetch<KIND>(a, matrix, m, n, old[0]);
+    static_for<2 * kParts>([&](auto hc) {
+      constexpr int h = decltype(hc)::value, p = h / 2;
+      if constexpr (h + 1 < 2 * kParts)
+        if (place((h + 1) / 2, &m, &n)) fetch<KIND>(a, matrix, m + (h + 1) % 2 * 32, n, old[(h + 1) % 2]);
+      const f32x4_t* part[2][2];
 #pragma unroll
-    for (int ih = 0; ih < WM / 4; ++ih)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int jh = 0; jh < WN / 2; ++jh) {
-        f32x4_t* part[4][2];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            settle<Shape::kAgpr>(acc[4 * ih + i][2 * jh + j]);
-            part[i][j] = &acc[4 * ih + i][2 * jh + j];
-          }
-        const int m = m0 + (wm * WM + 4 * ih) * 16, n = n0 + (wn * WN + 2 * jh) * 16;
-        if (m < a.M && n < a.N)  // sides are multiples of 64
-          finish_part<KIND>(a, part, matrix, m, n, !kSymmetric || m0 != n0, own);
+        for (int j = 0; j < 2; ++j) {
+          f32x4_t& s = acc[p / (WN / 2) * 4 + h % 2 * 2 + i][p % (WN / 2) * 2 + j];
+          settle<Shape::kAgpr>(s);
+          part[i][j] = &s;
+        }
+      if (place(p, &m, &n)) {
+        convert<KIND>(a, part, old[h % 2], matrix, m + h % 2 * 32, n, v + h % 2 * 2);
+        if constexpr (h % 2 == 1) write_part<KIND>(a, v, matrix, m, n, !kSymmetric || m0 != n0, own);
       }
+      __builtin_amdgcn_sched_barrier(0);
+    });
   }
 }
 
