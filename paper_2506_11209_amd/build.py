@@ -35,7 +35,7 @@ HIP_FLAGS = [
 
 # The 8-bit path and the routing of tokens to experts (ws_fp8.h, ws_experts.h).
 OPERATOR_SOURCES = ["ws_fp8_product.hip", "ws_fp8_quantize.hip", "ws_experts.hip", "ws_choose.hip", "ws_fp4.hip",
-                    "ws_orthogonal.hip"]
+                    "ws_orthogonal.hip", "ws_orthogonal_few.hip"]
 
 # Kernel modes (KernelMode in ws_gemm_kernel.hpp): the GEMM and the
 # calibration kernels of the performance model.

@@ -17,7 +17,7 @@
 // few directions dominate G, rounding X alone cost 6e-3 in the others.
 #include <math.h>
 
-#include "ws_orthogonal.h"
+#include "ws_orthogonal.hpp"
 #include "ws_tile.hpp"
 
 namespace wsg {
@@ -599,7 +599,11 @@ extern "C" {
 
 int64_t ws_orthogonal_workspace(int64_t rows, int64_t cols, int32_t batch) {
   if (!orth_sizes(rows, cols, batch)) return -1;
-  return rows == 0 || cols == 0 || batch == 0 ? 0 : layout(rows, cols, batch).all;
+  if (rows == 0 || cols == 0 || batch == 0) return 0;
+  const int64_t tiles = layout(rows, cols, batch).all;
+  if ((rows < cols ? rows : cols) > kFewRows) return tiles;
+  const int64_t few = few_workspace(rows, cols, batch);  // which of them runs depends on the steps
+  return few > tiles ? few : tiles;
 }
 
 ws_status ws_orthogonalize(const ws_matrix* G, int32_t steps, const ws_matrix* out, void* workspace, int64_t workspace_bytes,
@@ -610,6 +614,7 @@ ws_status ws_orthogonalize(const ws_matrix* G, int32_t steps, const ws_matrix* o
   const int64_t need = ws_orthogonal_workspace(G->rows, G->cols, G->batch);
   if (need < 0 || workspace_bytes < need || (need > 0 && (!workspace || (uintptr_t)workspace % 256))) return WS_ERR_INVALID_ARG;
   if (need == 0) return WS_OK;
+  if (by_gram_matrix(G->rows, G->cols, steps)) return orthogonalize_few(G, steps, out, workspace, stream);
   const Layout l = layout(G->rows, G->cols, G->batch);
   uint8_t* w = (uint8_t*)workspace;
   OrthStartArgs s{};
