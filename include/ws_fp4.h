@@ -8,12 +8,14 @@
  * row.  Powers of two, as in ws_fp8.h: scaling by them rounds nothing, and gfx950
  * widens codes to bf16 with the scale in one instruction, exactly.
  *
- * A matrix in 4 bits (ws_fp4_matrix) has columns padded with zero codes to a multiple
- * of 128.  128 columns of a row are 64 bytes: byte 16 g + 4 i + b holds columns
- * 32 i + 8 g + 2 b (low half) and 32 i + 8 g + 2 b + 1 (high half), g, i and b from 0
- * to 3, so that a lane's 16 bytes are its operands of four matrix instructions.
- * The scale of columns 32 j .. 32 j + 31 of row r is scales[r * ld_scales + j]; those
- * of padding are 1.
+ * A matrix in 4 bits (ws_fp4_matrix) lies in tiles of 16 rows by 128 columns, so that
+ * a product reads 1 KiB of codes and 64 bytes of scales in one piece each: rows padded to
+ * a multiple of 16 and columns to one of 128, with zero codes and scales of 1.  Tile j
+ * of 16 rows i has its codes at codes + i * ld + 1024 j: byte 256 g + 16 r + 4 k + b
+ * holds columns 32 k + 8 g + 2 b (low half) and 32 k + 8 g + 2 b + 1 (high half) of the
+ * tile's row r; g, k and b go from 0 to 3 (a lane's 16 bytes are its operands of four
+ * matrix instructions).  Its scales are at scales + i * ld_scales + 64 j: byte 4 r + k
+ * for columns 32 k .. 32 k + 31 of row r.
  *
  * Rounding of a block: amax is its largest |x|, the scale is the smallest power of two s
  * with amax <= 6 s (1 for amax = 0; at least 2^-127; at most 2^125, whose multiples
@@ -38,8 +40,8 @@ typedef struct {
   void* codes;            /* 16-byte aligned */
   uint8_t* scales;        /* 4-byte aligned */
   int64_t rows, cols;
-  int64_t ld;             /* bytes between rows: a multiple of 16, at least 64 ceil(cols / 128) */
-  int64_t ld_scales;      /* bytes between the scales of rows: a multiple of 4, at least 4 ceil(cols / 128) */
+  int64_t ld;             /* bytes between 16 rows and the next: a multiple of 16, at least 1024 ceil(cols / 128) */
+  int64_t ld_scales;      /* the same of scales: a multiple of 4, at least 64 ceil(cols / 128) */
   int32_t batch;          /* matrices of one size (weights of experts); 0 as in ws_fp8_matrix */
   int64_t stride_codes;   /* between them: a multiple of 16; they do not overlap */
   int64_t stride_scales;  /* a multiple of 4 */

@@ -27,15 +27,8 @@ struct Fp4CastArgs {
   void* out;
   uint8_t *codes, *scales;
   int64_t rows, cols, ld_w, ld, ld_scales, stride_w, stride_codes, stride_scales;
-  int64_t units, per_row;  // 128 columns of a row are a unit
+  int64_t tiles, down, across;  // of all matrices; of a matrix
 };
-
-// Largest over the 4 lanes of a quad, in all of them.
-__device__ __forceinline__ uint32_t max_quad(uint32_t x) {
-  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, true));  // quad_perm 1 0 3 2
-  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, true));  // quad_perm 2 3 0 1
-  return x;
-}
 
 template <typename T>
 __device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, float (&v)[8]) {
@@ -55,24 +48,36 @@ __device__ __forceinline__ void load8(const T* row, int64_t c, int64_t cols, flo
   }
 }
 
-// A quad of lanes takes 128 columns of a row, 8 of every 32 a lane.  Bound: memory.
+// A wave's tile: lane l has row l % 16, and of every 32 columns the 8 from 8 (l / 16).
+struct CastTile {
+  int64_t matrix, i, j;
+  bool there;
+};
+__device__ __forceinline__ CastTile cast_tile(const Fp4CastArgs& a) {
+  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), plane = a.down * a.across;
+  return CastTile{t / plane, t % plane / a.across, t % a.across, t < a.tiles};
+}
+
+// Bound: memory.
 template <typename T>
 __global__ __launch_bounds__(256) void fp4_quantize_kernel(Fp4CastArgs a) {
-  const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 2;
-  const int g = threadIdx.x & 3;
-  if (unit >= a.units) return;  // whole quads
-  const int64_t line = unit / a.per_row, b = unit % a.per_row, m = line / a.rows, r = line % a.rows;
-  const T* row = (const T*)a.w + m * a.stride_w + r * a.ld_w;
+  const CastTile t = cast_tile(a);
+  if (!t.there) return;  // whole waves
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int64_t b = t.j, row_at = 16 * t.i + r;
+  const T* row = (const T*)a.w + t.matrix * a.stride_w + row_at * a.ld_w;
+  const int64_t cols = row_at < a.rows ? a.cols : 0;  // rows of padding are zeros
   float v[4][8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) load8<T>(row, 128 * b + 32 * i + 8 * g, a.cols, v[i]);
+  for (int i = 0; i < 4; ++i) load8<T>(row, 128 * b + 32 * i + 8 * g, cols, v[i]);
   uint32_t code[4], scale = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint32_t amax = 0;  // of the magnitudes' bits, which are in their order; NaN above infinity
 #pragma unroll
     for (int j = 0; j < 8; ++j) amax = max(amax, __float_as_uint(v[i][j]) & 0x7fffffffu);
-    amax = max_quad(amax);
+    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16));
+    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32));
     // amax = f 2^e, 1 <= f < 2: 2^(e - 2) where f <= 1.5, else 2^(e - 1)
     const int e = (int)(amax >> 23) - ((amax & 0x7fffffu) <= 0x400000u ? 2 : 1);
     const int byte = amax >= 0x7f800000u ? 255 : amax == 0 ? kScaleOne : min(max(e, 0), 252);
@@ -89,9 +94,9 @@ __global__ __launch_bounds__(256) void fp4_quantize_kernel(Fp4CastArgs a) {
     }
     code[i] = c;
   }
-  *(i32x4_t*)(a.codes + m * a.stride_codes + r * a.ld + 64 * b + 16 * g) =
+  *(i32x4_t*)(a.codes + t.matrix * a.stride_codes + t.i * a.ld + 1024 * b + 16 * lane) =
       i32x4_t{(int)code[0], (int)code[1], (int)code[2], (int)code[3]};
-  if (g == 0) *(uint32_t*)(a.scales + m * a.stride_scales + r * a.ld_scales + 4 * b) = scale;
+  if (g == 0) *(uint32_t*)(a.scales + t.matrix * a.stride_scales + t.i * a.ld_scales + 64 * b + 4 * r) = scale;
 }
 
 // Eight codes of a dword times a scale, exactly.
@@ -109,31 +114,32 @@ __device__ __forceinline__ f16x8_t widen_f16(uint32_t c) {
 // As fp4_quantize_kernel, the other way.  T: float or bf16_t.
 template <typename T>
 __global__ __launch_bounds__(256) void fp4_dequantize_kernel(Fp4CastArgs a) {
-  const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 2;
-  const int g = threadIdx.x & 3;
-  if (unit >= a.units) return;
-  const int64_t line = unit / a.per_row, b = unit % a.per_row, m = line / a.rows, r = line % a.rows;
-  const i32x4_t code = *(const i32x4_t*)(a.codes + m * a.stride_codes + r * a.ld + 64 * b + 16 * g);
-  const uint32_t scale = *(const uint32_t*)(a.scales + m * a.stride_scales + r * a.ld_scales + 4 * b);
-  T* row = (T*)a.out + m * a.stride_w + r * a.ld_w;
+  const CastTile t = cast_tile(a);
+  if (!t.there) return;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int64_t b = t.j, row_at = 16 * t.i + r;
+  const i32x4_t code = *(const i32x4_t*)(a.codes + t.matrix * a.stride_codes + t.i * a.ld + 1024 * b + 16 * lane);
+  const uint32_t scale = *(const uint32_t*)(a.scales + t.matrix * a.stride_scales + t.i * a.ld_scales + 64 * b + 4 * r);
+  if (row_at >= a.rows) return;
+  T* row = (T*)a.out + t.matrix * a.stride_w + row_at * a.ld_w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float by = scale_value(scale >> (8 * i) & 255u);
     const f16x8_t h = widen_f16((uint32_t)code[i]);
     const int64_t c = 128 * b + 32 * i + 8 * g;
-    T t[8];
+    T v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t[j] = from_f32<T>((float)h[j] * by);
+    for (int j = 0; j < 8; ++j) v[j] = from_f32<T>((float)h[j] * by);
     if (c + 8 <= a.cols) {
       if constexpr (sizeof(T) == 4) {
-        store_n<T, 4>(row + c, t);
-        store_n<T, 4>(row + c + 4, t + 4);
+        store_n<T, 4>(row + c, v);
+        store_n<T, 4>(row + c + 4, v + 4);
       } else {
-        store_n<T, 8>(row + c, t);
+        store_n<T, 8>(row + c, v);
       }
     } else {
       for (int j = 0; j < 8; ++j)
-        if (c + j < a.cols) row[c + j] = t[j];
+        if (c + j < a.cols) row[c + j] = v[j];
     }
   }
 }
@@ -158,20 +164,14 @@ __device__ __forceinline__ f32x4_t multiply(f16x8_t x, f16x8_t w, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w, c, 0, 0, 0);
 }
 
-// Eight of a row's columns from k, zeros past its end and for no row.
+// Eight of a row's columns from k, zeros past its end.
 template <typename T>
-__device__ __forceinline__ i32x4_t load_row(const T* row, bool valid, int64_t k, int64_t K) {
-  i32x4_t v = {0, 0, 0, 0};
-  if (valid) {
-    if (k + 8 <= K) {
-      load_n<T, 8>(row + k, (T*)&v);
-    } else {
-      T t[8];
+__device__ __forceinline__ i32x4_t load_end(const T* row, int k, int K) {
+  T t[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[j] = k + j < K ? row[k + j] : from_f32<T>(0.0f);
-      __builtin_memcpy(&v, t, 16);
-    }
-  }
+  for (int j = 0; j < 8; ++j) t[j] = k + j < K ? row[k + j] : from_f32<T>(0.0f);
+  i32x4_t v;
+  __builtin_memcpy(&v, t, 16);
   return v;
 }
 
@@ -180,93 +180,122 @@ __device__ __forceinline__ void store_value(void* C, int64_t at, float v) {
   ((T*)C)[at] = from_f32<T>(v);
 }
 
-// A workgroup computes 16 MT rows of 16 NT columns; its W waves share out the
-// contraction, 256 columns at a time, and add up their parts through LDS in a fixed
-// order.  Operands go from memory straight to registers.  Bound: reading the weights.
-template <typename X, int MT, int NT, int W, bool GROUPED>
-__global__ __launch_bounds__(64 * W) void fp4_product_kernel(Fp4Args a) {
-  constexpr bool kBf16 = sizeof(X) == sizeof(bf16_t) && std::is_same<X, bf16_t>::value;
-  __shared__ f32x4_t part[W * MT * NT * 64];
+// A workgroup computes 16 MT rows of 16 NT columns: its waves share out the contraction,
+// 256 columns of A at a time, and add up their parts through LDS in a fixed order.
+// Operands go from memory straight to registers, a step's weights before the products of
+// the one before.  Rows that are not there read those of another and are not stored.
+// Bound: reading the weights (1 x 8192 x 8192: 9.4 us, 3.8 TB/s; by rows of codes instead
+// of tiles, 64 bytes of 16 rows a load and scales 4 bytes of each, 14.1; 55 of 64 groups
+// of 4096 x 2048 57 us, 4.3 TB/s, by rows 83); from about 16 rows on by reading those of A
+// for every strip (64 x 8192 x 8192: 45 us).
+template <typename X, int MT, int NT, bool GROUPED>
+__global__ __launch_bounds__(512) void fp4_product_kernel(Fp4Args a) {
+  constexpr bool kBf16 = std::is_same<X, bf16_t>::value;
+  extern __shared__ __align__(16) f32x4_t part[];  // waves x MT x NT x 64
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+  const int waves = blockDim.x >> 6;
   // strips of columns go round the XCDs, the tiles of rows of one strip follow each other on one
-  const int64_t turn = 8 * a.tiles_m, strip = blockIdx.x / turn * 8 + blockIdx.x % 8, tm = blockIdx.x % turn / 8;
+  const uint32_t turn = 8 * (uint32_t)a.tiles_m, strip = blockIdx.x / turn * 8 + blockIdx.x % 8, tm = blockIdx.x % turn / 8;
   if (strip >= a.strips) return;
-  int64_t m0 = tm * 16 * MT, m_end = a.M;
+  int64_t m0 = (int64_t)tm * 16 * MT, m_end = a.M;
   const uint8_t *codes = a.codes, *scales = a.scales;
-  bool zero = false;
+  bool zero = a.x_rows == 0;
   if constexpr (GROUPED) {
     const GroupTile gt = find_group_tile(a.offsets, a.groups, a.M, 16 * MT, tm);
     if (gt.group < 0) return;
     m0 = gt.lo + gt.index * 16 * MT;
     m_end = gt.hi;
-    zero = gt.group >= a.groups;
-    if (!zero) {
+    if (gt.group >= a.groups) {
+      zero = true;
+    } else {
       codes += gt.group * a.stride_codes;
       scales += gt.group * a.stride_scales;
     }
   }
-  const int64_t n0 = strip * 16 * NT;
+  const int64_t n0 = (int64_t)strip * 16 * NT;
   const X* x[MT];
-  bool valid[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int64_t m = m0 + 16 * i + r;
-    valid[i] = m < m_end && !zero;
-    int64_t from = valid[i] && a.index ? a.index[m] : m;
-    valid[i] = valid[i] && from >= 0 && from < a.x_rows;
-    x[i] = (const X*)a.x + (valid[i] ? from : 0) * a.ldx;
+    int64_t from = min(m0 + 16 * i + r, m_end - 1);
+    if (a.index) from = a.index[from];
+    x[i] = (const X*)a.x + (from >= 0 && from < a.x_rows ? from : 0) * a.ldx + 8 * g;
   }
-  const uint8_t *code_row[NT], *scale_row[NT];
+  const uint8_t *code_at[NT], *scale_at[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int64_t n = min(n0 + 16 * t + r, a.N - 1);  // past the last column: computed and not stored
-    code_row[t] = codes + n * a.ld + 16 * g;
-    scale_row[t] = scales + n * a.ld_scales;
+    const int64_t tile = min(n0 / 16 + t, (a.N - 1) / 16);  // past the last column: computed and not stored
+    code_at[t] = codes + tile * a.ld + 16 * lane;
+    scale_at[t] = scales + tile * a.ld_scales + 4 * r;
   }
   f32x4_t acc[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int t = 0; t < NT; ++t) acc[i][t] = f32x4_t{0, 0, 0, 0};
-  const int64_t blocks = zero ? 0 : (a.K + 127) / 128;
-  for (int64_t b0 = 2 * wave; b0 < blocks; b0 += 2 * W) {
-    i32x4_t code[2][NT];
-    uint32_t scale[2][NT];
+  const int blocks = zero ? 0 : (int)((a.K + 127) / 128), K = (int)a.K;
+  const auto load_codes = [&](int b0, i32x4_t (&code)[2][NT], uint32_t (&scale)[2][NT]) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int64_t b = min(b0 + u, blocks - 1);
+      const int b = min(b0 + u, blocks - 1);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        code[u][t] = *(const i32x4_t*)(code_row[t] + 64 * b);
-        scale[u][t] = *(const uint32_t*)(scale_row[t] + 4 * b);
+        code[u][t] = *(const i32x4_t*)(code_at[t] + 1024 * (int64_t)b);
+        scale[u][t] = *(const uint32_t*)(scale_at[t] + 64 * (int64_t)b);
       }
     }
+  };
+  const auto load_x = [&](int b, i32x4_t (&xv)[4][MT]) {
+    if (128 * b + 128 <= K) {  // the same for the wave
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      if (b0 + u >= blocks) break;
+      for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        i32x4_t xv[MT];
+        for (int i = 0; i < MT; ++i) load_n<X, 8>(x[i] + 128 * b + 32 * q, (X*)&xv[q][i]);
+    } else {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) xv[i] = load_row<X>(x[i], valid[i], 128 * (b0 + u) + 32 * q + 8 * g, a.K);
+      for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const float by = scale_value(scale[u][t] >> (8 * q) & 255u);
-          if constexpr (kBf16) {
-            const bf16x8_t w = widen_bf16((uint32_t)code[u][t][q], by);
+        for (int i = 0; i < MT; ++i) xv[q][i] = load_end(x[i], 128 * b + 32 * q, K - 8 * g);
+    }
+  };
+  const auto multiply_block = [&](const i32x4_t (&code)[NT], const uint32_t (&scale)[NT], const i32x4_t (&xv)[4][MT]) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) acc[i][t] = multiply(__builtin_bit_cast(bf16x8_t, xv[i]), w, acc[i][t]);
-          } else {  // binary16 does not reach as far as scales do: they are applied to the sums
-            const f16x8_t w = widen_f16((uint32_t)code[u][t][q]);
+    for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-              const f32x4_t p = multiply(__builtin_bit_cast(f16x8_t, xv[i]), w, f32x4_t{0, 0, 0, 0});
+      for (int t = 0; t < NT; ++t) {
+        const float by = scale_value(scale[t] >> (8 * q) & 255u);
+        if constexpr (kBf16) {
+          const bf16x8_t w = widen_bf16((uint32_t)code[t][q], by);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) acc[i][t][j] = fmaf(by, p[j], acc[i][t][j]);
-            }
+          for (int i = 0; i < MT; ++i) acc[i][t] = multiply(__builtin_bit_cast(bf16x8_t, xv[q][i]), w, acc[i][t]);
+        } else {  // binary16 does not reach as far as scales do: they are applied to the sums
+          const f16x8_t w = widen_f16((uint32_t)code[t][q]);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            const f32x4_t p = multiply(__builtin_bit_cast(f16x8_t, xv[q][i]), w, f32x4_t{0, 0, 0, 0});
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][t][j] = fmaf(by, p[j], acc[i][t][j]);
           }
         }
       }
+  };
+  int b0 = 2 * wave;
+  if (b0 < blocks) {
+    i32x4_t code[2][NT], next_code[2][NT], xv[2][4][MT];
+    uint32_t scale[2][NT], next_scale[2][NT];
+    load_codes(b0, next_code, next_scale);
+    for (; b0 < blocks; b0 += 2 * waves) {
+      load_x(b0, xv[0]);
+      if (b0 + 1 < blocks) load_x(b0 + 1, xv[1]);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          code[u][t] = next_code[u][t];
+          scale[u][t] = next_scale[u][t];
+        }
+      load_codes(b0 + 2 * waves, next_code, next_scale);
+      multiply_block(code[0], scale[0], xv[0]);
+      if (b0 + 1 < blocks) multiply_block(code[1], scale[1], xv[1]);
     }
   }
 #pragma unroll
@@ -275,19 +304,23 @@ __global__ __launch_bounds__(64 * W) void fp4_product_kernel(Fp4Args a) {
     for (int t = 0; t < NT; ++t) part[((wave * MT + i) * NT + t) * 64 + lane] = acc[i][t];
   __syncthreads();
   // lane l of a piece: rows 4 (l / 16) .., column l % 16
-  for (int j = tid; j < MT * NT * 64; j += 64 * W) {
+  for (int j = tid; j < MT * NT * 64; j += blockDim.x) {
     f32x4_t sum = part[j];
-    for (int w = 1; w < W; ++w) sum += part[w * MT * NT * 64 + j];
+    for (int w = 1; w < waves; ++w) sum += part[w * MT * NT * 64 + j];
     const int64_t m = m0 + j / (NT * 64) * 16 + (j & 63) / 16 * 4, n = n0 + j / 64 % NT * 16 + (j & 15);
     if (n >= a.N) continue;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (m + e >= m_end) break;
-      const int64_t at = (m + e) * a.ldc + n;
+    for (int k = 0; k < 4; ++k) {
+      if (m + k >= m_end) break;
+      if (a.index) {
+        const int32_t from = a.index[m + k];
+        if (from < 0 || from >= a.x_rows) sum[k] = 0.0f;
+      }
+      const int64_t at = (m + k) * a.ldc + n;
       switch (a.dtype) {  // the same for the whole launch
-        case WS_OUT_F32: store_value<float>(a.C, at, sum[e]); break;
-        case WS_OUT_BF16: store_value<bf16_t>(a.C, at, sum[e]); break;
-        default: store_value<f16_t>(a.C, at, sum[e]);
+        case WS_OUT_F32: store_value<float>(a.C, at, sum[k]); break;
+        case WS_OUT_BF16: store_value<bf16_t>(a.C, at, sum[k]); break;
+        default: store_value<f16_t>(a.C, at, sum[k]);
       }
     }
   }
@@ -297,12 +330,12 @@ __global__ __launch_bounds__(64 * W) void fp4_product_kernel(Fp4Args a) {
 
 bool valid_fp4(const ws_fp4_matrix* q, bool batched) {
   if (!q || q->rows < 0 || q->cols < 0 || q->rows > kMaxDim || q->cols > kMaxDim || q->batch < 0) return false;
-  const int64_t units = ceil_div(q->cols, 128);
-  if (q->ld % 16 || q->ld < 64 * units || q->ld > kMaxDim || q->ld_scales % 4 || q->ld_scales < 4 * units || q->ld_scales > kMaxDim)
+  const int64_t across = ceil_div(q->cols, 128), down = ceil_div(q->rows, 16);
+  if (q->ld % 16 || q->ld < 1024 * across || q->ld > kMaxDim || q->ld_scales % 4 || q->ld_scales < 64 * across || q->ld_scales > kMaxDim)
     return false;
   if (q->rows == 0 || q->cols == 0 || (batched && q->batch == 0)) return true;
-  if (q->batch > 1 && (q->stride_codes % 16 || q->stride_scales % 4 || q->stride_codes < (q->rows - 1) * q->ld + 64 * units ||
-                       q->stride_scales < (q->rows - 1) * q->ld_scales + 4 * units))
+  if (q->batch > 1 && (q->stride_codes % 16 || q->stride_scales % 4 || q->stride_codes < (down - 1) * q->ld + 1024 * across ||
+                       q->stride_scales < (down - 1) * q->ld_scales + 64 * across))
     return false;
   return q->codes && (uintptr_t)q->codes % 16 == 0 && q->scales && (uintptr_t)q->scales % 4 == 0;
 }
@@ -325,9 +358,10 @@ ws_status cast(const char* what, const ws_matrix* w, const ws_fp4_matrix* q, boo
   a.ld_scales = q->ld_scales;
   a.stride_codes = q->stride_codes;
   a.stride_scales = q->stride_scales;
-  a.per_row = ceil_div(w->cols, 128);
-  a.units = a.per_row * w->rows * w->batch;
-  const int64_t grid = ceil_div(a.units, 64);
+  a.across = ceil_div(w->cols, 128);
+  a.down = ceil_div(w->rows, 16);
+  a.tiles = a.across * a.down * w->batch;
+  const int64_t grid = ceil_div(a.tiles, 4);
   if (grid > max_workgroups(256)) return WS_ERR_INVALID_ARG;
   if (out)
     return launch(what, w->dtype == WS_OUT_F32 ? &fp4_quantize_kernel<float> : w->dtype == WS_OUT_BF16 ? &fp4_quantize_kernel<bf16_t>
@@ -336,15 +370,16 @@ ws_status cast(const char* what, const ws_matrix* w, const ws_fp4_matrix* q, boo
   return launch(what, w->dtype == WS_OUT_F32 ? &fp4_dequantize_kernel<float> : &fp4_dequantize_kernel<bf16_t>, grid, 256, 0, stream, a);
 }
 
-template <int MT, int NT, int W>
-ws_status launch_product(const char* what, bool bf16, bool grouped, hipStream_t stream, Fp4Args a) {
+template <int MT, int NT>
+ws_status launch_product(const char* what, bool bf16, bool grouped, int waves, hipStream_t stream, Fp4Args a) {
   a.strips = ceil_div(a.N, 16 * NT);
   a.tiles_m = grouped ? group_tiles(a.M, a.groups, 16 * MT, true) : ceil_div(a.M, 16 * MT);
+  while (waves > 1 && waves * 128 >= a.K) waves /= 2;  // of 256 columns each
   const int64_t grid = ceil_div(a.strips, 8) * 8 * a.tiles_m;
-  if (grid > max_workgroups(64 * W)) return WS_ERR_INVALID_ARG;
-  void (*kernel)(Fp4Args) = bf16 ? (grouped ? &fp4_product_kernel<bf16_t, MT, NT, W, true> : &fp4_product_kernel<bf16_t, MT, NT, W, false>)
-                                 : (grouped ? &fp4_product_kernel<f16_t, MT, NT, W, true> : &fp4_product_kernel<f16_t, MT, NT, W, false>);
-  return launch(what, kernel, grid, 64 * W, 0, stream, a);
+  if (grid > max_workgroups(64 * waves) || a.tiles_m > 1 << 28) return WS_ERR_INVALID_ARG;
+  void (*kernel)(Fp4Args) = bf16 ? (grouped ? &fp4_product_kernel<bf16_t, MT, NT, true> : &fp4_product_kernel<bf16_t, MT, NT, false>)
+                                 : (grouped ? &fp4_product_kernel<f16_t, MT, NT, true> : &fp4_product_kernel<f16_t, MT, NT, false>);
+  return launch(what, kernel, grid, 64 * waves, waves * MT * NT * 1024, stream, a);
 }
 
 ws_status product(const char* what, const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, int32_t groups,
@@ -376,9 +411,16 @@ ws_status product(const char* what, const ws_matrix* A, const int32_t* index, co
   a.dtype = C->dtype;
   const bool bf16 = A->dtype == WS_OUT_BF16;
   const int64_t rows = grouped ? (groups ? ceil_div(a.M, groups) : a.M) : a.M;  // of a group, on average
-  if (rows <= 16) return launch_product<1, 2, 4>(what, bf16, grouped, stream, a);
-  if (rows <= 32) return launch_product<2, 2, 4>(what, bf16, grouped, stream, a);
-  return launch_product<4, 2, 4>(what, bf16, grouped, stream, a);
+  // Eight waves to a contraction fill the card where there are few strips; where there
+  // are many, starting waves costs more than it hides.  us of 2 columns' tiles by 8 waves
+  // and of 4 by 4: 1 x 8192 x 8192 9.4 and 13.0, 128 rows of 55 of 64 groups of 4096 x 2048
+  // 94 and 57; 64 x 8192 x 8192 by 8 and 4 waves 44.8 and 49.4, 256 x 4096 x 4096 41.5 and 38.5.
+  const int64_t mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  const bool many = ceil_div(a.N, 32) * (grouped ? group_tiles(a.M, groups, 16 * (int)mt, false) : ceil_div(a.M, 16 * mt)) > 500;
+  if (mt == 1)
+    return many ? launch_product<1, 4>(what, bf16, grouped, 4, stream, a) : launch_product<1, 2>(what, bf16, grouped, 8, stream, a);
+  if (mt == 2) return launch_product<2, 2>(what, bf16, grouped, many ? 4 : 8, stream, a);
+  return launch_product<4, 2>(what, bf16, grouped, many ? 4 : 8, stream, a);
 }
 
 }  // namespace

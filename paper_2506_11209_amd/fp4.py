@@ -21,7 +21,7 @@ from . import wsgemm as _w
 from .fp8 import E8M0, _Call, _check, _elsewhere, _index, _matrix, _mp, _need, _result, _raw_stream, _up
 
 BLOCK = 32
-_UNIT = 128  # columns that are padded to
+_ROWS, _COLS = 16, 128  # of a tile
 
 
 class ws_fp4_matrix(ctypes.Structure):
@@ -41,32 +41,34 @@ for _name, _args in (("ws_fp4_quantize", [_mp, _fp, _p]), ("ws_fp4_dequantize", 
 class Fp4Matrix:
     """rows x cols in 4 bits, or a batch of such matrices (weights of experts).
 
-    ``codes`` ((batch x) rows x pitch, uint8): two codes a byte in the order of
-    include/ws_fp4.h, 64 bytes for 128 columns.  ``packed_scales`` ((batch x) rows x
-    pitch, e8m0): a scale for 32 columns, of which ``scales`` are those of whole or
-    partial blocks.  Columns are padded to a multiple of 128 with zero codes and scales
-    of 1; rows may be further apart."""
+    ``codes`` ((batch x) ceil(rows / 16) x pitch, uint8): tiles of 16 rows by 128
+    columns, 1024 bytes each, in the order of include/ws_fp4.h.  ``packed_scales``
+    ((batch x) ceil(rows / 16) x pitch, e8m0): their scales, 64 bytes for a tile;
+    ``scales`` gives them by row.  Rows and columns are padded with zero codes and
+    scales of 1; tiles of the next 16 rows may be further apart."""
 
     __slots__ = ("codes", "packed_scales", "rows", "cols", "_desc")
 
     def __init__(self, codes, scales, rows: int, cols: int):
         _need(codes, "codes", (torch.uint8,), (2, 3))
         _need(scales, "scales", (E8M0,), (codes.dim(),), codes.device)
-        cs, ss, shape, units = codes.stride(), scales.stride(), codes.shape, -(-cols // _UNIT)
+        if rows < 0 or cols < 0:
+            raise ValueError("%d x %d" % (rows, cols))
+        cs, ss, shape, down, across = codes.stride(), scales.stride(), codes.shape, -(-rows // _ROWS), -(-cols // _COLS)
         batch = shape[0] if len(shape) == 3 else 1
-        if cols < 0 or shape[-2] != rows or shape[-1] < 64 * units or (shape[-1] > 1 and cs[-1] != 1):
-            raise ValueError("codes %s of strides %s do not hold %d x %d values padded to 128 columns" % (tuple(shape), cs, rows, cols))
-        if tuple(scales.shape[:-1]) != tuple(shape[:-1]) or scales.shape[-1] < 4 * units or (scales.shape[-1] > 1 and ss[-1] != 1):
-            raise ValueError("scales %s of strides %s: expected %s" % (tuple(scales.shape), ss, tuple(shape[:-1]) + (4 * units,)))
-        ld = cs[-2] if rows > 1 and shape[-1] > 0 else _up(shape[-1], 16)
-        ld_scales = ss[-2] if rows > 1 and scales.shape[-1] > 0 else _up(scales.shape[-1], 4)
+        if shape[-2] != down or shape[-1] < 1024 * across or (shape[-1] > 1 and cs[-1] != 1):
+            raise ValueError("codes %s of strides %s do not hold %d x %d values in tiles of 16 x 128" % (tuple(shape), cs, rows, cols))
+        if tuple(scales.shape[:-1]) != tuple(shape[:-1]) or scales.shape[-1] < 64 * across or (scales.shape[-1] > 1 and ss[-1] != 1):
+            raise ValueError("scales %s of strides %s: expected %s" % (tuple(scales.shape), ss, tuple(shape[:-1]) + (64 * across,)))
+        ld = cs[-2] if down > 1 and shape[-1] > 0 else _up(shape[-1], 16)
+        ld_scales = ss[-2] if down > 1 and scales.shape[-1] > 0 else _up(scales.shape[-1], 4)
         if ld % 16 or codes.data_ptr() % 16 or (batch > 1 and cs[0] % 16):
-            raise ValueError("codes: rows have to start at multiples of 16 bytes, got strides %s" % (cs,))
+            raise ValueError("codes: tiles have to start at multiples of 16 bytes, got strides %s" % (cs,))
         if ld_scales % 4 or scales.data_ptr() % 4 or (batch > 1 and ss[0] % 4):
-            raise ValueError("scales: rows have to start at multiples of 4 bytes, got strides %s" % (ss,))
-        if rows > 0 and cols > 0 and (ld < 64 * units or ld_scales < 4 * units or (batch > 1 and (
-                cs[0] < (rows - 1) * ld + 64 * units or ss[0] < (rows - 1) * ld_scales + 4 * units))):
-            raise ValueError("rows and matrices may not overlap, got strides %s of codes and %s of scales" % (cs, ss))
+            raise ValueError("scales: tiles have to start at multiples of 4 bytes, got strides %s" % (ss,))
+        if rows > 0 and cols > 0 and (ld < 1024 * across or ld_scales < 64 * across or (batch > 1 and (
+                cs[0] < (down - 1) * ld + 1024 * across or ss[0] < (down - 1) * ld_scales + 64 * across))):
+            raise ValueError("tiles and matrices may not overlap, got strides %s of codes and %s of scales" % (cs, ss))
         self.codes, self.packed_scales, self.rows, self.cols = codes, scales, rows, cols
         self._desc = ws_fp4_matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, ld, ld_scales, batch,
                                    cs[0] if len(shape) == 3 else 0, ss[0] if len(shape) == 3 else 0)
@@ -78,20 +80,24 @@ class Fp4Matrix:
 
     @property
     def scales(self):
-        """(batch x) rows x ceil(cols / 32)."""
-        return self.packed_scales[..., : -(-self.cols // BLOCK)]
+        """(batch x) rows x ceil(cols / 32), e8m0: the scale of every 32 columns of a row."""
+        across = -(-self.cols // _COLS)
+        s = self.packed_scales[..., : 64 * across].view(torch.int32)  # 4 neighbours of a row
+        s = s.unflatten(-1, (across, _ROWS)).transpose(-1, -2)
+        s = s.reshape(-1).view(E8M0).view(s.shape[:-3] + (s.shape[-3] * _ROWS, 4 * across))
+        return s[..., : self.rows, : -(-self.cols // BLOCK)]
 
     @classmethod
     def empty(cls, rows: int, cols: int, batch: int | None = None, device="cuda"):
         if rows < 0 or cols < 0:
             raise ValueError("%d x %d" % (rows, cols))
-        units, lead = -(-cols // _UNIT), () if batch is None else (batch,)
+        down, across, lead = -(-rows // _ROWS), -(-cols // _COLS), () if batch is None else (batch,)
         q = object.__new__(cls)
-        q.codes = codes = torch.empty(lead + (rows, 64 * units), dtype=torch.uint8, device=device)
-        q.packed_scales = scales = torch.empty(lead + (rows, 4 * units), dtype=E8M0, device=device)
+        q.codes = codes = torch.empty(lead + (down, 1024 * across), dtype=torch.uint8, device=device)
+        q.packed_scales = scales = torch.empty(lead + (down, 64 * across), dtype=E8M0, device=device)
         q.rows, q.cols = rows, cols
-        q._desc = ws_fp4_matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, 64 * units, 4 * units, 1 if batch is None else batch,
-                                rows * 64 * units, rows * 4 * units)
+        q._desc = ws_fp4_matrix(codes.data_ptr(), scales.data_ptr(), rows, cols, 1024 * across, 64 * across, 1 if batch is None else batch,
+                                down * 1024 * across, down * 64 * across)
         return q
 
     def dequantize(self, out_dtype: str = "f32", out=None, stream=None):

@@ -37,16 +37,20 @@ def values(codes, scales, cols):
     return (codes.reshape(R, -1, 32) * s[..., None]).reshape(R, -1)[:, :cols]
 
 
-def unpack(bytes_, cols):
-    """Codes' values (rows x padded columns) of the packed bytes (uint8 rows x pitch)."""
-    R, n = bytes_.shape[0], -(-cols // 128)
-    out = np.zeros((R, n * 128))
+def unpack(codes, scales, rows, cols):
+    """(codes' values, scales' bytes) by row, rows x padded columns, of tiles of 16 x 128
+    (uint8 ceil(rows / 16) x pitch each)."""
+    down, across = -(-rows // 16), -(-cols // 128)
+    v, s = np.zeros((16 * down, 128 * across)), np.zeros((16 * down, 4 * across), np.uint8)
     signed = np.concatenate([CODES, -CODES])
-    for b in range(n):
-        for g in range(4):
-            for i in range(4):
+    for i in range(down):
+        for j in range(across):
+            t = codes[i, 1024 * j: 1024 * (j + 1)].reshape(4, 16, 4, 4)  # g, r, k, b
+            for g in range(4):
                 for k in range(4):
-                    byte = bytes_[:, 64 * b + 16 * g + 4 * i + k]
-                    c = 128 * b + 32 * i + 8 * g + 2 * k
-                    out[:, c], out[:, c + 1] = signed[byte & 15], signed[byte >> 4]
-    return out
+                    for b in range(4):
+                        byte, c = t[g, :, k, b], 128 * j + 32 * k + 8 * g + 2 * b
+                        v[16 * i: 16 * i + 16, c], v[16 * i: 16 * i + 16, c + 1] = signed[byte & 15], signed[byte >> 4]
+            s[16 * i: 16 * i + 16, 4 * j: 4 * j + 4] = scales[i, 64 * j: 64 * (j + 1)].reshape(16, 4)
+    assert (v[rows:] == 0).all() and (s[rows:] == 127).all()
+    return v[:rows], s[:rows]

@@ -31,6 +31,10 @@ def spread(shape, seed, dtype=torch.float32):
     return x.to(dtype)
 
 
+def unpacked(q):
+    return ref.unpack(q.codes.cpu().numpy(), q.packed_scales.view(torch.uint8).cpu().numpy(), q.rows, q.cols)
+
+
 @pytest.mark.parametrize("R,C", [(1, 1), (3, 31), (2, 32), (5, 33), (7, 127), (4, 128), (65, 129), (33, 257), (16, 1000), (130, 4104)])
 @pytest.mark.parametrize("name", TYPES)
 def test_quantize(R, C, name):
@@ -38,8 +42,9 @@ def test_quantize(R, C, name):
     w = spread((R, C), R * C, TYPES[name])
     q = fp4.quantize_weight(w.cuda())
     codes, scales = ref.quantize(w.double().numpy())
-    assert np.array_equal(q.packed_scales.view(torch.uint8).cpu().numpy(), scales)
-    assert np.array_equal(ref.unpack(q.codes.cpu().numpy(), C), codes)
+    got = unpacked(q)
+    assert np.array_equal(got[1], scales) and np.array_equal(got[0], codes)
+    assert np.array_equal(q.scales.view(torch.uint8).cpu().numpy(), scales[:, : -(-C // 32)])
     want = torch.from_numpy(ref.values(codes, scales, C))
     assert torch.equal(q.dequantize().cpu().double(), want)
     assert torch.equal(q.dequantize("bf16").cpu().double(), want)
@@ -53,7 +58,7 @@ def test_quantize_every_code_and_tie():
     w = w * torch.tensor([[1.0], [2.0 ** -100], [2.0 ** 90]])
     q = fp4.quantize_weight(w.cuda())
     codes, scales = ref.quantize(w.double().numpy())
-    assert np.array_equal(ref.unpack(q.codes.cpu().numpy(), 32), codes) and (q.scales.view(torch.uint8).cpu().flatten().tolist() == [127, 27, 217])
+    assert np.array_equal(unpacked(q)[0], codes) and (q.scales.view(torch.uint8).cpu().flatten().tolist() == [127, 27, 217])
 
 
 def test_quantize_ends_of_the_range():
@@ -63,7 +68,7 @@ def test_quantize_ends_of_the_range():
     w[4, 32] = -3.0
     q = fp4.quantize_weight(w.cuda())
     codes, scales = ref.quantize(w.double().numpy())
-    assert np.array_equal(q.packed_scales.view(torch.uint8).cpu().numpy(), scales)
+    assert np.array_equal(unpacked(q)[1], scales)
     got, want = q.dequantize().cpu().double().numpy(), ref.values(codes, scales, 64)
     assert np.array_equal(got, want, equal_nan=True) and np.isnan(got[2, :32]).all() and (got[2, 32:] == 0).all()
 
@@ -76,12 +81,13 @@ def test_quantize_batch_and_strides():
     for i in range(3):
         one = fp4.quantize_weight(w[i].contiguous())
         assert torch.equal(q.codes[i], one.codes) and torch.equal(q.packed_scales[i].view(torch.uint8), one.packed_scales.view(torch.uint8))
-    codes = torch.full((3, 33, 160), 7, dtype=torch.uint8, device="cuda")
-    scales = torch.full((3, 33, 12), 9, dtype=torch.uint8, device="cuda").view(fp4.E8M0)
+    codes = torch.full((3, 3, 2080), 7, dtype=torch.uint8, device="cuda")
+    scales = torch.full((3, 3, 132), 9, dtype=torch.uint8, device="cuda").view(fp4.E8M0)
     out = fp4.Fp4Matrix(codes, scales, 33, 130)
     assert fp4.quantize_weight(w, out=out) is out
-    assert torch.equal(codes[..., :128], q.codes) and (codes[..., 128:] == 7).all()
-    assert torch.equal(scales.view(torch.uint8)[..., :8], q.packed_scales.view(torch.uint8)) and (scales.view(torch.uint8)[..., 8:] == 9).all()
+    assert torch.equal(codes[..., :2048], q.codes) and (codes[..., 2048:] == 7).all()
+    assert torch.equal(scales.view(torch.uint8)[..., :128], q.packed_scales.view(torch.uint8)) and (scales.view(torch.uint8)[..., 128:] == 9).all()
+    assert torch.equal(out.scales.view(torch.uint8), q.scales.view(torch.uint8)) and q.scales.shape == (3, 33, 5)
     into = torch.full((3, 35, 140), 5.0, device="cuda")
     out.dequantize(out=into[:, 1:34, 3:133])
     assert torch.equal(into[:, 1:34, 3:133], q.dequantize()) and (into[:, 0] == 5).all() and (into[..., :3] == 5).all() and (into[..., 133:] == 5).all()
@@ -259,8 +265,8 @@ def test_refusals():
                  lambda: fp4.quantize_weight(torch.ones(4, 4)), lambda: fp4.quantize_weight(torch.ones(4, 4, device="cuda").double()),
                  lambda: fp4.quantize_weight(torch.ones(4, 8, device="cuda").t()), lambda: fp4.quantize_weight(torch.ones(41, 64, device="cuda"), out=W),
                  lambda: W.dequantize("f16"), lambda: W.dequantize(out=torch.zeros(40, 65, device="cuda")),
-                 lambda: fp4.Fp4Matrix(W.codes[:, :32], W.packed_scales, 40, 64), lambda: fp4.Fp4Matrix(W.codes, W.packed_scales[:, :3], 40, 64),
-                 lambda: fp4.Fp4Matrix(W.codes, W.packed_scales.view(torch.uint8), 40, 64), lambda: fp4.Fp4Matrix(W.codes, W.packed_scales, 41, 64),
+                 lambda: fp4.Fp4Matrix(W.codes[:, :1008], W.packed_scales, 40, 64), lambda: fp4.Fp4Matrix(W.codes, W.packed_scales[:, :60], 40, 64),
+                 lambda: fp4.Fp4Matrix(W.codes, W.packed_scales.view(torch.uint8), 40, 64), lambda: fp4.Fp4Matrix(W.codes, W.packed_scales, 49, 64),
                  lambda: fp4.Fp4Matrix(W.codes, W.packed_scales, 40, 129)):
         with pytest.raises(ValueError):
             call()
