@@ -23,7 +23,7 @@ extern "C" {
 #endif
 
 #define WS_MAX_EXPERTS 1024
-#define WS_MAX_CHOICES 64
+#define WS_MAX_CHOICES 32
 
 /* Bytes of device memory that ws_expert_choose needs (0: none, then workspace may
  * be NULL); -1 for sizes that it refuses. */

@@ -60,15 +60,46 @@ __device__ __forceinline__ uint32_t max_lanes(uint32_t x) {
 }
 
 // Logits in the order in which they are chosen: larger is earlier, NaN first of all,
-// both zeros the same, 0 for -inf, which is not chosen.
-__device__ __forceinline__ uint32_t rank_of(float x) {
-  const uint32_t b = __float_as_uint(x + 0.0f);
-  const uint32_t key = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-  return x != x ? 0xffffffffu : x == -INFINITY ? 0u : key;
-}
-__device__ __forceinline__ float logit_of(uint32_t key) {
-  return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
-}
+// both zeros the same, 0 for -inf, which is not chosen.  A rank of 16 bits leaves room
+// for the element's number, so that no two ranks are alike (kOwn): the largest is found
+// with one comparison an element, and is removed without looking for it.
+template <typename T>
+struct Rank {
+  static constexpr bool kOwn = sizeof(T) == 2;
+  static constexpr uint32_t kSign = kOwn ? 0x8000u : 0x80000000u, kAll = kOwn ? 0xffffu : 0xffffffffu;
+  static __device__ __forceinline__ uint32_t of(T v, int e) {
+    const float x = to_f32(v);
+    uint32_t b;
+    if constexpr (kOwn) {
+      uint16_t h;
+      __builtin_memcpy(&h, &v, 2);
+      b = h;
+    } else {
+      b = __float_as_uint(x);
+    }
+    b = x == 0.0f ? 0u : b;
+    b = b & kSign ? ~b & kAll : b | kSign;
+    b = x != x ? kAll : b;
+    if constexpr (kOwn) b = b << 16 | (0xffffu - (uint32_t)e);
+    return x == -INFINITY ? 0u : b;
+  }
+  static __device__ __forceinline__ float value(uint32_t rank) {
+    uint32_t b = kOwn ? rank >> 16 : rank;
+    b = b & kSign ? b ^ kSign : ~b & kAll;
+    if constexpr (kOwn) {
+      const uint16_t h = (uint16_t)b;
+      T v;
+      __builtin_memcpy(&v, &h, 2);
+      return to_f32(v);
+    }
+    return __uint_as_float(b);
+  }
+  static __device__ __forceinline__ int element(uint32_t rank) { return 0xffff - (int)(rank & 0xffffu); }
+};
+
+// e^(x - top) by the power of two: the difference and its product with log2(e) round,
+// by 2^-23 of the exponent together.
+__device__ __forceinline__ float exp_from(float x, float top) { return __builtin_amdgcn_exp2f((x - top) * 1.44269504088896341f); }
 
 // A row of up to L V logits on L lanes: lane i holds elements W i .. W i + W - 1 of
 // every W L, W as many as 16 bytes hold.
@@ -76,33 +107,65 @@ template <typename T, int L, int V>
 struct Row {
   static constexpr int kWide = 16 / (int)sizeof(T), W = V < kWide ? V : kWide;
   static __device__ __forceinline__ int element(int sub, int v) { return v / W * (L * W) + sub * W + v % W; }
-  static __device__ __forceinline__ void load(const T* row, int sub, int n, T (&x)[V]) {
+  // -inf past the row's n elements.  readable: elements from its first on that are the
+  // caller's, so that a row's end is read along with what follows it and is not taken.
+  static __device__ __forceinline__ void load(const T* row, int sub, int n, int64_t readable, T (&x)[V]) {
 #pragma unroll
     for (int v = 0; v < V; v += W) {
       const int e = element(sub, v);
-      if constexpr (W * sizeof(T) >= 4) {
-        if (e + W <= n) {
-          load_n<T, W>(row + e, x + v);
-          continue;
-        }
-      }
+      const T none = from_f32<T>(-INFINITY);
 #pragma unroll
-      for (int w = 0; w < W; ++w) x[v + w] = e + w < n ? row[e + w] : from_f32<T>(-INFINITY);
+      for (int w = 0; w < W; ++w) x[v + w] = none;
+      if constexpr (W * sizeof(T) >= 4) {
+        if (e < n && e + W <= readable) {
+          load_n<T, W>(row + e, x + v);
+        } else {
+#pragma unroll
+          for (int w = 0; w < W; ++w)
+            if (e + w < n) x[v + w] = row[e + w];
+        }
+        if (n % W)  // the same for the launch
+#pragma unroll
+          for (int w = 0; w < W; ++w) x[v + w] = e + w < n ? x[v + w] : none;
+      } else {
+        if (e < n) x[v] = row[e];
+      }
     }
   }
   static __device__ __forceinline__ void store(T* row, int sub, int n, const T (&x)[V]) {
 #pragma unroll
     for (int v = 0; v < V; v += W) {
-      const int e = element(sub, v);
+      const int e = element(sub, v), left = n - e;
       if constexpr (W * sizeof(T) >= 4) {
-        if (e + W <= n) {
+        if (left >= W) {
           store_n<T, W>(row + e, x + v);
           continue;
         }
-      }
+        if (left <= 0) continue;
+        T r[W];  // the row's end: the larger pieces first
 #pragma unroll
-      for (int w = 0; w < W; ++w)
-        if (e + w < n) row[e + w] = x[v + w];
+        for (int w = 0; w < W; ++w) r[w] = x[v + w];
+        T* to = row + e;
+        if constexpr (W >= 8) {
+          if (left & 4) {
+            store_n<T, 4>(to, r);
+            to += 4;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) r[w] = r[w + 4];
+          }
+        }
+        if constexpr (W >= 4) {
+          if (left & 2) {
+            to[0] = r[0];
+            to[1] = r[1];
+            to += 2;
+            r[0] = r[2];
+          }
+        }
+        if (left & 1) to[0] = r[0];
+      } else {
+        if (left > 0) row[e] = x[v];
+      }
     }
   }
 };
@@ -164,21 +227,21 @@ __global__ __launch_bounds__(64 * choose_waves<L>()) void choose_kernel(ChooseAr
   const int64_t step = (int64_t)a.blocks * kGroups;
   for (int64_t t = (int64_t)blockIdx.x * kGroups + tid / L; t < a.tokens; t += step) {
     T raw[V];
-    R::load((const T*)a.logits + t * a.ld, sub, a.experts, raw);
+    R::load((const T*)a.logits + t * a.ld, sub, a.experts, a.experts + (a.tokens - 1 - t) * a.ld, raw);
     uint32_t key[V], best = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      key[v] = R::element(sub, v) < a.experts ? rank_of(to_f32(raw[v])) : 0;
+      key[v] = Rank<T>::of(raw[v], R::element(sub, v));  // -inf past the last expert
       best = max(best, key[v]);
     }
     best = max_lanes<L>(best);
     const bool some = best != 0;
-    const float top = logit_of(best);
+    const float top = Rank<T>::value(best);
     if (some) {
       float p[V], sum = 0.0f;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        p[v] = R::element(sub, v) < a.experts ? expf(to_f32(raw[v]) - top) : 0.0f;
+        p[v] = exp_from(to_f32(raw[v]), top);
         sum += p[v];
       }
       const float by = 1.0f / sum_lanes<L>(sum);
@@ -199,13 +262,20 @@ __global__ __launch_bounds__(64 * choose_waves<L>()) void choose_kernel(ChooseAr
           best = max_lanes<L>(best);
         }
         if (best == 0) break;
-        uint32_t low = 0;  // the lowest element with it, as a large number
+        int e;
+        if constexpr (Rank<T>::kOwn) {
+          e = Rank<T>::element(best);
 #pragma unroll
-        for (int v = V - 1; v >= 0; --v) low = key[v] == best ? ~(uint32_t)R::element(sub, v) : low;
-        const int e = (int)~max_lanes<L>(low);
+          for (int v = 0; v < V; ++v) key[v] = key[v] == best ? 0 : key[v];
+        } else {
+          uint32_t low = 0;  // the lowest element with it, as a large number
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = R::element(sub, v) == e ? 0 : key[v];
-        const float x = expf(logit_of(best) - top);
+          for (int v = V - 1; v >= 0; --v) low = key[v] == best ? ~(uint32_t)R::element(sub, v) : low;
+          e = (int)~max_lanes<L>(low);
+#pragma unroll
+          for (int v = 0; v < V; ++v) key[v] = R::element(sub, v) == e ? 0 : key[v];
+        }
+        const float x = exp_from(Rank<T>::value(best), top);
         all += x;
         if (j - q * L == sub) {
           id[q] = e;
@@ -273,41 +343,45 @@ __global__ __launch_bounds__(64 * choose_waves<L>()) void choose_kernel(ChooseAr
 }
 
 constexpr int kFinishThreads = 1024;
+constexpr int finish_slices(int n) { return kFinishThreads / n > 0 ? kFinishThreads / n : 1; }
 
-// Adds up what the workgroups left, every expert's in a fixed order.
+// Adds up what the workgroups left, every column in a fixed order, and finishes.  Bound:
+// latency, of one workgroup's reads and of the launch (256 times 257 columns: 11 us; by
+// two launches, the first with 17 workgroups, as long).
 __global__ __launch_bounds__(kFinishThreads) void choose_finish_kernel(ChooseArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ double scratch[kFinishThreads / 32];
-  const int n = a.experts + 1, slices = kFinishThreads / n > 0 ? kFinishThreads / n : 1;
-  float* sums = (float*)smem;                 // slices x n
+  const int n = a.experts + 1, slices = finish_slices(n);
+  float* sums = (float*)smem;  // slices x n
   int32_t* counts = (int32_t*)(sums + slices * n);
+  constexpr int kAtOnce = 16;  // of sums, and of counts
   for (int i = threadIdx.x; i < slices * n; i += kFinishThreads) {
     const int e = i % n, slice = i / n;
     float s = 0.0f;
     int32_t c = 0;
-    for (int b0 = slice; b0 < a.blocks; b0 += 8 * slices) {  // 16 loads at once
-      float x[8];
-      int32_t y[8];
+    for (int b0 = slice; b0 < a.blocks; b0 += kAtOnce * slices) {
+      float x[kAtOnce];
+      int32_t y[kAtOnce];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int b = b0 + u * slices;
-        x[u] = b < a.blocks ? a.sums[(int64_t)b * n + e] : 0.0f;
-        y[u] = b < a.blocks ? a.parts[(int64_t)b * n + e] : 0;
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int64_t at = (int64_t)min(b0 + u * slices, a.blocks - 1) * n + e;
+        x[u] = a.sums[at];
+        y[u] = a.parts[at];
       }
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        s += x[u];
-        c += y[u];
+      for (int u = 0; u < kAtOnce; ++u) {
+        s += b0 + u * slices < a.blocks ? x[u] : 0.0f;
+        c += b0 + u * slices < a.blocks ? y[u] : 0;
       }
     }
-    sums[slice * n + e] = s;
-    counts[slice * n + e] = c;
+    sums[i] = s;
+    counts[i] = c;
   }
   __syncthreads();
   for (int e = threadIdx.x; e < n; e += kFinishThreads)
-    for (int i = 1; i < slices; ++i) {
-      sums[e] += sums[i * n + e];
-      counts[e] += counts[i * n + e];
+    for (int k = 1; k < slices; ++k) {
+      sums[e] += sums[k * n + e];
+      counts[e] += counts[k * n + e];
     }
   __syncthreads();
   finish(a, sums, counts, scratch);
@@ -338,7 +412,7 @@ __global__ __launch_bounds__(256) void choose_gradient_kernel(ChooseArgs a) {
   const int64_t step = (int64_t)gridDim.x * kGroups;
   for (int64_t t = (int64_t)blockIdx.x * kGroups + tid / L; t < a.tokens; t += step) {
     T raw[V];
-    R::load((const T*)a.logits + t * a.ld, sub, a.experts, raw);
+    R::load((const T*)a.logits + t * a.ld, sub, a.experts, a.experts + (a.tokens - 1 - t) * a.ld, raw);
     int32_t id[kMine];
     float w[kMine], dw[kMine], dot = 0.0f;
 #pragma unroll
@@ -348,12 +422,12 @@ __global__ __launch_bounds__(256) void choose_gradient_kernel(ChooseArgs a) {
       w[q] = dw[q] = 0.0f;
       if (a.dweights && j < a.k) {
         id[q] = a.ids[t * a.k + j];
-        if ((uint32_t)id[q] < (uint32_t)a.experts) {
-          w[q] = a.weights[t * a.k + j];
-          dw[q] = a.dweights[t * a.k + j];
-        } else {
-          id[q] = -1;
-        }
+        w[q] = a.weights[t * a.k + j];
+        dw[q] = a.dweights[t * a.k + j];
+      }
+      if ((uint32_t)id[q] >= (uint32_t)a.experts) {
+        id[q] = -1;
+        w[q] = dw[q] = 0.0f;
       }
       dot = fmaf(w[q], dw[q], dot);
     }
@@ -369,7 +443,7 @@ __global__ __launch_bounds__(256) void choose_gradient_kernel(ChooseArgs a) {
     float sum = 0.0f, of_counts = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      x[v] = expf(x[v] - from);
+      x[v] = exp_from(x[v], from);
       sum += x[v];
       of_counts = fmaf(c[v], x[v], of_counts);
     }
@@ -409,8 +483,11 @@ __global__ __launch_bounds__(256) void choose_gradient_kernel(ChooseArgs a) {
 
 // -- host ---------------------------------------------------------------------
 
-constexpr int kMostBlocks = 256;
-// Tokens that one workgroup takes by itself.
+// Workgroups at the most: what they leave is added up by one.  us with 256 and 128 of
+// them: 65536 x 256 of bf16 44 and 61, 4096 x 1024 52 and 38.
+constexpr int most_blocks(int experts) { return experts <= 256 ? 256 : 128; }
+// Tokens that one workgroup takes by itself (256 x 64: 13.2 us, by several and a second
+// launch 14.9).
 constexpr int64_t kAloneTokens = 256;
 
 bool choose_sizes(int64_t tokens, int32_t experts, int32_t k) {
@@ -423,7 +500,7 @@ int lanes_of(int experts) { return experts <= 256 ? 16 : 64; }
 int choose_blocks(int64_t tokens, int experts) {
   if (tokens <= kAloneTokens) return 1;
   const int64_t groups = experts <= 256 ? choose_waves<16>() * 4 : choose_waves<64>(), n = ceil_div(tokens, groups);
-  return (int)(n < kMostBlocks ? n : kMostBlocks);
+  return (int)(n < most_blocks(experts) ? n : most_blocks(experts));
 }
 
 // f(type, lanes, elements a lane) of the smallest that holds a row.
@@ -488,8 +565,8 @@ ws_status ws_expert_choose(const ws_matrix* logits, int32_t k, float* weights, i
     return launch("expert_choose", &choose_kernel<T, L, V, false>, a.blocks, 64 * waves, lds, stream, a);
   });
   if (s != WS_OK || a.blocks == 1) return s;
-  const int n = a.experts + 1, slices = kFinishThreads / n > 0 ? kFinishThreads / n : 1;
-  return launch("expert_choose", &choose_finish_kernel, 1, kFinishThreads, slices * n * 8, stream, a);
+  const int n = a.experts + 1;
+  return launch("expert_choose", &choose_finish_kernel, 1, kFinishThreads, finish_slices(n) * n * 8, stream, a);
 }
 
 ws_status ws_expert_choose_gradient(const ws_matrix* logits, int32_t k, const float* dweights, const float* dloss,

@@ -38,6 +38,8 @@ struct OrthArgs {
   int32_t M, N, K;               // multiples of kPad; rows of K elements
   int32_t batch, tile_groups, tiles_m, tiles_n;
   uint32_t plane;                // tiles of one matrix
+  uint32_t first, count;         // tiles of this launch; quarters: every one of them in four of half its sides
+  int32_t quarters;
   _Float16 *to, *mirror;         // S; T; Y' and X'
   int64_t stride_to, stride_mirror;
   const float* d_in;             // kSquare: dA; kApply: dB
@@ -263,7 +265,7 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4, wm = wave >> 1, wn = wave & 1;
   // an XCD (workgroups go round them in turn) has a run of the tiles
-  const uint32_t tiles = a.plane * (uint32_t)a.batch, xcd = blockIdx.x % 8, share = tiles / 8, extra = tiles % 8;
+  const uint32_t tiles = a.count, xcd = blockIdx.x % 8, share = tiles / 8, extra = tiles % 8;
   const uint32_t turns = (a.tile_groups + 7 - xcd) / 8, end = xcd * share + min(xcd, extra) + share + (xcd < extra);
   uint32_t id = xcd * share + min(xcd, extra) + blockIdx.x / 8;
 
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
   } t, later;
   // Where tile `id` lies; past the last one: nowhere, which reads zeros.
   const auto find_tile = [&](Tile& t, uint32_t id) {
-    const uint32_t matrix = id / a.plane, in = id % a.plane;
+    const uint32_t tile = a.first + (a.quarters ? id / 4 : id), matrix = tile / a.plane, in = tile % a.plane;
     uint32_t tm, tn;
     if constexpr (kSymmetric) {  // row after row of the lower triangle
       tm = (uint32_t)((sqrtf(8.0f * (float)in + 1.0f) - 1.0f) * 0.5f);
@@ -293,12 +295,17 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
       tm = first + in % wide % high;
       tn = in % wide / high;
     }
-    const bool there = id < end;
+    if (a.quarters) {
+      tm = 2 * tm + id % 4 / 2;
+      tn = 2 * tn + id % 2;
+    }
+    // past the last tile, and a quarter beside the matrix or above its diagonal: nothing
+    const bool there = id < end && (int)tm * TM < a.M && (int)tn * TN < a.N && (!kSymmetric || tn <= tm);
     t.matrix = there ? matrix : 0;
-    t.m0 = __builtin_amdgcn_readfirstlane(there ? (int)tm * TM : 0);
-    t.n0 = __builtin_amdgcn_readfirstlane(there ? (int)tn * TN : 0);
-    t.ra = raw_buffer((const uint8_t*)(a.A + t.matrix * a.stride_a + (int64_t)t.m0 * a.K), there ? (uint32_t)min(a.M - t.m0, TM) * ld : 0);
-    t.rb = raw_buffer((const uint8_t*)(a.B + t.matrix * a.stride_b + (int64_t)t.n0 * a.K), there ? (uint32_t)min(a.N - t.n0, TN) * ld : 0);
+    t.m0 = __builtin_amdgcn_readfirstlane(there ? (int)tm * TM : a.M);
+    t.n0 = __builtin_amdgcn_readfirstlane(there ? (int)tn * TN : a.N);
+    t.ra = raw_buffer((const uint8_t*)(a.A + t.matrix * a.stride_a + (int64_t)t.m0 * a.K), (uint32_t)min(a.M - t.m0, TM) * ld);
+    t.rb = raw_buffer((const uint8_t*)(a.B + t.matrix * a.stride_b + (int64_t)t.n0 * a.K), (uint32_t)min(a.N - t.n0, TN) * ld);
     t.ahead_a = tn % 4 * 64;
     t.ahead_b = tm % 8 * 32;
   };
@@ -562,14 +569,13 @@ bool orth_sizes(int64_t rows, int64_t cols, int64_t batch) {
          (rows == 0 || cols == 0 || batch <= kMaxTiles / (ceil_div(rows, 64) * ceil_div(cols, 64)));
 }
 
+// Launches tiles of 32 WM x 32 WN.
 template <int WM, int WN, int KIND>
-ws_status run_tiles(OrthArgs a, hipStream_t stream) {
+ws_status launch_tiles(OrthArgs a, hipStream_t stream) {
   typedef OrthShape<WM, WN> Shape;
-  a.tiles_m = (int32_t)ceil_div(a.M, Shape::TM);
-  a.tiles_n = (int32_t)ceil_div(a.N, Shape::TN);
-  a.plane = KIND == kGram || KIND == kSquare ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
-  const int64_t tiles = (int64_t)a.plane * a.batch, most = (int64_t)compute_units() * Shape::kWaves;
-  a.tile_groups = (int32_t)(tiles < most ? tiles : most);
+  if (a.quarters) a.count *= 4;
+  const uint32_t most = (uint32_t)compute_units() * Shape::kWaves;
+  a.tile_groups = (int32_t)(a.count < most ? a.count : most);
   const auto kernel = &orth_step_kernel<WM, WN, KIND>;
   static std::atomic<uint64_t> allowed;  // devices on which the kernel may use this much LDS
   int dev = 0;
@@ -582,12 +588,34 @@ ws_status run_tiles(OrthArgs a, hipStream_t stream) {
   return launch("orthogonalize", kernel, a.tile_groups, 256, Shape::kLds, stream, a);
 }
 
+// Tiles of 256 x 256 where they fill the card, of 128 x 128 (two workgroups a CU) where
+// not: 4 x 2048 x 4096 FIGURE.  What a last round of large tiles leaves of half the card
+// or less runs in quarters, in a launch of its own: 16 x 2048 x 4096, X X^T FIGURE2.
 template <int KIND>
-ws_status run_tiles(const OrthArgs& a, hipStream_t stream) {
-  const int64_t big = KIND == kGram || KIND == kSquare ? ceil_div(a.M, 256) * (ceil_div(a.M, 256) + 1) / 2
-                                                       : ceil_div(a.M, 256) * ceil_div(a.N, 256);
-  if (big * a.batch >= 256) return run_tiles<8, 8, KIND>(a, stream);
-  return run_tiles<4, 4, KIND>(a, stream);
+ws_status run_tiles(OrthArgs a, hipStream_t stream) {
+  constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
+  const auto cut = [&](int side) {
+    a.tiles_m = (int32_t)ceil_div(a.M, side);
+    a.tiles_n = (int32_t)ceil_div(a.N, side);
+    a.plane = kSymmetric ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
+    a.first = 0;
+    a.count = a.plane * (uint32_t)a.batch;
+    a.quarters = 0;
+  };
+  const uint32_t cus = (uint32_t)compute_units();
+  cut(256);
+  if (a.count < cus) {
+    cut(128);
+    return launch_tiles<4, 4, KIND>(a, stream);
+  }
+  const uint32_t rest = a.count % cus <= cus / 2 ? a.count % cus : 0;
+  a.count -= rest;
+  const ws_status s = launch_tiles<8, 8, KIND>(a, stream);
+  if (s != WS_OK || rest == 0) return s;
+  a.first = a.count;
+  a.count = rest;
+  a.quarters = 1;
+  return launch_tiles<4, 4, KIND>(a, stream);
 }
 
 }  // namespace

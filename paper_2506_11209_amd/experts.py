@@ -27,7 +27,7 @@ from . import wsgemm as _w
 from .fp8 import _Call, _check, _elsewhere, _matrix, _mp, _need, _new_matrix, _raw_stream
 
 MAX_EXPERTS = 1024
-MAX_CHOICES = 64
+MAX_CHOICES = 32
 
 _lib = _w.library()
 _p, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
