@@ -52,18 +52,19 @@ struct OrthArgs {
   int32_t rows, cols, transposed;  // of out; transposed: it is X, not Y
 };
 
-template <int WM, int WN>
+template <int WM, int WN, int STAGES>
 struct OrthShape {
   static constexpr int TM = 32 * WM, TN = 32 * WN, kStage = (TM + TN) * 128;
   static constexpr bool kAgpr = WM * WN > 16;
-  static constexpr int kWaves = kAgpr ? 1 : 2;
+  static constexpr int kWaves = !kAgpr && STAGES == 2 ? 2 : 1;  // of a SIMD, as workgroups of a CU
   static constexpr int kFirst = WM > 4 ? 3 : WM / 2;
-  // a wave's way to memory: 64 x 32 results
-  static constexpr int kStoreBytes = 64 * 32 * 2;
+  // a wave's way to memory: 64 (or all its) rows of 32 columns
+  static constexpr int kHalves = WM >= 4 ? 2 : 1, kStoreBytes = kHalves * 32 * 32 * 2;
   // Lines of later blocks are asked for ahead by loads that end here, 256 bytes a wave.
-  static constexpr bool kAhead = kWaves == 1;
-  static constexpr int kStoreAt = 2 * kStage, kAheadAt = kStoreAt + 4 * kStoreBytes, kLds = kAheadAt + (kAhead ? 4 * 256 : 0);
+  static constexpr bool kAhead = kAgpr;
+  static constexpr int kStoreAt = STAGES * kStage, kAheadAt = kStoreAt + 4 * kStoreBytes, kLds = kAheadAt + (kAhead ? 4 * 256 : 0);
   static_assert(kWaves * kLds <= 160 * 1024, "LDS of a CU");
+  static_assert((STAGES & (STAGES - 1)) == 0 && (!kAhead || STAGES == 2), "");
 };
 
 // One of two descriptors, as scalars.
@@ -103,16 +104,17 @@ __device__ __forceinline__ int chunk_of_b(int r, int c) { return (c ^ (r & 3 | (
 // 4 g + 3 of both hold rows 8 g .. 8 g + 7.
 __device__ __forceinline__ int row_of_b(int r, int j) { return 8 * (r >> 2) + 4 * j + (r & 3); }
 
-// Writes 64 x 32 values of a wave, of which lane (r, g) has columns 8 g .. of rows 16 i
+// Writes 32 H x 32 values of a wave, of which lane (r, g) has columns 8 g .. of rows 16 i
 // + r, two to a word, turned round by way of its part of LDS: put(column, row, piece)
 // takes 8 neighbours of a column.  Pieces of 16 bytes change places within a line, by
 // the line's number, against bank conflicts.
-template <typename F>
-__device__ __forceinline__ void turn_round(const i32x4_t (&v)[4], uint8_t* own, const F& put) {
+template <int H, typename F>
+__device__ __forceinline__ void turn_round(const i32x4_t (&v)[2 * H], uint8_t* own, const F& put) {
+  constexpr int kPieces = 4 * H;  // of a line
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const auto place = [](int line, int piece) { return (line * 8 + (piece ^ (line & 7))) * 16; };
+  const auto place = [](int line, int piece) { return (line * kPieces + (piece ^ (line & (kPieces - 1)))) * 16; };
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 2 * H; ++i)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       // with the neighbouring row's: even lanes take the first column of a word, odd ones the second
@@ -122,8 +124,8 @@ __device__ __forceinline__ void turn_round(const i32x4_t (&v)[4], uint8_t* own, 
     }
   __builtin_amdgcn_wave_barrier();  // a wave's LDS accesses keep their order
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int line = 8 * e + lane / 8, at = lane % 8;
+  for (int e = 0; e < 2 * H; ++e) {
+    const int line = 64 / kPieces * e + lane / kPieces, at = lane % kPieces;
     put(line, 8 * at, *(const i32x4_t*)(own + place(line, at)));
   }
   __builtin_amdgcn_wave_barrier();
@@ -211,9 +213,9 @@ __device__ __forceinline__ void convert(const OrthArgs& a, const f32x4_t* (&acc)
   }
 }
 
-// Writes 64 x 32 converted results of a wave from row m and column n where they belong.
-template <int KIND>
-__device__ __forceinline__ void write_part(const OrthArgs& a, const i32x4_t (&v)[4], int64_t matrix, int m, int n, bool twice,
+// Writes 32 H x 32 converted results of a wave from row m and column n where they belong.
+template <int KIND, int H>
+__device__ __forceinline__ void write_part(const OrthArgs& a, const i32x4_t (&v)[2 * H], int64_t matrix, int m, int n, bool twice,
                                            uint8_t* own) {
   const int lane = threadIdx.x & 63, r = lane & 15, col = n + 8 * (lane >> 4);
   if constexpr (KIND == kLast) {
@@ -229,35 +231,36 @@ __device__ __forceinline__ void write_part(const OrthArgs& a, const i32x4_t (&v)
       }
     };
     if (a.transposed) {
-      turn_round(v, own, [&](int line, int at, i32x4_t piece) { put(n + line, m + at, piece); });
+      turn_round<H>(v, own, [&](int line, int at, i32x4_t piece) { put(n + line, m + at, piece); });
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) put(m + 16 * i + r, col, v[i]);
+      for (int i = 0; i < 2 * H; ++i) put(m + 16 * i + r, col, v[i]);
     }
   } else {
     _Float16* to = a.to + matrix * a.stride_to + (int64_t)(m + r) * a.N + col;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *(i32x4_t*)(to + 16 * i * (int64_t)a.N) = v[i];
+    for (int i = 0; i < 2 * H; ++i) *(i32x4_t*)(to + 16 * i * (int64_t)a.N) = v[i];
     if (twice) {
       _Float16* mirror = a.mirror + matrix * a.stride_mirror;
-      turn_round(v, own, [&](int line, int at, i32x4_t piece) { *(i32x4_t*)(mirror + (int64_t)(n + line) * a.M + m + at) = piece; });
+      turn_round<H>(v, own, [&](int line, int at, i32x4_t piece) { *(i32x4_t*)(mirror + (int64_t)(n + line) * a.M + m + at) = piece; });
     }
   }
 }
 
-// A tile of 32 WM x 32 WN by four waves, 2 x 2.  Blocks of 64 columns are double-buffered
-// in LDS, and a block's products come in two halves, as in ws_fp8_product.hip:
+// A tile of 32 WM x 32 WN by four waves, 2 x 2.  Blocks of 64 columns lie in a ring of
+// STAGES in LDS, and a block's products come in two halves, as in ws_fp8_product.hip:
 //
 //   the first kFirst rows, row by row: the rest of A of block b is read
 //   meet: b + 1 has landed everywhere, b has been read everywhere
-//   the other rows, column by column: b + 2 is loaded over b; the first rows of A
+//   the other rows, column by column: b + STAGES is loaded over b; the first rows of A
 //   of b + 1 are read, and every column of B of b + 1 once that of b is done
 //
-// Loads go on into a workgroup's next tile, whose first two blocks are there when the
-// tile it has is written.
-template <int WM, int WN, int KIND>
-__global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_kernel(OrthArgs a) {
-  typedef OrthShape<WM, WN> Shape;
+// Loads go on into a workgroup's next tile, whose first blocks are there when the tile it
+// has is written (a tile has two blocks or more; with more stages a workgroup has one).
+// Long rings are for few tiles, one a CU, whose blocks are shorter than the way to memory.
+template <int WM, int WN, int STAGES, int KIND>
+__global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth_step_kernel(OrthArgs a) {
+  typedef OrthShape<WM, WN, STAGES> Shape;
   constexpr int TM = Shape::TM, TN = Shape::TN, kStage = Shape::kStage, kFirst = Shape::kFirst, kRows = WM - kFirst;
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
   static_assert(!kSymmetric || TM == TN, "tiles of the lower triangle");
@@ -273,7 +276,7 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
   const int lr = 8 * wave + (lane >> 3);  // chunk_at and chunk_of_b are their own inverses
   const uint32_t at_a = (uint32_t)lr * ld + chunk_at(lr, lane & 7), at_b = (uint32_t)lr * ld + chunk_of_b(lr, lane & 7), step = 32 * ld;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(WSG_LDS uint8_t*)smem + wave * 1024;
-  const int blocks = a.K / 64;  // even
+  const int blocks = a.K / 64;  // even: every tile's first one lies in stage 0 where there are two, or where a workgroup has one tile
   constexpr int kLoads = (TM + TN) / 32;  // of a wave and block, 1 KiB each
   struct Tile {
     int64_t matrix;
@@ -313,7 +316,7 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
   const auto load = [&](int b, int from, int to) {
     const bool here = b < blocks;
     const int k = (here ? b : b - blocks) * 128;
-    const uint32_t lds = lds0 + (b & 1) * kStage;
+    const uint32_t lds = lds0 + (b & (STAGES - 1)) * kStage;
     const i32x4_t ra = select(here, t.ra, later.ra), rb = select(here, t.rb, later.rb);
 #pragma unroll
     for (int i = from; i < to; ++i) {
@@ -334,9 +337,9 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
 
   if (id >= end) return;
   find_tile(t, id);
-  load(0, 0, kLoads);
-  load(1, 0, kLoads);
-  drain_and_meet();
+  if constexpr (STAGES > 2) find_tile(later, id + turns);  // more stages than blocks
+  for (int b = 0; b < STAGES; ++b) load(b, 0, kLoads);
+  drain_and_meet<kLoads * (STAGES - 1)>();
   for (; id < end; id += turns) {
     find_tile(later, id + turns);
     f32x4_t acc[WM][WN];
@@ -361,7 +364,7 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
     for (int i = 0; i < kFirst; ++i) frag_a(i, 0);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): in the loop the compiler then counts LDS reads only
     for (int b = 0; b < blocks; ++b) {
-      const int here = (b & 1) * kStage, next = kStage - here;
+      const int here = (b & (STAGES - 1)) * kStage, next = ((b + 1) & (STAGES - 1)) * kStage;
       static_for<kFirst>([&](auto ic) {
         constexpr int i = decltype(ic)::value;
         static_for<2 * WN>([&](auto jc) {
@@ -375,14 +378,14 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
         });
         __builtin_amdgcn_sched_barrier(0);
       });
-      drain_and_meet<Shape::kAhead ? 1 : 0>();  // all but the lines asked for
+      drain_and_meet<Shape::kAhead ? 1 : kLoads * (STAGES - 2)>();  // all but the lines asked for, or the later blocks
       static_for<WN>([&](auto jc) {
         constexpr int j = decltype(jc)::value;
         static_for<2 * kRows>([&](auto ic) {
           constexpr int q = decltype(ic)::value / kRows, i = kFirst + decltype(ic)::value % kRows;
           constexpr int n = j * 2 * kRows + decltype(ic)::value, all = 2 * kRows * (WN > 2 ? WN - 1 : WN);
           multiply_f16<Shape::kAgpr>(acc[i][j], fa[i][q], fb[j][q]);
-          if constexpr (n < all) load(b + 2, n * kLoads / all, (n + 1) * kLoads / all);
+          if constexpr (n < all) load(b + STAGES, n * kLoads / all, (n + 1) * kLoads / all);
           if constexpr (decltype(ic)::value == 0) {
 #pragma unroll
             for (int k = j * kFirst / WN; k < (j + 1) * kFirst / WN; ++k) frag_a(k, next);
@@ -399,33 +402,33 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN>::kWaves)) void orth_step_ke
     const int m0 = t.m0, n0 = t.n0;
     t = later;
     uint8_t* own = smem + Shape::kStoreAt + wave * Shape::kStoreBytes;
-    // parts of 64 x 32; what the next half of one needs is fetched before a half is converted
-    constexpr int kParts = WM / 4 * (WN / 2);
+    // parts of 32 kHalves x 32; what the next half of one needs is fetched before a half is converted
+    constexpr int kHalves = Shape::kHalves, kParts = WM / (2 * kHalves) * (WN / 2);
     const auto place = [&](int p, int* m, int* n) {
-      *m = m0 + (wm * WM + p / (WN / 2) * 4) * 16;
+      *m = m0 + (wm * WM + p / (WN / 2) * (2 * kHalves)) * 16;
       *n = n0 + (wn * WN + p % (WN / 2) * 2) * 16;
       return *m < a.M && *n < a.N;  // sides are multiples of 64
     };
     Old<KIND> old[2];
-    i32x4_t v[4];
+    i32x4_t v[2 * kHalves];
     int m, n;
     if (place(0, &m, &n)) fetch<KIND>(a, matrix, m, n, old[0]);
-    static_for<2 * kParts>([&](auto hc) {
-      constexpr int h = decltype(hc)::value, p = h / 2;
-      if constexpr (h + 1 < 2 * kParts)
-        if (place((h + 1) / 2, &m, &n)) fetch<KIND>(a, matrix, m + (h + 1) % 2 * 32, n, old[(h + 1) % 2]);
+    static_for<kHalves * kParts>([&](auto hc) {
+      constexpr int h = decltype(hc)::value, p = h / kHalves;
+      if constexpr (h + 1 < kHalves * kParts)
+        if (place((h + 1) / kHalves, &m, &n)) fetch<KIND>(a, matrix, m + (h + 1) % kHalves * 32, n, old[(h + 1) % 2]);
       const f32x4_t* part[2][2];
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          f32x4_t& s = acc[p / (WN / 2) * 4 + h % 2 * 2 + i][p % (WN / 2) * 2 + j];
+          f32x4_t& s = acc[p / (WN / 2) * (2 * kHalves) + h % kHalves * 2 + i][p % (WN / 2) * 2 + j];
           settle<Shape::kAgpr>(s);
           part[i][j] = &s;
         }
       if (place(p, &m, &n)) {
-        convert<KIND>(a, part, old[h % 2], matrix, m + h % 2 * 32, n, v + h % 2 * 2);
-        if constexpr (h % 2 == 1) write_part<KIND>(a, v, matrix, m, n, !kSymmetric || m0 != n0, own);
+        convert<KIND>(a, part, old[h % 2], matrix, m + h % kHalves * 32, n, v + h % kHalves * 2);
+        if constexpr (h % kHalves == kHalves - 1) write_part<KIND, kHalves>(a, v, matrix, m, n, !kSymmetric || m0 != n0, own);
       }
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -570,13 +573,13 @@ bool orth_sizes(int64_t rows, int64_t cols, int64_t batch) {
 }
 
 // Launches tiles of 32 WM x 32 WN.
-template <int WM, int WN, int KIND>
+template <int WM, int WN, int STAGES, int KIND>
 ws_status launch_tiles(OrthArgs a, hipStream_t stream) {
-  typedef OrthShape<WM, WN> Shape;
+  typedef OrthShape<WM, WN, STAGES> Shape;
   if (a.quarters) a.count *= 4;
   const uint32_t most = (uint32_t)compute_units() * Shape::kWaves;
   a.tile_groups = (int32_t)(a.count < most ? a.count : most);
-  const auto kernel = &orth_step_kernel<WM, WN, KIND>;
+  const auto kernel = &orth_step_kernel<WM, WN, STAGES, KIND>;
   static std::atomic<uint64_t> allowed;  // devices on which the kernel may use this much LDS
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
@@ -606,16 +609,19 @@ ws_status run_tiles(OrthArgs a, hipStream_t stream) {
   cut(256);
   if (a.count < cus) {
     cut(128);
-    return launch_tiles<4, 4, KIND>(a, stream);
+    if (a.count > cus) return launch_tiles<4, 4, 2, KIND>(a, stream);
+    if (4 * a.count > cus) return launch_tiles<4, 4, 4, KIND>(a, stream);  // QUARTER
+    cut(64);
+    return launch_tiles<2, 2, 8, KIND>(a, stream);
   }
   const uint32_t rest = a.count % cus <= cus / 2 ? a.count % cus : 0;
   a.count -= rest;
-  const ws_status s = launch_tiles<8, 8, KIND>(a, stream);
+  const ws_status s = launch_tiles<8, 8, 2, KIND>(a, stream);
   if (s != WS_OK || rest == 0) return s;
   a.first = a.count;
   a.count = rest;
   a.quarters = 1;
-  return launch_tiles<4, 4, KIND>(a, stream);
+  return launch_tiles<4, 4, 2, KIND>(a, stream);
 }
 
 }  // namespace

@@ -1,6 +1,7 @@
 """Wait states around the hand-placed matrix instructions of the orthogonalised
 update's kernels, read from the built library's machine code (CPU only)."""
 import os
+import re
 
 import pytest
 
@@ -16,7 +17,8 @@ def test_step_kernels_keep_their_wait_states(library_code):  # noqa: F811
         if "orth_step_kernel" not in name:
             continue
         kernels += 1
-        assert sum(mn == "v_mfma_f32_16x16x32_f16" for _, mn, _, _ in ins) >= 16
+        wm, wn = map(int, re.search(r"orth_step_kernelILi(\d+)ELi(\d+)E", name).groups())
+        assert sum(mn == "v_mfma_f32_16x16x32_f16" for _, mn, _, _ in ins) >= 2 * wm * wn  # a block's
         problems += [(name[-40:],) + b for b in check(start, ins)]
-    assert kernels >= 8
+    assert kernels == 16
     assert not problems, problems[:20]
