@@ -8,9 +8,16 @@ router's weights.  Backward: the gradient of the way back, the input gradients a
 grouped products with the transposed weights, the weight gradients as products
 over each expert's rows in 32 bits.
 
+The router's choice can come with a loss that keeps the experts evenly loaded
+(``layer(x, balance=True)``), the weights can be updated along orthogonalised
+directions (``orthogonal.OrthogonalMomentum``), and decoding can run on weights in 4
+bits (``layer.serving_weights(4)``).
+
     python -m paper_2506_11209_amd.expert_layer [--tokens 4096] [--experts 16] ...
 
-times a training step and a decoding step on the GPU and prints a line for each.
+times a training step and a decoding step on the GPU and prints a line for each;
+--balance 0.01 adds the balance loss to the training step, --update a line for an
+update of all weights, --bits 4 decodes with weights in 4 bits.
 """
 from __future__ import annotations
 
@@ -21,7 +28,7 @@ import time
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import experts, fp8
+from . import experts, fp4, fp8, orthogonal
 
 
 class _Experts(torch.autograd.Function):
@@ -97,18 +104,38 @@ class ExpertLayer(torch.nn.Module):
         score, ids = (x.float() @ self.router.t()).topk(self.k, dim=1)
         return score.softmax(1), ids
 
-    def forward(self, x):
+    def choose(self, x):
+        """(weights, ids, counts, loss): route with the experts' counts and the balance
+        loss (experts.choose)."""
+        return experts.choose(x.float() @ self.router.t(), self.k)
+
+    def forward(self, x, balance: bool = False):
+        """y; with balance (y, the balance loss)."""
+        if balance:
+            weights, ids, _, loss = self.choose(x)
+            return _Experts.apply(x, weights, self.w1, self.w2, ids), loss
         weights, ids = self.route(x)
         return _Experts.apply(x, weights, self.w1, self.w2, ids)
 
     @torch.no_grad()
-    def serving_weights(self):
-        """The experts' weights in 8 bits, laid out once for serve."""
+    def serving_weights(self, bits: int = 8):
+        """The experts' weights in 8 or 4 bits, laid out once for serve."""
+        if bits == 4:
+            return fp4.quantize_weight(self.w1), fp4.quantize_weight(self.w2)
+        if bits != 8:
+            raise ValueError("bits: 8 or 4, got %r" % (bits,))
         return fp8.quantize_weight(self.w1, transposed=False)[0], fp8.quantize_weight(self.w2, transposed=False)[0]
 
     @torch.no_grad()
     def serve(self, x, quantized):
-        """forward without what training keeps; quantized: serving_weights()."""
+        """forward without what training keeps; quantized: serving_weights().  With weights
+        in 4 bits the activations stay in bf16."""
+        if isinstance(quantized[0], fp4.Fp4Matrix):
+            weights, ids, _, _ = self.choose(x)
+            routes = experts.sort(ids, self.w1.shape[0])
+            h = fp4.grouped_product(x, quantized[0], routes.offsets, index=routes.token)
+            rows = fp4.grouped_product(torch.nn.functional.silu(h), quantized[1], routes.offsets)
+            return experts.combine(rows, routes, weights)
         weights, ids = self.route(x)
         routes = experts.sort(ids, self.w1.shape[0])
         h = fp8.grouped_product(fp8.quantize_rows(x, index=routes.token), quantized[0], routes.offsets)
@@ -131,22 +158,33 @@ def main(argv=None) -> None:
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, value in (("tokens", 4096), ("decode", 32), ("columns", 2048), ("hidden", 4096), ("experts", 16), ("k", 2), ("steps", 20)):
         ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--balance", type=float, default=0.0)
+    ap.add_argument("--update", action="store_true")
+    ap.add_argument("--bits", type=int, choices=(4, 8), default=8)
     a = ap.parse_args(argv)
     g = torch.Generator(device="cuda").manual_seed(0)
     layer = ExpertLayer(a.columns, a.hidden, a.experts, a.k, generator=g)
     x = torch.randn(a.tokens, a.columns, device="cuda", generator=g).bfloat16().requires_grad_()
     dy = torch.randn(a.tokens, a.columns, device="cuda", generator=g).bfloat16()
     few = x.detach()[: a.decode].contiguous()
-    quantized = layer.serving_weights()
+    quantized = layer.serving_weights(a.bits)
 
     def train():
         layer.zero_grad()
         x.grad = None
-        layer(x).backward(dy)
+        if a.balance:
+            y, loss = layer(x, balance=True)
+            torch.autograd.backward((y, a.balance * loss), (dy, None))
+        else:
+            layer(x).backward(dy)
 
     flops = 6.0 * a.tokens * a.k * a.columns * a.hidden * 2
     s = _time(train, a.steps)
     print(json.dumps({"step": "training", "tokens": a.tokens, "us": round(s * 1e6, 1), "tflops": round(flops / s / 1e12, 1)}), flush=True)
+    if a.update:
+        optimizer = orthogonal.OrthogonalMomentum(layer.parameters(), lr=1e-4)
+        s = _time(optimizer.step, a.steps)
+        print(json.dumps({"step": "update", "weights": sum(p.numel() for p in layer.parameters()), "us": round(s * 1e6, 1)}), flush=True)
     s = _time(lambda: layer.serve(few, quantized), a.steps)
     print(json.dumps({"step": "decoding", "tokens": few.shape[0], "us": round(s * 1e6, 1)}), flush=True)
 
