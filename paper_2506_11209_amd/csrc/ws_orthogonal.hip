@@ -539,8 +539,6 @@ __global__ __launch_bounds__(256) void orth_start_kernel(OrthStartArgs a) {
 
 // -- host ---------------------------------------------------------------------
 
-constexpr int64_t kMaxTiles = 1ll << 30;
-
 struct Layout {
   int64_t n, m;  // padded sides
   int64_t sums, X, Y0, Y1, rest, S, T, dA, dB, all;
@@ -567,9 +565,12 @@ Layout layout(int64_t rows, int64_t cols, int64_t batch) {
   return l;
 }
 
+// Sides, and what the launches hold: workgroups for 64 x 64 of the padded matrices, and 64
+// parts of each.
 bool orth_sizes(int64_t rows, int64_t cols, int64_t batch) {
-  return rows >= 0 && cols >= 0 && batch >= 0 && rows <= WS_ORTHOGONAL_SIDE && cols <= WS_ORTHOGONAL_SIDE && batch <= 1 << 20 &&
-         (rows == 0 || cols == 0 || batch <= kMaxTiles / (ceil_div(rows, 64) * ceil_div(cols, 64)));
+  if (rows < 0 || cols < 0 || batch < 0 || rows > WS_ORTHOGONAL_SIDE || cols > WS_ORTHOGONAL_SIDE) return false;
+  return rows == 0 || cols == 0 ||
+         (batch <= max_workgroups(256) / kMostParts && 4 * ceil_div(rows, kPad) * ceil_div(cols, kPad) * batch <= max_workgroups(256));
 }
 
 // Launches tiles of 32 WM x 32 WN.
@@ -667,7 +668,6 @@ ws_status ws_orthogonalize(const ws_matrix* G, int32_t steps, const ws_matrix* o
   const int64_t parts = ceil_div(G->rows * G->cols, 8 * kSumThreads * 4);
   s.parts = (int32_t)(parts < kMostParts ? parts : kMostParts);
   const int64_t grid = l.n / 64 * (l.m / 64) * G->batch;
-  if (grid > max_workgroups(256)) return WS_ERR_INVALID_ARG;
   ws_status st = launch("orthogonalize", G->dtype == WS_OUT_F32 ? &orth_sum_kernel<float> : G->dtype == WS_OUT_BF16 ? &orth_sum_kernel<bf16_t>
                                                                                                                    : &orth_sum_kernel<f16_t>,
                         (int64_t)s.parts * G->batch, kSumThreads, 0, stream, s);
