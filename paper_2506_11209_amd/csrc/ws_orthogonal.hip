@@ -56,7 +56,7 @@ template <int WM, int WN, int STAGES>
 struct OrthShape {
   static constexpr int TM = 32 * WM, TN = 32 * WN, kStage = (TM + TN) * 128;
   static constexpr bool kAgpr = WM * WN > 16;
-  static constexpr int kWaves = !kAgpr && STAGES == 2 ? 2 : 1;  // of a SIMD, as workgroups of a CU
+  static constexpr int kWaves = kAgpr || STAGES > 2 ? 1 : WM * WN > 4 ? 2 : 4;  // of a SIMD, as workgroups of a CU
   static constexpr int kFirst = WM > 4 ? 3 : WM / 2;
   // a wave's way to memory: 64 (or all its) rows of 32 columns
   static constexpr int kHalves = WM >= 4 ? 2 : 1, kStoreBytes = kHalves * 32 * 32 * 2;
@@ -446,7 +446,7 @@ struct OrthStartArgs {
   int64_t n, m;               // padded sides
 };
 
-constexpr int kSumThreads = 256, kMostParts = 64;
+constexpr int kSumThreads = 256, kMostParts = 256;
 
 __device__ __forceinline__ double sum_of_wave(double x) {
   for (int d = 32; d; d /= 2) x += __shfl_xor(x, d);
@@ -500,15 +500,20 @@ __global__ __launch_bounds__(256) void orth_start_kernel(OrthStartArgs a) {
   const int64_t across = cols / 64, plane = rows / 64 * across, matrix = blockIdx.x / plane, in = blockIdx.x % plane;
   const int64_t r0 = in / across * 64, c0 = in % across * 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  double sum = lane < a.parts ? a.sums[matrix * a.parts + lane] : 0.0;  // every wave by itself, in the same order
+  const T* G = (const T*)a.G + matrix * a.stride;
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {  // in flight before the sums are
+    const int64_t r = r0 + 4 * i + wave, c = c0 + lane;
+    v[i] = r < a.rows && c < a.cols ? to_f32(G[r * a.ld + c]) : 0.0f;
+  }
+  double sum = 0.0;  // every wave by itself, in the same order
+#pragma unroll
+  for (int i = 0; i < kMostParts; i += 64) sum += lane + i < a.parts ? a.sums[matrix * a.parts + lane + i] : 0.0;
   sum = sum_of_wave(sum);
   const double by = sum == 0.0 ? 0.0 : sum > 1.7e308 || sum != sum ? (double)NAN : (double)kUnit / sqrt(sum);
-  const T* G = (const T*)a.G + matrix * a.stride;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int64_t r = r0 + 4 * i + wave, c = c0 + lane;
-    tile[4 * i + wave][lane] = r < a.rows && c < a.cols ? (float)((double)to_f32(G[r * a.ld + c]) * by) : 0.0f;
-  }
+  for (int i = 0; i < 16; ++i) tile[4 * i + wave][lane] = (float)((double)v[i] * by);
   __syncthreads();
   _Float16 *X = a.X + matrix * a.n * a.m, *Y = a.Y + matrix * a.n * a.m, *rest = a.rest + matrix * a.n * a.m;
   // as G lies: Y (with its rest) where G is tall, else X
@@ -565,8 +570,8 @@ Layout layout(int64_t rows, int64_t cols, int64_t batch) {
   return l;
 }
 
-// Sides, and what the launches hold: workgroups for 64 x 64 of the padded matrices, and 64
-// parts of each.
+// Sides, and what the launches hold: workgroups for 64 x 64 of the padded matrices, and
+// kMostParts of each.
 bool orth_sizes(int64_t rows, int64_t cols, int64_t batch) {
   if (rows < 0 || cols < 0 || batch < 0 || rows > WS_ORTHOGONAL_SIDE || cols > WS_ORTHOGONAL_SIDE) return false;
   return rows == 0 || cols == 0 ||
@@ -592,9 +597,13 @@ ws_status launch_tiles(OrthArgs a, hipStream_t stream) {
   return launch("orthogonalize", kernel, a.tile_groups, 256, Shape::kLds, stream, a);
 }
 
-// Tiles of 256 x 256 where they fill the card, of 128 x 128 (two workgroups a CU) where
-// not: 4 x 2048 x 4096 FIGURE.  What a last round of large tiles leaves of half the card
-// or less runs in quarters, in a launch of its own: 16 x 2048 x 4096, X X^T FIGURE2.
+// Tiles of 256 x 256 where they fill the card.  What their last round leaves of half the
+// card or less runs in quarters, in a launch of its own (16 x 2048 x 4096: X X^T 300 us,
+// so 340; A^2 190, so 212).  Fewer: 128 x 128, two workgroups a CU, or with a long ring
+// where there is one a CU (1024 x 1024: 147 us for five steps, with two stages 252); 64 x 64
+// where even these would leave CUs without work (1024 columns of 2560: X X^T 13 us, in
+// 128 x 128 31), and for short contractions (4 x 188 x 1358: 125 us, in 128 x 128 142;
+// 2500 x 1000 the other way round, 214 and 208).
 template <int KIND>
 ws_status run_tiles(OrthArgs a, hipStream_t stream) {
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
@@ -611,8 +620,9 @@ ws_status run_tiles(OrthArgs a, hipStream_t stream) {
   if (a.count < cus) {
     cut(128);
     if (a.count > cus) return launch_tiles<4, 4, 2, KIND>(a, stream);
-    if (4 * a.count > cus) return launch_tiles<4, 4, 4, KIND>(a, stream);  // QUARTER
+    if (4 * a.count > cus && a.K > 512) return launch_tiles<4, 4, 4, KIND>(a, stream);
     cut(64);
+    if (a.count > cus) return launch_tiles<2, 2, 2, KIND>(a, stream);
     return launch_tiles<2, 2, 8, KIND>(a, stream);
   }
   const uint32_t rest = a.count % cus <= cus / 2 ? a.count % cus : 0;
