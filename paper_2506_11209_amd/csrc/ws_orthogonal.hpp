@@ -6,15 +6,13 @@
 
 namespace wsg {
 
-constexpr int kFewRows = 128;  // of the shorter side, at the most
-constexpr int kFewSteps = 6;   // see ws_orthogonal_few.hip
+constexpr int kFewRows = 64;  // of the shorter side, at the most
+constexpr int kFewSteps = 6;  // see ws_orthogonal_few.hip
 
-// Whether the Gram matrix alone is quicker.  us so and in tiles, five steps: 64 x 64 31
-// and 95, 64 x 2048 39 and 150, 128 x 512 140 and 129, 128 x 1024 147 and 152, 128 x 4096
-// 165 and 279.
+// Whether the Gram matrix alone is quicker.  us so and in tiles, five steps: 64 x 2048 38
+// and 110, 128 x 1024 148 and 97, 128 x 4096 165 and 147.
 inline bool by_gram_matrix(int64_t rows, int64_t cols, int32_t steps) {
-  const int64_t n = rows < cols ? rows : cols, m = rows < cols ? cols : rows;
-  return steps <= kFewSteps && (n <= 64 || (n <= kFewRows && m >= 1024));
+  return (rows < cols ? rows : cols) <= kFewRows && steps <= kFewSteps;
 }
 
 int64_t few_workspace(int64_t rows, int64_t cols, int64_t batch);

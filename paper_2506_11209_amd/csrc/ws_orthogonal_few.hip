@@ -1,4 +1,4 @@
-// Orthogonalised updates of matrices with a short side, n <= 128 (definitions:
+// Orthogonalised updates of matrices with a short side, n <= 64 (definitions:
 // ws_orthogonal.h).
 //
 // Every step multiplies X with a polynomial of A = X X^T, so all of them together
@@ -13,8 +13,6 @@
 // Sums: a part of G with very large or small values is scaled by a power of two of its
 // own, so that squares neither overflow nor vanish.
 #include <math.h>
-
-#include <atomic>
 
 #include "ws_fp8_common.hpp"
 #include "ws_orthogonal.hpp"
@@ -138,128 +136,96 @@ __global__ __launch_bounds__(64 * kGramWaves) void few_gram_kernel(FewArgs a) {
 
 template <int NT>
 struct FewShape {
-  static constexpr int kTiles = lower_tiles(NT), kWaves = kTiles < 16 ? kTiles : 16, kMine = (kTiles + kWaves - 1) / kWaves;
+  static constexpr int kWaves = lower_tiles(NT);  // a tile each
   static constexpr int kSide = 16 * NT, kPitch = kSide + 4;  // floats: rows spread over the banks
-  static constexpr int kLds = 2 * kSide * kPitch * 4;
 };
 
-// One workgroup's iteration.  Matrices are symmetric (polynomials of A_0): a wave has
-// tiles of the lower triangle and writes them to both places of one of two matrices in
-// LDS.  Bound: the products, 4 a step in a row; n = 64: about 0.9 us each.
+// One workgroup's iteration.  Matrices are symmetric (polynomials of A_0): a wave has a
+// tile of the lower triangle and writes it to both its places in one of two matrices in
+// LDS.  Bound: the latency of the products, 17 in a row for five steps, and of the meetings
+// between them (n = 16: 14 us, n = 64: 22 us).
 template <int NT>
 __global__ __launch_bounds__(64 * FewShape<NT>::kWaves) void few_iterate_kernel(FewArgs a) {
   typedef FewShape<NT> S;
-  constexpr int kMine = S::kMine;
-  extern __shared__ __align__(16) float lds[];
+  __shared__ __align__(16) float L[S::kSide * S::kPitch], R[S::kSide * S::kPitch];
   __shared__ float trace;
-  float *L = lds, *R = lds + S::kSide * S::kPitch;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
   const int64_t matrix = blockIdx.x;
-  int ti[kMine], tj[kMine];
-  bool have[kMine];
+  int ti, tj;
+  tile_at(wave, &ti, &tj);
+  const int row = 16 * ti + 4 * g, col = 16 * tj + r;  // the lane's: rows row .. row + 3
+  const auto put = [&](float* to, const f32x4_t& v) {
 #pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    const int t = wave + i * S::kWaves;
-    have[i] = t < S::kTiles;
-    tile_at(have[i] ? t : 0, &ti[i], &tj[i]);
-  }
-  // the tiles' lanes: rows 4 g .., column r
-  const auto put = [&](float* to, const f32x4_t (&v)[kMine]) {
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-      if (have[i]) {
-        const int row = 16 * ti[i] + 4 * g, col = 16 * tj[i] + r;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) to[(row + k) * S::kPitch + col] = v[i][k];
-        if (ti[i] != tj[i]) *(f32x4_t*)(to + col * S::kPitch + row) = v[i];
-      }
+    for (int k = 0; k < 4; ++k) to[(row + k) * S::kPitch + col] = v[k];
+    if (ti != tj) *(f32x4_t*)(to + col * S::kPitch + row) = v;
   };
-  const auto product = [&](const float* x, const float* y, f32x4_t (&v)[kMine]) {
+  const auto product = [&](const float* x, const float* y) {
+    f32x4_t u = {0, 0, 0, 0}, v = {0, 0, 0, 0};  // two sums, for half the way through each
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) v[i] = f32x4_t{0, 0, 0, 0};
-#pragma unroll 2
-    for (int k = 0; k < NT; ++k)
-#pragma unroll
-      for (int i = 0; i < kMine; ++i)
-        if (have[i]) {
-          const f32x4_t p = *(const f32x4_t*)(x + (16 * ti[i] + r) * S::kPitch + 16 * k + 4 * g);
-          const f32x4_t q = *(const f32x4_t*)(y + (16 * tj[i] + r) * S::kPitch + 16 * k + 4 * g);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[i] = multiply(p[e], q[e], v[i]);
-        }
+    for (int k = 0; k < NT; ++k) {
+      const f32x4_t p = *(const f32x4_t*)(x + (16 * ti + r) * S::kPitch + 16 * k + 4 * g);
+      const f32x4_t q = *(const f32x4_t*)(y + (16 * tj + r) * S::kPitch + 16 * k + 4 * g);
+      u = multiply(p[0], q[0], u);
+      v = multiply(p[1], q[1], v);
+      u = multiply(p[2], q[2], u);
+      v = multiply(p[3], q[3], v);
+    }
+    return u + v;
   };
   // G G^T, all parts with the largest one's scale
   const int its = lane < a.parts ? a.scales[matrix * a.parts + lane] : -kNotFinite;  // at most 64 parts
   int scale = its;
   for (int d = 32; d; d /= 2) scale = max(scale, __shfl_xor(scale, d));
   const int of_lane = 2 * max(its - scale, -200);  // what is left out is below 2^-149
-  f32x4_t A[kMine], Q[kMine], v[kMine];
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) A[i] = f32x4_t{0, 0, 0, 0};
+  f32x4_t A = {0, 0, 0, 0}, Q = {0, 0, 0, 0};
   if (scale > -kNotFinite && scale < kNotFinite) {
-    constexpr int kAtOnce = kMine > 1 ? 2 : 8;  // parts in flight
-    const f32x4_t* from = (const f32x4_t*)a.sums + matrix * a.parts * S::kTiles * 64;
+    constexpr int kAtOnce = 8;  // parts in flight
+    const f32x4_t* from = (const f32x4_t*)a.sums + matrix * a.parts * S::kWaves * 64;
     for (int p0 = 0; p0 < a.parts; p0 += kAtOnce) {
-      f32x4_t s[kAtOnce][kMine];
+      f32x4_t s[kAtOnce];
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u)
-#pragma unroll
-        for (int i = 0; i < kMine; ++i)
-          if (have[i]) s[u][i] = from[(min(p0 + u, a.parts - 1) * S::kTiles + wave + i * S::kWaves) * 64 + lane];
+      for (int u = 0; u < kAtOnce; ++u) s[u] = from[(min(p0 + u, a.parts - 1) * S::kWaves + wave) * 64 + lane];
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
         if (p0 + u >= a.parts) break;
         const int by = __builtin_amdgcn_readlane(of_lane, p0 + u);
 #pragma unroll
-        for (int i = 0; i < kMine; ++i)
-          if (have[i])
-#pragma unroll
-            for (int k = 0; k < 4; ++k) A[i][k] += ldexpf(s[u][i][k], by);
+        for (int k = 0; k < 4; ++k) A[k] += ldexpf(s[u][k], by);
       }
     }
   }
   put(L, A);
   __syncthreads();
   if (wave == 0) {
-    float sum = 0.0f;
-    for (int i = lane; i < S::kSide; i += 64) sum += L[i * S::kPitch + i];
+    float sum = lane < S::kSide ? L[lane * S::kPitch + lane] : 0.0f;  // a side has 64 at the most
     for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
     if (lane == 0) trace = sum;
   }
   __syncthreads();
-  const float sum = scale == kNotFinite ? NAN : trace, by = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-  for (int i = 0; i < kMine; ++i)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) A[i][k] *= by;
+  const float sum = scale == kNotFinite ? NAN : trace;
+  A *= sum == 0.0f ? 0.0f : 1.0f / sum;
   put(L, A);  // each value's own thread has put it there before
   __syncthreads();
   for (int step = 0; step < a.steps; ++step) {
     const bool last = step + 1 == a.steps;
-    product(L, L, v);  // A^2
+    f32x4_t T = product(L, L);  // A^2
 #pragma unroll
-    for (int i = 0; i < kMine; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        v[i][k] = fmaf(kC, v[i][k], fmaf(kB, A[i][k], ti[i] == tj[i] && 4 * g + k == r ? kA : 0.0f));
-    put(R, v);  // T
-    if (step == 0) {
-#pragma unroll
-      for (int i = 0; i < kMine; ++i) Q[i] = v[i];
-    }
+    for (int k = 0; k < 4; ++k) T[k] = fmaf(kC, T[k], fmaf(kB, A[k], row + k == col ? kA : 0.0f));
+    put(R, T);
+    if (step == 0) Q = T;
     __syncthreads();
     if (!last) {
-      product(R, L, v);
+      const f32x4_t v = product(R, L);
       __syncthreads();
       put(L, v);  // T A
       __syncthreads();
-      product(R, L, A);  // T A T: all of them commute
+      A = product(R, L);  // T A T: all of them commute
       __syncthreads();
     }
     if (step > 0) {
       put(L, Q);
       __syncthreads();
-      product(R, L, Q);
+      Q = product(R, L);
       __syncthreads();
     }
     if (!last) {
@@ -267,18 +233,11 @@ __global__ __launch_bounds__(64 * FewShape<NT>::kWaves) void few_iterate_kernel(
       __syncthreads();
     }
   }
-  const float root = sum == 0.0f ? 0.0f : 1.0f / sqrtf(sum);
+  Q *= sum == 0.0f ? 0.0f : 1.0f / sqrtf(sum);
   float* to = a.Q + matrix * S::kSide * S::kSide;
 #pragma unroll
-  for (int i = 0; i < kMine; ++i)
-    if (have[i]) {
-      const int row = 16 * ti[i] + 4 * g, col = 16 * tj[i] + r;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) Q[i][k] *= root;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) to[(row + k) * S::kSide + col] = Q[i][k];
-      if (ti[i] != tj[i]) *(f32x4_t*)(to + col * S::kSide + row) = Q[i];
-    }
+  for (int k = 0; k < 4; ++k) to[(row + k) * S::kSide + col] = Q[k];
+  if (ti != tj) *(f32x4_t*)(to + col * S::kSide + row) = Q;
   if (tid == 0) a.scale[matrix] = scale > -kNotFinite && scale < kNotFinite ? scale : 0;
 }
 
@@ -356,9 +315,9 @@ FewLayout few_layout(int64_t rows, int64_t cols, int64_t batch) {
   FewLayout l{};
   l.n = rows < cols ? rows : cols;
   l.m = rows < cols ? cols : rows;
-  l.nt = l.n <= 16 ? 1 : l.n <= 32 ? 2 : l.n <= 64 ? 4 : 8;
-  // Parts: as many as the iteration's workgroup adds up quickly (64 KiB to 288 KiB of sums)
-  const int most = l.nt == 1 ? 64 : l.nt == 2 ? 32 : l.nt == 4 ? 16 : 8;
+  l.nt = l.n <= 16 ? 1 : l.n <= 32 ? 2 : 4;
+  // Parts: as many as the iteration's workgroup adds up quickly (64 KiB to 160 KiB of sums)
+  const int most = l.nt == 1 ? 64 : l.nt == 2 ? 32 : 16;
   l.each = (int)(ceil_div(ceil_div(l.m, most), 64) * 64);
   l.parts = (int)ceil_div(l.m, l.each);
   const auto take = [&](int64_t bytes) {
@@ -375,17 +334,8 @@ FewLayout few_layout(int64_t rows, int64_t cols, int64_t batch) {
 
 template <typename T, int NT>
 ws_status run_few(const FewArgs& a, int64_t batch, hipStream_t stream) {
-  typedef FewShape<NT> S;
-  static std::atomic<uint64_t> allowed;  // devices on which the iteration may use this much LDS
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e == hipSuccess && (dev >= 64 || !(allowed.load(std::memory_order_acquire) >> dev & 1))) {
-    e = hipFuncSetAttribute((const void*)&few_iterate_kernel<NT>, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
-    if (e == hipSuccess && dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_acq_rel);
-  }
-  if (e != hipSuccess) return hip_fail("hipFuncSetAttribute", e);
   ws_status s = launch("orthogonalize", &few_gram_kernel<T, NT>, batch * a.parts, 64 * kGramWaves, 0, stream, a);
-  if (s == WS_OK) s = launch("orthogonalize", &few_iterate_kernel<NT>, batch, 64 * S::kWaves, S::kLds, stream, a);
+  if (s == WS_OK) s = launch("orthogonalize", &few_iterate_kernel<NT>, batch, 64 * FewShape<NT>::kWaves, 0, stream, a);
   if (s == WS_OK) s = launch("orthogonalize", &few_apply_kernel<T, NT>, batch * ceil_div(a.m, 64), 256, 0, stream, a);
   return s;
 }
@@ -395,8 +345,7 @@ ws_status run_few(const FewArgs& a, int nt, int64_t batch, hipStream_t stream) {
   switch (nt) {
     case 1: return run_few<T, 1>(a, batch, stream);
     case 2: return run_few<T, 2>(a, batch, stream);
-    case 4: return run_few<T, 4>(a, batch, stream);
-    default: return run_few<T, 8>(a, batch, stream);
+    default: return run_few<T, 4>(a, batch, stream);
   }
 }
 
