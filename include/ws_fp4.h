@@ -53,21 +53,32 @@ ws_status ws_fp4_quantize(const ws_matrix* w, const ws_fp4_matrix* out, hipStrea
 /* out (f32 or bf16) <- the values of q, exactly (bf16: from 2^-126 up). */
 ws_status ws_fp4_dequantize(const ws_fp4_matrix* q, const ws_matrix* out, hipStream_t stream);
 
+/* out[r][j] <- the scale of columns 32 j .. 32 j + 31 of row r: rows x ceil(cols / 32)
+ * bytes, `ld` between rows, `stride` between matrices of a batch. */
+ws_status ws_fp4_scales(const ws_fp4_matrix* q, uint8_t* out, int64_t ld, int64_t stride, hipStream_t stream);
+
+/* Bytes of device memory that a product of M rows, N columns and K contracted ones needs
+ * (0: none, then workspace may be NULL), in `groups` groups or -1 for ws_fp4_product; -1
+ * for sizes that it refuses. */
+int64_t ws_fp4_product_workspace(int64_t M, int64_t N, int64_t K, int32_t groups);
+
 /* C <- A B^T: B is N x K in 4 bits; C (f32, bf16 or f16) is M x N; its row m is row
  * index[m] of A (a negative or too large index: a row of zeros), or row m for index
  * NULL (then A has M rows).  A is bf16 or f16, K columns.  Products and sums in
  * binary32, rounded once (bf16: operand values below 2^-126 count as 0).  Made for
  * the rows of a decoding step: the weights are read once for every 64 rows.  Results
- * depend on the operands and sizes only: no atomics. */
+ * depend on the operands and sizes only: no atomics.  The workspace (16-byte aligned) is
+ * written before it is read; calls on other streams need another. */
 ws_status ws_fp4_product(const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, const ws_matrix* C,
-                         hipStream_t stream);
+                         void* workspace, int64_t workspace_bytes, hipStream_t stream);
 
 /* The same by group: row r of C is its row of A times B_g^T, for the group g whose
  * rows offsets[g] .. offsets[g + 1] - 1 hold r (int32 on the device, not decreasing);
  * rows in no group, before the first or after the last, become zeros.  B is a batch of
  * `groups` matrices. */
 ws_status ws_fp4_grouped_product(const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, int32_t groups,
-                                 const int32_t* offsets, const ws_matrix* C, hipStream_t stream);
+                                 const int32_t* offsets, const ws_matrix* C, void* workspace, int64_t workspace_bytes,
+                                 hipStream_t stream);
 
 #ifdef __cplusplus
 }

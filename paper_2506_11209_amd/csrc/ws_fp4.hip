@@ -144,6 +144,24 @@ __global__ __launch_bounds__(256) void fp4_dequantize_kernel(Fp4CastArgs a) {
   }
 }
 
+struct Fp4ScaleArgs {
+  const uint8_t* scales;
+  uint8_t* out;
+  int64_t rows, across, cols, ld_scales, stride_scales, ld, stride, all;  // cols: of out; all: threads
+};
+
+// A thread takes the four scales of 128 columns of a row.
+__global__ __launch_bounds__(256) void fp4_scales_kernel(Fp4ScaleArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= a.all) return;
+  const int64_t b = i % a.across, line = i / a.across, r = line % a.rows, m = line / a.rows;
+  const uint32_t s = *(const uint32_t*)(a.scales + m * a.stride_scales + r / 16 * a.ld_scales + 64 * b + r % 16 * 4);
+  uint8_t* to = a.out + m * a.stride + r * a.ld + 4 * b;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (4 * b + k < a.cols) to[k] = (uint8_t)(s >> (8 * k));
+}
+
 // -- products --------------------------------------------------------------------
 
 struct Fp4Args {
@@ -152,6 +170,7 @@ struct Fp4Args {
   void* C;
   const int32_t *index, *offsets;
   int64_t ldx, ld, ld_scales, stride_codes, stride_scales, ldc;
+  uint8_t* arranged;  // A by operands (fp4_arrange_kernel), or null
   int64_t M, x_rows, N, K;
   int64_t tiles_m, strips;
   int32_t groups, dtype;
@@ -180,45 +199,93 @@ __device__ __forceinline__ void store_value(void* C, int64_t at, float v) {
   ((T*)C)[at] = from_f32<T>(v);
 }
 
+// The rows of one tile of 16 MT rows.
+struct RowTile {
+  int64_t m0, m_end;
+  int group;  // -1: there is no such tile; `groups` and more: rows of no group
+};
+template <int MT, bool GROUPED>
+__device__ __forceinline__ RowTile row_tile(const Fp4Args& a, int64_t tm) {
+  if constexpr (GROUPED) {
+    const GroupTile gt = find_group_tile(a.offsets, a.groups, a.M, 16 * MT, tm);
+    return RowTile{gt.lo + gt.index * 16 * MT, gt.hi, gt.group};
+  }
+  return RowTile{tm * 16 * MT, a.M, 0};
+}
+
+// A by operands of the matrix instruction: for 16 rows and 128 columns 4 KiB, lane l's 16
+// bytes of the k-th quarter at 1024 k + 16 l.  A wave's load of it is one piece; of A itself
+// it is 64 bytes each of 16 rows (choose() has what both take).  Zeros past the last column
+// and for rows that are not there.  Bound: latency, one trip to memory and back.
+template <typename X, int MT, bool GROUPED>
+__global__ __launch_bounds__(256) void fp4_arrange_kernel(Fp4Args a) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int blocks = (int)((a.K + 127) / 128), per = (blocks + 3) / 4;  // a workgroup has four blocks of a tile
+  const int64_t tm = blockIdx.x / per;
+  const int b = blockIdx.x % per * 4 + (threadIdx.x >> 6);
+  const RowTile t = row_tile<MT, GROUPED>(a, tm);
+  if (b >= blocks || t.group < 0 || (GROUPED && t.group >= a.groups)) return;
+  const int K = (int)a.K - 8 * g;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t m = t.m0 + 16 * i + r;
+    int64_t from = m < t.m_end ? (a.index ? a.index[m] : m) : -1;
+    if (from >= a.x_rows) from = -1;
+    const X* x = (const X*)a.x + (from < 0 ? 0 : from) * a.ldx + 8 * g;
+    uint8_t* to = a.arranged + ((tm * MT + i) * (int64_t)blocks + b) * 4096 + 16 * lane;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int k = 128 * b + 32 * q;
+      i32x4_t v = {0, 0, 0, 0};
+      if (from >= 0) {
+        if (k + 8 <= K) load_n<X, 8>(x + k, (X*)&v);
+        else v = load_end(x, k, K);
+      }
+      *(i32x4_t*)(to + 1024 * q) = v;
+    }
+  }
+}
+
 // A workgroup computes 16 MT rows of 16 NT columns: its waves share out the contraction,
 // 256 columns of A at a time, and add up their parts through LDS in a fixed order.
 // Operands go from memory straight to registers, a step's weights before the products of
 // the one before.  Rows that are not there read those of another and are not stored.
-// Bound: reading the weights (1 x 8192 x 8192: 9.4 us, 3.8 TB/s; by rows of codes instead
-// of tiles, 64 bytes of 16 rows a load and scales 4 bytes of each, 14.1; 55 of 64 groups
-// of 4096 x 2048 57 us, 4.3 TB/s, by rows 83); from about 16 rows on by reading those of A
-// for every strip (64 x 8192 x 8192: 45 us).
-template <typename X, int MT, int NT, bool GROUPED>
+// Bound: reading the weights (1 x 8192 x 8192: 8.6 us, 4.2 TB/s; by rows of codes instead
+// of tiles, 64 bytes of 16 rows a load and scales 4 bytes of each, 14.1; 55 of 64 groups of
+// 4096 x 2048 51 us, 4.8 TB/s, by rows 83); from about 16 rows on by reading those of A
+// for every strip (64 x 8192 x 8192: 25 us, 1024 x 8192 x 8192: 205, 0.67 PFLOP/s).
+template <typename X, int MT, int NT, bool GROUPED, bool ARRANGED>
 __global__ __launch_bounds__(512) void fp4_product_kernel(Fp4Args a) {
   constexpr bool kBf16 = std::is_same<X, bf16_t>::value;
   extern __shared__ __align__(16) f32x4_t part[];  // waves x MT x NT x 64
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
   const int waves = blockDim.x >> 6;
-  // strips of columns go round the XCDs, the tiles of rows of one strip follow each other on one
-  const uint32_t turn = 8 * (uint32_t)a.tiles_m, strip = blockIdx.x / turn * 8 + blockIdx.x % 8, tm = blockIdx.x % turn / 8;
+  // Strips of columns go round the XCDs, all of a tile of rows before the next, whose rows
+  // stay in the L2: they are more bytes than a strip's codes.  All tiles of a strip before
+  // the next strip instead: 2048 x 2048 x 2048 84 us for 42, 1024 x 8192 x 8192 337 for 205,
+  // 2048 rows of 64 groups of 4096 x 2048 266 for 133, 128 rows 60 for 56.
+  const uint32_t turn = ((uint32_t)a.strips + 7) / 8 * 8, strip = blockIdx.x % turn, tm = blockIdx.x / turn;
   if (strip >= a.strips) return;
-  int64_t m0 = (int64_t)tm * 16 * MT, m_end = a.M;
+  const RowTile rows = row_tile<MT, GROUPED>(a, tm);
+  if (rows.group < 0) return;
+  const int64_t m0 = rows.m0, m_end = rows.m_end;
+  const bool zero = a.x_rows == 0 || (GROUPED && rows.group >= a.groups);
   const uint8_t *codes = a.codes, *scales = a.scales;
-  bool zero = a.x_rows == 0;
-  if constexpr (GROUPED) {
-    const GroupTile gt = find_group_tile(a.offsets, a.groups, a.M, 16 * MT, tm);
-    if (gt.group < 0) return;
-    m0 = gt.lo + gt.index * 16 * MT;
-    m_end = gt.hi;
-    if (gt.group >= a.groups) {
-      zero = true;
-    } else {
-      codes += gt.group * a.stride_codes;
-      scales += gt.group * a.stride_scales;
-    }
+  if (GROUPED && !zero) {
+    codes += rows.group * a.stride_codes;
+    scales += rows.group * a.stride_scales;
   }
   const int64_t n0 = (int64_t)strip * 16 * NT;
   const X* x[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    int64_t from = min(m0 + 16 * i + r, m_end - 1);
-    if (a.index) from = a.index[from];
-    x[i] = (const X*)a.x + (from >= 0 && from < a.x_rows ? from : 0) * a.ldx + 8 * g;
+    if constexpr (ARRANGED) {
+      x[i] = (const X*)(a.arranged + ((int64_t)tm * MT + i) * ((a.K + 127) / 128) * 4096 + 16 * lane);
+    } else {
+      int64_t from = min(m0 + 16 * i + r, m_end - 1);
+      if (a.index) from = a.index[from];
+      x[i] = (const X*)a.x + (from >= 0 && from < a.x_rows ? from : 0) * a.ldx + 8 * g;
+    }
   }
   const uint8_t *code_at[NT], *scale_at[NT];
 #pragma unroll
@@ -245,7 +312,12 @@ __global__ __launch_bounds__(512) void fp4_product_kernel(Fp4Args a) {
     }
   };
   const auto load_x = [&](int b, i32x4_t (&xv)[4][MT]) {
-    if (128 * b + 128 <= K) {  // the same for the wave
+    if constexpr (ARRANGED) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) xv[q][i] = *(const i32x4_t*)(x[i] + 2048 * (int64_t)b + 512 * q);
+    } else if (128 * b + 128 <= K) {  // the same for the wave
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -370,27 +442,71 @@ ws_status cast(const char* what, const ws_matrix* w, const ws_fp4_matrix* q, boo
   return launch(what, w->dtype == WS_OUT_F32 ? &fp4_dequantize_kernel<float> : &fp4_dequantize_kernel<bf16_t>, grid, 256, 0, stream, a);
 }
 
-template <int MT, int NT>
-ws_status launch_product(const char* what, bool bf16, bool grouped, int waves, hipStream_t stream, Fp4Args a) {
+template <typename X, int MT, int NT, bool GROUPED>
+ws_status launch_product(const char* what, int waves, hipStream_t stream, Fp4Args a) {
   a.strips = ceil_div(a.N, 16 * NT);
-  a.tiles_m = grouped ? group_tiles(a.M, a.groups, 16 * MT, true) : ceil_div(a.M, 16 * MT);
+  a.tiles_m = GROUPED ? group_tiles(a.M, a.groups, 16 * MT, true) : ceil_div(a.M, 16 * MT);
   while (waves > 1 && waves * 128 >= a.K) waves /= 2;  // of 256 columns each
-  const int64_t grid = ceil_div(a.strips, 8) * 8 * a.tiles_m;
+  const int64_t grid = ceil_div(a.strips, 8) * 8 * a.tiles_m, lds = waves * MT * NT * 1024;
   if (grid > max_workgroups(64 * waves) || a.tiles_m > 1 << 28) return WS_ERR_INVALID_ARG;
-  void (*kernel)(Fp4Args) = bf16 ? (grouped ? &fp4_product_kernel<bf16_t, MT, NT, true> : &fp4_product_kernel<bf16_t, MT, NT, false>)
-                                 : (grouped ? &fp4_product_kernel<f16_t, MT, NT, true> : &fp4_product_kernel<f16_t, MT, NT, false>);
-  return launch(what, kernel, grid, 64 * waves, waves * MT * NT * 1024, stream, a);
+  if constexpr (MT > 1)
+    if (a.arranged) {
+      const int64_t first = a.tiles_m * ceil_div(ceil_div(a.K, 128), 4);
+      if (first > max_workgroups(256)) return WS_ERR_INVALID_ARG;
+      const ws_status s = launch(what, &fp4_arrange_kernel<X, MT, GROUPED>, first, 256, 0, stream, a);
+      return s != WS_OK ? s : launch(what, &fp4_product_kernel<X, MT, NT, GROUPED, true>, grid, 64 * waves, lds, stream, a);
+    }
+  return launch(what, &fp4_product_kernel<X, MT, NT, GROUPED, false>, grid, 64 * waves, lds, stream, a);
+}
+
+// Rows of a group on average, and what follows from them.
+struct Choice {
+  int mt;         // tiles of 16 rows a workgroup has
+  bool many;      // strips
+  int64_t bytes;  // of A by operands, 0 where it is read as it lies
+};
+// Eight waves to a contraction fill the card where there are few strips; where there are
+// many, starting waves costs more than it hides.  us of 2 columns' tiles by 8 waves and of
+// 4 by 4: 1 x 8192 x 8192 9.4 and 13.0, 128 rows of 55 of 64 groups of 4096 x 2048 94 and
+// 57; from A as it lies, 64 x 8192 x 8192 by 8 and 4 waves 44.8 and 49.4, 256 x 4096 x 4096
+// 41.5 and 38.5.
+// A by operands takes a launch more, about 4 us of the host's, and pays where a workgroup
+// loads 128 blocks of 16 rows and 128 columns, or all together 2^15 of them.  us from A and
+// by operands: 64 x 16 x 8192 35.5 and 21.8, 32 x 1000 x 8192 19.1 and 14.4, 64 x 4096 x 4096
+// 21.0 and 15.4, 512 x 2048 x 2048 21.5 and 18.0, 2048 x 2048 x 2048 73 and 42; below,
+// 32 x 4096 x 4096 11.7 and 12.4, 512 x 1024 x 1024 9.2 and 13.1, 256 x 2048 x 2048 13.0 and 13.6.
+Choice choose(int64_t M, int64_t N, int64_t K, int64_t groups) {
+  const int64_t rows = groups > 0 ? ceil_div(M, groups) : M;
+  Choice c{};
+  c.mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  const int64_t tiles = groups > 0 ? group_tiles(M, groups, 16 * c.mt, false) : ceil_div(M, 16 * c.mt);
+  const int64_t strips = ceil_div(N, 32) * tiles, blocks = c.mt * ceil_div(K, 128);  // blocks: of a workgroup
+  c.many = strips > 500;
+  if (c.mt > 1 && groups != 0 && (blocks >= 128 || strips * blocks >= 1 << 15))
+    c.bytes = (groups >= 0 ? group_tiles(M, groups, 16 * c.mt, true) : tiles) * blocks * 4096;
+  return c;
+}
+
+template <typename X, bool GROUPED>
+ws_status launch_product(const char* what, const Choice& c, hipStream_t stream, const Fp4Args& a) {
+  if (c.mt == 1)
+    return c.many ? launch_product<X, 1, 4, GROUPED>(what, 4, stream, a) : launch_product<X, 1, 2, GROUPED>(what, 8, stream, a);
+  if (c.mt == 2) return launch_product<X, 2, 2, GROUPED>(what, c.many ? 4 : 8, stream, a);
+  return launch_product<X, 4, 2, GROUPED>(what, c.many ? 4 : 8, stream, a);
 }
 
 ws_status product(const char* what, const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, int32_t groups,
-                  const int32_t* offsets, const ws_matrix* C, hipStream_t stream) {
+                  const int32_t* offsets, const ws_matrix* C, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
   const bool grouped = groups >= 0;
   if (!valid(A) || A->batch > 1 || !valid(C) || C->batch > 1 || !valid_fp4(B, grouped)) return WS_ERR_INVALID_ARG;
   if (A->dtype == WS_OUT_F32 || A->cols != B->cols || C->cols != B->rows || (!index && A->rows != C->rows) || (uintptr_t)index % 4)
     return WS_ERR_INVALID_ARG;
   if (grouped ? B->batch != groups || groups > 1 << 20 || !offsets || (uintptr_t)offsets % 4 : B->batch > 1) return WS_ERR_INVALID_ARG;
   if (C->rows == 0 || C->cols == 0) return WS_OK;
+  const Choice c = choose(C->rows, C->cols, A->cols, groups);
+  if (workspace_bytes < c.bytes || (c.bytes > 0 && (!workspace || (uintptr_t)workspace % 16))) return WS_ERR_INVALID_ARG;
   Fp4Args a{};
+  a.arranged = c.bytes > 0 ? (uint8_t*)workspace : nullptr;
   a.x = A->data;
   a.codes = (const uint8_t*)B->codes;
   a.scales = B->scales;
@@ -409,18 +525,9 @@ ws_status product(const char* what, const ws_matrix* A, const int32_t* index, co
   a.K = A->cols;
   a.groups = groups;
   a.dtype = C->dtype;
-  const bool bf16 = A->dtype == WS_OUT_BF16;
-  const int64_t rows = grouped ? (groups ? ceil_div(a.M, groups) : a.M) : a.M;  // of a group, on average
-  // Eight waves to a contraction fill the card where there are few strips; where there
-  // are many, starting waves costs more than it hides.  us of 2 columns' tiles by 8 waves
-  // and of 4 by 4: 1 x 8192 x 8192 9.4 and 13.0, 128 rows of 55 of 64 groups of 4096 x 2048
-  // 94 and 57; 64 x 8192 x 8192 by 8 and 4 waves 44.8 and 49.4, 256 x 4096 x 4096 41.5 and 38.5.
-  const int64_t mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  const bool many = ceil_div(a.N, 32) * (grouped ? group_tiles(a.M, groups, 16 * (int)mt, false) : ceil_div(a.M, 16 * mt)) > 500;
-  if (mt == 1)
-    return many ? launch_product<1, 4>(what, bf16, grouped, 4, stream, a) : launch_product<1, 2>(what, bf16, grouped, 8, stream, a);
-  if (mt == 2) return launch_product<2, 2>(what, bf16, grouped, many ? 4 : 8, stream, a);
-  return launch_product<4, 2>(what, bf16, grouped, many ? 4 : 8, stream, a);
+  if (A->dtype == WS_OUT_BF16)
+    return grouped ? launch_product<bf16_t, true>(what, c, stream, a) : launch_product<bf16_t, false>(what, c, stream, a);
+  return grouped ? launch_product<f16_t, true>(what, c, stream, a) : launch_product<f16_t, false>(what, c, stream, a);
 }
 
 }  // namespace
@@ -438,14 +545,41 @@ ws_status ws_fp4_dequantize(const ws_fp4_matrix* q, const ws_matrix* out, hipStr
   return cast("fp4_dequantize", out, q, false, stream);
 }
 
-ws_status ws_fp4_product(const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, const ws_matrix* C, hipStream_t stream) {
-  return product("fp4_product", A, index, B, -1, nullptr, C, stream);
+ws_status ws_fp4_scales(const ws_fp4_matrix* q, uint8_t* out, int64_t ld, int64_t stride, hipStream_t stream) {
+  if (!valid_fp4(q, true) || ld < ceil_div(q->cols, WS_FP4_BLOCK) || ld > kMaxDim) return WS_ERR_INVALID_ARG;
+  if (q->rows == 0 || q->cols == 0 || q->batch == 0) return WS_OK;
+  Fp4ScaleArgs a{};
+  a.cols = ceil_div(q->cols, WS_FP4_BLOCK);
+  if (!out || (q->batch > 1 && stride < (q->rows - 1) * ld + a.cols)) return WS_ERR_INVALID_ARG;
+  a.scales = q->scales;
+  a.out = out;
+  a.rows = q->rows;
+  a.across = ceil_div(q->cols, 128);
+  a.ld_scales = q->ld_scales;
+  a.stride_scales = q->stride_scales;
+  a.ld = ld;
+  a.stride = stride;
+  a.all = a.across * a.rows * q->batch;
+  const int64_t grid = ceil_div(a.all, 256);
+  if (grid > max_workgroups(256)) return WS_ERR_INVALID_ARG;
+  return launch("fp4_scales", &fp4_scales_kernel, grid, 256, 0, stream, a);
+}
+
+int64_t ws_fp4_product_workspace(int64_t M, int64_t N, int64_t K, int32_t groups) {
+  if (M < 0 || N < 0 || K < 0 || M > kMaxDim || N > kMaxDim || K > kMaxDim || groups < -1 || groups > 1 << 20) return -1;
+  return M == 0 || N == 0 ? 0 : choose(M, N, K, groups).bytes;
+}
+
+ws_status ws_fp4_product(const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, const ws_matrix* C, void* workspace,
+                         int64_t workspace_bytes, hipStream_t stream) {
+  return product("fp4_product", A, index, B, -1, nullptr, C, workspace, workspace_bytes, stream);
 }
 
 ws_status ws_fp4_grouped_product(const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, int32_t groups,
-                                 const int32_t* offsets, const ws_matrix* C, hipStream_t stream) {
+                                 const int32_t* offsets, const ws_matrix* C, void* workspace, int64_t workspace_bytes,
+                                 hipStream_t stream) {
   if (groups < 0) return WS_ERR_INVALID_ARG;
-  return product("fp4_grouped_product", A, index, B, groups, offsets, C, stream);
+  return product("fp4_grouped_product", A, index, B, groups, offsets, C, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -31,11 +31,14 @@ class ws_fp4_matrix(ctypes.Structure):
 
 
 _lib = _w.library()
-_p, _i32 = ctypes.c_void_p, ctypes.c_int32
+_p, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
 _fp = ctypes.POINTER(ws_fp4_matrix)
-for _name, _args in (("ws_fp4_quantize", [_mp, _fp, _p]), ("ws_fp4_dequantize", [_fp, _mp, _p]),
-                     ("ws_fp4_product", [_mp, _p, _fp, _mp, _p]), ("ws_fp4_grouped_product", [_mp, _p, _fp, _i32, _p, _mp, _p])):
-    getattr(_lib, _name).argtypes, getattr(_lib, _name).restype = _args, _i32
+for _name, _args, _res in (("ws_fp4_quantize", [_mp, _fp, _p], _i32), ("ws_fp4_dequantize", [_fp, _mp, _p], _i32),
+                           ("ws_fp4_scales", [_fp, _p, _i64, _i64, _p], _i32),
+                           ("ws_fp4_product_workspace", [_i64, _i64, _i64, _i32], _i64),
+                           ("ws_fp4_product", [_mp, _p, _fp, _mp, _p, _i64, _p], _i32),
+                           ("ws_fp4_grouped_product", [_mp, _p, _fp, _i32, _p, _mp, _p, _i64, _p], _i32)):
+    getattr(_lib, _name).argtypes, getattr(_lib, _name).restype = _args, _res
 
 
 class Fp4Matrix:
@@ -81,11 +84,13 @@ class Fp4Matrix:
     @property
     def scales(self):
         """(batch x) rows x ceil(cols / 32), e8m0: the scale of every 32 columns of a row."""
-        across = -(-self.cols // _COLS)
-        s = self.packed_scales[..., : 64 * across].view(torch.int32)  # 4 neighbours of a row
-        s = s.unflatten(-1, (across, _ROWS)).transpose(-1, -2)
-        s = s.reshape(-1).view(E8M0).view(s.shape[:-3] + (s.shape[-3] * _ROWS, 4 * across))
-        return s[..., : self.rows, : -(-self.cols // BLOCK)]
+        codes, cols = self.codes, -(-self.cols // BLOCK)
+        if _elsewhere(codes, None):
+            with _Call(codes.device, None, []):
+                return self.scales
+        out = torch.empty(codes.shape[:-2] + (self.rows, cols), dtype=E8M0, device=codes.device)
+        _check(_lib.ws_fp4_scales(self._desc, out.data_ptr(), cols, self.rows * cols, _raw_stream(codes.device.index)), "ws_fp4_scales")
+        return out
 
     @classmethod
     def empty(cls, rows: int, cols: int, batch: int | None = None, device="cuda"):
@@ -141,6 +146,12 @@ def _rows(A, B, index):
     return m, 0 if index is None else _index(index, "index", rows, A.device), rows
 
 
+def _work(rows, B, groups, A):
+    """Work memory of a product and its size."""
+    need = _lib.ws_fp4_product_workspace(rows, B.rows, B.cols, groups)
+    return (torch.empty(need, dtype=torch.uint8, device=A.device) if need > 0 else None), max(need, 0)
+
+
 def product(A, B: Fp4Matrix, C=None, out_dtype: str = "bf16", index=None, stream=None):
     """A B^T: A is rows x K in bf16 or f16, B is N x K in 4 bits; sums in binary32,
     rounded once to C (its type counts) or a new tensor of out_dtype ("f32", "bf16",
@@ -152,7 +163,8 @@ def product(A, B: Fp4Matrix, C=None, out_dtype: str = "bf16", index=None, stream
         with _Call(A.device, stream, [A, B.codes, B.packed_scales, C, index]):
             return product(A, B, C, out_dtype, index)
     C, mc = _result(C, out_dtype, (rows, B.rows), A.device)
-    _check(_lib.ws_fp4_product(m, at, B._desc, mc, _raw_stream(A.get_device())), "ws_fp4_product")
+    work, need = _work(rows, B, -1, A)
+    _check(_lib.ws_fp4_product(m, at, B._desc, mc, work.data_ptr() if need else 0, need, _raw_stream(A.get_device())), "ws_fp4_product")
     return C
 
 
@@ -169,5 +181,7 @@ def grouped_product(A, B: Fp4Matrix, offsets, C=None, out_dtype: str = "bf16", i
     _need(offsets, "offsets", (torch.int32,), (1,), A.device)
     off = _index(offsets, "offsets", B.batch + 1, A.device)
     C, mc = _result(C, out_dtype, (rows, B.rows), A.device)
-    _check(_lib.ws_fp4_grouped_product(m, at, B._desc, B.batch, off, mc, _raw_stream(A.get_device())), "ws_fp4_grouped_product")
+    work, need = _work(rows, B, B.batch, A)
+    _check(_lib.ws_fp4_grouped_product(m, at, B._desc, B.batch, off, mc, work.data_ptr() if need else 0, need,
+                                       _raw_stream(A.get_device())), "ws_fp4_grouped_product")
     return C

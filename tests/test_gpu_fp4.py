@@ -108,7 +108,8 @@ def weights(N, K, seed, lead=()):
 
 
 SHAPES = [(1, 1, 1), (1, 17, 31), (2, 16, 32), (15, 33, 100), (16, 64, 128), (17, 65, 129), (31, 70, 255), (33, 128, 513), (49, 31, 384),
-          (64, 48, 640), (65, 129, 1000), (130, 40, 2049), (1, 300, 4104)]
+          (64, 48, 640), (65, 129, 1000), (130, 40, 2049), (1, 300, 4104),
+          (20, 50, 8200), (70, 40, 4100), (1100, 2000, 1000)]  # the last three with A by operands
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -147,12 +148,13 @@ def groups_of(counts, before=0, after=0):
 
 
 @pytest.mark.parametrize("counts,before,after", [((3, 0, 1, 20), 0, 0), ((0, 0), 2, 3), ((40, 70, 0, 5), 1, 0), ((1,) * 30, 0, 17), ((0, 129), 5, 2),
-                                                 ((16, 32, 64), 0, 0)])
+                                                 ((16, 32, 64), 0, 0), ((100, 0, 17, 300), 3, 4)])
 @pytest.mark.parametrize("name", ("bf16", "f16"))
-def test_grouped_product(counts, before, after, name):
-    log("case fp4 grouped %s %d %d %s" % (counts, before, after, name))
+@pytest.mark.parametrize("N,K", [(70, 300), (40, 8300)])  # the second with A by operands, where groups are large
+def test_grouped_product(counts, before, after, name, N, K):
+    log("case fp4 grouped %s %d %d %s %d x %d" % (counts, before, after, name, N, K))
     off, M = groups_of(counts, before, after)
-    N, K, E = 70, 300, len(counts)
+    E = len(counts)
     x, w = integers((23, K), 1, 3).to(TYPES[name]), weights(N, K, 2, (E,))
     W = fp4.quantize_weight(w.cuda())
     index = torch.randint(-1, 25, (M,), generator=torch.Generator().manual_seed(3)).to(torch.int32)  # -1, 23 and 24: no row

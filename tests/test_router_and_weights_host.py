@@ -70,6 +70,10 @@ def test_casts():
     for other in (coded(41, 200), coded(40, 199), coded(40, 200, batch=2)):
         assert lib.ws_fp4_quantize(x, other, None) == INVALID and lib.ws_fp4_dequantize(other, x, None) == INVALID
     assert lib.ws_fp4_dequantize(q, matrix(40, 200, dtype=F16), None) == INVALID  # does not hold the values
+    for bad in CODED:
+        assert lib.ws_fp4_scales(change(q, **bad), AT, 7, 280, None) == INVALID, bad
+    assert lib.ws_fp4_scales(q, None, 7, 280, None) == INVALID and lib.ws_fp4_scales(q, AT, 6, 280, None) == INVALID
+    assert lib.ws_fp4_scales(coded(40, 200, batch=2), AT, 7, 279, None) == INVALID
     two = matrix(40, 200, batch=2, stride=40 * 200)
     for bad in (dict(stride_codes=3 * 2048 - 16), dict(stride_codes=3 * 2048 + 8), dict(stride_scales=3 * 128 - 4), dict(stride_scales=3 * 128 + 2)):
         assert lib.ws_fp4_quantize(two, coded(40, 200, batch=2, **bad), None) == INVALID, bad
@@ -81,20 +85,30 @@ def test_products():
     A, B, C = matrix(8, 200, dtype=BF16), coded(40, 200), matrix(8, 40)
     weights = coded(40, 200, batch=3)
     for bad in PLAIN:
-        assert lib.ws_fp4_product(change(A, **bad), None, B, C, None) == INVALID, bad
-        assert lib.ws_fp4_product(A, None, B, change(C, **bad), None) == INVALID, bad
-        assert lib.ws_fp4_grouped_product(change(A, **bad), None, weights, 3, AT, C, None) == INVALID, bad
+        assert lib.ws_fp4_product(change(A, **bad), None, B, C, None, 0, None) == INVALID, bad
+        assert lib.ws_fp4_product(A, None, B, change(C, **bad), None, 0, None) == INVALID, bad
+        assert lib.ws_fp4_grouped_product(change(A, **bad), None, weights, 3, AT, C, None, 0, None) == INVALID, bad
     for bad in CODED:
-        assert lib.ws_fp4_product(A, None, change(B, **bad), C, None) == INVALID, bad
-        assert lib.ws_fp4_grouped_product(A, None, change(weights, **bad), 3, AT, C, None) == INVALID, bad
+        assert lib.ws_fp4_product(A, None, change(B, **bad), C, None, 0, None) == INVALID, bad
+        assert lib.ws_fp4_grouped_product(A, None, change(weights, **bad), 3, AT, C, None, 0, None) == INVALID, bad
     for a, b, c in ((matrix(8, 200), B, C), (A, coded(40, 199), C), (A, coded(41, 200), C), (A, B, matrix(9, 40)), (A, weights, C)):
-        assert lib.ws_fp4_product(a, None, b, c, None) == INVALID
-    assert lib.ws_fp4_product(A, AT + 2, B, C, None) == INVALID
+        assert lib.ws_fp4_product(a, None, b, c, None, 0, None) == INVALID
+    assert lib.ws_fp4_product(A, AT + 2, B, C, None, 0, None) == INVALID
     for groups, offsets in ((2, AT), (-1, AT), (3, None), (3, AT + 1)):
-        assert lib.ws_fp4_grouped_product(A, None, weights, groups, offsets, C, None) == INVALID
+        assert lib.ws_fp4_grouped_product(A, None, weights, groups, offsets, C, None, 0, None) == INVALID
+    # work memory, where there are many loads of A
+    need = lib.ws_fp4_product_workspace(64, 8192, 8192, -1)
+    many = (matrix(64, 8192, dtype=BF16), None, coded(8192, 8192), matrix(64, 8192))
+    assert need == 64 * 8192 * 2 and lib.ws_fp4_product_workspace(8, 40, 200, -1) == 0 and lib.ws_fp4_product_workspace(0, 8192, 8192, -1) == 0
+    assert lib.ws_fp4_product_workspace(20, 50, 8200, -1) == 2 * 65 * 4096 and lib.ws_fp4_product_workspace(70, 40, 4100, -1) == 2 * 4 * 33 * 4096
+    assert lib.ws_fp4_product_workspace(1 << 30, 1 << 30, 1 << 30, 1 << 20) > 0 and lib.ws_fp4_product_workspace(70, 40, 8192, 0) == 0
+    for work, bytes_ in ((None, 0), (None, need), (AT, need - 1), (AT + 8, need)):
+        assert lib.ws_fp4_product(*many, work, bytes_, None) == INVALID
+    for sizes in ((-1, 5, 5, -1), (5, -1, 5, -1), (5, 5, -1, -1), (5, 5, 5, -2), ((1 << 30) + 1, 5, 5, -1), (5, 5, 5, (1 << 20) + 1)):
+        assert lib.ws_fp4_product_workspace(*sizes) == -1, sizes
     # no rows of A: they come by an index, or there are none
-    assert lib.ws_fp4_product(matrix(0, 200, dtype=BF16, data=0), None, B, C, None) == INVALID
-    assert lib.ws_fp4_product(matrix(0, 200, dtype=BF16, data=0), None, B, matrix(0, 40, data=0), None) == w.WS_OK
+    assert lib.ws_fp4_product(matrix(0, 200, dtype=BF16, data=0), None, B, C, None, 0, None) == INVALID
+    assert lib.ws_fp4_product(matrix(0, 200, dtype=BF16, data=0), None, B, matrix(0, 40, data=0), None, 0, None) == w.WS_OK
 
 
 def test_orthogonalize():
