@@ -66,7 +66,7 @@ int64_t ws_fp4_product_workspace(int64_t M, int64_t N, int64_t K, int32_t groups
  * index[m] of A (a negative or too large index: a row of zeros), or row m for index
  * NULL (then A has M rows).  A is bf16 or f16, K columns.  Products and sums in
  * binary32, rounded once (bf16: operand values below 2^-126 count as 0).  Made for
- * the rows of a decoding step: the weights are read once for every 64 rows.  Results
+ * the rows of a decoding step: the weights are read once for every 16 to 64 rows.  Results
  * depend on the operands and sizes only: no atomics.  The workspace (16-byte aligned) is
  * written before it is read; calls on other streams need another. */
 ws_status ws_fp4_product(const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, const ws_matrix* C,

@@ -253,7 +253,7 @@ __global__ __launch_bounds__(256) void fp4_arrange_kernel(Fp4Args a) {
 // Bound: reading the weights (1 x 8192 x 8192: 8.6 us, 4.2 TB/s; by rows of codes instead
 // of tiles, 64 bytes of 16 rows a load and scales 4 bytes of each, 14.1; 55 of 64 groups of
 // 4096 x 2048 51 us, 4.8 TB/s, by rows 83); from about 16 rows on by reading those of A
-// for every strip (64 x 8192 x 8192: 25 us, 1024 x 8192 x 8192: 205, 0.67 PFLOP/s).
+// for every strip (256 x 4096 x 4096: 24 us, 1024 x 8192 x 8192: 205, 0.67 PFLOP/s).
 template <typename X, int MT, int NT, bool GROUPED, bool ARRANGED>
 __global__ __launch_bounds__(512) void fp4_product_kernel(Fp4Args a) {
   constexpr bool kBf16 = std::is_same<X, bf16_t>::value;
@@ -470,19 +470,24 @@ struct Choice {
 // 4 by 4: 1 x 8192 x 8192 9.4 and 13.0, 128 rows of 55 of 64 groups of 4096 x 2048 94 and
 // 57; from A as it lies, 64 x 8192 x 8192 by 8 and 4 waves 44.8 and 49.4, 256 x 4096 x 4096
 // 41.5 and 38.5.
-// A by operands takes a launch more, about 4 us of the host's, and pays where a workgroup
-// loads 128 blocks of 16 rows and 128 columns, or all together 2^15 of them.  us from A and
-// by operands: 64 x 16 x 8192 35.5 and 21.8, 32 x 1000 x 8192 19.1 and 14.4, 64 x 4096 x 4096
-// 21.0 and 15.4, 512 x 2048 x 2048 21.5 and 18.0, 2048 x 2048 x 2048 73 and 42; below,
-// 32 x 4096 x 4096 11.7 and 12.4, 512 x 1024 x 1024 9.2 and 13.1, 256 x 2048 x 2048 13.0 and 13.6.
+// A workgroup takes fewer rows where the launch has under three workgroups a CU.  us of all
+// 64 (or 32) rows in one and so: 40 x 4104 x 4100 17.0 and 11.5, 64 x 4096 x 4096 15.5 and
+// 10.2, 64 x 100 x 8192 22.3 and 11.5, 256 x 2048 x 2048 13.1 and 9.5; of two a CU
+// 512 x 2048 x 2048 18.1 and 16.4, but 64 x 8192 x 8192 23.4 and 26.7.
+// A by operands takes a launch more, about 4 us of the host's, and pays from 2^15 blocks of
+// 16 rows and 128 columns on.  us from A and by operands: 512 x 2048 x 2048 21.5 and 18.0,
+// 256 x 4096 x 4096 38 and 25, 2048 x 2048 x 2048 73 and 42; below, 512 x 1024 x 1024 9.2 and
+// 13.1, 256 x 2048 x 2048 13.0 and 13.6.
 Choice choose(int64_t M, int64_t N, int64_t K, int64_t groups) {
   const int64_t rows = groups > 0 ? ceil_div(M, groups) : M;
   Choice c{};
   c.mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  const int64_t tiles = groups > 0 ? group_tiles(M, groups, 16 * c.mt, false) : ceil_div(M, 16 * c.mt);
-  const int64_t strips = ceil_div(N, 32) * tiles, blocks = c.mt * ceil_div(K, 128);  // blocks: of a workgroup
+  const auto count = [&] { return groups > 0 ? group_tiles(M, groups, 16 * c.mt, false) : ceil_div(M, 16 * c.mt); };
+  while (c.mt > 1 && ceil_div(N, 32) * count() < 768) c.mt /= 2;
+  const int64_t tiles = count();
+  const int64_t strips = ceil_div(N, 32) * tiles, blocks = c.mt * ceil_div(K, 128);  // blocks: a workgroup's
   c.many = strips > 500;
-  if (c.mt > 1 && groups != 0 && (blocks >= 128 || strips * blocks >= 1 << 15))
+  if (c.mt > 1 && groups != 0 && blocks > 0 && strips >= ceil_div(1 << 15, blocks))
     c.bytes = (groups >= 0 ? group_tiles(M, groups, 16 * c.mt, true) : tiles) * blocks * 4096;
   return c;
 }

@@ -109,7 +109,8 @@ def weights(N, K, seed, lead=()):
 
 SHAPES = [(1, 1, 1), (1, 17, 31), (2, 16, 32), (15, 33, 100), (16, 64, 128), (17, 65, 129), (31, 70, 255), (33, 128, 513), (49, 31, 384),
           (64, 48, 640), (65, 129, 1000), (130, 40, 2049), (1, 300, 4104),
-          (20, 50, 8200), (70, 40, 4100), (1100, 2000, 1000)]  # the last three with A by operands
+          (20, 24600, 300), (33, 24600, 160),  # two and four tiles of rows a workgroup
+          (20, 25000, 2600), (1100, 1400, 1300), (2100, 800, 1281)]  # and so with A by operands
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -150,7 +151,7 @@ def groups_of(counts, before=0, after=0):
 @pytest.mark.parametrize("counts,before,after", [((3, 0, 1, 20), 0, 0), ((0, 0), 2, 3), ((40, 70, 0, 5), 1, 0), ((1,) * 30, 0, 17), ((0, 129), 5, 2),
                                                  ((16, 32, 64), 0, 0), ((100, 0, 17, 300), 3, 4)])
 @pytest.mark.parametrize("name", ("bf16", "f16"))
-@pytest.mark.parametrize("N,K", [(70, 300), (40, 8300)])  # the second with A by operands, where groups are large
+@pytest.mark.parametrize("N,K", [(70, 300), (4200, 300), (4200, 2650)])  # the last with A by operands, where groups are large
 def test_grouped_product(counts, before, after, name, N, K):
     log("case fp4 grouped %s %d %d %s %d x %d" % (counts, before, after, name, N, K))
     off, M = groups_of(counts, before, after)

@@ -97,11 +97,13 @@ def test_products():
     for groups, offsets in ((2, AT), (-1, AT), (3, None), (3, AT + 1)):
         assert lib.ws_fp4_grouped_product(A, None, weights, groups, offsets, C, None, 0, None) == INVALID
     # work memory, where there are many loads of A
-    need = lib.ws_fp4_product_workspace(64, 8192, 8192, -1)
-    many = (matrix(64, 8192, dtype=BF16), None, coded(8192, 8192), matrix(64, 8192))
-    assert need == 64 * 8192 * 2 and lib.ws_fp4_product_workspace(8, 40, 200, -1) == 0 and lib.ws_fp4_product_workspace(0, 8192, 8192, -1) == 0
-    assert lib.ws_fp4_product_workspace(20, 50, 8200, -1) == 2 * 65 * 4096 and lib.ws_fp4_product_workspace(70, 40, 4100, -1) == 2 * 4 * 33 * 4096
-    assert lib.ws_fp4_product_workspace(1 << 30, 1 << 30, 1 << 30, 1 << 20) > 0 and lib.ws_fp4_product_workspace(70, 40, 8192, 0) == 0
+    need = lib.ws_fp4_product_workspace(256, 8192, 8192, -1)
+    many = (matrix(256, 8192, dtype=BF16), None, coded(8192, 8192), matrix(256, 8192))
+    assert need == 256 * 8192 * 2 and lib.ws_fp4_product_workspace(8, 40, 200, -1) == 0 and lib.ws_fp4_product_workspace(0, 8192, 8192, -1) == 0
+    assert lib.ws_fp4_product_workspace(20, 25000, 2600, -1) == 2 * 21 * 4096 and lib.ws_fp4_product_workspace(33, 24600, 160, -1) == 0
+    assert lib.ws_fp4_product_workspace(1100, 1400, 1300, -1) == 18 * 4 * 11 * 4096
+    assert lib.ws_fp4_product_workspace(112, 4200, 2650, 3) == (112 + 31 * 5) // 32 * 2 * 21 * 4096
+    assert lib.ws_fp4_product_workspace(1 << 30, 1 << 30, 1 << 30, 1 << 20) > 0 and lib.ws_fp4_product_workspace(700, 8192, 8192, 0) == 0
     for work, bytes_ in ((None, 0), (None, need), (AT, need - 1), (AT + 8, need)):
         assert lib.ws_fp4_product(*many, work, bytes_, None) == INVALID
     for sizes in ((-1, 5, 5, -1), (5, -1, 5, -1), (5, 5, -1, -1), (5, 5, 5, -2), ((1 << 30) + 1, 5, 5, -1), (5, 5, 5, (1 << 20) + 1)):
