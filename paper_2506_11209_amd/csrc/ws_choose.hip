@@ -60,34 +60,34 @@ __device__ __forceinline__ uint32_t max_lanes(uint32_t x) {
 }
 
 // Logits in the order in which they are chosen: larger is earlier, NaN first of all,
-// both zeros the same, 0 for -inf, which is not chosen.  A rank of 16 bits leaves room
-// for the element's number, so that no two ranks are alike (kOwn): the largest is found
-// with one comparison an element, and is removed without looking for it.
+// both zeros the same, what is below kLeast is not chosen.  A rank of 16 bits leaves room
+// for the element's number, so that no two ranks are alike (kOwn) and the next below one
+// is found without a mark on what went before.
 template <typename T>
 struct Rank {
   static constexpr bool kOwn = sizeof(T) == 2;
-  static constexpr uint32_t kSign = kOwn ? 0x8000u : 0x80000000u, kAll = kOwn ? 0xffffu : 0xffffffffu;
-  static __device__ __forceinline__ uint32_t of(T v, int e) {
-    const float x = to_f32(v);
+  // above -inf, whose bits are ff80 of bf16, fc00 of f16 and ff800000
+  static constexpr uint32_t kLeast = std::is_same<T, f16_t>::value ? 0x04000000u : 0x00800000u;
+  // What of() takes of an element's number.
+  static __device__ __forceinline__ uint32_t mark(int e) { return kOwn ? 0x8000ffffu - (uint32_t)e : 0x80000000u; }
+  static __device__ __forceinline__ uint32_t nan(uint32_t mark) { return kOwn ? 0xffff0000u | mark : 0xffffffffu; }
+  // Of all but NaN.
+  static __device__ __forceinline__ uint32_t of(T v, uint32_t mark) {
     uint32_t b;
-    if constexpr (kOwn) {
-      uint16_t h;
-      __builtin_memcpy(&h, &v, 2);
-      b = h;
+    if constexpr (std::is_same<T, f16_t>::value) {
+      const _Float16 h = v.v + (_Float16)0.0f;  // -0 becomes +0
+      uint16_t bits;
+      __builtin_memcpy(&bits, &h, 2);
+      b = (uint32_t)bits << 16;
     } else {
-      b = __float_as_uint(x);
+      b = __float_as_uint(to_f32(v) + 0.0f);
     }
-    b = x == 0.0f ? 0u : b;
-    b = b & kSign ? ~b & kAll : b | kSign;
-    b = x != x ? kAll : b;
-    if constexpr (kOwn) b = b << 16 | (0xffffu - (uint32_t)e);
-    return x == -INFINITY ? 0u : b;
+    return b ^ (((uint32_t)((int32_t)b >> 31) & (kOwn ? 0x7fff0000u : 0x7fffffffu)) | mark);
   }
   static __device__ __forceinline__ float value(uint32_t rank) {
-    uint32_t b = kOwn ? rank >> 16 : rank;
-    b = b & kSign ? b ^ kSign : ~b & kAll;
+    const uint32_t b = rank & 0x80000000u ? rank ^ 0x80000000u : ~rank;
     if constexpr (kOwn) {
-      const uint16_t h = (uint16_t)b;
+      const uint16_t h = (uint16_t)(b >> 16);
       T v;
       __builtin_memcpy(&v, &h, 2);
       return to_f32(v);
@@ -224,19 +224,26 @@ __global__ __launch_bounds__(64 * choose_waves<L>()) void choose_kernel(ChooseAr
     sums[v] = 0.0f;
     counts[v] = 0;
   }
+  typedef Rank<T> K;
   const int64_t step = (int64_t)a.blocks * kGroups;
   for (int64_t t = (int64_t)blockIdx.x * kGroups + tid / L; t < a.tokens; t += step) {
     T raw[V];
     R::load((const T*)a.logits + t * a.ld, sub, a.experts, a.experts + (a.tokens - 1 - t) * a.ld, raw);
     uint32_t key[V], best = 0;
+    bool nan = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      key[v] = Rank<T>::of(raw[v], R::element(sub, v));  // -inf past the last expert
-      best = max(best, key[v]);
+      key[v] = K::of(raw[v], K::mark(R::element(sub, v)));  // -inf past the last expert
+      nan |= __builtin_isunordered(to_f32(raw[v]), to_f32(raw[v ^ (V > 1)]));
     }
+    if (__any(nan))
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = to_f32(raw[v]) != to_f32(raw[v]) ? K::nan(K::mark(R::element(sub, v))) : key[v];
+#pragma unroll
+    for (int v = 0; v < V; ++v) best = max(best, key[v]);
     best = max_lanes<L>(best);
-    const bool some = best != 0;
-    const float top = Rank<T>::value(best);
+    const bool some = best >= K::kLeast;
+    const float top = K::value(best);
     if (some) {
       float p[V], sum = 0.0f;
 #pragma unroll
@@ -248,53 +255,60 @@ __global__ __launch_bounds__(64 * choose_waves<L>()) void choose_kernel(ChooseAr
 #pragma unroll
       for (int v = 0; v < V; ++v) sums[v] = fmaf(p[v], by, sums[v]);
     }
+    // a lane has the choices j = sub, sub + L ..
+    uint32_t rank[kMine], last = ~0u;
     int32_t id[kMine];
-    float w[kMine], all = 0.0f;
 #pragma unroll
     for (int q = 0; q < kMine; ++q) {
+      rank[q] = 0;
       id[q] = -1;
-      w[q] = 0.0f;
       for (int j = q * L; j < a.k && j < (q + 1) * L; ++j) {
         if (j > 0) {
-          best = 0;
+          uint32_t next = 0;
+          if constexpr (K::kOwn) {  // of the differences, those of ranks below wrap and are the largest
 #pragma unroll
-          for (int v = 0; v < V; ++v) best = max(best, key[v]);
-          best = max_lanes<L>(best);
+            for (int v = 0; v < V; ++v) next = max(next, key[v] - best);
+            next = max_lanes<L>(next) + best;
+            best = next < best ? next : 0;
+          } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) next = max(next, key[v]);
+            best = max_lanes<L>(next);
+          }
         }
-        if (best == 0) break;
-        int e;
-        if constexpr (Rank<T>::kOwn) {
-          e = Rank<T>::element(best);
-#pragma unroll
-          for (int v = 0; v < V; ++v) key[v] = key[v] == best ? 0 : key[v];
-        } else {
+        if (best < K::kLeast) break;
+        last = best;
+        const bool mine = j - q * L == sub;
+        rank[q] = mine ? best : rank[q];
+        if constexpr (!K::kOwn) {
           uint32_t low = 0;  // the lowest element with it, as a large number
 #pragma unroll
           for (int v = V - 1; v >= 0; --v) low = key[v] == best ? ~(uint32_t)R::element(sub, v) : low;
-          e = (int)~max_lanes<L>(low);
+          const int e = (int)~max_lanes<L>(low);
+          id[q] = mine ? e : id[q];
 #pragma unroll
           for (int v = 0; v < V; ++v) key[v] = R::element(sub, v) == e ? 0 : key[v];
         }
-        const float x = exp_from(Rank<T>::value(best), top);
-        all += x;
-        if (j - q * L == sub) {
-          id[q] = e;
-          w[q] = x;
-        }
       }
     }
-    const float by = 1.0f / all;
+    float w[kMine], all = 0.0f;
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+      if (K::kOwn && rank[q] != 0) id[q] = K::element(rank[q]);
+      w[q] = rank[q] != 0 ? exp_from(K::value(rank[q]), top) : 0.0f;
+      all += w[q];
+    }
+    const float by = 1.0f / sum_lanes<L>(all);
 #pragma unroll
     for (int q = 0; q < kMine; ++q) {
       const int j = q * L + sub;
       if (j < a.k) {
         a.ids[t * a.k + j] = id[q];
-        a.weights[t * a.k + j] = id[q] >= 0 ? w[q] * by : 0.0f;
+        a.weights[t * a.k + j] = rank[q] != 0 ? w[q] * by : 0.0f;
       }
     }
-    // what has no rank left, but had one
 #pragma unroll
-    for (int v = 0; v < V; ++v) counts[v] += key[v] == 0 && to_f32(raw[v]) != -INFINITY;
+    for (int v = 0; v < V; ++v) counts[v] += K::kOwn ? key[v] >= last : key[v] == 0;
     with += some;
   }
   // the wave's tokens, then the workgroup's
