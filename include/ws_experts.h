@@ -43,7 +43,7 @@ int64_t ws_expert_choose_workspace(int64_t tokens, int32_t experts, int32_t k);
  * +inf.  k up to experts and WS_MAX_CHOICES, experts up to WS_MAX_EXPERTS, at most
  * 2^30 choices.  weights and ids: tokens * k, dense; counts: experts + 1; all
  * 4-byte aligned.  Exponentials and sums in binary32 or more; results do not depend
- * on anything but logits and sizes.  The workspace (4-byte aligned) is written
+ * on anything but logits and sizes.  The workspace (8-byte aligned) is written
  * before it is read; calls on other streams need another. */
 ws_status ws_expert_choose(const ws_matrix* logits, int32_t k, float* weights, int32_t* ids, int32_t* counts,
                            float* loss, void* workspace, int64_t workspace_bytes, hipStream_t stream);

@@ -16,6 +16,8 @@ struct ChooseArgs {
   float *weights, *loss, *sums;  // sums: blocks x (experts + 1), of probabilities; null for one workgroup alone
   int32_t *ids, *counts, *parts;  // parts: blocks x (experts + 1), counts
   const float *dweights, *dloss;
+  double* products;  // choose_finish_kernel's workgroups x 3
+  uint32_t* ended;   // of them
   int64_t tokens, ld, ld_d;
   int32_t experts, k, blocks;
 };
@@ -174,7 +176,7 @@ struct Row {
 template <int L>
 constexpr int choose_waves() { return L == 16 ? 16 : 8; }
 
-// What the sums of probabilities and the counts give; by one workgroup, S_e and c_e in LDS.
+// What the sums of probabilities and the counts give, S_e and c_e in LDS.
 __device__ __forceinline__ void finish(const ChooseArgs& a, const float* sums, const int32_t* counts, double* scratch) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
   double dot = 0.0, all = 0.0;
@@ -213,6 +215,7 @@ __global__ __launch_bounds__(64 * choose_waves<L>()) void choose_kernel(ChooseAr
   constexpr int kWaves = choose_waves<L>(), kGroups = kWaves * 64 / L, kMine = (WS_MAX_CHOICES + L - 1) / L;
   extern __shared__ __align__(16) uint8_t smem[];
   const int n = a.experts + 1;  // the last: tokens with a choice
+  if (!ALONE && blockIdx.x == 0 && threadIdx.x == 0) *a.ended = 0;  // read by the next launch
   float* lds_sums = (float*)smem;                    // waves x n
   int32_t* lds_counts = (int32_t*)(lds_sums + kWaves * n);  // waves x n
   __shared__ double scratch[2 * kWaves];
@@ -356,49 +359,87 @@ __global__ __launch_bounds__(64 * choose_waves<L>()) void choose_kernel(ChooseAr
   }
 }
 
-constexpr int kFinishThreads = 1024;
-constexpr int finish_slices(int n) { return kFinishThreads / n > 0 ? kFinishThreads / n : 1; }
+// Adds up what the workgroups left: a workgroup takes 16 columns, in a fixed order, and
+// the last to end the products of all of them.  Bound: latency (256 times 257 columns:
+// 5.0 us; by one workgroup 11.9).
+constexpr int kFinishCols = 16, kFinishSlices = 16, kFinishReads = 16;  // blocks: at most slices x reads
+constexpr int finish_groups(int experts) { return experts / kFinishCols + 1; }
 
-// Adds up what the workgroups left, every column in a fixed order, and finishes.  Bound:
-// latency, of one workgroup's reads and of the launch (256 times 257 columns: 11 us; by
-// two launches, the first with 17 workgroups, as long).
-__global__ __launch_bounds__(kFinishThreads) void choose_finish_kernel(ChooseArgs a) {
-  extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ double scratch[kFinishThreads / 32];
-  const int n = a.experts + 1, slices = finish_slices(n);
-  float* sums = (float*)smem;  // slices x n
-  int32_t* counts = (int32_t*)(sums + slices * n);
-  constexpr int kAtOnce = 16;  // of sums, and of counts
-  for (int i = threadIdx.x; i < slices * n; i += kFinishThreads) {
-    const int e = i % n, slice = i / n;
-    float s = 0.0f;
-    int32_t c = 0;
-    for (int b0 = slice; b0 < a.blocks; b0 += kAtOnce * slices) {
-      float x[kAtOnce];
-      int32_t y[kAtOnce];
+__global__ __launch_bounds__(kFinishCols* kFinishSlices) void choose_finish_kernel(ChooseArgs a) {
+  __shared__ float sums[kFinishSlices][kFinishCols];
+  __shared__ int32_t counts[kFinishSlices][kFinishCols];
+  __shared__ double scratch[3][4];
+  __shared__ bool last;
+  const int tid = threadIdx.x, col = tid % kFinishCols, slice = tid / kFinishCols;
+  const int n = a.experts + 1, e = blockIdx.x * kFinishCols + col, groups = gridDim.x;
+  float x[kFinishReads], s = 0.0f;
+  int32_t y[kFinishReads], c = 0;
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        const int64_t at = (int64_t)min(b0 + u * slices, a.blocks - 1) * n + e;
-        x[u] = a.sums[at];
-        y[u] = a.parts[at];
-      }
+  for (int u = 0; u < kFinishReads; ++u) {
+    const int64_t at = (int64_t)min(slice + kFinishSlices * u, a.blocks - 1) * n + min(e, n - 1);
+    x[u] = a.sums[at];
+    y[u] = a.parts[at];
+  }
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        s += b0 + u * slices < a.blocks ? x[u] : 0.0f;
-        c += b0 + u * slices < a.blocks ? y[u] : 0;
-      }
+  for (int u = 0; u < kFinishReads; ++u) {
+    s += slice + kFinishSlices * u < a.blocks ? x[u] : 0.0f;
+    c += slice + kFinishSlices * u < a.blocks ? y[u] : 0;
+  }
+  sums[slice][col] = s;
+  counts[slice][col] = c;
+  __syncthreads();
+  double dot = 0.0, all = 0.0, with = 0.0;
+  if (slice == 0 && e < n) {
+    for (int i = 1; i < kFinishSlices; ++i) {
+      s += sums[i][col];
+      c += counts[i][col];
     }
-    sums[i] = s;
-    counts[i] = c;
+    a.counts[e] = c;
+    dot = e < a.experts ? (double)c * (double)s : 0.0;
+    all = e < a.experts ? (double)c : 0.0;
+    with = e < a.experts ? 0.0 : (double)c;
+  }
+  for (int d = kFinishCols / 2; d; d /= 2) {
+    dot += __shfl_xor(dot, d);
+    all += __shfl_xor(all, d);
+    with += __shfl_xor(with, d);
+  }
+  if (tid == 0) {
+    double* mine = a.products + 3 * blockIdx.x;
+    mine[0] = dot;
+    mine[1] = all;
+    mine[2] = with;
+    __threadfence();
+    last = atomicAdd(a.ended, 1u) == (uint32_t)groups - 1;
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < n; e += kFinishThreads)
-    for (int k = 1; k < slices; ++k) {
-      sums[e] += sums[k * n + e];
-      counts[e] += counts[k * n + e];
-    }
+  if (!last) return;
+  __threadfence();
+  const auto take = [&](int k) {
+    return tid < groups ? __hip_atomic_load(a.products + 3 * tid + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+  };
+  dot = take(0);
+  all = take(1);
+  with = take(2);
+  for (int d = 32; d; d /= 2) {
+    dot += __shfl_xor(dot, d);
+    all += __shfl_xor(all, d);
+    with += __shfl_xor(with, d);
+  }
+  if (tid % 64 == 0) {
+    scratch[0][tid / 64] = dot;
+    scratch[1][tid / 64] = all;
+    scratch[2][tid / 64] = with;
+  }
   __syncthreads();
-  finish(a, sums, counts, scratch);
+  if (tid == 0) {
+    for (int w = 1; w < 4; ++w) {
+      dot += scratch[0][w];
+      all += scratch[1][w];
+      with += scratch[2][w];
+    }
+    *a.loss = with > 0.0 ? (float)((double)a.experts * dot / (all * with)) : 0.0f;
+  }
 }
 
 // L lanes take a token: its softmax again from its logits, what its weights ask of its
@@ -497,11 +538,10 @@ __global__ __launch_bounds__(256) void choose_gradient_kernel(ChooseArgs a) {
 
 // -- host ---------------------------------------------------------------------
 
-// Workgroups at the most: what they leave is added up by one.  us with 256 and 128 of
-// them: 65536 x 256 of bf16 44 and 61, 4096 x 1024 52 and 38.
-constexpr int most_blocks(int experts) { return experts <= 256 ? 256 : 128; }
-// Tokens that one workgroup takes by itself (256 x 64: 13.2 us, by several and a second
-// launch 14.9).
+constexpr int kMostBlocks = 256;  // one a CU
+static_assert(kMostBlocks <= kFinishSlices * kFinishReads && finish_groups(WS_MAX_EXPERTS) <= kFinishCols * kFinishSlices, "sizes");
+// Tokens that one workgroup takes by itself (256 x 64: 12.2 us, by several and a second
+// launch 14.8).
 constexpr int64_t kAloneTokens = 256;
 
 bool choose_sizes(int64_t tokens, int32_t experts, int32_t k) {
@@ -514,7 +554,7 @@ int lanes_of(int experts) { return experts <= 256 ? 16 : 64; }
 int choose_blocks(int64_t tokens, int experts) {
   if (tokens <= kAloneTokens) return 1;
   const int64_t groups = experts <= 256 ? choose_waves<16>() * 4 : choose_waves<64>(), n = ceil_div(tokens, groups);
-  return (int)(n < most_blocks(experts) ? n : most_blocks(experts));
+  return (int)(n < kMostBlocks ? n : kMostBlocks);
 }
 
 // f(type, lanes, elements a lane) of the smallest that holds a row.
@@ -548,14 +588,14 @@ extern "C" {
 int64_t ws_expert_choose_workspace(int64_t tokens, int32_t experts, int32_t k) {
   if (!choose_sizes(tokens, experts, k)) return -1;
   const int blocks = choose_blocks(tokens, experts);
-  return blocks == 1 ? 0 : (int64_t)blocks * (experts + 1) * 8;
+  return blocks == 1 ? 0 : (int64_t)finish_groups(experts) * 24 + 8 + (int64_t)blocks * (experts + 1) * 8;
 }
 
 ws_status ws_expert_choose(const ws_matrix* logits, int32_t k, float* weights, int32_t* ids, int32_t* counts, float* loss,
                            void* workspace, int64_t workspace_bytes, hipStream_t stream) {
   if (!valid(logits) || logits->batch > 1 || logits->cols > WS_MAX_EXPERTS) return WS_ERR_INVALID_ARG;
   const int64_t need = ws_expert_choose_workspace(logits->rows, (int32_t)logits->cols, k);
-  if (need < 0 || workspace_bytes < need || (need > 0 && !aligned4(workspace)) || !aligned4(counts) || !aligned4(loss) ||
+  if (need < 0 || workspace_bytes < need || (need > 0 && (!workspace || (uintptr_t)workspace % 8)) || !aligned4(counts) || !aligned4(loss) ||
       (logits->rows > 0 && (!aligned4(weights) || !aligned4(ids))))
     return WS_ERR_INVALID_ARG;
   ChooseArgs a{};
@@ -569,8 +609,12 @@ ws_status ws_expert_choose(const ws_matrix* logits, int32_t k, float* weights, i
   a.experts = (int32_t)logits->cols;
   a.k = k;
   a.blocks = choose_blocks(a.tokens, a.experts);
-  a.sums = (float*)workspace;
-  a.parts = (int32_t*)workspace + (int64_t)a.blocks * (a.experts + 1);
+  if (a.blocks > 1) {
+    a.products = (double*)workspace;
+    a.ended = (uint32_t*)(a.products + 3 * finish_groups(a.experts));
+    a.sums = (float*)(a.ended + 2);
+    a.parts = (int32_t*)(a.sums + (int64_t)a.blocks * (a.experts + 1));
+  }
   const ws_status s = by_type(logits->dtype, a.experts, [&](auto type, auto lanes, auto each) {
     typedef decltype(type) T;
     constexpr int L = decltype(lanes)::value, V = decltype(each)::value, waves = choose_waves<L>();
@@ -579,8 +623,7 @@ ws_status ws_expert_choose(const ws_matrix* logits, int32_t k, float* weights, i
     return launch("expert_choose", &choose_kernel<T, L, V, false>, a.blocks, 64 * waves, lds, stream, a);
   });
   if (s != WS_OK || a.blocks == 1) return s;
-  const int n = a.experts + 1;
-  return launch("expert_choose", &choose_finish_kernel, 1, kFinishThreads, finish_slices(n) * n * 8, stream, a);
+  return launch("expert_choose", &choose_finish_kernel, finish_groups(a.experts), kFinishCols * kFinishSlices, 0, stream, a);
 }
 
 ws_status ws_expert_choose_gradient(const ws_matrix* logits, int32_t k, const float* dweights, const float* dloss,

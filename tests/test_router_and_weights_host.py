@@ -40,7 +40,7 @@ def test_choose():
 
     for bad in (dict(k=0), dict(k=65), dict(weights=None), dict(ids=None), dict(counts=None), dict(loss=None), dict(ids=AT + 2),
                 dict(weights=AT + 1), dict(counts=AT + 2), dict(loss=AT + 2), dict(x=matrix(100, 64, batch=2, stride=6400)), dict(x=matrix(100, 1025)),
-                dict(x=matrix(100000, 64)), dict(x=matrix(100000, 64), work=AT, bytes_=need - 1), dict(x=matrix(100000, 64), work=AT + 2, bytes_=need)):
+                dict(x=matrix(100000, 64)), dict(x=matrix(100000, 64), work=AT, bytes_=need - 1), dict(x=matrix(100000, 64), work=AT + 4, bytes_=need)):
         assert call(**bad) == INVALID, bad
     for bad in PLAIN:
         assert call(x=change(x, **bad)) == INVALID, bad
