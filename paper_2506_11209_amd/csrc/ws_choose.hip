@@ -209,6 +209,9 @@ __device__ __forceinline__ void finish(const ChooseArgs& a, const float* sums, c
 // largest (and lowest) left, the first of which is the softmax's maximum too.  Sums of
 // probabilities and counts stay in the lanes over a workgroup's tokens and pass LDS at
 // the end, in a fixed order.  ALONE: one workgroup.
+// Bound: instructions, some 35 for a logit and 8 choices (65536 x 256 of bf16, 8 choices:
+// 25.8 us, 1.4 TB/s; with ranks cleared of what went before instead of differences 34.6;
+// with the next token's row under way meanwhile 26.7).
 template <typename T, int L, int V, bool ALONE>
 __global__ __launch_bounds__(64 * choose_waves<L>()) void choose_kernel(ChooseArgs a) {
   typedef Row<T, L, V> R;
@@ -443,7 +446,9 @@ __global__ __launch_bounds__(kFinishCols* kFinishSlices) void choose_finish_kern
 }
 
 // L lanes take a token: its softmax again from its logits, what its weights ask of its
-// choices by way of a row in LDS, and one write.  Bound: memory.
+// choices by way of a row in LDS, and one write; the next token's values are under way
+// meanwhile.  Bound: instructions and latency (65536 x 256 of bf16: 22 us, 67 MB, 3.1 TB/s,
+// of f32 24 us, 5.5 TB/s; 30001 x 100 of bf16 9.5; 8192 x 64 of f32 4.0, 1 TB/s).
 template <typename T, int L, int V>
 __global__ __launch_bounds__(256) void choose_gradient_kernel(ChooseArgs a) {
   typedef Row<T, L, V> R;
@@ -451,35 +456,56 @@ __global__ __launch_bounds__(256) void choose_gradient_kernel(ChooseArgs a) {
   __shared__ float rows[kGroups][L * V];
   const int tid = threadIdx.x, sub = tid % L;
   float* row = rows[tid / L];
-  // counts, and what of the loss belongs to one choice of one token
-  float c[V], all = 0.0f;
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int e = R::element(sub, v);
-    c[v] = e < a.experts ? (float)a.counts[e] : 0.0f;
-    all += c[v];
-    row[e] = 0.0f;
-  }
-  const float n = (float)a.counts[a.experts];
-  all = sum_lanes<L>(all);
-  const float scale = a.dloss && all > 0.0f && n > 0.0f ? *a.dloss * (float)a.experts / all / n : 0.0f;
-  __builtin_amdgcn_wave_barrier();
-  const int64_t step = (int64_t)gridDim.x * kGroups;
-  for (int64_t t = (int64_t)blockIdx.x * kGroups + tid / L; t < a.tokens; t += step) {
-    T raw[V];
-    R::load((const T*)a.logits + t * a.ld, sub, a.experts, a.experts + (a.tokens - 1 - t) * a.ld, raw);
-    int32_t id[kMine];
-    float w[kMine], dw[kMine], dot = 0.0f;
+  T raw[V], next[V];
+  int32_t id[kMine], next_id[kMine];
+  float w[kMine], next_w[kMine], dw[kMine], next_dw[kMine];
+  const auto load = [&](int64_t t) {
+    if (t >= a.tokens) return;
+    R::load((const T*)a.logits + t * a.ld, sub, a.experts, a.experts + (a.tokens - 1 - t) * a.ld, next);
 #pragma unroll
     for (int q = 0; q < kMine; ++q) {
       const int j = q * L + sub;
-      id[q] = -1;
-      w[q] = dw[q] = 0.0f;
+      next_id[q] = -1;
+      next_w[q] = next_dw[q] = 0.0f;
       if (a.dweights && j < a.k) {
-        id[q] = a.ids[t * a.k + j];
-        w[q] = a.weights[t * a.k + j];
-        dw[q] = a.dweights[t * a.k + j];
+        next_id[q] = a.ids[t * a.k + j];
+        next_w[q] = a.weights[t * a.k + j];
+        next_dw[q] = a.dweights[t * a.k + j];
       }
+    }
+  };
+  const int64_t step = (int64_t)gridDim.x * kGroups;
+  int64_t t = (int64_t)blockIdx.x * kGroups + tid / L;
+  load(t);
+  // counts, and what of the loss belongs to one choice of one token
+  float c[V], all = 0.0f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {  // loads without a branch, so that they are under way together
+    c[v] = (float)a.counts[min(R::element(sub, v), a.experts - 1)];
+    row[R::element(sub, v)] = 0.0f;
+  }
+  const float n = (float)a.counts[a.experts], dloss = a.dloss ? *a.dloss : 0.0f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    c[v] = R::element(sub, v) < a.experts ? c[v] : 0.0f;
+    all += c[v];
+  }
+  all = sum_lanes<L>(all);
+  const float scale = a.dloss && all > 0.0f && n > 0.0f ? dloss * (float)a.experts / all / n : 0.0f;
+  __builtin_amdgcn_wave_barrier();
+  for (; t < a.tokens; t += step) {
+    float dot = 0.0f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) raw[v] = next[v];
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+      id[q] = next_id[q];
+      w[q] = next_w[q];
+      dw[q] = next_dw[q];
+    }
+    load(t + step);
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
       if ((uint32_t)id[q] >= (uint32_t)a.experts) {
         id[q] = -1;
         w[q] = dw[q] = 0.0f;
@@ -506,18 +532,36 @@ __global__ __launch_bounds__(256) void choose_gradient_kernel(ChooseArgs a) {
     const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
     of_counts = sum_lanes<L>(of_counts) * by;
     dot = sum_lanes<L>(dot);
-    // what a choice is asked, added up where an id comes twice: the same for all its places
+    // what a choice is asked, added up where an id comes twice: the same for all its places;
+    // then the row holds another place than one's own
     float asked[kMine];
+    bool twice = false;
 #pragma unroll
-    for (int q = 0; q < kMine; ++q) asked[q] = 0.0f;
-    if (a.dweights) {
+    for (int q = 0; q < kMine; ++q) {
+      asked[q] = w[q] * (dw[q] - dot);
+      if (id[q] >= 0) __hip_atomic_store(row + id[q], (float)(q * L + sub), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int q = 0; q < kMine; ++q)
+      if (id[q] >= 0)
+        twice |= __hip_atomic_load(row + id[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT) != (float)(q * L + sub);
+    __builtin_amdgcn_wave_barrier();
+    if (__any(twice)) {
+      float of[kMine];
+#pragma unroll
+      for (int q = 0; q < kMine; ++q) {
+        of[q] = asked[q];
+        asked[q] = 0.0f;
+      }
 #pragma unroll
       for (int o = 0; o < kMine; ++o)
+#pragma unroll 1
         for (int j = 0; j < L && o * L + j < a.k; ++j) {
           const int other = __shfl(id[o], j, L);
-          const float of = __shfl(w[o] * (dw[o] - dot), j, L);
+          const float more = __shfl(of[o], j, L);
 #pragma unroll
-          for (int q = 0; q < kMine; ++q) asked[q] += other == id[q] ? of : 0.0f;
+          for (int q = 0; q < kMine; ++q) asked[q] += other == id[q] ? more : 0.0f;
         }
     }
 #pragma unroll
@@ -649,7 +693,8 @@ ws_status ws_expert_choose_gradient(const ws_matrix* logits, int32_t k, const fl
   a.ld_d = dlogits->ld;
   a.experts = (int32_t)logits->cols;
   a.k = k;
-  const int64_t most = 2048, n = ceil_div(a.tokens, 256 / lanes_of(a.experts));
+  // us with 512, 1024 and 2048 workgroups at the most: 65536 x 256 of bf16 24.0, 22.1 and 27.8
+  const int64_t most = 1024, n = ceil_div(a.tokens, 256 / lanes_of(a.experts));
   return by_type(logits->dtype, a.experts, [&](auto type, auto lanes, auto each) {
     return launch("expert_choose_gradient", &choose_gradient_kernel<decltype(type), decltype(lanes)::value, decltype(each)::value>,
                   n < most ? n : most, 256, 0, stream, a);

@@ -91,6 +91,13 @@ def _logits(logits):
     return m
 
 
+def _dense(t, what, dtype, shape, device):
+    """Refuses all but a contiguous tensor of this type and shape."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        _need(t, what, (dtype,), (len(shape),), device)
+        raise ValueError("%s: expected contiguous %s, got %s of strides %s" % (what, tuple(shape), tuple(t.shape), t.stride()))
+
+
 def choose(logits, k: int, stream=None):
     """(weights, ids, counts, loss) of a router's logits (tokens x experts; f32, bf16
     or f16).  ids (tokens x k, int32): each token's k largest logits, the largest
@@ -130,18 +137,13 @@ def choose_gradient(dweights, dloss, logits, weights, ids, counts, out=None, str
     m = _logits(logits)
     device = logits.device
     _need(ids, "ids", (torch.int32,), (2,), device)
-    tokens, k = ids.shape
+    tokens, k = shape = ids.shape
     if tokens != m.rows or not 0 < k <= min(m.cols, MAX_CHOICES) or not ids.is_contiguous():
-        raise ValueError("ids: expected contiguous %d x k, k up to %d, got %s" % (m.rows, min(m.cols, MAX_CHOICES), tuple(ids.shape)))
-    for t, what in ((weights, "weights"), (dweights, "dweights")):
-        if t is None and what == "dweights":
-            continue
-        _need(t, what, (torch.float32,), (2,), device)
-        if t.shape != ids.shape or not t.is_contiguous():
-            raise ValueError("%s: expected contiguous %s, got %s" % (what, tuple(ids.shape), tuple(t.shape)))
-    _need(counts, "counts", (torch.int32,), (1,), device)
-    if counts.numel() != m.cols + 1 or not counts.is_contiguous():
-        raise ValueError("counts: expected %d contiguous values, got %s" % (m.cols + 1, tuple(counts.shape)))
+        raise ValueError("ids: expected contiguous %d x k, k up to %d, got %s" % (m.rows, min(m.cols, MAX_CHOICES), tuple(shape)))
+    _dense(weights, "weights", torch.float32, shape, device)
+    if dweights is not None:
+        _dense(dweights, "dweights", torch.float32, shape, device)
+    _dense(counts, "counts", torch.int32, (m.cols + 1,), device)
     if dloss is not None:
         _need(dloss, "dloss", (torch.float32,), (0, 1), device)
         if dloss.numel() != 1:
