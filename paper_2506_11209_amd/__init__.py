@@ -12,6 +12,8 @@ raises if it has not been built.
 
 ``fp8`` and ``experts`` are operators of layers of experts in 8 bits over torch
 tensors, from the same library (``include/ws_fp8.h``, ``include/ws_experts.h``);
+``fp4`` has weights in 4 bits and their products (``include/ws_fp4.h``),
+``orthogonal`` orthogonalised updates (``include/ws_orthogonal.h``);
 ``expert_layer`` is a layer that uses them.
 """
 

@@ -33,7 +33,8 @@ HIP_FLAGS = [
     "-I" + CSRC, "-I" + os.path.join(ROOT, "include"), "-I" + BUILD,
 ]
 
-# The 8-bit path and the routing of tokens to experts (ws_fp8.h, ws_experts.h).
+# The 8-bit path, routing, weights in 4 bits and orthogonalised updates (ws_fp8.h,
+# ws_experts.h, ws_fp4.h, ws_orthogonal.h).
 OPERATOR_SOURCES = ["ws_fp8_product.hip", "ws_fp8_quantize.hip", "ws_experts.hip", "ws_choose.hip", "ws_fp4.hip",
                     "ws_orthogonal.hip", "ws_orthogonal_few.hip"]
 
