@@ -407,7 +407,7 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth
     const auto place = [&](int p, int* m, int* n) {
       *m = m0 + (wm * WM + p / (WN / 2) * (2 * kHalves)) * 16;
       *n = n0 + (wn * WN + p % (WN / 2) * 2) * 16;
-      return *m < a.M && *n < a.N;  // sides are multiples of 64
+      return *m < a.M && *n < a.N;  // sides are multiples of kPad
     };
     Old<KIND> old[2];
     i32x4_t v[2 * kHalves];

@@ -28,7 +28,8 @@ def orthogonalize(G, steps: int = 5, out=None, stream=None):
     """G (rows x columns, or a batch of such matrices; f32, bf16 or f16) with its
     singular values brought near 1 by ``steps`` Newton-Schulz steps, in bf16: X = G /
     |G|, then X <- a X + (b A + c A^2) X with A = X X^T.  Each matrix of a batch for
-    itself; zeros stay zeros, a matrix with an infinity or NaN becomes NaN."""
+    itself; zeros stay zeros, a matrix with an infinity or NaN becomes NaN.  out may not
+    overlap G."""
     m = _matrix(G, "G", (2, 3))
     if not 1 <= steps <= MAX_STEPS:
         raise ValueError("steps: 1 to %d, got %r" % (MAX_STEPS, steps))
@@ -54,7 +55,8 @@ def orthogonalize(G, steps: int = 5, out=None, stream=None):
 class OrthogonalMomentum(torch.optim.Optimizer):
     """Momentum whose updates are orthogonalised: for matrices and batches of them (the
     weights of experts), b <- momentum b + g, u = g + momentum b (or b, without nesterov),
-    w <- (1 - lr weight_decay) w - lr max(1, rows / columns)^0.5 orthogonalize(u)."""
+    w <- (1 - lr weight_decay) w - lr max(1, rows / columns)^0.5 orthogonalize(u).
+    b is kept in binary32 whatever the parameters' type."""
 
     def __init__(self, params, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, steps: int = 5):
         if lr < 0 or not 0 <= momentum < 1 or weight_decay < 0 or not 1 <= steps <= MAX_STEPS:
@@ -68,6 +70,13 @@ class OrthogonalMomentum(torch.optim.Optimizer):
                 del self.param_groups[-1]
                 raise ValueError("parameters have to be matrices or batches of them, got %s" % (tuple(p.shape),))
 
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)  # which rounds to the parameters' type
+        own = [p for group in self.param_groups for p in group["params"]]
+        for p, i in zip(own, (i for group in state_dict["param_groups"] for i in group["params"])):
+            if i in state_dict["state"]:
+                self.state[p]["momentum"] = state_dict["state"][i]["momentum"].to(p.device, torch.float32, copy=True)
+
     @torch.no_grad()
     def step(self, closure=None):
         loss = None
@@ -80,7 +89,7 @@ class OrthogonalMomentum(torch.optim.Optimizer):
                     continue
                 state, momentum = self.state[p], group["momentum"]
                 if "momentum" not in state:
-                    state["momentum"] = torch.zeros_like(p, memory_format=torch.contiguous_format)
+                    state["momentum"] = torch.zeros_like(p, dtype=torch.float32, memory_format=torch.contiguous_format)
                 b = state["momentum"]
                 b.mul_(momentum).add_(p.grad)
                 u = torch.add(p.grad, b, alpha=momentum) if group["nesterov"] else b

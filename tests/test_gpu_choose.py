@@ -101,6 +101,27 @@ def test_rows_apart_and_unaligned():
     assert torch.equal(into[:, 3:36], dense) and (into[:, :3] == 9).all() and (into[:, 36:] == 9).all()
 
 
+def test_rows_beyond_32_bits():
+    """Rows more than 2^31 elements apart, of logits and of their gradient."""
+    log("case choose far apart")
+    x = make(4, 40, 8, torch.bfloat16, masked=0.0)
+    view = torch.empty(3 * 2**30 + 40, dtype=torch.bfloat16, device="cuda").as_strided((4, 40), (2**30, 1))
+    view.copy_(x)
+    out = experts.choose(view, 3)
+    check(x, 3, out)
+    dw = torch.randn(4, 3, device="cuda")
+    want = experts.choose_gradient(dw, out[3], x.cuda(), *out[:3])
+    assert torch.equal(experts.choose_gradient(dw, out[3], view, *out[:3], out=view), want)
+
+
+def test_smallest_values():
+    """Subnormal logits keep their order, on both sides of the zeros."""
+    log("case choose subnormal")
+    for dtype, tiny in ((torch.float32, 2.0**-149), (torch.bfloat16, 2.0**-133), (torch.float16, 2.0**-24)):
+        x = torch.tensor([[tiny, 3 * tiny, 0.0, -tiny, -0.0, -2 * tiny, 2 * tiny]], dtype=dtype)
+        assert experts.choose(x.cuda(), 7)[1].tolist() == [[1, 6, 0, 2, 4, 3, 5]]
+
+
 def test_nothing_to_choose():
     log("case choose nothing")
     for x in (torch.empty(0, 5), torch.full((3, 5), -torch.inf), torch.full((4000, 5), -torch.inf)):
@@ -215,6 +236,38 @@ def test_on_another_stream():
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(out, want))
     assert torch.equal(d, experts.choose_gradient(dw, None, x, *want[:3]))
+
+
+def test_two_calls_at_once():
+    log("case choose two streams")
+    x = [make(20000, 200, s, torch.bfloat16).cuda() for s in range(2)]
+    want = [experts.choose(v, 4) for v in x]
+    streams = [torch.cuda.Stream() for _ in x]
+    torch.cuda.synchronize()
+    got = [(i, experts.choose(x[i], 4, stream=streams[i])) for _ in range(4) for i in range(2)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i, out in got for a, b in zip(out, want[i]))
+
+
+def test_an_id_twice_beside_others():
+    """A token with an id twice leaves the others of its wave as they are."""
+    log("case choose twice")
+    x = make(8, 64, 4, torch.float32, masked=0.0, hidden=0.0).cuda()
+    out = experts.choose(x, 4)
+    dw = torch.randn(8, 4, device="cuda")
+    want = experts.choose_gradient(dw, out[3], x, *out[:3])
+    ids = out[1].clone()
+    ids[2, 3] = ids[2, 0]
+    got = experts.choose_gradient(dw, out[3], x, out[0], ids, out[2])
+    others = [t for t in range(8) if t != 2]
+    assert torch.equal(got[others], want[others])
+    w, g = out[0][2].double(), dw[2].double()
+    asked = w * (g - (w * g).sum())
+    change = torch.zeros(64, dtype=torch.float64, device="cuda")
+    change[ids[2, 0].long()] += asked[3]
+    change[out[1][2, 3].long()] -= asked[3]
+    # four values rounded at most eight times each, of at most twice the largest product
+    assert ((got[2] - want[2]).double() - change).abs().max() <= 64 * 2.0**-24 * float((w.max() * g.abs().max() * 2 + want[2].abs().max()))
 
 
 def test_refusals():

@@ -255,6 +255,54 @@ def test_captured_on_a_stream_and_again():
         assert torch.equal(one, fp4.product(x, fp4.quantize_weight(w[1].cuda() * (i + 1)), out_dtype="f32"))
 
 
+def test_offsets_beyond_32_bits():
+    """Matrices and rows more than 2^31 elements apart."""
+    log("case fp4 far apart")
+    w, x = spread((3, 40, 200), 5, torch.bfloat16), spread((5, 200), 6, torch.bfloat16).clamp(-4, 4)
+    room = torch.empty(3 * 2**30 + 2**16, dtype=torch.bfloat16, device="cuda")
+    far = room.as_strided((3, 40, 200), (5 * 2**28, 1000, 1))
+    far.copy_(w)
+    W, want = fp4.quantize_weight(far), fp4.quantize_weight(w.cuda())
+    assert torch.equal(W.codes, want.codes) and torch.equal(W.packed_scales.view(torch.uint8), want.packed_scales.view(torch.uint8))
+    back = room.as_strided((3, 40, 200), (5 * 2**28, 300, 1))
+    assert torch.equal(W.dequantize(out=back), want.dequantize("bf16"))
+    codes = room.view(torch.uint8).as_strided((3,) + want.codes.shape[1:], (5 * 2**29, want.codes.shape[2], 1))
+    codes.copy_(want.codes)
+    W = fp4.Fp4Matrix(codes, want.packed_scales, 40, 200)
+    off = torch.tensor([0, 2, 3, 5], dtype=torch.int32, device="cuda")
+    assert torch.equal(fp4.grouped_product(x.cuda(), W, off), fp4.grouped_product(x.cuda(), want, off))
+    rows, out = room.as_strided((5, 200), (3 * 2**28, 1)), room.as_strided((5, 40), (3 * 2**28, 1), 4096)
+    rows.copy_(x)
+    fp4.product(rows, fp4.quantize_weight(w[0].cuda()), C=out)
+    assert torch.equal(out, fp4.product(x.cuda(), fp4.quantize_weight(w[0].cuda())))
+
+
+def test_rows_by_operands_captured_and_at_once():
+    """Products that lay their rows out in work memory, replayed beside eager ones and on
+    two streams."""
+    log("case fp4 work memory")
+    W = fp4.quantize_weight(spread((1400, 1300), 7).cuda())
+    x = [torch.randn(1100, 1300, device="cuda").bfloat16() for _ in range(2)]
+    index = torch.randint(-3, 1103, (1200,), dtype=torch.int32, device="cuda")
+    want = [fp4.product(v, W, index=index) for v in x]
+    inside = (index >= 0) & (index < 1100)
+    assert torch.equal(want[0][inside], fp4.product(x[0], W)[index[inside].long()]) and (want[0][~inside] == 0).all()
+    streams = [torch.cuda.Stream() for _ in x]
+    torch.cuda.synchronize()
+    got = [(i, fp4.product(x[i], W, index=index, stream=streams[i])) for _ in range(3) for i in range(2)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i]) for i, y in got)
+    graph, at = torch.cuda.CUDAGraph(), x[0].clone()
+    with torch.cuda.graph(graph):
+        out = fp4.product(at, W, index=index)
+    for i in (1, 0, 1):
+        at.copy_(x[i])
+        graph.replay()
+        assert torch.equal(fp4.product(x[1 - i], W, index=index), want[1 - i])
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[i])
+
+
 def test_refusals():
     log("case fp4 refusals")
     W, E = fp4.quantize_weight(torch.ones(40, 64, device="cuda")), fp4.quantize_weight(torch.ones(2, 40, 64, device="cuda"))

@@ -247,6 +247,30 @@ def test_optimizer():
         orthogonal.OrthogonalMomentum([torch.nn.Parameter(torch.zeros(3, device="cuda"))])
 
 
+def test_optimizer_keeps_momentum_in_32_bits():
+    log("case orthogonal momentum of bf16")
+    g = torch.Generator().manual_seed(1)
+    w = torch.randn(30, 50, generator=g).bfloat16()
+    grads = [torch.randn(30, 50, generator=g).bfloat16().cuda() for _ in range(3)]
+
+    def run(steps, opt):
+        for d in steps:
+            opt.param_groups[0]["params"][0].grad = d.clone()
+            opt.step()
+
+    one = orthogonal.OrthogonalMomentum([torch.nn.Parameter(w.cuda())], lr=0.1, momentum=0.9)
+    run(grads[:2], one)
+    p = one.param_groups[0]["params"][0]
+    b = one.state[p]["momentum"]
+    assert b.dtype == torch.float32 and torch.equal(b, torch.zeros_like(b).add_(grads[0]).mul_(0.9).add_(grads[1]))
+    other = orthogonal.OrthogonalMomentum([torch.nn.Parameter(p.detach().clone())], lr=0.5)
+    other.load_state_dict(one.state_dict())
+    run(grads[2:], one)
+    run(grads[2:], other)
+    q = other.param_groups[0]["params"][0]
+    assert torch.equal(p, q) and torch.equal(one.state[p]["momentum"], other.state[q]["momentum"])
+
+
 def test_refusals():
     log("case orthogonalize refusals")
     G = torch.zeros(6, 8, device="cuda")
