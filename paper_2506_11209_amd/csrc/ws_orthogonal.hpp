@@ -9,7 +9,7 @@ namespace wsg {
 constexpr int kFewRows = 64;  // of the shorter side, at the most
 constexpr int kFewSteps = 6;  // see ws_orthogonal_few.hip
 
-// Whether the Gram matrix alone is quicker.  us so and in tiles, five steps: 64 x 2048 38
+// Whether the Gram matrix alone is quicker.  us so and in tiles, five steps: 64 x 2048 32
 // and 110, 128 x 1024 148 and 97, 128 x 4096 165 and 147.
 inline bool by_gram_matrix(int64_t rows, int64_t cols, int32_t steps) {
   return (rows < cols ? rows : cols) <= kFewRows && steps <= kFewSteps;

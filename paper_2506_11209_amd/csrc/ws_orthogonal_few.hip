@@ -141,13 +141,14 @@ struct FewShape {
 };
 
 // One workgroup's iteration.  Matrices are symmetric (polynomials of A_0): a wave has a
-// tile of the lower triangle and writes it to both its places in one of two matrices in
-// LDS.  Bound: the latency of the products, 17 in a row for five steps, and of the meetings
-// between them (n = 16: 14 us, n = 64: 22 us).
+// tile of the lower triangle and writes it to both its places in a matrix in LDS.  Bound:
+// latency, of the way to memory and of three products in a row a step (T Q beside T A)
+// with the meetings between them (n = 16: 6.4 us, n = 32: 8.3, n = 64, where it is the
+// products themselves on one CU: 19).
 template <int NT>
 __global__ __launch_bounds__(64 * FewShape<NT>::kWaves) void few_iterate_kernel(FewArgs a) {
   typedef FewShape<NT> S;
-  __shared__ __align__(16) float L[S::kSide * S::kPitch], R[S::kSide * S::kPitch];
+  __shared__ __align__(16) float L[S::kSide * S::kPitch], R[S::kSide * S::kPitch], Z[S::kSide * S::kPitch];
   __shared__ float trace;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
   const int64_t matrix = blockIdx.x;
@@ -173,18 +174,22 @@ __global__ __launch_bounds__(64 * FewShape<NT>::kWaves) void few_iterate_kernel(
     return u + v;
   };
   // G G^T, all parts with the largest one's scale
+  constexpr int kAtOnce = NT == 1 ? 32 : 16;  // parts in flight
+  const f32x4_t* from = (const f32x4_t*)a.sums + (matrix * a.parts * S::kWaves + wave) * 64 + lane;
+  f32x4_t s[kAtOnce];
+  const auto load = [&](int p0) {
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) s[u] = from[min(p0 + u, a.parts - 1) * S::kWaves * 64];
+  };
   const int its = lane < a.parts ? a.scales[matrix * a.parts + lane] : -kNotFinite;  // at most 64 parts
+  load(0);
   int scale = its;
   for (int d = 32; d; d /= 2) scale = max(scale, __shfl_xor(scale, d));
   const int of_lane = 2 * max(its - scale, -200);  // what is left out is below 2^-149
   f32x4_t A = {0, 0, 0, 0}, Q = {0, 0, 0, 0};
   if (scale > -kNotFinite && scale < kNotFinite) {
-    constexpr int kAtOnce = 8;  // parts in flight
-    const f32x4_t* from = (const f32x4_t*)a.sums + matrix * a.parts * S::kWaves * 64;
     for (int p0 = 0; p0 < a.parts; p0 += kAtOnce) {
-      f32x4_t s[kAtOnce];
-#pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) s[u] = from[(min(p0 + u, a.parts - 1) * S::kWaves + wave) * 64 + lane];
+      if (p0 > 0) load(p0);
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
         if (p0 + u >= a.parts) break;
@@ -212,26 +217,19 @@ __global__ __launch_bounds__(64 * FewShape<NT>::kWaves) void few_iterate_kernel(
 #pragma unroll
     for (int k = 0; k < 4; ++k) T[k] = fmaf(kC, T[k], fmaf(kB, A[k], row + k == col ? kA : 0.0f));
     put(R, T);
-    if (step == 0) Q = T;
+    if (step > 0) put(Z, Q);
     __syncthreads();
-    if (!last) {
-      const f32x4_t v = product(R, L);
-      __syncthreads();
-      put(L, v);  // T A
-      __syncthreads();
-      A = product(R, L);  // T A T: all of them commute
-      __syncthreads();
-    }
-    if (step > 0) {
-      put(L, Q);
-      __syncthreads();
-      Q = product(R, L);
-      __syncthreads();
-    }
-    if (!last) {
-      put(L, A);
-      __syncthreads();
-    }
+    f32x4_t v = A;
+    if (!last) v = product(R, L);  // T A
+    Q = step > 0 ? product(R, Z) : T;
+    if (last) break;
+    __syncthreads();
+    put(L, v);
+    __syncthreads();
+    A = product(R, L);  // T A T: all of them commute
+    __syncthreads();
+    put(L, A);
+    __syncthreads();
   }
   Q *= sum == 0.0f ? 0.0f : 1.0f / sqrtf(sum);
   float* to = a.Q + matrix * S::kSide * S::kSide;
