@@ -58,8 +58,8 @@ ws_status ws_fp4_dequantize(const ws_fp4_matrix* q, const ws_matrix* out, hipStr
 ws_status ws_fp4_scales(const ws_fp4_matrix* q, uint8_t* out, int64_t ld, int64_t stride, hipStream_t stream);
 
 /* Bytes of device memory that a product of M rows, N columns and K contracted ones needs
- * (0: none, then workspace may be NULL), in `groups` groups or -1 for ws_fp4_product; -1
- * for sizes that it refuses. */
+ * (0: none, then workspace may be NULL; so for up to 16 rows, of a group on average), in
+ * `groups` groups or -1 for ws_fp4_product; -1 for sizes that it refuses. */
 int64_t ws_fp4_product_workspace(int64_t M, int64_t N, int64_t K, int32_t groups);
 
 /* C <- A B^T: B is N x K in 4 bits; C (f32, bf16 or f16) is M x N; its row m is row

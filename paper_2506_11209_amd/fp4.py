@@ -148,6 +148,8 @@ def _rows(A, B, index):
 
 def _work(rows, B, groups, A):
     """Work memory of a product and its size."""
+    if rows <= 16 * max(groups, 1):  # none: not asked for, as these are the shortest calls
+        return None, 0
     need = _lib.ws_fp4_product_workspace(rows, B.rows, B.cols, groups)
     return (torch.empty(need, dtype=torch.uint8, device=A.device) if need > 0 else None), max(need, 0)
 

@@ -108,6 +108,8 @@ def test_products():
         assert lib.ws_fp4_product(*many, work, bytes_, None) == INVALID
     for sizes in ((-1, 5, 5, -1), (5, -1, 5, -1), (5, 5, -1, -1), (5, 5, 5, -2), ((1 << 30) + 1, 5, 5, -1), (5, 5, 5, (1 << 20) + 1)):
         assert lib.ws_fp4_product_workspace(*sizes) == -1, sizes
+    for rows, groups in ((16, -1), (16, 1), (64, 4), (16 << 20, 1 << 20)):
+        assert lib.ws_fp4_product_workspace(rows, 1 << 20, 1 << 20, groups) == 0
     # no rows of A: they come by an index, or there are none
     assert lib.ws_fp4_product(matrix(0, 200, dtype=BF16, data=0), None, B, C, None, 0, None) == INVALID
     assert lib.ws_fp4_product(matrix(0, 200, dtype=BF16, data=0), None, B, matrix(0, 40, data=0), None, 0, None) == w.WS_OK
