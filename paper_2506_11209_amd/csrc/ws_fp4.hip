@@ -262,8 +262,10 @@ __global__ __launch_bounds__(256) void fp4_arrange_kernel(Fp4Args a) {
 // of tiles, 64 bytes of 16 rows a load and scales 4 bytes of each, 14.1; 55 of 64 groups of
 // 4096 x 2048 51 us, 4.8 TB/s, by rows 83); from about 16 rows on by reading those of A
 // for every strip (256 x 4096 x 4096: 24 us, 1024 x 8192 x 8192: 205, 0.67 PFLOP/s).
+// (Of 64 rows with the registers of four waves; of fewer with those of eight, and so more
+// workgroups a CU.)
 template <typename X, int MT, int NT, bool GROUPED, bool ARRANGED>
-__global__ __launch_bounds__(512) void fp4_product_kernel(Fp4Args a) {
+__global__ __launch_bounds__(MT > 2 ? 256 : 512) void fp4_product_kernel(Fp4Args a) {
   constexpr bool kBf16 = std::is_same<X, bf16_t>::value;
   extern __shared__ __align__(16) f32x4_t part[];  // waves x MT x NT x 64
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
@@ -470,14 +472,13 @@ ws_status launch_product(const char* what, int waves, hipStream_t stream, Fp4Arg
 // Rows of a group on average, and what follows from them.
 struct Choice {
   int mt;         // tiles of 16 rows a workgroup has
-  bool many;      // strips
+  bool many;      // strips, of 16 rows
   int64_t bytes;  // of A by operands, 0 where it is read as it lies
 };
-// Eight waves to a contraction fill the card where there are few strips; where there are
-// many, starting waves costs more than it hides.  us of 2 columns' tiles by 8 waves and of
-// 4 by 4: 1 x 8192 x 8192 9.4 and 13.0, 128 rows of 55 of 64 groups of 4096 x 2048 94 and
-// 57; from A as it lies, 64 x 8192 x 8192 by 8 and 4 waves 44.8 and 49.4, 256 x 4096 x 4096
-// 41.5 and 38.5.
+// Of 16 rows, workgroups of 2 tiles' columns and eight waves where there are few strips, of
+// 4 and four waves where there are many and starting waves costs more than it hides.  us:
+// 1 x 8192 x 8192 9.4 and 13.0, 128 rows of 55 of 64 groups of 4096 x 2048 94 and 57.  More
+// rows have many strips, and four waves.
 // A workgroup takes fewer rows where the launch has under three workgroups a CU.  us of all
 // 64 (or 32) rows in one and so: 40 x 4104 x 4100 17.0 and 11.5, 64 x 4096 x 4096 15.5 and
 // 10.2, 64 x 100 x 8192 22.3 and 11.5, 256 x 2048 x 2048 13.1 and 9.5; of two a CU
@@ -504,8 +505,8 @@ template <typename X, bool GROUPED>
 ws_status launch_product(const char* what, const Choice& c, hipStream_t stream, const Fp4Args& a) {
   if (c.mt == 1)
     return c.many ? launch_product<X, 1, 4, GROUPED>(what, 4, stream, a) : launch_product<X, 1, 2, GROUPED>(what, 8, stream, a);
-  if (c.mt == 2) return launch_product<X, 2, 2, GROUPED>(what, c.many ? 4 : 8, stream, a);
-  return launch_product<X, 4, 2, GROUPED>(what, c.many ? 4 : 8, stream, a);
+  if (c.mt == 2) return launch_product<X, 2, 2, GROUPED>(what, 4, stream, a);
+  return launch_product<X, 4, 2, GROUPED>(what, 4, stream, a);
 }
 
 ws_status product(const char* what, const ws_matrix* A, const int32_t* index, const ws_fp4_matrix* B, int32_t groups,
