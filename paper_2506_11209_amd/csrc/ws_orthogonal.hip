@@ -586,14 +586,9 @@ ws_status launch_tiles(OrthArgs a, hipStream_t stream) {
   const uint32_t most = (uint32_t)compute_units() * Shape::kWaves;
   a.tile_groups = (int32_t)(a.count < most ? a.count : most);
   const auto kernel = &orth_step_kernel<WM, WN, STAGES, KIND>;
-  static std::atomic<uint64_t> allowed;  // devices on which the kernel may use this much LDS
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e == hipSuccess && (dev >= 64 || !(allowed.load(std::memory_order_acquire) >> dev & 1))) {
-    e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, Shape::kLds);
-    if (e == hipSuccess && dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_acq_rel);
-  }
-  if (e != hipSuccess) return hip_fail("hipFuncSetAttribute", e);
+  static std::atomic<uint64_t> allowed;
+  const ws_status s = allow_lds((const void*)kernel, Shape::kLds, allowed);
+  if (s != WS_OK) return s;
   return launch("orthogonalize", kernel, a.tile_groups, 256, Shape::kLds, stream, a);
 }
 

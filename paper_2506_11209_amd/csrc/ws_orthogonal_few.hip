@@ -4,14 +4,15 @@
 // Every step multiplies X with a polynomial of A = X X^T, so all of them together
 // multiply the first X with one n x n matrix Q: with T = a + b A + c A^2, Q <- T Q and
 // A <- T A T.  Three launches whatever the number of steps: A_0 = G G^T over parts of the
-// long side, the iteration by one workgroup in LDS, and Q G.  All in binary32: an error
-// of A in a direction grows as A itself does there, 12 times a step, so that directions
-// of singular value s (of G / |G|) come out within about 2^-23 / s^2, where products in
-// binary16 would leave them 2^-10 / s^2.  A is not made from X again, and so parts from
-// it a little more with every step: more than kFewSteps run in tiles.
+// long side, the iteration by one workgroup in LDS, and Q G.
 //
-// Sums: a part of G with very large or small values is scaled by a power of two of its
-// own, so that squares neither overflow nor vanish.
+// A and the iteration are in binary64: A is not made from X again, so that its error in a
+// direction grows as A itself does there, 12 times a step, and a direction of singular
+// value s (of G / |G|) comes out within a few u / s^2.  With binary32's u = 2^-24, five
+// steps were off by up to 1.3e-3 (in norm) and six by up to 2e-2, where one value is 1 and
+// the others 1/1000; now what is left is Q and its product with G in binary32, 2^-24 of the
+// largest value of Q, 3.5^steps, and so 1e-4 for kFewSteps.  More steps run in tiles.
+// Squares of binary32 values neither overflow nor vanish in binary64.
 #include <math.h>
 
 #include "ws_fp8_common.hpp"
@@ -20,7 +21,7 @@
 namespace wsg {
 namespace {
 
-constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr double kA = 3.4445, kB = -4.7750, kC = 2.0315;
 
 struct FewArgs {
   const void* G;
@@ -28,12 +29,12 @@ struct FewArgs {
   int64_t ld, stride, ld_out, stride_out;
   int32_t n, m, tall, steps;  // tall: rows of G are the long side
   int32_t parts, each;        // of the long side, a multiple of 16
-  float* sums;                // batch x parts x tiles x 64 x 4: lower triangle of G G^T
-  int32_t* scales;            // batch x parts: their values are those of G times 2^-scale; kNotFinite
-  float* Q;                   // batch x (16 NT)^2, by 1 / sqrt(trace)
-  int32_t* scale;             // batch: the scale of Q G
+  double* sums;               // batch x parts x tiles x 64 x 4: lower triangle of G G^T
+  float* Q;                   // batch x (16 NT)^2, by 2^scale / sqrt(trace)
+  int32_t* scale;             // batch: Q belongs to G times 2^-scale
 };
-constexpr int kNotFinite = 1 << 20;
+
+typedef double f64x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int lower_tiles(int nt) { return nt * (nt + 1) / 2; }
 // Tile t of the lower triangle, row after row.
@@ -67,6 +68,8 @@ __device__ __forceinline__ f32x4_t four(const T* G, const FewArgs& a, int row, i
 }
 
 __device__ __forceinline__ f32x4_t multiply(float x, float y, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(x, y, c, 0, 0, 0); }
+// Of its sums lane (r, g) has rows g, g + 4 .. of column r; in binary32 rows 4 g, 4 g + 1 ..
+__device__ __forceinline__ f64x4_t multiply(double x, double y, f64x4_t c) { return __builtin_amdgcn_mfma_f64_16x16x4f64(x, y, c, 0, 0, 0); }
 
 constexpr int kGramWaves = 4;
 
@@ -75,97 +78,80 @@ constexpr int kGramWaves = 4;
 template <typename T, int NT>
 __global__ __launch_bounds__(64 * kGramWaves) void few_gram_kernel(FewArgs a) {
   constexpr int kTiles = lower_tiles(NT);
-  __shared__ f32x4_t sums[kTiles * 64];
-  __shared__ uint32_t top[kGramWaves];
+  __shared__ f64x4_t sums[kTiles * 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
   const int64_t matrix = blockIdx.x / a.parts;
   const int part = blockIdx.x % a.parts, lo = part * a.each, hi = min(lo + a.each, a.m);
   const T* G = (const T*)a.G + matrix * a.stride;
-  f32x4_t acc[kTiles];
-  uint32_t most = 0;  // magnitudes' bits are in their order; NaN above infinity
-  // All of the part with values times 2^-scale; a step's loads go out before the one
-  // before it is multiplied.  Parts are whole 16s, but for the last one's end.
-  const auto add_up = [&](int scale) {
+  f64x4_t acc[kTiles];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) acc[t] = f32x4_t{0, 0, 0, 0};
-    f32x4_t f[NT], next[NT];
+  for (int t = 0; t < kTiles; ++t) acc[t] = f64x4_t{0, 0, 0, 0};
+  // A step's loads go out before the one before it is multiplied.  Parts are whole 16s, but
+  // for the last one's end.
+  f32x4_t f[NT], next[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) next[t] = four(G, a, 16 * t + r, lo + 16 * wave + 4 * g);
-    for (int k0 = lo + 16 * wave; k0 < hi; k0 += 16 * kGramWaves) {
+  for (int t = 0; t < NT; ++t) next[t] = four(G, a, 16 * t + r, lo + 16 * wave + 4 * g);
+  for (int k0 = lo + 16 * wave; k0 < hi; k0 += 16 * kGramWaves) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        f[t] = next[t];
-        next[t] = four(G, a, 16 * t + r, min(k0 + 16 * kGramWaves, a.m) + 4 * g);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          most = max(most, __float_as_uint(f[t][i]) & 0x7fffffffu);
-          f[t][i] = ldexpf(f[t][i], -scale);
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-          for (int j = 0; j <= i; ++j) acc[i * (i + 1) / 2 + j] = multiply(f[i][k], f[j][k], acc[i * (i + 1) / 2 + j]);
+    for (int t = 0; t < NT; ++t) {
+      f[t] = next[t];
+      next[t] = four(G, a, 16 * t + r, min(k0 + 16 * kGramWaves, a.m) + 4 * g);
     }
-  };
-  add_up(0);
-  for (int d = 32; d; d /= 2) most = max(most, (uint32_t)__shfl_xor((int)most, d));
-  if (lane == 0) top[wave] = most;
-  __syncthreads();
-  for (int w = 0; w < kGramWaves; ++w) most = max(most, top[w]);
-  // Gradients between 2^-40 and 2^40 at the largest need no scale.
-  int scale = 0;
-  if (most >= 0x7f800000u) scale = kNotFinite;
-  else if (most == 0) scale = -kNotFinite;
-  else if (most < (87u << 23) || most >= (167u << 23)) {
-    scale = ilogbf(__uint_as_float(most));
-    add_up(scale);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j <= i; ++j)
+          acc[i * (i + 1) / 2 + j] = multiply((double)f[i][k], (double)f[j][k], acc[i * (i + 1) / 2 + j]);
   }
-  if (tid == 0) a.scales[blockIdx.x] = scale;
   for (int w = 0; w < kGramWaves; ++w) {
     if (wave == w)
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) sums[t * 64 + lane] = w ? sums[t * 64 + lane] + acc[t] : acc[t];
     __syncthreads();
   }
-  f32x4_t* to = (f32x4_t*)a.sums + (int64_t)blockIdx.x * kTiles * 64;
+  f64x4_t* to = (f64x4_t*)a.sums + (int64_t)blockIdx.x * kTiles * 64;
   for (int i = tid; i < kTiles * 64; i += 64 * kGramWaves) to[i] = sums[i];
 }
 
 template <int NT>
 struct FewShape {
   static constexpr int kWaves = lower_tiles(NT);  // a tile each
-  static constexpr int kSide = 16 * NT, kPitch = kSide + 4;  // floats: rows spread over the banks
+  static constexpr int kSide = 16 * NT, kPitch = kSide + 2;  // doubles: rows spread over the banks
+  static constexpr int kBytes = 3 * kSide * kPitch * 8;
 };
 
 // One workgroup's iteration.  Matrices are symmetric (polynomials of A_0): a wave has a
 // tile of the lower triangle and writes it to both its places in a matrix in LDS.  Bound:
 // latency, of the way to memory and of three products in a row a step (T Q beside T A)
-// with the meetings between them (n = 16: 6.4 us, n = 32: 8.3, n = 64, where it is the
-// products themselves on one CU: 19).
+// with the meetings between them (n = 16: 8.0 us, n = 32: 11.8, n = 64, where it is the
+// products themselves on one CU: 33).
 template <int NT>
 __global__ __launch_bounds__(64 * FewShape<NT>::kWaves) void few_iterate_kernel(FewArgs a) {
   typedef FewShape<NT> S;
-  __shared__ __align__(16) float L[S::kSide * S::kPitch], R[S::kSide * S::kPitch], Z[S::kSide * S::kPitch];
-  __shared__ float trace;
+  extern __shared__ __align__(16) uint8_t smem[];
+  double* L = (double*)smem;
+  double *R = L + S::kSide * S::kPitch, *Z = R + S::kSide * S::kPitch;
+  __shared__ double trace;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
   const int64_t matrix = blockIdx.x;
   int ti, tj;
   tile_at(wave, &ti, &tj);
-  const int row = 16 * ti + 4 * g, col = 16 * tj + r;  // the lane's: rows row .. row + 3
-  const auto put = [&](float* to, const f32x4_t& v) {
+  const int row = 16 * ti + g, col = 16 * tj + r;  // the lane's: rows row, row + 4 ..
+  const auto put = [&](double* to, const f64x4_t& v) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) to[(row + k) * S::kPitch + col] = v[k];
-    if (ti != tj) *(f32x4_t*)(to + col * S::kPitch + row) = v;
+    for (int k = 0; k < 4; ++k) {
+      to[(row + 4 * k) * S::kPitch + col] = v[k];
+      if (ti != tj) to[col * S::kPitch + row + 4 * k] = v[k];
+    }
   };
-  const auto product = [&](const float* x, const float* y) {
-    f32x4_t u = {0, 0, 0, 0}, v = {0, 0, 0, 0};  // two sums, for half the way through each
+  const auto product = [&](const double* x, const double* y) {
+    f64x4_t u = {0, 0, 0, 0}, v = {0, 0, 0, 0};  // two sums, for half the way through each
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
-      const f32x4_t p = *(const f32x4_t*)(x + (16 * ti + r) * S::kPitch + 16 * k + 4 * g);
-      const f32x4_t q = *(const f32x4_t*)(y + (16 * tj + r) * S::kPitch + 16 * k + 4 * g);
+      const double* p = x + (16 * ti + r) * S::kPitch + 16 * k + 4 * g;
+      const double* q = y + (16 * tj + r) * S::kPitch + 16 * k + 4 * g;
       u = multiply(p[0], q[0], u);
       v = multiply(p[1], q[1], v);
       u = multiply(p[2], q[2], u);
@@ -173,53 +159,40 @@ __global__ __launch_bounds__(64 * FewShape<NT>::kWaves) void few_iterate_kernel(
     }
     return u + v;
   };
-  // G G^T, all parts with the largest one's scale
-  constexpr int kAtOnce = NT == 1 ? 32 : 16;  // parts in flight
-  const f32x4_t* from = (const f32x4_t*)a.sums + (matrix * a.parts * S::kWaves + wave) * 64 + lane;
-  f32x4_t s[kAtOnce];
-  const auto load = [&](int p0) {
+  // G G^T
+  constexpr int kAtOnce = 16;  // parts in flight
+  const f64x4_t* from = (const f64x4_t*)a.sums + (matrix * a.parts * S::kWaves + wave) * 64 + lane;
+  f64x4_t A = {0, 0, 0, 0}, Q = {0, 0, 0, 0};
+  for (int p0 = 0; p0 < a.parts; p0 += kAtOnce) {
+    f64x4_t s[kAtOnce];
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) s[u] = from[min(p0 + u, a.parts - 1) * S::kWaves * 64];
-  };
-  const int its = lane < a.parts ? a.scales[matrix * a.parts + lane] : -kNotFinite;  // at most 64 parts
-  load(0);
-  int scale = its;
-  for (int d = 32; d; d /= 2) scale = max(scale, __shfl_xor(scale, d));
-  const int of_lane = 2 * max(its - scale, -200);  // what is left out is below 2^-149
-  f32x4_t A = {0, 0, 0, 0}, Q = {0, 0, 0, 0};
-  if (scale > -kNotFinite && scale < kNotFinite) {
-    for (int p0 = 0; p0 < a.parts; p0 += kAtOnce) {
-      if (p0 > 0) load(p0);
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        if (p0 + u >= a.parts) break;
-        const int by = __builtin_amdgcn_readlane(of_lane, p0 + u);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) A[k] += ldexpf(s[u][k], by);
-      }
-    }
+    for (int u = 0; u < kAtOnce; ++u)
+      if (p0 + u < a.parts) A += s[u];
   }
   put(L, A);
   __syncthreads();
   if (wave == 0) {
-    float sum = lane < S::kSide ? L[lane * S::kPitch + lane] : 0.0f;  // a side has 64 at the most
+    double sum = lane < S::kSide ? L[lane * S::kPitch + lane] : 0.0;  // a side has 64 at the most
     for (int d = 32; d; d /= 2) sum += __shfl_xor(sum, d);
     if (lane == 0) trace = sum;
   }
   __syncthreads();
-  const float sum = scale == kNotFinite ? NAN : trace;
-  A *= sum == 0.0f ? 0.0f : 1.0f / sum;
+  // Sums of finite squares stay below 2^256 2^22; an infinity or NaN makes all of Q NaN.
+  const double sum = trace < INFINITY ? trace : (double)NAN;
+  A *= sum == 0.0 ? 0.0 : 1.0 / sum;
   put(L, A);  // each value's own thread has put it there before
   __syncthreads();
   for (int step = 0; step < a.steps; ++step) {
     const bool last = step + 1 == a.steps;
-    f32x4_t T = product(L, L);  // A^2
+    f64x4_t T = product(L, L);  // A^2
 #pragma unroll
-    for (int k = 0; k < 4; ++k) T[k] = fmaf(kC, T[k], fmaf(kB, A[k], row + k == col ? kA : 0.0f));
+    for (int k = 0; k < 4; ++k) T[k] = fma(kC, T[k], fma(kB, A[k], row + 4 * k == col ? kA : 0.0));
     put(R, T);
     if (step > 0) put(Z, Q);
     __syncthreads();
-    f32x4_t v = A;
+    f64x4_t v = A;
     if (!last) v = product(R, L);  // T A
     Q = step > 0 ? product(R, Z) : T;
     if (last) break;
@@ -231,12 +204,18 @@ __global__ __launch_bounds__(64 * FewShape<NT>::kWaves) void few_iterate_kernel(
     put(L, A);
     __syncthreads();
   }
-  Q *= sum == 0.0f ? 0.0f : 1.0f / sqrtf(sum);
+  // G's largest value is within sqrt(trace) and 1 / sqrt(n m) of it: both factors of Q G
+  // stay inside binary32's range
+  const double norm = sqrt(sum);
+  const int scale = sum > 0.0 ? ilogb(norm) : 0;
+  Q *= sum == 0.0 ? 0.0 : ldexp(1.0, scale) / norm;
   float* to = a.Q + matrix * S::kSide * S::kSide;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) to[(row + k) * S::kSide + col] = Q[k];
-  if (ti != tj) *(f32x4_t*)(to + col * S::kSide + row) = Q;
-  if (tid == 0) a.scale[matrix] = scale > -kNotFinite && scale < kNotFinite ? scale : 0;
+  for (int k = 0; k < 4; ++k) {
+    to[(row + 4 * k) * S::kSide + col] = (float)Q[k];
+    if (ti != tj) to[col * S::kSide + row + 4 * k] = (float)Q[k];
+  }
+  if (tid == 0) a.scale[matrix] = scale;
 }
 
 // Q G: a wave takes 16 of the long side.  The operands are passed in the order that
@@ -306,7 +285,7 @@ __global__ __launch_bounds__(256) void few_apply_kernel(FewArgs a) {
 
 struct FewLayout {
   int nt, parts, each;
-  int64_t n, m, sums, scales, Q, scale, all;
+  int64_t n, m, sums, Q, scale, all;
 };
 
 FewLayout few_layout(int64_t rows, int64_t cols, int64_t batch) {
@@ -314,7 +293,7 @@ FewLayout few_layout(int64_t rows, int64_t cols, int64_t batch) {
   l.n = rows < cols ? rows : cols;
   l.m = rows < cols ? cols : rows;
   l.nt = l.n <= 16 ? 1 : l.n <= 32 ? 2 : 4;
-  // Parts: as many as the iteration's workgroup adds up quickly (64 KiB to 160 KiB of sums)
+  // Parts: as many as the iteration's workgroup adds up quickly (128 KiB to 320 KiB of sums)
   const int most = l.nt == 1 ? 64 : l.nt == 2 ? 32 : 16;
   l.each = (int)(ceil_div(ceil_div(l.m, most), 64) * 64);
   l.parts = (int)ceil_div(l.m, l.each);
@@ -323,8 +302,7 @@ FewLayout few_layout(int64_t rows, int64_t cols, int64_t batch) {
     l.all += ceil_div(bytes, 256) * 256;
     return at;
   };
-  l.sums = take(batch * l.parts * lower_tiles(l.nt) * 1024);
-  l.scales = take(batch * l.parts * 4);
+  l.sums = take(batch * l.parts * lower_tiles(l.nt) * 2048);
   l.Q = take(batch * 256 * l.nt * l.nt * 4);
   l.scale = take(batch * 4);
   return l;
@@ -333,7 +311,9 @@ FewLayout few_layout(int64_t rows, int64_t cols, int64_t batch) {
 template <typename T, int NT>
 ws_status run_few(const FewArgs& a, int64_t batch, hipStream_t stream) {
   ws_status s = launch("orthogonalize", &few_gram_kernel<T, NT>, batch * a.parts, 64 * kGramWaves, 0, stream, a);
-  if (s == WS_OK) s = launch("orthogonalize", &few_iterate_kernel<NT>, batch, 64 * FewShape<NT>::kWaves, 0, stream, a);
+  static std::atomic<uint64_t> allowed;
+  if (s == WS_OK) s = allow_lds((const void*)&few_iterate_kernel<NT>, FewShape<NT>::kBytes, allowed);
+  if (s == WS_OK) s = launch("orthogonalize", &few_iterate_kernel<NT>, batch, 64 * FewShape<NT>::kWaves, FewShape<NT>::kBytes, stream, a);
   if (s == WS_OK) s = launch("orthogonalize", &few_apply_kernel<T, NT>, batch * ceil_div(a.m, 64), 256, 0, stream, a);
   return s;
 }
@@ -367,8 +347,7 @@ ws_status orthogonalize_few(const ws_matrix* G, int32_t steps, const ws_matrix* 
   a.steps = steps;
   a.parts = l.parts;
   a.each = l.each;
-  a.sums = (float*)(w + l.sums);
-  a.scales = (int32_t*)(w + l.scales);
+  a.sums = (double*)(w + l.sums);
   a.Q = (float*)(w + l.Q);
   a.scale = (int32_t*)(w + l.scale);
   if (G->dtype == WS_OUT_F32) return run_few<float>(a, l.nt, G->batch, stream);
