@@ -342,6 +342,8 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth
   drain_and_meet<kLoads * (STAGES - 1)>();
   for (; id < end; id += turns) {
     find_tile(later, id + turns);
+    // The first meeting leaves a load under way as the others do: not one of block 1's.
+    if constexpr (Shape::kAhead) ask_ahead(3);
     f32x4_t acc[WM][WN];
 #pragma unroll
     for (int i = 0; i < WM; ++i)
