@@ -13,8 +13,10 @@
 // S and T are symmetric: tiles below their diagonal are computed and written twice.
 // Why diagonals are kept apart: once singular values are near 1, A and T are near
 // multiples of the identity, and rounding these to binary16 cost most of the error
-// (1.0e-3 to 2.3e-3 of the result so, 1e-4 to 1e-3 apart).  Why X is two values: where a
-// few directions dominate G, rounding X alone cost 6e-3 in the others.
+// (1.0e-3 to 2.3e-3 of the result so, 1e-4 to 1e-3 apart, of values that are alike).
+//
+// Short sides, and more than five steps (in_two_values): X, Y, S and T are two binary16
+// values each, of the same unit, and a product is three; see FINE.
 #include <math.h>
 
 #include "ws_orthogonal.hpp"
@@ -32,10 +34,15 @@ typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 enum Kind { kGram, kSquare, kApply, kLast };
 
+// FINE, in what follows: X, Y, S and T are sums of two binary16 values, whose rows lie one
+// behind the other, twice as long.
+template <bool FINE>
+constexpr int kRow = FINE ? 2 : 1;
+
 struct OrthArgs {
   const _Float16 *A, *B;         // operands, `batch` of them
   int64_t stride_a, stride_b;    // elements between them
-  int32_t M, N, K;               // multiples of kPad; rows of K elements
+  int32_t M, N, K;               // multiples of kPad; rows of K elements (FINE: twice)
   int32_t batch, tile_groups, tiles_m, tiles_n;
   uint32_t plane;                // tiles of one matrix
   uint32_t first, count;         // tiles of this launch; quarters: every one of them in four of half its sides
@@ -45,18 +52,18 @@ struct OrthArgs {
   const float* d_in;             // kSquare: dA; kApply: dB
   float* d_out;                  // kGram: dA; kSquare: dB
   int64_t stride_d;
-  _Float16* rest;                // of Y
+  _Float16* rest;                // of Y, where not FINE
   // kLast
   uint16_t* out;
   int64_t ld_out, stride_out;
   int32_t rows, cols, transposed;  // of out; transposed: it is X, not Y
 };
 
-template <int WM, int WN, int STAGES>
+template <int WM, int WN, int STAGES, bool FINE = false>
 struct OrthShape {
-  static constexpr int TM = 32 * WM, TN = 32 * WN, kStage = (TM + TN) * 128;
+  static constexpr int TM = 32 * WM, TN = 32 * WN, kPart = (TM + TN) * 128, kStage = kRow<FINE> * kPart;
   static constexpr bool kAgpr = WM * WN > 16;
-  static constexpr int kWaves = kAgpr || STAGES > 2 ? 1 : WM * WN > 4 ? 2 : 4;  // of a SIMD, as workgroups of a CU
+  static constexpr int kWaves = kAgpr || STAGES > 2 ? 1 : (WM * WN > 4 ? 2 : 4) / kRow<FINE>;  // of a SIMD, as workgroups of a CU
   static constexpr int kFirst = WM > 4 ? 3 : WM / 2;
   // a wave's way to memory: 64 (or all its) rows of 32 columns
   static constexpr int kHalves = WM >= 4 ? 2 : 1, kStoreBytes = kHalves * 32 * 32 * 2;
@@ -135,32 +142,33 @@ __device__ __forceinline__ void turn_round(const i32x4_t (&v)[2 * H], uint8_t* o
 // column n, lane (r, g) columns 8 g .. of rows 16 i + r.
 template <int KIND>
 struct Old {
-  f16x8_t value[2], rest[2];  // kSquare: S; kApply, kLast: Y
+  f16x8_t value[2], rest[2];  // kSquare: S (its rest where FINE); kApply, kLast: Y
   f32x4_t dn[2];
   float dm[2];
 };
-template <int KIND>
+template <int KIND, bool FINE>
 __device__ __forceinline__ void fetch(const OrthArgs& a, int64_t matrix, int m, int n, Old<KIND>& o) {
   const int lane = threadIdx.x & 63, row = m + (lane & 15), col = n + 8 * (lane >> 4);
   if constexpr (KIND != kGram) {
     const float* d_in = a.d_in + matrix * a.stride_d;
     o.dn[0] = *(const f32x4_t*)(d_in + col);
     o.dn[1] = *(const f32x4_t*)(d_in + col + 4);
-    const int64_t at = matrix * a.stride_a + (int64_t)row * a.K + col;  // kApply, kLast: N == K
+    const int64_t at = matrix * a.stride_a + (int64_t)row * (kRow<FINE> * a.K) + col;  // kApply, kLast: N == K
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      o.value[i] = *(const f16x8_t*)(a.A + at + 16 * i * a.K);
+      o.value[i] = *(const f16x8_t*)(a.A + at + 16 * i * (kRow<FINE> * a.K));
+      if constexpr (FINE) o.rest[i] = *(const f16x8_t*)(a.A + at + 16 * i * (2 * a.K) + a.K);
+      else if constexpr (KIND != kSquare) o.rest[i] = *(const f16x8_t*)(a.rest + at + 16 * i * a.K);
       if constexpr (KIND == kSquare) o.dm[i] = d_in[row + 16 * i];
-      else o.rest[i] = *(const f16x8_t*)(a.rest + at + 16 * i * a.K);
     }
   }
 }
 
 // What the kind of launch makes of the sums of 32 x 32 results from row m and column n;
-// the rest of X is written at once.
-template <int KIND>
+// what v leaves goes to `low` (FINE), or, of X, to memory at once.
+template <int KIND, bool FINE>
 __device__ __forceinline__ void convert(const OrthArgs& a, const f32x4_t* (&acc)[2][2], const Old<KIND>& o, int64_t matrix, int m,
-                                        int n, i32x4_t* v) {
+                                        int n, i32x4_t* v, i32x4_t* low) {
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, col = n + 8 * g;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -172,10 +180,12 @@ __device__ __forceinline__ void convert(const OrthArgs& a, const f32x4_t* (&acc)
       if constexpr (KIND == kGram) {
         x[k] = s;
       } else if constexpr (KIND == kSquare) {  // in units of kUnit
-        const float square = fmaf(o.dm[i] + o.dn[k / 4][k % 4], (float)o.value[i][k], s);
-        x[k] = fmaf(kC, square, kB * (float)o.value[i][k]);
+        float own = (float)o.value[i][k];
+        if constexpr (FINE) own += (float)o.rest[i][k];
+        const float square = fmaf(o.dm[i] + o.dn[k / 4][k % 4], own, s);
+        x[k] = fmaf(kC, square, kB * own);
       } else {
-        x[k] = fmaf(o.dn[k / 4][k % 4], fmaf((float)o.rest[i][k], 1.0f / kRest, (float)o.value[i][k]), s);
+        x[k] = fmaf(o.dn[k / 4][k % 4], fmaf((float)o.rest[i][k], FINE ? 1.0f : 1.0f / kRest, (float)o.value[i][k]), s);
       }
     }
     if constexpr (KIND == kGram || KIND == kSquare) {
@@ -203,7 +213,12 @@ __device__ __forceinline__ void convert(const OrthArgs& a, const f32x4_t* (&acc)
 #pragma unroll
       for (int k = 0; k < 8; ++k) t[k] = (_Float16)x[k];
       v[i] = __builtin_bit_cast(i32x4_t, t);
-      if constexpr (KIND == kApply) {
+      if constexpr (FINE) {
+        f16x8_t left;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) left[k] = (_Float16)(x[k] - (float)t[k]);
+        low[i] = __builtin_bit_cast(i32x4_t, left);
+      } else if constexpr (KIND == kApply) {
         f16x8_t left;
 #pragma unroll
         for (int k = 0; k < 8; ++k) left[k] = (_Float16)((x[k] - (float)t[k]) * kRest);
@@ -214,9 +229,9 @@ __device__ __forceinline__ void convert(const OrthArgs& a, const f32x4_t* (&acc)
 }
 
 // Writes 32 H x 32 converted results of a wave from row m and column n where they belong.
-template <int KIND, int H>
-__device__ __forceinline__ void write_part(const OrthArgs& a, const i32x4_t (&v)[2 * H], int64_t matrix, int m, int n, bool twice,
-                                           uint8_t* own) {
+template <int KIND, int H, bool FINE>
+__device__ __forceinline__ void write_part(const OrthArgs& a, const i32x4_t (&v)[2 * H], const i32x4_t (&low)[2 * H], int64_t matrix,
+                                           int m, int n, bool twice, uint8_t* own) {
   const int lane = threadIdx.x & 63, r = lane & 15, col = n + 8 * (lane >> 4);
   if constexpr (KIND == kLast) {
     uint16_t* out = a.out + matrix * a.stride_out;
@@ -237,12 +252,18 @@ __device__ __forceinline__ void write_part(const OrthArgs& a, const i32x4_t (&v)
       for (int i = 0; i < 2 * H; ++i) put(m + 16 * i + r, col, v[i]);
     }
   } else {
-    _Float16* to = a.to + matrix * a.stride_to + (int64_t)(m + r) * a.N + col;
+    constexpr int R = kRow<FINE>;
+    _Float16* to = a.to + matrix * a.stride_to + (int64_t)(m + r) * (R * a.N) + col;
 #pragma unroll
-    for (int i = 0; i < 2 * H; ++i) *(i32x4_t*)(to + 16 * i * (int64_t)a.N) = v[i];
+    for (int i = 0; i < 2 * H; ++i) {
+      *(i32x4_t*)(to + 16 * i * (int64_t)(R * a.N)) = v[i];
+      if constexpr (FINE) *(i32x4_t*)(to + 16 * i * (int64_t)(R * a.N) + a.N) = low[i];
+    }
     if (twice) {
       _Float16* mirror = a.mirror + matrix * a.stride_mirror;
-      turn_round<H>(v, own, [&](int line, int at, i32x4_t piece) { *(i32x4_t*)(mirror + (int64_t)(n + line) * a.M + m + at) = piece; });
+      turn_round<H>(v, own, [&](int line, int at, i32x4_t piece) { *(i32x4_t*)(mirror + (int64_t)(n + line) * (R * a.M) + m + at) = piece; });
+      if constexpr (FINE)
+        turn_round<H>(low, own, [&](int line, int at, i32x4_t piece) { *(i32x4_t*)(mirror + (int64_t)(n + line) * (R * a.M) + a.M + m + at) = piece; });
     }
   }
 }
@@ -258,10 +279,14 @@ __device__ __forceinline__ void write_part(const OrthArgs& a, const i32x4_t (&v)
 // Loads go on into a workgroup's next tile, whose first blocks are there when the tile it
 // has is written (a tile has two blocks or more; with more stages a workgroup has one).
 // Long rings are for few tiles, one a CU, whose blocks are shorter than the way to memory.
-template <int WM, int WN, int STAGES, int KIND>
-__global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth_step_kernel(OrthArgs a) {
-  typedef OrthShape<WM, WN, STAGES> Shape;
+// FINE: a stage has the rests of A and B too, for three products: A's rests by B, A by
+// B's rests, A by B; what both rests would give is below 2^-22 of the last.  (As three times
+// the contraction instead, one product a block: 128 x 4096 341 us, 4 x 188 x 1358 227.)
+template <int WM, int WN, int STAGES, int KIND, bool FINE>
+__device__ __forceinline__ void orth_step(const OrthArgs& a) {
+  typedef OrthShape<WM, WN, STAGES, FINE> Shape;
   constexpr int TM = Shape::TM, TN = Shape::TN, kStage = Shape::kStage, kFirst = Shape::kFirst, kRows = WM - kFirst;
+  constexpr int kProducts = FINE ? 6 : 2;  // of two fragments and a block
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
   static_assert(!kSymmetric || TM == TN, "tiles of the lower triangle");
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -272,12 +297,12 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth
   const uint32_t turns = (a.tile_groups + 7 - xcd) / 8, end = xcd * share + min(xcd, extra) + share + (xcd < extra);
   uint32_t id = xcd * share + min(xcd, extra) + blockIdx.x / 8;
 
-  const uint32_t ld = (uint32_t)a.K * 2;  // bytes between rows of both operands
+  const uint32_t ld = (uint32_t)a.K * (2 * kRow<FINE>);  // bytes between rows of both operands
   const int lr = 8 * wave + (lane >> 3);  // chunk_at and chunk_of_b are their own inverses
   const uint32_t at_a = (uint32_t)lr * ld + chunk_at(lr, lane & 7), at_b = (uint32_t)lr * ld + chunk_of_b(lr, lane & 7), step = 32 * ld;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(WSG_LDS uint8_t*)smem + wave * 1024;
   const int blocks = a.K / 64;  // even: every tile's first one lies in stage 0 where there are two, or where a workgroup has one tile
-  constexpr int kLoads = (TM + TN) / 32;  // of a wave and block, 1 KiB each
+  constexpr int kHalf = (TM + TN) / 32, kLoads = kRow<FINE> * kHalf;  // of a wave and block, 1 KiB each
   struct Tile {
     int64_t matrix;
     int m0, n0;
@@ -307,8 +332,8 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth
     t.matrix = there ? matrix : 0;
     t.m0 = __builtin_amdgcn_readfirstlane(there ? (int)tm * TM : a.M);
     t.n0 = __builtin_amdgcn_readfirstlane(there ? (int)tn * TN : a.N);
-    t.ra = raw_buffer((const uint8_t*)(a.A + t.matrix * a.stride_a + (int64_t)t.m0 * a.K), (uint32_t)min(a.M - t.m0, TM) * ld);
-    t.rb = raw_buffer((const uint8_t*)(a.B + t.matrix * a.stride_b + (int64_t)t.n0 * a.K), (uint32_t)min(a.N - t.n0, TN) * ld);
+    t.ra = raw_buffer((const uint8_t*)(a.A + t.matrix * a.stride_a + (int64_t)t.m0 * (kRow<FINE> * a.K)), (uint32_t)min(a.M - t.m0, TM) * ld);
+    t.rb = raw_buffer((const uint8_t*)(a.B + t.matrix * a.stride_b + (int64_t)t.n0 * (kRow<FINE> * a.K)), (uint32_t)min(a.N - t.n0, TN) * ld);
     t.ahead_a = tn % 4 * 64;
     t.ahead_b = tm % 8 * 32;
   };
@@ -319,9 +344,10 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth
     const uint32_t lds = lds0 + (b & (STAGES - 1)) * kStage;
     const i32x4_t ra = select(here, t.ra, later.ra), rb = select(here, t.rb, later.rb);
 #pragma unroll
-    for (int i = from; i < to; ++i) {
-      if (i < TM / 32) load_to_lds(ra, at_a + i * step, k, lds + i * 4096);
-      else load_to_lds(rb, at_b + (i - TM / 32) * step, k, lds + i * 4096);
+    for (int l = from; l < to; ++l) {
+      const int i = l % kHalf, at = l / kHalf * ((int)ld / 2) + k;  // rests: the second half of a row
+      if (i < TM / 32) load_to_lds(ra, at_a + i * step, at, lds + l * 4096);
+      else load_to_lds(rb, at_b + (i - TM / 32) * step, at, lds + l * 4096);
     }
   };
   // Asks for lines of a block, so that they are in the L2 when they are loaded: 32 rows
@@ -351,15 +377,24 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth
       for (int j = 0; j < WN; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
     const int fa0 = (wm * WM * 16 + r) * 128, a0 = fa0 + chunk_at(r, g), a1 = fa0 + chunk_at(r, g + 4);
     const int fb0 = (TM + wn * WN * 16 + row_of_b(r, 0)) * 128, b0 = fb0 + chunk_of_b(row_of_b(r, 0), g), b1 = fb0 + chunk_of_b(row_of_b(r, 0), g + 4);
-    i32x4_t fa[WM][2], fb[WN][2];
+    i32x4_t fa[WM][2 * kRow<FINE>], fb[WN][2 * kRow<FINE>];  // two of the values, two of their rests
     const auto frag_a = [&](int i, int stage) {
-      fa[i][0] = *(const i32x4_t*)(smem + stage + a0 + i * 2048);
-      fa[i][1] = *(const i32x4_t*)(smem + stage + a1 + i * 2048);
+#pragma unroll
+      for (int p = 0; p < kRow<FINE>; ++p) {
+        fa[i][2 * p] = *(const i32x4_t*)(smem + stage + p * Shape::kPart + a0 + i * 2048);
+        fa[i][2 * p + 1] = *(const i32x4_t*)(smem + stage + p * Shape::kPart + a1 + i * 2048);
+      }
     };
     const auto frag_b = [&](int j, int stage) {
-      fb[j][0] = *(const i32x4_t*)(smem + stage + b0 + j / 2 * 4096 + j % 2 * 512);
-      fb[j][1] = *(const i32x4_t*)(smem + stage + b1 + j / 2 * 4096 + j % 2 * 512);
+#pragma unroll
+      for (int p = 0; p < kRow<FINE>; ++p) {
+        fb[j][2 * p] = *(const i32x4_t*)(smem + stage + p * Shape::kPart + b0 + j / 2 * 4096 + j % 2 * 512);
+        fb[j][2 * p + 1] = *(const i32x4_t*)(smem + stage + p * Shape::kPart + b1 + j / 2 * 4096 + j % 2 * 512);
+      }
     };
+    // product q of a block: rests by values, values by rests, values by values
+    const auto of_a = [](int q) { return kProducts - q > 4 ? q + 2 : q % 2; };
+    const auto of_b = [](int q) { return FINE && q / 2 == 1 ? q % 2 + 2 : q % 2; };
 #pragma unroll
     for (int j = 0; j < WN; ++j) frag_b(j, 0);
 #pragma unroll
@@ -369,10 +404,10 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth
       const int here = (b & (STAGES - 1)) * kStage, next = ((b + 1) & (STAGES - 1)) * kStage;
       static_for<kFirst>([&](auto ic) {
         constexpr int i = decltype(ic)::value;
-        static_for<2 * WN>([&](auto jc) {
-          constexpr int q = decltype(jc)::value / WN, j = decltype(jc)::value % WN, n = i * 2 * WN + decltype(jc)::value;
-          constexpr int all = kFirst * WN;  // slots: the first half of these products
-          multiply_f16<Shape::kAgpr>(acc[i][j], fa[i][q], fb[j][q]);
+        static_for<kProducts * WN>([&](auto jc) {
+          constexpr int q = decltype(jc)::value / WN, j = decltype(jc)::value % WN, n = i * kProducts * WN + decltype(jc)::value;
+          constexpr int all = kFirst * kProducts / 2 * WN;  // slots: the first half of these products
+          multiply_f16<Shape::kAgpr>(acc[i][j], fa[i][of_a(q)], fb[j][of_b(q)]);
           if constexpr (n < all) {
 #pragma unroll
             for (int k = n * kRows / all; k < (n + 1) * kRows / all; ++k) frag_a(kFirst + k, here);
@@ -383,10 +418,10 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth
       drain_and_meet<Shape::kAhead ? 1 : kLoads * (STAGES - 2)>();  // all but the lines asked for, or the later blocks
       static_for<WN>([&](auto jc) {
         constexpr int j = decltype(jc)::value;
-        static_for<2 * kRows>([&](auto ic) {
+        static_for<kProducts * kRows>([&](auto ic) {
           constexpr int q = decltype(ic)::value / kRows, i = kFirst + decltype(ic)::value % kRows;
-          constexpr int n = j * 2 * kRows + decltype(ic)::value, all = 2 * kRows * (WN > 2 ? WN - 1 : WN);
-          multiply_f16<Shape::kAgpr>(acc[i][j], fa[i][q], fb[j][q]);
+          constexpr int n = j * kProducts * kRows + decltype(ic)::value, all = kProducts * kRows * (WN > 2 ? WN - 1 : WN);
+          multiply_f16<Shape::kAgpr>(acc[i][j], fa[i][of_a(q)], fb[j][of_b(q)]);
           if constexpr (n < all) load(b + STAGES, n * kLoads / all, (n + 1) * kLoads / all);
           if constexpr (decltype(ic)::value == 0) {
 #pragma unroll
@@ -412,13 +447,13 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth
       return *m < a.M && *n < a.N;  // sides are multiples of kPad
     };
     Old<KIND> old[2];
-    i32x4_t v[2 * kHalves];
+    i32x4_t v[2 * kHalves], low[2 * kHalves];
     int m, n;
-    if (place(0, &m, &n)) fetch<KIND>(a, matrix, m, n, old[0]);
+    if (place(0, &m, &n)) fetch<KIND, FINE>(a, matrix, m, n, old[0]);
     static_for<kHalves * kParts>([&](auto hc) {
       constexpr int h = decltype(hc)::value, p = h / kHalves;
       if constexpr (h + 1 < kHalves * kParts)
-        if (place((h + 1) / kHalves, &m, &n)) fetch<KIND>(a, matrix, m + (h + 1) % kHalves * 32, n, old[(h + 1) % 2]);
+        if (place((h + 1) / kHalves, &m, &n)) fetch<KIND, FINE>(a, matrix, m + (h + 1) % kHalves * 32, n, old[(h + 1) % 2]);
       const f32x4_t* part[2][2];
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -429,12 +464,21 @@ __global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth
           part[i][j] = &s;
         }
       if (place(p, &m, &n)) {
-        convert<KIND>(a, part, old[h % 2], matrix, m + h % kHalves * 32, n, v + h % kHalves * 2);
-        if constexpr (h % kHalves == kHalves - 1) write_part<KIND, kHalves>(a, v, matrix, m, n, !kSymmetric || m0 != n0, own);
+        convert<KIND, FINE>(a, part, old[h % 2], matrix, m + h % kHalves * 32, n, v + h % kHalves * 2, low + h % kHalves * 2);
+        if constexpr (h % kHalves == kHalves - 1) write_part<KIND, kHalves, FINE>(a, v, low, matrix, m, n, !kSymmetric || m0 != n0, own);
       }
       __builtin_amdgcn_sched_barrier(0);
     });
   }
+}
+
+template <int WM, int WN, int STAGES, int KIND>
+__global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES>::kWaves)) void orth_step_kernel(OrthArgs a) {
+  orth_step<WM, WN, STAGES, KIND, false>(a);
+}
+template <int WM, int WN, int STAGES, int KIND>
+__global__ __launch_bounds__(256, (OrthShape<WM, WN, STAGES, true>::kWaves)) void orth_fine_kernel(OrthArgs a) {
+  orth_step<WM, WN, STAGES, KIND, true>(a);
 }
 
 // -- the start -------------------------------------------------------------------
@@ -444,7 +488,7 @@ struct OrthStartArgs {
   int64_t rows, cols, ld, stride;
   double* sums;
   int32_t parts, transposed;  // transposed: Y is G^T, X is G
-  _Float16 *X, *Y, *rest;
+  _Float16 *X, *Y, *rest;     // rest: where not FINE
   int64_t n, m;               // padded sides
 };
 
@@ -495,7 +539,7 @@ __global__ __launch_bounds__(kSumThreads) void orth_sum_kernel(OrthStartArgs a) 
 }
 
 // 64 x 64 values of G, normalised, to X, Y and what they leave; zeros around.
-template <typename T>
+template <typename T, bool FINE>
 __global__ __launch_bounds__(256) void orth_start_kernel(OrthStartArgs a) {
   __shared__ float tile[64][65];
   const int64_t rows = a.transposed ? a.n : a.m, cols = a.transposed ? a.m : a.n;  // padded sides of G
@@ -517,7 +561,9 @@ __global__ __launch_bounds__(256) void orth_start_kernel(OrthStartArgs a) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) tile[4 * i + wave][lane] = (float)((double)v[i] * by);
   __syncthreads();
-  _Float16 *X = a.X + matrix * a.n * a.m, *Y = a.Y + matrix * a.n * a.m, *rest = a.rest + matrix * a.n * a.m;
+  constexpr int R = kRow<FINE>;
+  constexpr float unit = FINE ? 1.0f : kRest;  // of rests
+  _Float16 *X = a.X + matrix * a.n * a.m * R, *Y = a.Y + matrix * a.n * a.m * R;
   // as G lies: Y (with its rest) where G is tall, else X
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -527,19 +573,20 @@ __global__ __launch_bounds__(256) void orth_start_kernel(OrthStartArgs a) {
     for (int k = 0; k < 8; ++k) {
       const float x = tile[row][c + k], y = tile[c + k][row];
       hi[k] = (_Float16)x;
-      lo[k] = (_Float16)((x - (float)hi[k]) * kRest);
+      lo[k] = (_Float16)((x - (float)hi[k]) * unit);
       thi[k] = (_Float16)y;
-      tlo[k] = (_Float16)((y - (float)thi[k]) * kRest);
+      tlo[k] = (_Float16)((y - (float)thi[k]) * unit);
     }
-    const int64_t straight = (r0 + row) * cols + c0 + c, turned = (c0 + row) * rows + r0 + c;
-    if (a.transposed) {
-      *(i32x4_t*)(X + straight) = *(const i32x4_t*)hi;
-      *(i32x4_t*)(Y + turned) = *(const i32x4_t*)thi;
-      *(i32x4_t*)(rest + turned) = *(const i32x4_t*)tlo;
+    const int64_t straight = (r0 + row) * cols * R + c0 + c, turned = (c0 + row) * rows * R + r0 + c;
+    _Float16 *s = a.transposed ? X : Y, *t = a.transposed ? Y : X;
+    *(i32x4_t*)(s + straight) = *(const i32x4_t*)hi;
+    *(i32x4_t*)(t + turned) = *(const i32x4_t*)thi;
+    if constexpr (FINE) {
+      *(i32x4_t*)(s + straight + cols) = *(const i32x4_t*)lo;
+      *(i32x4_t*)(t + turned + rows) = *(const i32x4_t*)tlo;
     } else {
-      *(i32x4_t*)(Y + straight) = *(const i32x4_t*)hi;
-      *(i32x4_t*)(rest + straight) = *(const i32x4_t*)lo;
-      *(i32x4_t*)(X + turned) = *(const i32x4_t*)thi;
+      _Float16* rest = a.rest + matrix * a.n * a.m;
+      *(i32x4_t*)(rest + (a.transposed ? turned : straight)) = *(const i32x4_t*)(a.transposed ? tlo : lo);
     }
   }
 }
@@ -551,8 +598,9 @@ struct Layout {
   int64_t sums, X, Y0, Y1, rest, S, T, dA, dB, all;
 };
 
-Layout layout(int64_t rows, int64_t cols, int64_t batch) {
+Layout layout(int64_t rows, int64_t cols, int64_t batch, bool fine) {
   Layout l{};
+  const int64_t size = fine ? 4 : 2;  // of a value
   l.n = ceil_div(rows < cols ? rows : cols, kPad) * kPad;
   l.m = ceil_div(rows < cols ? cols : rows, kPad) * kPad;
   const auto take = [&](int64_t bytes) {
@@ -561,12 +609,12 @@ Layout layout(int64_t rows, int64_t cols, int64_t batch) {
     return at;
   };
   l.sums = take(batch * kMostParts * 8);
-  l.X = take(batch * l.n * l.m * 2);
-  l.Y0 = take(batch * l.n * l.m * 2);
-  l.Y1 = take(batch * l.n * l.m * 2);
-  l.rest = take(batch * l.n * l.m * 2);
-  l.S = take(batch * l.n * l.n * 2);
-  l.T = take(batch * l.n * l.n * 2);
+  l.X = take(batch * l.n * l.m * size);
+  l.Y0 = take(batch * l.n * l.m * size);
+  l.Y1 = take(batch * l.n * l.m * size);
+  l.rest = take(fine ? 0 : batch * l.n * l.m * 2);
+  l.S = take(batch * l.n * l.n * size);
+  l.T = take(batch * l.n * l.n * size);
   l.dA = take(batch * l.n * 4);
   l.dB = take(batch * l.n * 4);
   return l;
@@ -580,14 +628,34 @@ bool orth_sizes(int64_t rows, int64_t cols, int64_t batch) {
          (batch <= max_workgroups(256) / kMostParts && 4 * ceil_div(rows, kPad) * ceil_div(cols, kPad) * batch <= max_workgroups(256));
 }
 
+template <bool FINE>
+auto start_kernel(int32_t dtype) {
+  return dtype == WS_OUT_F32 ? &orth_start_kernel<float, FINE> : dtype == WS_OUT_BF16 ? &orth_start_kernel<bf16_t, FINE> : &orth_start_kernel<f16_t, FINE>;
+}
+
+// Where operands of one binary16 value would cost more than the rounding to bf16, 1.7e-3 in
+// norm.  Products T X leave the rest of X out: where a part of the directions stands out,
+// that is noise in the others.  The largest error after five steps of operands of one value that a
+// replay over many spectra found (a quarter to half of the singular values 1, the others
+// 1/1000): 4.3e-3 for 128 rows, 3.0e-3 for 256, 2.3e-3 for 400, 1.95e-3 for 512, 1.7e-3 for 640 and more; after
+// twenty 2e-2.  Of two: 2e-5 after five steps, 1e-4 after twenty.  us of two and of one,
+// five steps: 200 x 700 125 and 102, 128 x 4096 203 and 146, 384 x 384 121 and 101,
+// 512 x 4096 253 and 190, 1000 x 2500 315 and 203, 16 of 1024 x 2048 2540 and 1230.
+constexpr int64_t kFineSide = 384;
+constexpr int32_t kCoarseSteps = 5;
+bool in_two_values(int64_t rows, int64_t cols, int32_t steps) { return (rows < cols ? rows : cols) <= kFineSide || steps > kCoarseSteps; }
+
 // Launches tiles of 32 WM x 32 WN.
-template <int WM, int WN, int STAGES, int KIND>
+template <int WM, int WN, int STAGES, int KIND, bool FINE = false>
 ws_status launch_tiles(OrthArgs a, hipStream_t stream) {
-  typedef OrthShape<WM, WN, STAGES> Shape;
+  typedef OrthShape<WM, WN, STAGES, FINE> Shape;
   if (a.quarters) a.count *= 4;
   const uint32_t most = (uint32_t)compute_units() * Shape::kWaves;
   a.tile_groups = (int32_t)(a.count < most ? a.count : most);
-  const auto kernel = &orth_step_kernel<WM, WN, STAGES, KIND>;
+  const auto kernel = [] {
+    if constexpr (FINE) return &orth_fine_kernel<WM, WN, STAGES, KIND>;
+    else return &orth_step_kernel<WM, WN, STAGES, KIND>;
+  }();
   static std::atomic<uint64_t> allowed;
   const ws_status s = allow_lds((const void*)kernel, Shape::kLds, allowed);
   if (s != WS_OK) return s;
@@ -601,7 +669,10 @@ ws_status launch_tiles(OrthArgs a, hipStream_t stream) {
 // where even these would leave CUs without work (1024 columns of 2560: X X^T 13 us, in
 // 128 x 128 31), and for short contractions (4 x 188 x 1358: 125 us, in 128 x 128 142;
 // 2500 x 1000 the other way round, 214 and 208).
-template <int KIND>
+// FINE, whose blocks have three times the products: 128 x 128 from four rounds on (16 of
+// 384 x 4096: 966 us, in 64 x 64 1001; below, 100 of 250 x 300 472 and 361), else 64 x 64,
+// with a long ring where there is one a CU (128 x 4096 203, with two stages 253).
+template <int KIND, bool FINE>
 ws_status run_tiles(OrthArgs a, hipStream_t stream) {
   constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
   const auto cut = [&](int side) {
@@ -613,23 +684,44 @@ ws_status run_tiles(OrthArgs a, hipStream_t stream) {
     a.quarters = 0;
   };
   const uint32_t cus = (uint32_t)compute_units();
-  cut(256);
-  if (a.count < cus) {
+  if constexpr (FINE) {
     cut(128);
-    if (a.count > cus) return launch_tiles<4, 4, 2, KIND>(a, stream);
-    if (4 * a.count > cus && a.K > 512) return launch_tiles<4, 4, 4, KIND>(a, stream);
+    if (a.count > 4 * cus) return launch_tiles<4, 4, 2, KIND, true>(a, stream);
     cut(64);
-    if (a.count > cus) return launch_tiles<2, 2, 2, KIND>(a, stream);
-    return launch_tiles<2, 2, 8, KIND>(a, stream);
+    if (a.count > cus) return launch_tiles<2, 2, 2, KIND, true>(a, stream);
+    return launch_tiles<2, 2, 4, KIND, true>(a, stream);
+  } else {
+    cut(256);
+    if (a.count < cus) {
+      cut(128);
+      if (a.count > cus) return launch_tiles<4, 4, 2, KIND>(a, stream);
+      if (4 * a.count > cus && a.K > 512) return launch_tiles<4, 4, 4, KIND>(a, stream);
+      cut(64);
+      if (a.count > cus) return launch_tiles<2, 2, 2, KIND>(a, stream);
+      return launch_tiles<2, 2, 8, KIND>(a, stream);
+    }
+    const uint32_t rest = a.count % cus <= cus / 2 ? a.count % cus : 0;
+    a.count -= rest;
+    const ws_status s = launch_tiles<8, 8, 2, KIND>(a, stream);
+    if (s != WS_OK || rest == 0) return s;
+    a.first = a.count;
+    a.count = rest;
+    a.quarters = 1;
+    return launch_tiles<4, 4, 2, KIND>(a, stream);
   }
-  const uint32_t rest = a.count % cus <= cus / 2 ? a.count % cus : 0;
-  a.count -= rest;
-  const ws_status s = launch_tiles<8, 8, 2, KIND>(a, stream);
-  if (s != WS_OK || rest == 0) return s;
-  a.first = a.count;
-  a.count = rest;
-  a.quarters = 1;
-  return launch_tiles<4, 4, 2, KIND>(a, stream);
+}
+
+template <bool FINE>
+ws_status run_steps(const OrthArgs& gram, const OrthArgs& square, OrthArgs apply, _Float16* Y0, _Float16* Y1, int steps, hipStream_t stream) {
+  ws_status s = WS_OK;
+  for (int i = 0; i < steps && s == WS_OK; ++i) {
+    s = run_tiles<kGram, FINE>(gram, stream);
+    if (s == WS_OK) s = run_tiles<kSquare, FINE>(square, stream);
+    apply.A = i & 1 ? Y1 : Y0;
+    apply.to = i & 1 ? Y0 : Y1;
+    if (s == WS_OK) s = i + 1 < steps ? run_tiles<kApply, FINE>(apply, stream) : run_tiles<kLast, FINE>(apply, stream);
+  }
+  return s;
 }
 
 }  // namespace
@@ -642,9 +734,9 @@ extern "C" {
 int64_t ws_orthogonal_workspace(int64_t rows, int64_t cols, int32_t batch) {
   if (!orth_sizes(rows, cols, batch)) return -1;
   if (rows == 0 || cols == 0 || batch == 0) return 0;
-  const int64_t tiles = layout(rows, cols, batch).all;
-  if ((rows < cols ? rows : cols) > kFewRows) return tiles;
-  const int64_t few = few_workspace(rows, cols, batch);  // which of them runs depends on the steps
+  // which of them runs depends on the steps
+  const int64_t tiles = layout(rows, cols, batch, true).all;
+  const int64_t few = (rows < cols ? rows : cols) > kFewRows ? 0 : few_workspace(rows, cols, batch);
   return few > tiles ? few : tiles;
 }
 
@@ -657,7 +749,9 @@ ws_status ws_orthogonalize(const ws_matrix* G, int32_t steps, const ws_matrix* o
   if (need < 0 || workspace_bytes < need || (need > 0 && (!workspace || (uintptr_t)workspace % 256))) return WS_ERR_INVALID_ARG;
   if (need == 0) return WS_OK;
   if (by_gram_matrix(G->rows, G->cols, steps)) return orthogonalize_few(G, steps, out, workspace, stream);
-  const Layout l = layout(G->rows, G->cols, G->batch);
+  const bool fine = in_two_values(G->rows, G->cols, steps);
+  const int64_t row = fine ? 2 : 1;
+  const Layout l = layout(G->rows, G->cols, G->batch, fine);
   uint8_t* w = (uint8_t*)workspace;
   OrthStartArgs s{};
   s.G = G->data;
@@ -679,29 +773,27 @@ ws_status ws_orthogonalize(const ws_matrix* G, int32_t steps, const ws_matrix* o
                                                                                                                    : &orth_sum_kernel<f16_t>,
                         (int64_t)s.parts * G->batch, kSumThreads, 0, stream, s);
   if (st == WS_OK)
-    st = launch("orthogonalize", G->dtype == WS_OUT_F32 ? &orth_start_kernel<float> : G->dtype == WS_OUT_BF16 ? &orth_start_kernel<bf16_t>
-                                                                                                               : &orth_start_kernel<f16_t>,
-                grid, 256, 0, stream, s);
+    st = launch("orthogonalize", fine ? start_kernel<true>(G->dtype) : start_kernel<false>(G->dtype), grid, 256, 0, stream, s);
   OrthArgs gram{}, square{}, apply{};
   gram.batch = square.batch = apply.batch = G->batch;
   gram.A = gram.B = (const _Float16*)(w + l.X);
-  gram.stride_a = gram.stride_b = l.n * l.m;
+  gram.stride_a = gram.stride_b = l.n * l.m * row;
   gram.M = gram.N = (int32_t)l.n;
   gram.K = (int32_t)l.m;
   gram.to = gram.mirror = (_Float16*)(w + l.S);
-  gram.stride_to = gram.stride_mirror = l.n * l.n;
+  gram.stride_to = gram.stride_mirror = l.n * l.n * row;
   gram.d_out = (float*)(w + l.dA);
   gram.stride_d = square.stride_d = apply.stride_d = l.n;
   square.A = square.B = (const _Float16*)(w + l.S);
-  square.stride_a = square.stride_b = l.n * l.n;
+  square.stride_a = square.stride_b = l.n * l.n * row;
   square.M = square.N = square.K = (int32_t)l.n;
   square.to = square.mirror = (_Float16*)(w + l.T);
-  square.stride_to = square.stride_mirror = l.n * l.n;
+  square.stride_to = square.stride_mirror = l.n * l.n * row;
   square.d_in = (const float*)(w + l.dA);
   square.d_out = (float*)(w + l.dB);
   apply.B = (const _Float16*)(w + l.T);
-  apply.stride_a = apply.stride_to = apply.stride_mirror = l.n * l.m;
-  apply.stride_b = l.n * l.n;
+  apply.stride_a = apply.stride_to = apply.stride_mirror = l.n * l.m * row;
+  apply.stride_b = l.n * l.n * row;
   apply.M = (int32_t)l.m;
   apply.N = apply.K = (int32_t)l.n;
   apply.mirror = (_Float16*)(w + l.X);
@@ -713,14 +805,9 @@ ws_status ws_orthogonalize(const ws_matrix* G, int32_t steps, const ws_matrix* o
   apply.rows = (int32_t)out->rows;
   apply.cols = (int32_t)out->cols;
   apply.transposed = s.transposed;
-  for (int i = 0; i < steps && st == WS_OK; ++i) {
-    st = run_tiles<kGram>(gram, stream);
-    if (st == WS_OK) st = run_tiles<kSquare>(square, stream);
-    apply.A = (const _Float16*)(w + (i & 1 ? l.Y1 : l.Y0));
-    apply.to = (_Float16*)(w + (i & 1 ? l.Y0 : l.Y1));
-    if (st == WS_OK) st = i + 1 < steps ? run_tiles<kApply>(apply, stream) : run_tiles<kLast>(apply, stream);
-  }
-  return st;
+  if (st != WS_OK) return st;
+  _Float16 *Y0 = (_Float16*)(w + l.Y0), *Y1 = (_Float16*)(w + l.Y1);
+  return fine ? run_steps<true>(gram, square, apply, Y0, Y1, steps, stream) : run_steps<false>(gram, square, apply, Y0, Y1, steps, stream);
 }
 
 }  // extern "C"

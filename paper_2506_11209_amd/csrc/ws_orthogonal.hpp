@@ -24,8 +24,8 @@ inline ws_status allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>&
 constexpr int kFewRows = 64;  // of the shorter side, at the most
 constexpr int kFewSteps = 6;  // see ws_orthogonal_few.hip
 
-// Whether the Gram matrix alone is quicker.  us so and in tiles, five steps: 64 x 2048 47
-// and 110, 128 x 1024 148 and 97, 128 x 4096 165 and 147.
+// Whether the Gram matrix alone is quicker.  us so and in tiles, five steps: 16 x 2048 15 and
+// 146, 64 x 512 45 and 100, 64 x 2048 48 and 147; 128 rows in binary64 are more than a CU's LDS.
 inline bool by_gram_matrix(int64_t rows, int64_t cols, int32_t steps) {
   return (rows < cols ? rows : cols) <= kFewRows && steps <= kFewSteps;
 }

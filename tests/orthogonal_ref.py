@@ -30,6 +30,8 @@ def spectrum(name, n):
         s[1:] = float(name[4:])
     elif name.startswith("eighth "):
         s[max(1, n // 8):] = float(name[7:])
+    elif name.startswith("quarter "):
+        s[max(1, n // 4):] = float(name[8:])
     elif name.startswith("half "):
         s[max(1, n // 2):] = float(name[5:])
     elif name.startswith("rank "):  # the others are nothing but what float32 leaves of them
