@@ -24,6 +24,18 @@ for _name, _args, _res in (("ws_orthogonal_workspace", [_i64, _i64, _i32], _i64)
     getattr(_lib, _name).argtypes, getattr(_lib, _name).restype = _args, _res
 
 
+def _counts(steps) -> bool:
+    return isinstance(steps, int) and 1 <= steps <= MAX_STEPS
+
+
+def _need_bytes(rows: int, cols: int, batch: int, what: str) -> int:
+    """Work memory for a batch of matrices; refuses sizes that no launch holds."""
+    need = _lib.ws_orthogonal_workspace(rows, cols, batch) if max(rows, cols, batch) < 1 << 31 else -1
+    if need < 0:
+        raise ValueError("%s: sizes %s are too large" % (what, (batch, rows, cols)))
+    return need
+
+
 def orthogonalize(G, steps: int = 5, out=None, stream=None):
     """G (rows x columns, or a batch of such matrices; f32, bf16 or f16) with its
     singular values brought near 1 by ``steps`` Newton-Schulz steps, in bf16: X = G /
@@ -31,11 +43,9 @@ def orthogonalize(G, steps: int = 5, out=None, stream=None):
     itself; zeros stay zeros, a matrix with an infinity or NaN becomes NaN.  out may not
     overlap G."""
     m = _matrix(G, "G", (2, 3))
-    if not 1 <= steps <= MAX_STEPS:
+    if not _counts(steps):
         raise ValueError("steps: 1 to %d, got %r" % (MAX_STEPS, steps))
-    need = _lib.ws_orthogonal_workspace(m.rows, m.cols, m.batch) if m.batch < 1 << 31 else -1
-    if need < 0:
-        raise ValueError("orthogonalize: sizes %s are too large" % (tuple(G.shape),))
+    need = _need_bytes(m.rows, m.cols, m.batch, "orthogonalize")
     if out is not None and (out.shape != G.shape or out.dtype != torch.bfloat16):
         raise ValueError("out: expected %s bf16, got %s %s" % (tuple(G.shape), tuple(out.shape), out.dtype))
     if _elsewhere(G, stream):
@@ -56,19 +66,32 @@ class OrthogonalMomentum(torch.optim.Optimizer):
     """Momentum whose updates are orthogonalised: for matrices and batches of them (the
     weights of experts), b <- momentum b + g, u = g + momentum b (or b, without nesterov),
     w <- (1 - lr weight_decay) w - lr max(1, rows / columns)^0.5 orthogonalize(u).
-    b is kept in binary32 whatever the parameters' type."""
+    b is kept in binary32 whatever the parameters' type.  Sizes and options are checked when
+    a group is added, and all gradients before a step changes anything."""
 
     def __init__(self, params, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, steps: int = 5):
-        if lr < 0 or not 0 <= momentum < 1 or weight_decay < 0 or not 1 <= steps <= MAX_STEPS:
+        defaults = dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, steps=steps)
+        self._check_options(defaults)
+        super().__init__(params, defaults)
+
+    @staticmethod
+    def _check_options(group):
+        lr, momentum, weight_decay, steps = (group[k] for k in ("lr", "momentum", "weight_decay", "steps"))
+        if not lr >= 0 or not 0 <= momentum < 1 or not weight_decay >= 0 or not _counts(steps):
             raise ValueError("lr %r, momentum %r, weight_decay %r, steps %r" % (lr, momentum, weight_decay, steps))
-        super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, steps=steps))
 
     def add_param_group(self, param_group):
         super().add_param_group(param_group)
-        for p in self.param_groups[-1]["params"]:
-            if p.dim() not in (2, 3):
-                del self.param_groups[-1]
-                raise ValueError("parameters have to be matrices or batches of them, got %s" % (tuple(p.shape),))
+        group = self.param_groups[-1]
+        try:
+            self._check_options(group)
+            for p in group["params"]:
+                if p.dim() not in (2, 3):
+                    raise ValueError("parameters have to be matrices or batches of them, got %s" % (tuple(p.shape),))
+                _need_bytes(p.shape[-2], p.shape[-1], p.shape[0] if p.dim() == 3 else 1, "parameter")
+        except ValueError:
+            del self.param_groups[-1]
+            raise
 
     def load_state_dict(self, state_dict):
         super().load_state_dict(state_dict)  # which rounds to the parameters' type
@@ -83,6 +106,12 @@ class OrthogonalMomentum(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        for group in self.param_groups:  # all of it before the first change
+            self._check_options(group)
+            for p in group["params"]:
+                if p.grad is not None and (p.grad.layout != torch.strided or not p.grad.is_cuda or p.grad.dtype not in _CODES):
+                    raise ValueError("gradients have to be dense cuda tensors of f32, bf16 or f16, got %s of %s on %s" % (
+                        p.grad.layout, p.grad.dtype, p.grad.device))
         for group in self.param_groups:
             for p in group["params"]:
                 if p.grad is None:
