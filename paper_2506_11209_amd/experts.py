@@ -14,13 +14,14 @@ Streams and errors as in ``fp8``.  choose, gather and combine are recorded by
 autograd (once: their gradients are not differentiated again), so that the last
 three lines are what their results' backward does; results in memory of the
 caller's (``out``) cannot be, and ask for torch.no_grad() where an input requires a
-gradient.
+gradient.  Forward mode is refused (NotImplementedError).
 """
 from __future__ import annotations
 
 import ctypes
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import wsgemm as _w
@@ -41,6 +42,12 @@ for _name, _args, _res in (
         ("ws_expert_combine", [_mp, _i32, _p, _p, _mp, _p], _i32),
         ("ws_expert_combine_gradient", [_mp, _mp, _i32, _i32, _p, _p, _p, _mp, _p, _p], _i32)):
     getattr(_lib, _name).argtypes, getattr(_lib, _name).restype = _args, _res
+
+
+def _no_forward_mode(what, *tensors):
+    """Refuses inputs with a tangent, which the kernels would drop."""
+    if forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise NotImplementedError("%s: not differentiated in forward mode" % what)
 
 
 class Routes:
@@ -113,6 +120,7 @@ def choose(logits, k: int, stream=None):
     if need < 0:
         raise ValueError("choose: 1 to %d of the %d experts and at most 2^30 choices, got k = %r for %d tokens" % (
             MAX_CHOICES, experts, k, tokens))
+    _no_forward_mode("choose", logits)
     if _elsewhere(logits, stream):
         with _Call(logits.device, stream, [logits]):
             return choose(logits, k)
@@ -242,6 +250,7 @@ def gather(x, routes: Routes, out=None, stream=None):
     tokens, k = routes.place.shape
     if m.rows != tokens:
         raise ValueError("x: %d rows for %d tokens" % (m.rows, tokens))
+    _no_forward_mode("gather", x)
     if _elsewhere(x, stream):
         with _Call(x.device, stream, [x, routes.offsets, routes.place, out]):
             return gather(x, routes, out)
@@ -260,6 +269,7 @@ def combine(h, routes: Routes, weights=None, out=None, stream=None):
     if m.rows != routes.token.numel():
         raise ValueError("h: %d rows for %d choices" % (m.rows, routes.token.numel()))
     w, (tokens, k) = _weights(weights, routes), routes.place.shape
+    _no_forward_mode("combine", h, weights)
     if _elsewhere(h, stream):
         with _Call(h.device, stream, [h, routes.place, weights, out]):
             return combine(h, routes, weights, out)
