@@ -209,8 +209,9 @@ __device__ __forceinline__ void finish(const ChooseArgs& a, const float* sums, c
 // largest (and lowest) left, the first of which is the softmax's maximum too.  Sums of
 // probabilities and counts stay in the lanes over a workgroup's tokens and pass LDS at
 // the end, in a fixed order.  ALONE: one workgroup.
-// Bound: instructions, some 35 for a logit and 8 choices (65536 x 256 of bf16, 8 choices:
-// 25.8 us, 1.4 TB/s; with ranks cleared of what went before instead of differences 34.6;
+// Bound: instructions, some 35 for a logit and 8 choices, about 15 us of issue, and the
+// latency of the lanes' maxima, one choice after the other with four waves a SIMD (65536 x
+// 256 of bf16, 8 choices: 25.8 us, 1.4 TB/s; with ranks cleared of what went before instead of differences 34.6;
 // with the next token's row under way meanwhile 26.7).
 template <typename T, int L, int V, bool ALONE>
 __global__ __launch_bounds__(64 * choose_waves<L>()) void choose_kernel(ChooseArgs a) {

@@ -259,9 +259,10 @@ __global__ __launch_bounds__(256) void fp4_arrange_kernel(Fp4Args a) {
 // Operands go from memory straight to registers, a step's weights before the products of
 // the one before.  Rows that are not there read those of another and are not stored.
 // Bound: reading the weights (1 x 8192 x 8192: 8.6 us, 4.2 TB/s; by rows of codes instead
-// of tiles, 64 bytes of 16 rows a load and scales 4 bytes of each, 14.1; 55 of 64 groups of
-// 4096 x 2048 51 us, 4.8 TB/s, by rows 83); from about 16 rows on by reading those of A
-// for every strip (256 x 4096 x 4096: 24 us, 1024 x 8192 x 8192: 205, 0.67 PFLOP/s).
+// of tiles, 64 bytes of 16 rows a load and scales 4 bytes of each, 14.1; 128 rows in 53 to 56 of
+// 64 groups of 4096 x 2048 43 to 55 us, by rows of codes 83); from about 16 rows on by this
+// split, in which A is read once for every 32 columns (256 x 4096 x 4096: 24 us, 1024 x 8192 x
+// 8192: 205, 0.67 PFLOP/s).
 // (Of 64 rows with the registers of four waves; of fewer with those of eight, and so more
 // workgroups a CU.)
 template <typename X, int MT, int NT, bool GROUPED, bool ARRANGED>
@@ -476,9 +477,15 @@ struct Choice {
   int64_t bytes;  // of A by operands, 0 where it is read as it lies
 };
 // Of 16 rows, workgroups of 2 tiles' columns and eight waves where there are few strips, of
-// 4 and four waves where there are many and starting waves costs more than it hides.  us:
-// 1 x 8192 x 8192 9.4 and 13.0, 128 rows of 55 of 64 groups of 4096 x 2048 94 and 57.  More
-// rows have many strips, and four waves.
+// 4 and four waves where there are many and starting waves costs more than it hides.  us so
+// and so, by strips of 32 columns: 256 (1 x 8192 x 8192) 11.2 and 14.7, of 16 rows 14.5 and 16.5;
+// 384 (12288 x 4096) 11.0 and 10.4, 14.6 and 11.5; 512 (16384 x 4096) 10.8 and 11.1, 14.7 and
+// 12.4; 768 14.4 and 15.5, 19.9 and 18.8; 1024 17.4 and 17.1, 24.8 and 20.1; 2048 29.6 and
+// 28.6, 44.3 and 34.4; 128 rows of 57 of 64 groups of 4096 x 2048 92 and 53.  More rows have
+// many strips, and four waves.
+// Rows of a group on average: one full group among empty ones runs in tiles of 16 rows too
+// (256 rows in one of 64 of 4096 x 2048 24.8 us, in a matrix by itself 17.9, in all of them 58;
+// 1024 rows 60.6, 44.1 and 73.1).
 // A workgroup takes fewer rows where the launch has under three workgroups a CU.  us of all
 // 64 (or 32) rows in one and so: 40 x 4104 x 4100 17.0 and 11.5, 64 x 4096 x 4096 15.5 and
 // 10.2, 64 x 100 x 8192 22.3 and 11.5, 256 x 2048 x 2048 13.1 and 9.5; of two a CU
