@@ -86,9 +86,10 @@ def test_short_sides_of_many_steps(R, steps):
 BATCHES = [
     (1, 250, 300, 5),   # two values; 64 x 64, long rings
     (40, 250, 300, 5),  # 64 x 64, two stages
-    (100, 250, 300, 5), # 128 x 128
     (100, 250, 300, 7),
+    (350, 250, 300, 5), # 128 x 128: 1050 and 2100 of them
     (20, 640, 700, 6),
+    (80, 520, 520, 6),  # 1200 of 128 x 128, five a side
     (12, 500, 512, 5),  # one value; 64 x 64, two stages
     (48, 600, 700, 5),  # 288 lower tiles of 256 x 256: a round, and 32 in quarters; five 128s a side
     (100, 520, 650, 5), # two rounds and 88 in quarters
@@ -122,7 +123,7 @@ def test_batches_by_their_tiles(B, R, C, steps):
         assert ok, (i, off, bound)
 
 
-@pytest.mark.parametrize("B,R,C", [(48, 1024, 1024), (60, 512, 1024), (100, 256, 256), (40, 256, 1024)])
+@pytest.mark.parametrize("B,R,C", [(48, 1024, 1024), (60, 512, 1024), (350, 256, 256), (40, 256, 1024)])
 def test_signs_in_batches(B, R, C):
     """One step of entries +-1 / 2^k: X, A and A^2 are exact, and so is all of it but T off its
     diagonal, which one binary16 value rounds by 2^-11, two by 2^-22 (and sums in binary32, of less)."""
