@@ -139,3 +139,20 @@ def test_signs_in_batches(B, R, C):
         unit = 2.0 ** -11 if R > 384 else 2.0 ** -21
         bound = (2.0 ** -8 * want.abs() + unit * (T - T.diagonal().diag()).abs() @ X.abs()) * (1 + 1e-3) + 1e-5 * X.abs().max()
         assert ((got[i] - want).abs() <= bound).all(), i
+
+
+@pytest.mark.parametrize("R,C", [(64, 65536), (65536, 20), (100, 65536), (65536, 300)])
+def test_longest_sides(R, C):
+    """Sums of 65536 products: binary32's of values of both signs grow as their square root."""
+    log("case orthogonalize %d x %d" % (R, C))
+    for i, name in enumerate(("noise", "eighth 0.001")):
+        check(ref.matrix(R, C, name, seed=i), 5, by_hand(5))
+
+
+def test_many_short_matrices():
+    log("case orthogonalize 3000 of 66 x 70 and of 30 x 40")
+    for R, C in ((66, 70), (30, 40)):
+        G = torch.randn(3000, R, C, generator=torch.Generator().manual_seed(R))
+        got = orthogonal.orthogonalize(G.cuda()).cpu()
+        for i in (0, 1, 1499, 2998, 2999):
+            assert ref.within(got[i], ref.orthogonalize(G[i]), by_hand(5))[0], i
