@@ -9,17 +9,17 @@
  * those above 0.01 to 0.7 .. 1.2, and the result near U V^T of G = U S V^T.
  *
  * Precision: how far the result is from the exact iteration (in norm), before it is
- * rounded to bf16, which costs 1.7e-3.  A shorter side up to 64 and up to six steps:
- * below 1e-4 (five) and 4e-4 (six), by way of A in binary64.  Longer ones: products are of
- * binary16 values with sums in binary32.  What the steps amplify is kept apart from what
- * is rounded: X as the sum of two binary16 values, the diagonals of A and of a + b A +
- * c A^2 in binary32.  A shorter side up to 384, or more than five steps of any: all
- * operands are such sums, as good as binary32: below 2e-4 after five steps, 5e-4 after
- * six (where a direction of 1e-4 of the largest has grown for eight, up to 2e-3).  Shorter sides over 384 up to five steps:
- * operands of one binary16 value; 2e-4 to 9e-4 where directions are alike or fall off
- * evenly, up to 2.4e-3 (over 512: 1.8e-3) where a part of them stands out over a rest
- * of 1/1000.  The same matrix in another batch may round otherwise.
- * A matrix with an infinity or NaN becomes NaN.
+ * rounded to bf16, which costs 1.7e-3. A shorter side up to 64 and up to six steps: below
+ * 1e-4 (five) and 4e-4 (six), by way of A in binary64. Longer ones: products are of
+ * binary16 values with sums in binary32. What the steps amplify is kept apart from what is
+ * rounded: X as the sum of two binary16 values, the diagonals of A and of a + b A + c A^2
+ * in binary32. A shorter side up to 384, or more than five steps of any: all operands are
+ * such sums, as good as binary32: below 2e-4 after five steps, 5e-4 after six, 2e-3 after
+ * more. Shorter sides over 384 up to five steps: operands of one binary16 value; 2e-4 to
+ * 9e-4 where directions are alike or fall off evenly, up to 1.5e-3 where one stands out,
+ * up to 2.4e-3 (over 512: 1.8e-3) where a quarter to half of them stands out over a rest
+ * of 1/1000. The same matrix in another batch may round otherwise. A matrix with an
+ * infinity or NaN becomes NaN.
  *
  * Calls, pointers, sizes and errors as in ws_fp8.h.
  */

@@ -53,11 +53,11 @@ def by_hand(steps):
 
 
 @pytest.mark.parametrize("R,C", [(65, 128), (66, 1024), (128, 1024), (300, 100), (256, 512), (384, 384), (200, 4100), (1000, 70)])
-@pytest.mark.parametrize("steps", (1, 5, 6, 20))
+@pytest.mark.parametrize("steps", (1, 5, 6, 20, 100))
 def test_sides_of_some_hundred(R, C, steps):
     log("case orthogonalize %d x %d, %d steps" % (R, C, steps))
     for i, name in enumerate(NAMES):
-        if steps == 20 and name.startswith("rank"):
+        if steps >= 20 and name.startswith("rank"):
             continue  # the rounding of G itself arrives
         dtype = (torch.float32, torch.bfloat16, torch.float16)[i % 3]
         off, bound = check(ref.matrix(R, C, name, seed=i).to(dtype), steps, by_hand(steps))
@@ -74,7 +74,7 @@ def test_longer_sides(R, C, steps):
 
 
 @pytest.mark.parametrize("R", (16, 40, 64))
-@pytest.mark.parametrize("steps", (7, 20))
+@pytest.mark.parametrize("steps", (7, 20, 100))
 def test_short_sides_of_many_steps(R, steps):
     """The other way round than up to six."""
     log("case orthogonalize %d x 500, %d steps" % (R, steps))
